@@ -9,6 +9,8 @@
  * library computes exactly that step:
  *
  *   spexis_append_kv         write the k+1 new K/V rows of every sequence into the cache
+ *   spexis_rotate_append_kv  the same, with the rotary position embedding of q and k on the way
+ *   spexis_rotate_append_kv8  the same into a cache held in 8 bits with a scale per block and head
  *   spexis_verify_attention  causal grouped-query attention of those rows over the cache
  *   spexis_accept            ratio tests, residual / bonus sampling, outputs
  *   spexis_lm_head           logits = h W^T with fused softmax statistics (next to accept)
@@ -62,6 +64,18 @@
  *   The layout lets the attention kernel load both matrix-core operands straight from HBM
  *   with fully coalesced 16-byte loads (K: eight head-dim values of one slot; V: eight
  *   slots of one head-dim index, in the order the score tile produces them).
+ *
+ * 8-bit cache layout (e4m3 codes, one byte each: sign, 4 exponent and 3 mantissa bits, no infinity,
+ * largest value 448), one pool for K and one for V, and one array of scales
+ *   units of 16 slots: unit = slot / 16, u = slot % 16; a (block, head) holds block_size / 16 units
+ *   K pool  [num_blocks][Hkv][units][D/16][16][16]
+ *           element at ((((blk*Hkv + h)*units + unit)*(D/16) + d/16)*16 + u)*16 + d%16
+ *   V pool  [num_blocks][Hkv][units][D/64][32][2][2][8]
+ *           element at ((((((blk*Hkv + h)*units + unit)*(D/64) + d/64)*32 + d%32)*2 + (u>>2 & 1))*2
+ *           + (d>>5 & 1))*8 + (u>>3)*4 + (u&3)
+ *   scales  [num_blocks][Hkv][2] fp32, K then V: element = code * scales[blk][h][K or V]
+ *   Half the bytes of the bf16 cache; the order again hands the attention kernel 16-byte loads that are
+ *   whole matrix-core operands (K: 16 head-dim values of one slot; V: 8 slots of two head-dim indices).
  */
 #ifndef SPEXIS_H
 #define SPEXIS_H
@@ -93,6 +107,10 @@ extern "C" {
 #define SPEXIS_INPUT_PROBS 0
 #define SPEXIS_INPUT_LOGITS 1
 
+/* which elements of a head the rotary position embedding turns together */
+#define SPEXIS_ROTARY_HALVES 0  /* i and i + rotary_dim/2 */
+#define SPEXIS_ROTARY_PAIRS 1   /* 2i and 2i + 1 */
+
 /* Library version (SPEXIS_VERSION). */
 int spexis_version(void);
 
@@ -122,6 +140,65 @@ int spexis_append_kv(void* k_cache, void* v_cache, int32_t num_blocks, int32_t n
                      const int32_t* block_tables, int32_t max_blocks_per_seq,
                      int32_t total_tokens, int32_t max_query_len, const void* new_k,
                      const void* new_v, void* stream);
+
+/*
+ * spexis_rotate_append_kv -- spexis_append_kv for keys that are not rotated yet (the verifying model's
+ * layers rotate q and k by position before its attention): q and the new keys turn by their token's angles,
+ * the rotated keys and the values go into the cache, the rotated queries to q_out.  One launch.
+ * With c_i = cos_sin[pos][i], s_i = cos_sin[pos][rotary_dim/2 + i], i < rotary_dim/2, the pair
+ * (a, b) = (i, i + rotary_dim/2) or (2i, 2i + 1) of a head becomes
+ *   y_a = x_a c_i - x_b s_i,   y_b = x_b c_i + x_a s_i
+ * (fp32, one rounding to bf16); elements from rotary_dim on are copied.
+ *
+ *   new_k, new_v  [total_tokens][Hkv][head_dim] bf16 (read)
+ *   cos_sin       [max_position][rotary_dim] fp32 (read): cosines, then sines, of every position
+ *   style         SPEXIS_ROTARY_HALVES or SPEXIS_ROTARY_PAIRS
+ *   positions     [total_tokens] int32: the row of cos_sin of every token, or NULL: the token's place in its
+ *                 sequence, L_b + j.  (It does not change where rows are stored.)
+ *   q, q_out      [total_tokens][Hq][head_dim] bf16, read and written; q_out may be q.  Both NULL: keys only
+ *                 (num_q_heads is then not read)
+ * Other arguments as spexis_append_kv; pools, rows and table 16-byte aligned.  Any number of new tokens a
+ * sequence, prompts included; a sequence's blocks that receive rows must be its own.
+ * Supported: rotary_dim a multiple of 16, 16 .. head_dim; head_dim in {64, 128}, block_size in {16, 32}.
+ * Errors: INVALID_ARGUMENT, UNSUPPORTED, HIP.
+ */
+int spexis_rotate_append_kv(void* k_cache, void* v_cache, int32_t num_blocks, int32_t num_kv_heads,
+                            int32_t block_size, int32_t head_dim, int32_t num_seqs,
+                            const int32_t* query_start_loc, const int32_t* seq_lens,
+                            const int32_t* block_tables, int32_t max_blocks_per_seq,
+                            int32_t total_tokens, int32_t max_query_len, const void* new_k,
+                            const void* new_v, const float* cos_sin, int32_t max_position,
+                            int32_t rotary_dim, int32_t style, const int32_t* positions,
+                            const void* q, int32_t num_q_heads, void* q_out, void* stream);
+
+/*
+ * spexis_rotate_append_kv8 -- the same into the 8-bit cache.  For every (block, KV head) that receives rows, and
+ * for K and V apart:
+ *   need  = the least power of two, from 2^-100 up, with |x| <= 448 * need for every finite element x of
+ *           the new rows
+ *   scale = need where the block holds no earlier row of the sequence (slots before the first new one),
+ *           else max(old scale, need): a scale is never lowered under rows that use it
+ *   new rows:      code = e4m3(x / scale), x the fp32 value (rotated: the sum rounded once to fp32),
+ *                  to nearest even; a NaN or an infinity is stored as NaN
+ *   earlier rows of a block whose scale grew: code = e4m3(code * old scale / scale)
+ * Slots behind the sequence's last token keep their codes, other blocks and scales are not touched.  A power of
+ * two costs no precision (codes are floating point) and re-coding earlier rows is exact but for the format's
+ * subnormal codes, those below 2^-6.  Scales of blocks that hold rows must be positive
+ * and finite; a caller that fills blocks by other means uses powers of two.
+ *   scales  [num_blocks][Hkv][2] fp32 (read and written)
+ *   cos_sin NULL with max_position 0: nothing is rotated (style and rotary_dim are not read; q, q_out and
+ *           positions NULL)
+ * Other arguments and errors as spexis_rotate_append_kv.
+ */
+int spexis_rotate_append_kv8(void* k_cache, void* v_cache, float* scales, int32_t num_blocks,
+                             int32_t num_kv_heads, int32_t block_size, int32_t head_dim,
+                             int32_t num_seqs, const int32_t* query_start_loc,
+                             const int32_t* seq_lens, const int32_t* block_tables,
+                             int32_t max_blocks_per_seq, int32_t total_tokens,
+                             int32_t max_query_len, const void* new_k, const void* new_v,
+                             const float* cos_sin, int32_t max_position, int32_t rotary_dim,
+                             int32_t style, const int32_t* positions, const void* q,
+                             int32_t num_q_heads, void* q_out, void* stream);
 
 /*
  * Bytes of workspace spexis_verify_attention needs for these host-side bounds (> 0 whenever

@@ -7,6 +7,7 @@
 #include <cmath>
 #include <cstdarg>
 #include <cstdio>
+#include <initializer_list>
 #include <mutex>
 #include <numeric>
 #include <string>
@@ -118,6 +119,39 @@ AcceptLayout accept_layout(int64_t B, int64_t V, int64_t max_k) {
   return l;
 }
 
+bool misaligned(std::initializer_list<const void*> ps) {
+  for (const void* p : ps)
+    if (reinterpret_cast<uintptr_t>(p) % 16 != 0) return true;
+  return false;
+}
+
+// The checks that both rotating appends share, and the launch.  max_position 0: no rotation (8-bit cache only).
+int rotate_append(const char* name, const spexis::RotateParams& p, int32_t max_query_len, void* stream) {
+  if (p.num_blocks <= 0 || p.hkv <= 0 || p.num_seqs < 0 || p.max_blocks <= 0 || p.total_tokens < 0 ||
+      max_query_len <= 0)
+    return fail(SPEXIS_ERR_INVALID_ARGUMENT, "%s: non-positive size", name);
+  if (bad_cache_shape(p.block_size, p.head_dim))
+    return fail(SPEXIS_ERR_UNSUPPORTED, "%s: block_size %d / head_dim %d not in {16,32} x {64,128}", name,
+                p.block_size, p.head_dim);
+  if (p.max_position > 0) {
+    if (p.rot < 16 || p.rot > p.head_dim || p.rot % 16 != 0)
+      return fail(SPEXIS_ERR_UNSUPPORTED, "%s: rotary_dim %d is not a multiple of 16 in 16..head_dim", name, p.rot);
+    if (p.style != SPEXIS_ROTARY_HALVES && p.style != SPEXIS_ROTARY_PAIRS)
+      return fail(SPEXIS_ERR_INVALID_ARGUMENT, "%s: style %d", name, p.style);
+  }
+  if ((p.q || p.q_out) && p.hq <= 0) return fail(SPEXIS_ERR_INVALID_ARGUMENT, "%s: non-positive size", name);
+  if (spexis::rotate_append_waves(p.total_tokens, p.block_size, p.num_seqs, p.hkv) + p.total_tokens >= (1ll << 31) ||
+      (int64_t)p.max_blocks * p.block_size >= (1ll << 31))
+    return fail(SPEXIS_ERR_UNSUPPORTED, "%s: more than 2^31 rows or slots", name);
+  if (p.num_seqs == 0 || p.total_tokens == 0) return ok();
+  if (!p.k_cache || !p.v_cache || !p.qsl || !p.seq_lens || !p.block_tables || !p.new_k || !p.new_v ||
+      (p.max_position > 0 && !p.cos_sin) || !p.q != !p.q_out)
+    return fail(SPEXIS_ERR_INVALID_ARGUMENT, "%s: null pointer", name);
+  if (misaligned({p.k_cache, p.v_cache, p.new_k, p.new_v, p.q, p.q_out, p.cos_sin}))
+    return fail(SPEXIS_ERR_INVALID_ARGUMENT, "%s: a pointer that is not 16-byte aligned", name);
+  return hip_result(spexis::launch_rotate_append(p, (hipStream_t)stream), name);
+}
+
 }  // namespace
 
 extern "C" {
@@ -145,6 +179,37 @@ int spexis_append_kv(void* k_cache, void* v_cache, int32_t num_blocks, int32_t n
                          num_blocks, num_kv_heads, block_size, head_dim, num_seqs, max_blocks_per_seq,
                          total_tokens};
   return hip_result(spexis::launch_append(p, (hipStream_t)stream), "spexis_append_kv");
+}
+
+int spexis_rotate_append_kv(void* k_cache, void* v_cache, int32_t num_blocks, int32_t num_kv_heads,
+                            int32_t block_size, int32_t head_dim, int32_t num_seqs, const int32_t* query_start_loc,
+                            const int32_t* seq_lens, const int32_t* block_tables, int32_t max_blocks_per_seq,
+                            int32_t total_tokens, int32_t max_query_len, const void* new_k, const void* new_v,
+                            const float* cos_sin, int32_t max_position, int32_t rotary_dim, int32_t style,
+                            const int32_t* positions, const void* q, int32_t num_q_heads, void* q_out, void* stream) {
+  const char* name = "spexis_rotate_append_kv";
+  if (max_position <= 0) return fail(SPEXIS_ERR_INVALID_ARGUMENT, "%s: non-positive size", name);
+  spexis::RotateParams p{k_cache, v_cache, nullptr, query_start_loc, seq_lens, block_tables, new_k, new_v, q, q_out,
+                         cos_sin, positions, num_blocks, num_kv_heads, block_size, head_dim, num_seqs,
+                         max_blocks_per_seq, total_tokens, num_q_heads, rotary_dim, max_position, style, 0, 0};
+  return rotate_append(name, p, max_query_len, stream);
+}
+
+int spexis_rotate_append_kv8(void* k_cache, void* v_cache, float* scales, int32_t num_blocks, int32_t num_kv_heads,
+                             int32_t block_size, int32_t head_dim, int32_t num_seqs, const int32_t* query_start_loc,
+                             const int32_t* seq_lens, const int32_t* block_tables, int32_t max_blocks_per_seq,
+                             int32_t total_tokens, int32_t max_query_len, const void* new_k, const void* new_v,
+                             const float* cos_sin, int32_t max_position, int32_t rotary_dim, int32_t style,
+                             const int32_t* positions, const void* q, int32_t num_q_heads, void* q_out,
+                             void* stream) {
+  const char* name = "spexis_rotate_append_kv8";
+  if (max_position < 0 || (max_position == 0 && (cos_sin || q || q_out || positions)))
+    return fail(SPEXIS_ERR_INVALID_ARGUMENT, "%s: a rotation without a table", name);
+  spexis::RotateParams p{k_cache, v_cache, scales, query_start_loc, seq_lens, block_tables, new_k, new_v, q, q_out,
+                         cos_sin, positions, num_blocks, num_kv_heads, block_size, head_dim, num_seqs,
+                         max_blocks_per_seq, total_tokens, num_q_heads, rotary_dim, max_position, style, 0, 0};
+  if (num_seqs > 0 && total_tokens > 0 && !scales) return fail(SPEXIS_ERR_INVALID_ARGUMENT, "%s: null pointer", name);
+  return rotate_append(name, p, max_query_len, stream);
 }
 
 size_t spexis_verify_attention_workspace_size(int32_t num_seqs, int32_t num_q_heads, int32_t num_kv_heads,

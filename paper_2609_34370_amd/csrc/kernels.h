@@ -17,6 +17,29 @@ struct AppendParams {
   int num_blocks, hkv, block_size, head_dim, num_seqs, max_blocks, total_tokens;
 };
 
+// The rotating appends (bf16 cache, or 8-bit cache with `scales`).
+struct RotateParams {
+  void* k_cache;
+  void* v_cache;
+  float* scales;             // [num_blocks][hkv][2], K and V; null: bf16 cache
+  const int32_t* qsl;
+  const int32_t* seq_lens;
+  const int32_t* block_tables;
+  const void* new_k;
+  const void* new_v;
+  const void* q;             // [T][hq][D] bf16, or null: no queries
+  void* q_out;
+  const float* cos_sin;      // [max_position][rot]: cosines, then sines; null: nothing turns
+  const int32_t* positions;  // [T], or null: the token's place in its sequence
+  int num_blocks, hkv, block_size, head_dim, num_seqs, max_blocks, total_tokens;
+  int hq, rot, max_position, style;   // style 0: elements i and i + rot/2 turn together; 1: 2i and 2i+1
+  int append_waves, query_waves;      // set by the launcher
+};
+// Waves that write rows: one per KV head and block index (csrc/rotate.hip).
+inline int64_t rotate_append_waves(int64_t tokens, int64_t block_size, int64_t num_seqs, int64_t hkv) {
+  return (tokens / block_size + 2 * num_seqs) * hkv;
+}
+
 constexpr int kAttnHdrInts = 8;           // per-wave header of the partial an item's first wave leaves
 constexpr int kAttnMinTilesPerWave = 2;   // floor of the even split (short batches)
 constexpr int kAttnMaxWaves = 1024;       // waves of the even split: one per SIMD of 256 CUs
@@ -199,6 +222,7 @@ constexpr int kAcceptMaxRounds = 8;  // test rounds: widths 2, 4, 8, ... cover m
 constexpr int kAcceptSub = 4096;     // vocab entries per partial result (one workgroup's share)
 
 hipError_t launch_append(const AppendParams& p, hipStream_t s);
+hipError_t launch_rotate_append(RotateParams p, hipStream_t s);
 hipError_t launch_attention(const AttnParams& p, hipStream_t s);
 
 hipError_t launch_select(const SelectParams& p, hipStream_t s);

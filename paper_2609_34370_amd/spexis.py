@@ -25,6 +25,7 @@ SPEXIS_ERR_WORKSPACE_TOO_SMALL = -3
 SPEXIS_ERR_HIP = -4
 SPEXIS_INPUT_PROBS = 0
 SPEXIS_INPUT_LOGITS = 1
+SPEXIS_ROTARY_HALVES, SPEXIS_ROTARY_PAIRS = 0, 1
 SPEXIS_ROW_OK, SPEXIS_ROW_EMPTY, SPEXIS_ROW_BAD_VALUE, SPEXIS_ROW_BAD_TOKEN, SPEXIS_ROW_INTERNAL = 0, 1, 2, 3, 4
 
 
@@ -57,6 +58,12 @@ def lib():
     L.spexis_last_error.argtypes, L.spexis_last_error.restype = [], ctypes.c_char_p
     L.spexis_append_kv.argtypes = [P, P, i32, i32, i32, i32, i32, P, P, P, i32, i32, i32, P, P, P]
     L.spexis_append_kv.restype = ctypes.c_int
+    L.spexis_rotate_append_kv.argtypes = [P, P, i32, i32, i32, i32, i32, P, P, P, i32, i32, i32, P, P, P, i32, i32, i32,
+                                          P, P, i32, P, P]
+    L.spexis_rotate_append_kv.restype = ctypes.c_int
+    L.spexis_rotate_append_kv8.argtypes = [P, P, P, i32, i32, i32, i32, i32, P, P, P, i32, i32, i32, P, P, P, i32, i32,
+                                           i32, P, P, i32, P, P]
+    L.spexis_rotate_append_kv8.restype = ctypes.c_int
     L.spexis_verify_attention_workspace_size.argtypes = [i32, i32, i32, i32, i32, i32, i32]
     L.spexis_verify_attention_workspace_size.restype = sz
     L.spexis_verify_attention.argtypes = [P, P, i32, i32, i32, i32, i32, P, P, P, i32, i32, i32, i32, P, i32, f32,
@@ -138,6 +145,38 @@ def spexis_append_kv(k_cache, v_cache, num_blocks, num_kv_heads, block_size, hea
         head_dim, query_start_loc.shape[0] - 1, _ptr(query_start_loc, torch.int32), _ptr(seq_lens, torch.int32),
         _ptr(block_tables, torch.int32), block_tables.shape[1], total_tokens, max_query_len,
         _ptr(new_k, torch.bfloat16), _ptr(new_v, torch.bfloat16), _stream(stream)))
+
+
+def _table(cos_sin):
+    """(rows, width) of a rotation table."""
+    return (0, 0) if cos_sin is None else tuple(cos_sin.shape)
+
+
+def spexis_rotate_append_kv(k_cache, v_cache, num_blocks, num_kv_heads, block_size, head_dim, query_start_loc,
+                            seq_lens, block_tables, total_tokens, max_query_len, new_k, new_v, cos_sin,
+                            style=SPEXIS_ROTARY_HALVES, positions=None, q=None, q_out=None, stream=None) -> None:
+    """cos_sin [max_position][rotary_dim] fp32; q and q_out [T][Hq][head_dim] bf16 (q_out may be q)."""
+    _check(lib().spexis_rotate_append_kv(
+        _ptr(k_cache, torch.bfloat16), _ptr(v_cache, torch.bfloat16), num_blocks, num_kv_heads, block_size,
+        head_dim, query_start_loc.shape[0] - 1, _ptr(query_start_loc, torch.int32), _ptr(seq_lens, torch.int32),
+        _ptr(block_tables, torch.int32), block_tables.shape[1], total_tokens, max_query_len,
+        _ptr(new_k, torch.bfloat16), _ptr(new_v, torch.bfloat16), _ptr(cos_sin, torch.float32), *_table(cos_sin), style,
+        _ptr(positions, torch.int32), _ptr(q, torch.bfloat16), 0 if q is None else q.shape[1],
+        _ptr(q_out, torch.bfloat16), _stream(stream)))
+
+
+def spexis_rotate_append_kv8(k_cache, v_cache, scales, num_blocks, num_kv_heads, block_size, head_dim,
+                             query_start_loc, seq_lens, block_tables, total_tokens, max_query_len, new_k, new_v,
+                             cos_sin=None, style=SPEXIS_ROTARY_HALVES, positions=None, q=None, q_out=None,
+                             stream=None) -> None:
+    """Pools torch.float8_e4m3fn, scales [num_blocks][Hkv][2] fp32; without cos_sin nothing is rotated."""
+    _check(lib().spexis_rotate_append_kv8(
+        _ptr(k_cache, torch.float8_e4m3fn), _ptr(v_cache, torch.float8_e4m3fn), _ptr(scales, torch.float32), num_blocks,
+        num_kv_heads, block_size, head_dim, query_start_loc.shape[0] - 1, _ptr(query_start_loc, torch.int32),
+        _ptr(seq_lens, torch.int32), _ptr(block_tables, torch.int32), block_tables.shape[1], total_tokens,
+        max_query_len, _ptr(new_k, torch.bfloat16), _ptr(new_v, torch.bfloat16), _ptr(cos_sin, torch.float32),
+        *_table(cos_sin), style, _ptr(positions, torch.int32), _ptr(q, torch.bfloat16), 0 if q is None else q.shape[1],
+        _ptr(q_out, torch.bfloat16), _stream(stream)))
 
 
 def spexis_verify_attention_workspace_size(num_seqs, num_q_heads, num_kv_heads, head_dim, max_query_len, max_seq_len,

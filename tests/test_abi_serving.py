@@ -1,0 +1,48 @@
+"""Refusals of the rotating appends, the attention over the 8-bit cache and the log probabilities: scalar arguments
+are checked on the host before any device call (no GPU needed)."""
+import ctypes
+import os
+
+import pytest
+import torch
+
+from paper_2609_34370_amd import spexis as sx
+
+pytestmark = [pytest.mark.skipif(not os.path.exists(sx.LIB_PATH), reason="libspexis.so not built"),
+              pytest.mark.skipif(torch.cuda.is_available(), reason="fake-pointer validation runs only without a GPU")]
+
+FAKE, ODD = ctypes.c_void_p(256), ctypes.c_void_p(264)
+INVALID, UNSUPPORTED, SMALL = sx.SPEXIS_ERR_INVALID_ARGUMENT, sx.SPEXIS_ERR_UNSUPPORTED, sx.SPEXIS_ERR_WORKSPACE_TOO_SMALL
+
+
+def rotate(in8, **kw):
+    a = dict(k=FAKE, v=FAKE, sc=FAKE, nb=10, hkv=2, bs=16, d=64, B=2, qsl=FAKE, sl=FAKE, bt=FAKE, mb=4, T=4, mq=2,
+             nk=FAKE, nv=FAKE, cs=FAKE, mp=100, rot=64, style=0, pos=None, q=FAKE, hq=8, qo=FAKE)
+    a.update(kw)
+    f = sx.lib().spexis_rotate_append_kv8 if in8 else sx.lib().spexis_rotate_append_kv
+    return f(a["k"], a["v"], *([a["sc"]] if in8 else []), a["nb"], a["hkv"], a["bs"], a["d"], a["B"], a["qsl"], a["sl"],
+             a["bt"], a["mb"], a["T"], a["mq"], a["nk"], a["nv"], a["cs"], a["mp"], a["rot"], a["style"], a["pos"], a["q"],
+             a["hq"], a["qo"], None)
+
+
+@pytest.mark.parametrize("in8", [False, True])
+def test_rotating_appends(in8):
+    for kw in (dict(nb=0), dict(hkv=0), dict(B=-1), dict(mb=0), dict(T=-1), dict(mq=0), dict(mp=0), dict(mp=-1), dict(style=2),
+               dict(hq=0), dict(k=None), dict(v=None), dict(qsl=None), dict(sl=None), dict(bt=None), dict(nk=None),
+               dict(nv=None), dict(cs=None), dict(q=None), dict(qo=None), dict(k=ODD), dict(nv=ODD), dict(cs=ODD),
+               dict(q=ODD), dict(qo=ODD)):
+        assert rotate(in8, **kw) == INVALID, kw
+        assert (b"kv8" in sx.lib().spexis_last_error()) == in8
+    for kw in (dict(bs=8), dict(bs=64), dict(d=96), dict(rot=8), dict(rot=24), dict(rot=80), dict(rot=0),
+               dict(T=2**30, hkv=64, mq=2**29), dict(mb=2**28)):
+        assert rotate(in8, **kw) == UNSUPPORTED, kw
+    assert rotate(in8, B=0, k=None, nk=None, q=None, qo=None, qsl=None) == 0
+    assert rotate(in8, T=0, k=None, nk=None, q=None, qo=None, sl=None, sc=None) == 0
+
+
+def test_8_bit_append_without_rotation():
+    assert rotate(True, sc=None) == INVALID
+    none = dict(cs=None, mp=0, rot=0, style=9, q=None, qo=None, hq=0)
+    assert rotate(True, T=0, **none) == 0
+    for kw in (dict(q=FAKE, qo=FAKE, hq=8), dict(pos=FAKE), dict(cs=FAKE)):
+        assert rotate(True, **dict(none, **kw)) == INVALID, kw

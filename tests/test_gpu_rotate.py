@@ -1,0 +1,207 @@
+"""The rotating appends against the 64-bit forms of oracle/serving.py.
+
+  * bf16 cache: V bit for bit; rotated rows within one rounding to bf16 (2^-8 of the value) and the two products
+    and the sum in fp32 before it (3 * 2^-24 of |x_a c| + |x_b s|);
+  * 8-bit cache: codes and scales bit for bit (the sum of two exact products is rounded once in 64 bits and once to
+    32 on both sides, and every scale is a power of two);
+  * every other element of the pools and scales as it was.
+"""
+import sys
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import serving as osv
+from paper_2609_34370_amd import spexis as sx
+from tests import layout_ref
+
+pytestmark = pytest.mark.gpu
+
+
+def say(*a):
+    print(*a, file=sys.stderr, flush=True)
+
+
+def batch(n, ctx, bs, seed, spare=2):
+    """qsl, S, tables over a randomly permuted pool with `spare` blocks that no sequence has."""
+    n, ctx = np.asarray(n, np.int32), np.asarray(ctx, np.int32)
+    qsl = np.zeros(len(n) + 1, np.int32)
+    qsl[1:] = np.cumsum(n)
+    S = ctx + n
+    nblk = -(-S // bs)
+    total = int(nblk.sum()) + spare
+    perm = np.random.default_rng(seed).permutation(total).astype(np.int32)
+    tables = np.zeros((len(n), max(int(nblk.max()), 1)), np.int32)
+    off = 0
+    for b in range(len(n)):
+        tables[b, : nblk[b]] = perm[off: off + nblk[b]]
+        off += nblk[b]
+    return qsl, S, tables, total
+
+
+def table(positions, rot, seed=0):
+    ang = np.arange(positions)[:, None] * 10000.0 ** (-np.arange(rot // 2) / (rot // 2))[None, :]
+    return np.concatenate([np.cos(ang), np.sin(ang)], axis=1).astype(np.float32)
+
+
+def bf16(shape, r, special=False):
+    x = torch.from_numpy(r.standard_normal(shape).astype(np.float32) * np.exp2(r.integers(-3, 4, shape)).astype(np.float32))
+    if special:
+        flat = x.view(-1)
+        at = torch.from_numpy(r.integers(0, flat.numel(), max(flat.numel() // 500, 3)))
+        flat[at] = torch.tensor([float("nan"), float("inf"), -float("inf"), 0.0, 3e38])[torch.arange(len(at)) % 5]
+    return x.to(torch.bfloat16)
+
+
+def dev(a, dtype=None):
+    return torch.as_tensor(a, dtype=dtype).cuda()
+
+
+def _magnitude(x, cs, positions, style):
+    """|x_a c| + |x_b s| of every element: its fp32 error is in units of it."""
+    r, a = cs.shape[1], np.abs(np.asarray(x, np.float64))
+    m = a.copy()
+    c, s = np.abs(cs[positions, : r // 2])[:, None], np.abs(cs[positions, r // 2:])[:, None]
+    i, j = (slice(0, r // 2), slice(r // 2, r)) if style == 0 else (slice(0, r, 2), slice(1, r, 2))
+    m[..., i], m[..., j] = a[..., i] * c + a[..., j] * s, a[..., j] * c + a[..., i] * s
+    return m
+
+
+def same_codes(got, want):
+    off = np.argwhere(got != want)
+    assert not len(off), (len(off), off[:8].tolist(), got[got != want][:8].tolist(), want[got != want][:8].tolist())
+
+
+SHAPES = [
+    # hq, hkv, D, bs, rot, style, new tokens, cached tokens
+    (8, 2, 64, 16, 32, 1, [5, 5, 5, 5], [32, 200, 47, 15]),
+    (32, 8, 128, 16, 128, 0, [5, 1, 0, 9, 3], [100, 15, 16, 0, 31]),
+    (28, 4, 128, 32, 128, 0, [9, 9, 1], [31, 500, 1]),
+    (3, 3, 64, 32, 64, 0, [33, 0, 1, 64, 7], [0, 5, 63, 32, 30]),
+    (7, 1, 128, 16, 16, 1, [130, 17], [3, 0]),
+    (4, 2, 128, 32, 64, 1, [1], [0]),
+    (16, 2, 64, 16, 48, 0, [1] * 70, list(range(70))),
+    (2, 2, 64, 16, 16, 0, [0, 0, 2, 0], [9, 0, 16, 4]),
+]
+
+
+@pytest.mark.parametrize("shape", range(len(SHAPES)))
+@pytest.mark.parametrize("given", [False, True])
+def test_bf16_cache(shape, given):
+    hq, hkv, D, bs, rot, style, n, ctx = SHAPES[shape]
+    r = np.random.default_rng(shape)
+    qsl, S, tables, blocks = batch(n, ctx, bs, shape)
+    T = int(qsl[-1])
+    say(f"[rotate bf16] {SHAPES[shape][:6]} T={T} positions given: {given}")
+    new_k, new_v, q = bf16((T, hkv, D), r), bf16((T, hkv, D), r), bf16((T, hq, D), r)
+    k0, v0 = (bf16((blocks * hkv * bs * D,), r) for _ in range(2))
+    cs = table(int(S.max()) + 90, rot)
+    at = osv.token_positions(qsl, S)
+    pos = r.integers(0, cs.shape[0], T) if given else at
+    k, v, qo = k0.cuda(), v0.cuda(), torch.zeros((T, hq, D), dtype=torch.bfloat16, device="cuda")
+    sx.spexis_rotate_append_kv(k, v, blocks, hkv, bs, D, dev(qsl), dev(S), dev(tables), T, int(max(n)), new_k.cuda(),
+                               new_v.cuda(), dev(cs), style=style, positions=dev(pos, torch.int32) if given else None,
+                               q=q.cuda(), q_out=qo)
+    torch.cuda.synchronize()
+
+    def near(got, x):
+        ref = osv.rotate(x.double().numpy(), cs, pos, style)
+        bound = 2.0 ** -8 * np.abs(ref) + 3 * 2.0 ** -24 * _magnitude(x.double().numpy(), cs, pos, style)
+        assert (np.abs(got - ref) <= bound).all()
+
+    near(qo.double().cpu().numpy(), q)
+    want_v = v0.view(torch.int16).numpy().copy()
+    got_k, seen = k.double().cpu().numpy(), np.zeros(k0.numel(), bool)
+    rows = np.zeros((T, hkv, D))
+    for b in range(len(n)):
+        lo, hi = int(qsl[b]), int(qsl[b + 1])
+        layout_ref.scatter_seq(want_v, "v", tables[b], new_v.view(torch.int16).numpy()[lo:hi], hkv, bs, D, start=int(ctx[b]))
+        layout_ref.scatter_seq(seen, "k", tables[b], np.ones((hi - lo, hkv, D), bool), hkv, bs, D, start=int(ctx[b]))
+        if hi > lo:
+            rows[lo:hi] = layout_ref.gather_seq(got_k, "k", tables[b], int(S[b]), hkv, bs, D)[int(ctx[b]):]
+    near(rows, new_k)
+    assert np.array_equal(v.view(torch.int16).cpu().numpy(), want_v)
+    assert np.array_equal(k.view(torch.int16).cpu().numpy()[~seen], k0.view(torch.int16).numpy()[~seen])
+
+
+def pool8(shape, r):
+    """Codes of every kind, NaN codes among them, and scales that are powers of two."""
+    return r.integers(0, 256, shape).astype(np.uint8)
+
+
+@pytest.mark.parametrize("shape", range(len(SHAPES)))
+@pytest.mark.parametrize("turned,special", [(True, False), (True, True), (False, True)])
+def test_8_bit_cache(shape, turned, special):
+    hq, hkv, D, bs, rot, style, n, ctx = SHAPES[shape]
+    r = np.random.default_rng(100 + shape)
+    qsl, S, tables, blocks = batch(n, ctx, bs, shape)
+    T = int(qsl[-1])
+    say(f"[rotate 8 bit] {SHAPES[shape][:6]} T={T} turned {turned} special values {special}")
+    new_k, new_v, q = bf16((T, hkv, D), r, special), bf16((T, hkv, D), r, special), bf16((T, hq, D), r)
+    codes = [pool8((blocks, bs, hkv, D), r) for _ in range(2)]
+    scales = np.exp2(r.integers(-9, 2, (blocks, hkv, 2))).astype(np.float32)
+    places = osv.places8(blocks, hkv, bs, D)
+    pools = []
+    for c, p in zip(codes, places):
+        flat = np.zeros(c.size, np.uint8)
+        flat[p] = c
+        pools.append(dev(flat).view(torch.float8_e4m3fn))
+    sc = dev(scales)
+    cs = table(int(S.max()) + 1, rot)
+    pos = osv.token_positions(qsl, S)
+    args = (blocks, hkv, bs, D, dev(qsl), dev(S), dev(tables), T, int(max(n)), new_k.cuda(), new_v.cuda())
+    qd = q.cuda()
+    rotation = dict(cos_sin=dev(cs), style=style, q=qd, q_out=qd) if turned else {}
+    with np.errstate(invalid="ignore", over="ignore"):
+        rk = osv.rotate(new_k.double().numpy(), cs, pos, style) if turned else new_k.double().numpy()
+        rk = rk.astype(np.float32)
+        for part, rows in enumerate((rk, new_v.float().numpy())):
+            one = scales[:, :, part].copy()
+            osv.append8(codes[part], one, qsl, S, tables, rows)
+            scales[:, :, part] = one
+    for again in range(2):   # the same rows once more change nothing
+        if again and turned:
+            rotation.update(q=None, q_out=None)
+        sx.spexis_rotate_append_kv8(*pools, sc, *args, **rotation)
+        torch.cuda.synchronize()
+        assert np.array_equal(sc.cpu().numpy(), scales)
+        for pool, c, p in zip(pools, codes, places):
+            same_codes(pool.view(torch.uint8).cpu().numpy()[p], c)
+    if turned:
+        ref = osv.rotate(q.double().numpy(), cs, pos, style)
+        bound = 2.0 ** -8 * np.abs(ref) + 3 * 2.0 ** -24 * _magnitude(q.double().numpy(), cs, pos, style)
+        assert (np.abs(qd.double().cpu().numpy() - ref) <= bound).all()
+
+
+def test_a_long_prompt_and_many_sequences():
+    """One prompt over hundreds of blocks, and more sequences than a wave has lanes (two probes of the search)."""
+    hq, hkv, D, bs, rot = 2, 2, 64, 16, 16
+    r = np.random.default_rng(5)
+    for n, ctx in (([3000], [77]), (r.integers(0, 4, 300).tolist(), r.integers(0, 40, 300).tolist())):
+        qsl, S, tables, blocks = batch(n, ctx, bs, 9)
+        T = int(qsl[-1])
+        new = [bf16((T, hkv, D), r) for _ in range(2)]
+        codes = [pool8((blocks, bs, hkv, D), r) for _ in range(2)]
+        scales = np.ones((blocks, hkv, 2), np.float32)
+        places = osv.places8(blocks, hkv, bs, D)
+        pools = [torch.zeros(c.size, dtype=torch.uint8, device="cuda") for c in codes]
+        for f, c, p in zip(pools, codes, places):
+            f.copy_(dev(c.reshape(-1)[np.argsort(p.reshape(-1))]))
+        pools = [f.view(torch.float8_e4m3fn) for f in pools]
+        sc = dev(scales)
+        sx.spexis_rotate_append_kv8(*pools, sc, blocks, hkv, bs, D, dev(qsl), dev(S), dev(tables), T, int(max(n)),
+                                    new[0].cuda(), new[1].cuda())
+        torch.cuda.synchronize()
+        for part in range(2):
+            one = scales[:, :, part].copy()
+            osv.append8(codes[part], one, qsl, S, tables, new[part].double().numpy())
+            assert np.array_equal(sc[:, :, part].cpu().numpy(), one)
+            same_codes(pools[part].view(torch.uint8).cpu().numpy()[places[part]], codes[part])
+
+
+def test_without_new_tokens_nothing_is_touched():
+    sx.spexis_rotate_append_kv8(None, None, None, 4, 2, 16, 64, dev(np.zeros(3, np.int32)), None, dev(np.zeros((2, 1), np.int32)),
+                                0, 1, None, None)
+    sx.spexis_rotate_append_kv(None, None, 4, 2, 16, 64, dev(np.zeros(3, np.int32)), None, dev(np.zeros((2, 1), np.int32)),
+                               0, 1, None, None, dev(table(1, 16)))
