@@ -12,6 +12,7 @@
  *   spexis_rotate_append_kv  the same, with the rotary position embedding of q and k on the way
  *   spexis_rotate_append_kv8  the same into a cache held in 8 bits with a scale per block and head
  *   spexis_verify_attention  causal grouped-query attention of those rows over the cache
+ *   spexis_verify_attention_kv8  the same over the 8-bit cache
  *   spexis_accept            ratio tests, residual / bonus sampling, outputs
  *   spexis_lm_head           logits = h W^T with fused softmax statistics (next to accept)
  *   spexis_lm_head_gather    the same, also gathering each row's logit at a given column
@@ -245,6 +246,33 @@ int spexis_verify_attention(const void* k_cache, const void* v_cache, int32_t nu
                             int32_t num_q_heads, float scale, void* out,
                             int32_t kv_chunk_tokens, void* workspace, size_t workspace_bytes,
                             void* stream);
+
+/* Bytes of workspace spexis_verify_attention_kv8 needs (> 0 whenever the sizes are valid, else 0). */
+size_t spexis_verify_attention_kv8_workspace_size(int32_t num_seqs, int32_t num_q_heads,
+                                                  int32_t num_kv_heads, int32_t head_dim,
+                                                  int32_t max_query_len, int32_t max_seq_len,
+                                                  int32_t kv_chunk_tokens);
+
+/*
+ * spexis_verify_attention_kv8 -- spexis_verify_attention over the 8-bit cache: k[b,t,g] and v[b,t,g] are
+ * code * scales[block][g][K or V].  Codes are widened to bf16, which holds them and their scale exactly; products
+ * accumulate in fp32, the softmax weights are rounded to bf16 in front of the product with V as there.
+ *   scales  [num_blocks][Hkv][2] fp32, positive powers of two (spexis_rotate_append_kv8 writes no others; of any
+ *           other value only the exponent counts); 8-byte entries, 16-byte aligned like the pools, q, out and
+ *           workspace
+ *   workspace >= spexis_verify_attention_kv8_workspace_size(...) bytes
+ * A NaN code of a key that a query token sees makes its output NaN; slots behind the sequence may hold anything.
+ * Other arguments, supported shapes and errors as spexis_verify_attention.
+ */
+int spexis_verify_attention_kv8(const void* k_cache, const void* v_cache, const float* scales,
+                                int32_t num_blocks, int32_t num_kv_heads, int32_t block_size,
+                                int32_t head_dim, int32_t num_seqs, const int32_t* query_start_loc,
+                                const int32_t* seq_lens, const int32_t* block_tables,
+                                int32_t max_blocks_per_seq, int32_t total_tokens,
+                                int32_t max_query_len, int32_t max_seq_len, const void* q,
+                                int32_t num_q_heads, float scale, void* out,
+                                int32_t kv_chunk_tokens, void* workspace, size_t workspace_bytes,
+                                void* stream);
 
 /*
  * spexis_softmax_rows -- the probabilities p = softmax(logits / T) and q that the acceptance

@@ -109,10 +109,11 @@ def append8(codes, scales, qsl, seq_lens, tables, rows):
 
 
 def attention8(k_codes, v_codes, scales, qsl, seq_lens, tables, q, scale) -> np.ndarray:
-    """Causal attention of every query token over its sequence; q [T][Hq][D]; scales [block][Hkv][2]."""
+    """Causal attention of every query token over its sequence; q [T][Hq][D]; scales [block][Hkv][2].  Also the
+    weighted mean of |v| and the largest sum of |q_d k_d| * scale of a key, which errors are measured in."""
     hkv, D, bs = k_codes.shape[2], k_codes.shape[3], k_codes.shape[1]
     q = np.asarray(q, dtype=np.float64)
-    out = np.zeros(q.shape)
+    out, mean, most = np.zeros(q.shape), np.zeros(q.shape), np.zeros(q.shape[:2])
     G = q.shape[1] // hkv
     for b in range(len(seq_lens)):
         S = int(seq_lens[b])
@@ -128,8 +129,11 @@ def attention8(k_codes, v_codes, scales, qsl, seq_lens, tables, q, scale) -> np.
             for h in range(q.shape[1]):
                 x = k[:seen, h // G] @ q[int(qsl[b]) + j, h] * scale
                 p = np.exp(x - x.max())
-                out[int(qsl[b]) + j, h] = p @ v[:seen, h // G] / p.sum()
-    return out
+                at = int(qsl[b]) + j, h
+                out[at] = p @ v[:seen, h // G] / p.sum()
+                mean[at] = p @ np.abs(v[:seen, h // G]) / p.sum()
+                most[at] = (np.abs(k[:seen, h // G]) @ np.abs(q[at])).max() * abs(scale)
+    return out, mean, most
 
 
 # ------------------------------------------------------------------ log probabilities

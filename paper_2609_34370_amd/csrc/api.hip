@@ -152,6 +152,79 @@ int rotate_append(const char* name, const spexis::RotateParams& p, int32_t max_q
   return hip_result(spexis::launch_rotate_append(p, (hipStream_t)stream), name);
 }
 
+// Both attention calls: their checks, their shares and the launch.
+int verify_attention(const char* name, bool in8, const void* k_cache, const void* v_cache, const float* scales, int32_t num_blocks,
+                     int32_t num_kv_heads, int32_t block_size, int32_t head_dim,
+                     int32_t num_seqs, const int32_t* query_start_loc,
+                     const int32_t* seq_lens, const int32_t* block_tables,
+                     int32_t max_blocks_per_seq, int32_t total_tokens,
+                     int32_t max_query_len, int32_t max_seq_len, const void* q,
+                     int32_t num_q_heads, float scale, void* out,
+                     int32_t kv_chunk_tokens, void* workspace, size_t workspace_bytes,
+                     void* stream) {
+  if (num_blocks <= 0 || num_kv_heads <= 0 || num_q_heads <= 0 || num_seqs < 0 || max_blocks_per_seq <= 0 ||
+      total_tokens < 0 || max_query_len <= 0 || max_seq_len <= 0 || kv_chunk_tokens < 0)
+    return fail(SPEXIS_ERR_INVALID_ARGUMENT, "%s: non-positive size", name);
+  if (num_q_heads % num_kv_heads != 0)
+    return fail(SPEXIS_ERR_INVALID_ARGUMENT, "%s: %d query heads not a multiple of %d KV heads",
+                name, num_q_heads, num_kv_heads);
+  if (!std::isfinite(scale)) return fail(SPEXIS_ERR_INVALID_ARGUMENT, "%s: scale not finite", name);
+  if (bad_cache_shape(block_size, head_dim))
+    return fail(SPEXIS_ERR_UNSUPPORTED, "%s: block_size %d / head_dim %d not in {16,32} x {64,128}",
+                name, block_size, head_dim);
+  const int group = num_q_heads / num_kv_heads;
+  if ((int64_t)group * max_query_len > kMaxRows)
+    return fail(SPEXIS_ERR_UNSUPPORTED, "%s: (Hq/Hkv)*max_query_len = %d > %d",
+                name, group * max_query_len, kMaxRows);
+  if ((int64_t)max_blocks_per_seq * block_size < max_query_len)
+    return fail(SPEXIS_ERR_INVALID_ARGUMENT, "%s: block tables hold fewer slots than a query", name);
+  // every tile index of the stream fits in 32 bits
+  if ((int64_t)num_seqs * (((int64_t)max_blocks_per_seq * block_size + 31) / 32) >= (1ll << 31))
+    return fail(SPEXIS_ERR_UNSUPPORTED, "%s: more than 2^31 key tiles", name);
+  if (num_seqs == 0 || total_tokens == 0) return ok();
+  if (!k_cache || !v_cache || !query_start_loc || !seq_lens || !block_tables || !q || !out || (in8 && !scales))
+    return fail(SPEXIS_ERR_INVALID_ARGUMENT, "%s: null pointer", name);
+  if (in8 && misaligned({k_cache, v_cache, scales, q, out, workspace}))
+    return fail(SPEXIS_ERR_INVALID_ARGUMENT, "%s: a pointer that is not 16-byte aligned", name);
+  if (q == out) return fail(SPEXIS_ERR_INVALID_ARGUMENT, "%s: out aliases q", name);
+  int tpw, nshares, nwaves, skew;
+  if (!attn_waves(num_seqs, num_kv_heads, max_seq_len, kv_chunk_tokens, &tpw, &nshares, &nwaves, &skew))
+    return fail(SPEXIS_ERR_UNSUPPORTED, "%s: kv_chunk_tokens %d asks for too many waves",
+                name, kv_chunk_tokens);
+  const size_t need = spexis_verify_attention_workspace_size(num_seqs, num_q_heads, num_kv_heads, head_dim,
+                                                             max_query_len, max_seq_len, kv_chunk_tokens);
+  if (!workspace || workspace_bytes < need)
+    return fail(SPEXIS_ERR_WORKSPACE_TOO_SMALL, "%s: workspace %zu bytes < %zu needed",
+                name, workspace_bytes, need);
+  spexis::AttnParams p{};
+  p.k_cache = k_cache;
+  p.v_cache = v_cache;
+  p.qsl = query_start_loc;
+  p.seq_lens = seq_lens;
+  p.block_tables = block_tables;
+  p.q = q;
+  p.out = out;
+  p.ws = static_cast<float*>(workspace);
+  p.num_blocks = num_blocks;
+  p.hkv = num_kv_heads;
+  p.block_size = block_size;
+  p.head_dim = head_dim;
+  p.num_seqs = num_seqs;
+  p.max_blocks = max_blocks_per_seq;
+  p.total_tokens = total_tokens;
+  p.hq = num_q_heads;
+  p.group = group;
+  p.rmax = group * max_query_len;
+  p.least = kv_chunk_tokens > 0 ? spexis::AttnLeast{tpw, INT32_MAX, 0, INT32_MAX, INT32_MAX}
+                                : spexis::attn_least(num_seqs, num_kv_heads, head_dim, p.rmax);
+  p.nshares = nshares;
+  p.nwaves = nwaves;
+  p.skew = skew;
+  p.scale_log2e = (float)((double)scale * 1.4426950408889634);
+  p.scales = scales;
+  return hip_result(in8 ? spexis::launch_attention8(p, (hipStream_t)stream) : spexis::launch_attention(p, (hipStream_t)stream), name);
+}
+
 }  // namespace
 
 extern "C" {
@@ -232,64 +305,30 @@ int spexis_verify_attention(const void* k_cache, const void* v_cache, int32_t nu
                             int32_t num_q_heads, float scale, void* out,
                             int32_t kv_chunk_tokens, void* workspace, size_t workspace_bytes,
                             void* stream) {
-  if (num_blocks <= 0 || num_kv_heads <= 0 || num_q_heads <= 0 || num_seqs < 0 || max_blocks_per_seq <= 0 ||
-      total_tokens < 0 || max_query_len <= 0 || max_seq_len <= 0 || kv_chunk_tokens < 0)
-    return fail(SPEXIS_ERR_INVALID_ARGUMENT, "spexis_verify_attention: non-positive size");
-  if (num_q_heads % num_kv_heads != 0)
-    return fail(SPEXIS_ERR_INVALID_ARGUMENT, "spexis_verify_attention: %d query heads not a multiple of %d KV heads",
-                num_q_heads, num_kv_heads);
-  if (!std::isfinite(scale)) return fail(SPEXIS_ERR_INVALID_ARGUMENT, "spexis_verify_attention: scale not finite");
-  if (bad_cache_shape(block_size, head_dim))
-    return fail(SPEXIS_ERR_UNSUPPORTED, "spexis_verify_attention: block_size %d / head_dim %d not in {16,32} x {64,128}",
-                block_size, head_dim);
-  const int group = num_q_heads / num_kv_heads;
-  if ((int64_t)group * max_query_len > kMaxRows)
-    return fail(SPEXIS_ERR_UNSUPPORTED, "spexis_verify_attention: (Hq/Hkv)*max_query_len = %d > %d",
-                group * max_query_len, kMaxRows);
-  if ((int64_t)max_blocks_per_seq * block_size < max_query_len)
-    return fail(SPEXIS_ERR_INVALID_ARGUMENT, "spexis_verify_attention: block tables hold fewer slots than a query");
-  // every tile index of the stream fits in 32 bits
-  if ((int64_t)num_seqs * (((int64_t)max_blocks_per_seq * block_size + 31) / 32) >= (1ll << 31))
-    return fail(SPEXIS_ERR_UNSUPPORTED, "spexis_verify_attention: more than 2^31 key tiles");
-  if (num_seqs == 0 || total_tokens == 0) return ok();
-  if (!k_cache || !v_cache || !query_start_loc || !seq_lens || !block_tables || !q || !out)
-    return fail(SPEXIS_ERR_INVALID_ARGUMENT, "spexis_verify_attention: null pointer");
-  if (q == out) return fail(SPEXIS_ERR_INVALID_ARGUMENT, "spexis_verify_attention: out aliases q");
-  int tpw, nshares, nwaves, skew;
-  if (!attn_waves(num_seqs, num_kv_heads, max_seq_len, kv_chunk_tokens, &tpw, &nshares, &nwaves, &skew))
-    return fail(SPEXIS_ERR_UNSUPPORTED, "spexis_verify_attention: kv_chunk_tokens %d asks for too many waves",
-                kv_chunk_tokens);
-  const size_t need = spexis_verify_attention_workspace_size(num_seqs, num_q_heads, num_kv_heads, head_dim,
-                                                             max_query_len, max_seq_len, kv_chunk_tokens);
-  if (!workspace || workspace_bytes < need)
-    return fail(SPEXIS_ERR_WORKSPACE_TOO_SMALL, "spexis_verify_attention: workspace %zu bytes < %zu needed",
-                workspace_bytes, need);
-  spexis::AttnParams p{};
-  p.k_cache = k_cache;
-  p.v_cache = v_cache;
-  p.qsl = query_start_loc;
-  p.seq_lens = seq_lens;
-  p.block_tables = block_tables;
-  p.q = q;
-  p.out = out;
-  p.ws = static_cast<float*>(workspace);
-  p.num_blocks = num_blocks;
-  p.hkv = num_kv_heads;
-  p.block_size = block_size;
-  p.head_dim = head_dim;
-  p.num_seqs = num_seqs;
-  p.max_blocks = max_blocks_per_seq;
-  p.total_tokens = total_tokens;
-  p.hq = num_q_heads;
-  p.group = group;
-  p.rmax = group * max_query_len;
-  p.least = kv_chunk_tokens > 0 ? spexis::AttnLeast{tpw, INT32_MAX, 0, INT32_MAX, INT32_MAX}
-                                : spexis::attn_least(num_seqs, num_kv_heads, head_dim, p.rmax);
-  p.nshares = nshares;
-  p.nwaves = nwaves;
-  p.skew = skew;
-  p.scale_log2e = (float)((double)scale * 1.4426950408889634);
-  return hip_result(spexis::launch_attention(p, (hipStream_t)stream), "spexis_verify_attention");
+  return verify_attention("spexis_verify_attention", false, k_cache, v_cache, nullptr, num_blocks, num_kv_heads, block_size, head_dim, num_seqs,
+                          query_start_loc, seq_lens, block_tables, max_blocks_per_seq, total_tokens, max_query_len,
+                          max_seq_len, q, num_q_heads, scale, out, kv_chunk_tokens, workspace, workspace_bytes, stream);
+}
+
+size_t spexis_verify_attention_kv8_workspace_size(int32_t num_seqs, int32_t num_q_heads, int32_t num_kv_heads,
+                                                  int32_t head_dim, int32_t max_query_len, int32_t max_seq_len,
+                                                  int32_t kv_chunk_tokens) {
+  return spexis_verify_attention_workspace_size(num_seqs, num_q_heads, num_kv_heads, head_dim, max_query_len,
+                                                max_seq_len, kv_chunk_tokens);
+}
+
+int spexis_verify_attention_kv8(const void* k_cache, const void* v_cache, const float* scales, int32_t num_blocks,
+                                int32_t num_kv_heads, int32_t block_size, int32_t head_dim,
+                                int32_t num_seqs, const int32_t* query_start_loc,
+                                const int32_t* seq_lens, const int32_t* block_tables,
+                                int32_t max_blocks_per_seq, int32_t total_tokens,
+                                int32_t max_query_len, int32_t max_seq_len, const void* q,
+                                int32_t num_q_heads, float scale, void* out,
+                                int32_t kv_chunk_tokens, void* workspace, size_t workspace_bytes,
+                                void* stream) {
+  return verify_attention("spexis_verify_attention_kv8", true, k_cache, v_cache, scales, num_blocks, num_kv_heads, block_size, head_dim, num_seqs,
+                          query_start_loc, seq_lens, block_tables, max_blocks_per_seq, total_tokens, max_query_len,
+                          max_seq_len, q, num_q_heads, scale, out, kv_chunk_tokens, workspace, workspace_bytes, stream);
 }
 
 int spexis_softmax_rows(const float* logits, float* probs, int64_t rows, int32_t vocab, float temperature,

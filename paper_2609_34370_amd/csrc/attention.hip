@@ -28,104 +28,9 @@
 //                                           bits 2 and 3 swapped, so the 8 keys a lane needs
 //                                           for k-step s are 16 contiguous bytes; B = P^T is
 //                                           exactly the lane's score values 8s..8s+7.
-#include "common.h"
-#include "kernels.h"
+#include "attention.h"
 
 namespace spexis {
-
-// Lane l and lane l ^ 32 combined, in one cross-half lane swap (v_permlane32_swap): the swap of a
-// value with itself leaves the lower half's value in the first result and the upper half's in the
-// second, in every lane.
-__device__ __forceinline__ float halves_max(float v) {
-  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
-}
-__device__ __forceinline__ float halves_sum(float v) {
-  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
-}
-
-constexpr float kNegBig = -1.0e30f;   // finite "minus infinity" of the running maxima
-
-// acc[mt] *= alpha (alpha per lane: the lane's query row), in place on the registers that hold the
-// accumulators.  Written out because otherwise the compiler keeps a second copy of every
-// accumulator in vector registers, refreshed by one v_accvgpr_read per accumulator on every tile,
-// for the rare tiles that take this path.  The hazard checks do not look inside inline assembly:
-// the leading s_nops give an accumulator's last MFMA its 18+ wait states before the first read
-// (this is its own basic block, so no MFMA is scheduled in between), the trailing one covers the
-// last write before the next MFMA reads it as its C operand.
-template <int MT>
-__device__ __forceinline__ void scale_acc(f32x16 (&acc)[MT], float alpha) {
-  asm volatile("s_nop 7\n\ts_nop 7\n\ts_nop 7");
-#pragma unroll
-  for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      float v = acc[mt][e], t;
-      asm volatile("v_accvgpr_read_b32 %1, %0\n\tv_mul_f32 %1, %1, %2\n\tv_accvgpr_write_b32 %0, %1"
-                   : "+a"(v), "=&v"(t)
-                   : "v"(alpha));
-      acc[mt][e] = v;
-    }
-  asm volatile("s_nop 4");
-}
-constexpr float kLazy = 8.0f;         // base-2 headroom before the running maximum moves
-constexpr int kWaitVmcnt0 = 0x0F70;   // s_waitcnt operand: vmcnt(0), expcnt and lgkmcnt not waited
-
-// Read-only view of an int32 array: loads through it at wave-uniform addresses become scalar
-// loads, counted apart from the vector loads of the tiles.
-typedef const __attribute__((address_space(4))) int32_t sint32;
-
-struct SeqGeo {
-  int q0, n, S, nt;   // first query token, query tokens, keys, 32-key tiles (0: no query)
-};
-
-// Geometry of sequence b, clamped so that every address derived from it stays in its buffer.
-template <typename Ptr>
-__device__ __forceinline__ SeqGeo seq_geo(const AttnParams& p, Ptr qsl, Ptr seq_lens, int b) {
-  SeqGeo g;
-  g.q0 = clampi(qsl[b], 0, p.total_tokens);
-  const int q1 = clampi(qsl[b + 1], g.q0, p.total_tokens);
-  g.n = min(q1 - g.q0, p.rmax / p.group);
-  g.S = clampi(seq_lens[b], max(g.n, 1), p.max_blocks * p.block_size);
-  g.nt = g.n >= 1 ? (g.S + 31) >> 5 : 0;
-  return g;
-}
-
-// Position in a head's tile stream: sequence, tile of the sequence, and the sequence's size.
-struct Cursor {
-  int b, t, nt, S;
-};
-
-__device__ __forceinline__ void advance(const AttnParams& p, Cursor& c) {
-  if (++c.t < c.nt) return;
-  c.t = 0;
-  SeqGeo g;
-  do {
-    if (c.b + 1 >= p.num_seqs) return;   // never past the stream's end; stay on a valid item
-    ++c.b;
-    g = seq_geo(p, (sint32*)p.qsl, (sint32*)p.seq_lens, c.b);
-  } while (g.nt == 0);
-  c.nt = g.nt;
-  c.S = g.S;
-}
-
-// Share geometry of a head's tile stream: shares pair up, shares 2j and 2j+1 covering tiles
-// [2jP, 2(j+1)P), the first (the wave on an even XCD) P + dlt of them and the second P - dlt.
-// dlt = 0 gives equal shares of P.
-// P of a head's `total` tiles: an even split over its shares, but at least attn_least_tiles each.
-__device__ __forceinline__ int share_tiles(const AttnParams& p, int total) {
-  return max(attn_least_tiles(p.least, total), (total + p.nshares - 1) / p.nshares);
-}
-__device__ __forceinline__ int share_delta(int P, int skew) { return (int)(((int64_t)P * skew) >> 10); }
-__device__ __forceinline__ int64_t share_first(int s, int P, int dlt) {
-  return (int64_t)(s >> 1) * 2 * P + (s & 1) * (P + dlt);
-}
-__device__ __forceinline__ int share_size(int s, int P, int dlt) { return (s & 1) ? P - dlt : P + dlt; }
-__device__ __forceinline__ int share_of(int g, int P, int dlt) {
-  const int j = g / (2 * P);
-  return 2 * j + (g - 2 * P * j >= P + dlt ? 1 : 0);
-}
 
 template <int D, int BS, int NT>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1)))
@@ -162,61 +67,10 @@ void verify_attn_kernel(AttnParams p) {
   const int h = h_, share = s_;
   if (share >= p.nshares) return no_share();
 
-  // ---- this wave's share [g0, g0 + cnt) of head h's tile stream
-  int total, P, b0 = 0, f0 = 0;   // P: the tiles of a share
-  Cursor start;
-  if (p.num_seqs <= kWave) {
-    // one pass: lane b holds sequence b's geometry; the share start is read from the lanes
-    const SeqGeo gl = lane < p.num_seqs ? seq_geo(p, p.qsl, p.seq_lens, lane) : SeqGeo{0, 0, 0, 0};
-    const int incl = wave_incl_scan_i32(gl.nt, lane);
-    total = __builtin_amdgcn_readlane(incl, kWave - 1);   // < 2^31 (host)
-    P = share_tiles(p, total);
-    if (share_first(share, P, share_delta(P, p.skew)) >= total) return no_share();
-    const int g0 = (int)share_first(share, P, share_delta(P, p.skew));
-    const uint64_t hit = __builtin_amdgcn_ballot_w64(incl > g0);
-    if (hit == 0) return no_share();
-    const int l0 = __builtin_ctzll(hit);
-    b0 = l0;
-    f0 = __builtin_amdgcn_readlane(incl - gl.nt, l0);
-    start.b = b0;
-    start.nt = __builtin_amdgcn_readlane(gl.nt, l0);
-    start.S = __builtin_amdgcn_readlane(gl.S, l0);
-    start.t = g0 - f0;
-  } else {
-    int per_lane = 0;
-    for (int base = 0; base < p.num_seqs; base += kWave)
-      if (base + lane < p.num_seqs) per_lane += seq_geo(p, p.qsl, p.seq_lens, base + lane).nt;
-    total = __builtin_amdgcn_readfirstlane(wave_sum_i32(per_lane));   // < 2^31 (host)
-    P = share_tiles(p, total);
-    if (share_first(share, P, share_delta(P, p.skew)) >= total) return no_share();
-    const int g0 = (int)share_first(share, P, share_delta(P, p.skew));
-    // the sequence holding tile g0, and the stream index of its first tile
-    int before = 0;
-    for (int base = 0; base < p.num_seqs; base += kWave) {
-      const int b = base + lane;
-      const int v = b < p.num_seqs ? seq_geo(p, p.qsl, p.seq_lens, b).nt : 0;
-      const int incl = wave_incl_scan_i32(v, lane);
-      const uint64_t hit = __builtin_amdgcn_ballot_w64(before + incl > g0);
-      if (hit != 0) {
-        const int l0 = __builtin_ctzll(hit);
-        b0 = base + l0;
-        f0 = before + __builtin_amdgcn_readlane(incl - v, l0);
-        break;
-      }
-      before += __builtin_amdgcn_readlane(incl, kWave - 1);
-    }
-    b0 = __builtin_amdgcn_readfirstlane(b0);
-    f0 = __builtin_amdgcn_readfirstlane(f0);
-    const SeqGeo g = seq_geo(p, (sint32*)p.qsl, (sint32*)p.seq_lens, b0);
-    if (g.nt == 0 || g0 < f0 || g0 - f0 >= g.nt) return no_share();   // inputs changed under us
-    start.b = b0;
-    start.nt = g.nt;
-    start.S = g.S;
-    start.t = g0 - f0;
-  }
-  const int dlt = share_delta(P, p.skew);
-  const int g0 = (int)share_first(share, P, dlt);
-  const int cnt = min(share_size(share, P, dlt), total - g0);
+  Share sh;   // this wave's share [g0, g0 + cnt) of head h's tile stream
+  if (!find_share(p, share, lane, sh)) return no_share();
+  const int P = sh.P, dlt = sh.dlt, g0 = sh.g0, cnt = sh.cnt;
+  const Cursor start = sh.start;
 
   const uint16_t* kc = reinterpret_cast<const uint16_t*>(p.k_cache);
   const uint16_t* vc = reinterpret_cast<const uint16_t*>(p.v_cache);
@@ -758,11 +612,8 @@ __global__ __launch_bounds__(512) void attn_merge_wide_kernel(AttnParams p, int 
   __builtin_nontemporal_store(w, reinterpret_cast<u32x4*>(orow));
 }
 
-template <int D, int BS, int NT>
-static hipError_t launch_attn_t(const AttnParams& p, hipStream_t s) {
-  hipLaunchKernelGGL((verify_attn_kernel<D, BS, NT>), dim3((unsigned)(p.nwaves / 4)), dim3(256), 0, s, p);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
+template <int D>
+static hipError_t launch_merge_t(const AttnParams& p, hipStream_t s) {
   // Few, long items: at least kMergeWideShares shares per sequence (the call, wide merge against
   // attn_merge_kernel: 30.3 against 60.7 us at one sequence of 16384 keys, 25.7 against 30.8 at 4 of
   // 1000-4096, 30.2 against 32.0 at 8 of them, where there are 16 shares a sequence; 45.4 against 43.0
@@ -780,6 +631,18 @@ static hipError_t launch_attn_t(const AttnParams& p, hipStream_t s) {
   else
     hipLaunchKernelGGL((attn_merge_kernel<D, 4>), dim3((unsigned)p.nwaves), dim3(512), 0, s, p);
   return hipGetLastError();
+}
+
+hipError_t launch_attn_merge(const AttnParams& p, hipStream_t s) {
+  return p.head_dim == 128 ? launch_merge_t<128>(p, s) : launch_merge_t<64>(p, s);
+}
+
+template <int D, int BS, int NT>
+static hipError_t launch_attn_t(const AttnParams& p, hipStream_t s) {
+  hipLaunchKernelGGL((verify_attn_kernel<D, BS, NT>), dim3((unsigned)(p.nwaves / 4)), dim3(256), 0, s, p);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  return launch_merge_t<D>(p, s);
 }
 
 template <int D, int BS>

@@ -105,6 +105,7 @@ struct AttnParams {
   int nwaves;            // waves of the attention grid (4 per workgroup, >= nshares * hkv)
   int skew;              // 0: equal shares; else paired shares, the even-XCD one skew/1024 longer
   float scale_log2e;     // scale * log2(e): scores live in the base-2 domain
+  const float* scales;   // 8-bit cache: [num_blocks][hkv][2], K and V
 };
 
 // One partial slot: [rmax][D] unnormalised output, then rmax reference maxima and rmax sums.
@@ -224,6 +225,9 @@ constexpr int kAcceptSub = 4096;     // vocab entries per partial result (one wo
 hipError_t launch_append(const AppendParams& p, hipStream_t s);
 hipError_t launch_rotate_append(RotateParams p, hipStream_t s);
 hipError_t launch_attention(const AttnParams& p, hipStream_t s);
+hipError_t launch_attention8(const AttnParams& p, hipStream_t s);   // 8-bit cache (p.scales)
+// The partials of the items cut between shares, combined (after either attention kernel).
+hipError_t launch_attn_merge(const AttnParams& p, hipStream_t s);
 
 hipError_t launch_select(const SelectParams& p, hipStream_t s);
 hipError_t launch_lookahead(const LookaheadParams& p, hipStream_t s);

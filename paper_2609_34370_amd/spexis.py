@@ -69,6 +69,11 @@ def lib():
     L.spexis_verify_attention.argtypes = [P, P, i32, i32, i32, i32, i32, P, P, P, i32, i32, i32, i32, P, i32, f32,
                                           P, i32, P, sz, P]
     L.spexis_verify_attention.restype = ctypes.c_int
+    L.spexis_verify_attention_kv8_workspace_size.argtypes = [i32, i32, i32, i32, i32, i32, i32]
+    L.spexis_verify_attention_kv8_workspace_size.restype = sz
+    L.spexis_verify_attention_kv8.argtypes = [P, P, P, i32, i32, i32, i32, i32, P, P, P, i32, i32, i32, i32, P, i32, f32,
+                                              P, i32, P, sz, P]
+    L.spexis_verify_attention_kv8.restype = ctypes.c_int
     L.spexis_softmax_rows.argtypes = [P, P, i64, i32, f32, P]
     L.spexis_softmax_rows.restype = ctypes.c_int
     L.spexis_accept_workspace_size.argtypes = [i32, i32, i32]
@@ -195,6 +200,24 @@ def spexis_verify_attention(k_cache, v_cache, num_blocks, num_kv_heads, block_si
         _ptr(block_tables, torch.int32), block_tables.shape[1], total_tokens, max_query_len, max_seq_len,
         _ptr(q, torch.bfloat16), num_q_heads, ctypes.c_float(scale), _ptr(out, torch.bfloat16), kv_chunk_tokens,
         _ptr(workspace), ws_bytes, _stream(stream)))
+
+
+def spexis_verify_attention_kv8_workspace_size(num_seqs, num_q_heads, num_kv_heads, head_dim, max_query_len, max_seq_len,
+                                               kv_chunk_tokens=0) -> int:
+    return int(lib().spexis_verify_attention_kv8_workspace_size(num_seqs, num_q_heads, num_kv_heads, head_dim,
+                                                                max_query_len, max_seq_len, kv_chunk_tokens))
+
+
+def spexis_verify_attention_kv8(k_cache, v_cache, scales, num_blocks, num_kv_heads, block_size, head_dim,
+                                query_start_loc, seq_lens, block_tables, total_tokens, max_query_len, max_seq_len, q,
+                                num_q_heads, scale, out, workspace, kv_chunk_tokens=0, stream=None) -> None:
+    """Pools torch.float8_e4m3fn, scales [num_blocks][Hkv][2] fp32 (powers of two)."""
+    _check(lib().spexis_verify_attention_kv8(
+        _ptr(k_cache, torch.float8_e4m3fn), _ptr(v_cache, torch.float8_e4m3fn), _ptr(scales, torch.float32), num_blocks,
+        num_kv_heads, block_size, head_dim, query_start_loc.shape[0] - 1, _ptr(query_start_loc, torch.int32),
+        _ptr(seq_lens, torch.int32), _ptr(block_tables, torch.int32), block_tables.shape[1], total_tokens, max_query_len,
+        max_seq_len, _ptr(q, torch.bfloat16), num_q_heads, scale, _ptr(out, torch.bfloat16), kv_chunk_tokens,
+        _ptr(workspace), workspace.numel() * workspace.element_size(), _stream(stream)))
 
 
 def spexis_softmax_rows(logits, probs, temperature=1.0, stream=None) -> None:

@@ -46,3 +46,27 @@ def test_8_bit_append_without_rotation():
     assert rotate(True, T=0, **none) == 0
     for kw in (dict(q=FAKE, qo=FAKE, hq=8), dict(pos=FAKE), dict(cs=FAKE)):
         assert rotate(True, **dict(none, **kw)) == INVALID, kw
+
+
+def attend(**kw):
+    a = dict(k=FAKE, v=FAKE, sc=FAKE, nb=10, hkv=2, bs=16, d=64, B=2, qsl=FAKE, sl=FAKE, bt=FAKE, mb=4, T=4, mq=2, ms=40,
+             q=FAKE, hq=8, scale=0.125, out=ctypes.c_void_p(512), chunk=0, ws=FAKE, wsb=1 << 30)
+    a.update(kw)
+    return sx.lib().spexis_verify_attention_kv8(a["k"], a["v"], a["sc"], a["nb"], a["hkv"], a["bs"], a["d"], a["B"],
+                                                a["qsl"], a["sl"], a["bt"], a["mb"], a["T"], a["mq"], a["ms"], a["q"], a["hq"],
+                                                a["scale"], a["out"], a["chunk"], a["ws"], a["wsb"], None)
+
+
+def test_attention_over_the_8_bit_cache():
+    for kw in (dict(nb=0), dict(hkv=0), dict(hq=0), dict(hq=7), dict(B=-1), dict(mb=0), dict(T=-1), dict(mq=0), dict(ms=0),
+               dict(chunk=-1), dict(scale=float("nan")), dict(mb=1, mq=17, hq=2), dict(k=None), dict(v=None), dict(sc=None),
+               dict(qsl=None), dict(sl=None), dict(bt=None), dict(q=None), dict(out=None), dict(out=FAKE), dict(k=ODD),
+               dict(sc=ODD), dict(ws=ODD)):
+        assert attend(**kw) == INVALID, kw
+        assert b"spexis_verify_attention_kv8" in sx.lib().spexis_last_error()
+    for kw in (dict(bs=8), dict(d=96), dict(hq=66, mq=2), dict(mb=2**27, B=2**11), dict(chunk=32, B=2**20, mb=2**6, ms=2**16)):
+        assert attend(**kw) == UNSUPPORTED, kw
+    need = sx.spexis_verify_attention_kv8_workspace_size(2, 8, 2, 64, 2, 40)
+    assert need > 0 and attend(wsb=need - 1) == SMALL and attend(ws=None) == SMALL
+    assert attend(B=0, k=None, ws=None) == 0 and attend(T=0, q=None, ws=None) == 0
+    assert sx.spexis_verify_attention_kv8_workspace_size(0, 8, 2, 64, 2, 40) == 0

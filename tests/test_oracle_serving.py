@@ -78,10 +78,10 @@ def test_attention8_is_a_mean_under_equal_scores():
     r = np.random.default_rng(3)
     v = r.integers(0, 120, (2, 16, 1, 64)).astype(np.uint8)
     scales = np.array([[[1.0, 2.0]], [[4.0, 0.5]]], dtype=np.float32)
-    out = osv.attention8(np.zeros_like(v), v, scales, [0, 2], [20], np.array([[1, 0]]), r.standard_normal((2, 3, 64)), 0.1)
+    out, mean, most = osv.attention8(np.zeros_like(v), v, scales, [0, 2], [20], np.array([[1, 0]]), r.standard_normal((2, 3, 64)), 0.1)
     rows = np.concatenate([osv.E4M3[v[1, :, 0]] * 0.5, osv.E4M3[v[0, :, 0]] * 2.0])
     for j in range(2):
-        assert np.allclose(out[j], rows[: 19 + j].mean(axis=0))
+        assert np.allclose(out[j], rows[: 19 + j].mean(axis=0)) and np.array_equal(out, mean) and not most.any()
 
 
 def test_logprobs_closed_forms():
