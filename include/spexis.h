@@ -25,6 +25,7 @@
  *   spexis_linear_split      several linear layers of one input (q, k, v) in one projection
  *   spexis_pack_weight       weight layout of the projections above (done once per weight)
  *   spexis_sample_tokens     one token per row of logits or probabilities, with its probability
+ *   spexis_token_logprobs    log probabilities of given tokens, entropies and top alternatives
  *   spexis_softmax_rows      temperature softmax of logit rows (probability inputs)
  *
  * Conventions shared by every entry point
@@ -107,6 +108,10 @@ extern "C" {
 /* input kinds of spexis_accept */
 #define SPEXIS_INPUT_PROBS 0
 #define SPEXIS_INPUT_LOGITS 1
+
+/* types of logits */
+#define SPEXIS_TYPE_F32 0
+#define SPEXIS_TYPE_BF16 1
 
 /* which elements of a head the rotary position embedding turns together */
 #define SPEXIS_ROTARY_HALVES 0  /* i and i + rotary_dim/2 */
@@ -286,6 +291,36 @@ int spexis_verify_attention_kv8(const void* k_cache, const void* v_cache, const 
  */
 int spexis_softmax_rows(const float* logits, float* probs, int64_t rows, int32_t vocab,
                         float temperature, void* stream);
+
+/* Bytes of workspace spexis_token_logprobs needs (0: none, or sizes that it refuses). */
+size_t spexis_token_logprobs_workspace_size(int32_t num_items, int32_t vocab, int32_t top_n);
+
+/*
+ * spexis_token_logprobs -- log probabilities of given tokens under softmax(logits / T), with the entropy and the
+ * top alternatives of their rows: of the tokens that acceptance emitted (what a serving loop returns with them), or
+ * of a prompt's.  Item i asks for token_ids[i] in logit row row_ids[i] (row i where row_ids is NULL); with
+ * p = softmax(row / T):
+ *   logprobs[i] = ln p(token);   entropy[i] = -sum_v p(v) ln p(v)   (in nats; terms with p(v) = 0 are 0)
+ *   top_ids[i][j], top_logprobs[i][j]: the top_n entries of largest logit, largest first, equal logits lower
+ *                 index first; past the row's `vocab` entries -1 and -inf
+ * A token of logit -inf has log probability -inf.  An item whose token or row is out of range has none: its row is
+ * not read, and it gets 0, 0, -1 and -inf (spexis_accept's out_tokens can be passed as they are, with
+ * row_ids[b*(max_k+1) + j] = qsl[b] + j: positions behind the emitted tokens hold -1).  A row without a distribution
+ * (a NaN or +inf, or nothing above -inf) gives NaN, NaN, -1 and NaN.
+ *   logits_type   SPEXIS_TYPE_F32 or SPEXIS_TYPE_BF16 (fp32 arithmetic)
+ *   logits        num_rows rows of vocab entries, row_stride >= vocab entries apart, aligned to an entry (read)
+ *   row_ids       [num_items] int32 or NULL (then num_items <= num_rows);  token_ids  [num_items] int32
+ *   top_n         host: 0 .. 32;  top_ids [num_items][top_n] int32, top_logprobs fp32 (not used with top_n = 0)
+ *   logprobs      [num_items] fp32;  entropy [num_items] fp32 or NULL
+ *   workspace     >= spexis_token_logprobs_workspace_size(num_items, vocab, top_n) bytes, 16-byte aligned (may be
+ *                 NULL where that is 0)
+ * Supported: vocab <= 4194304.  Errors: INVALID_ARGUMENT, UNSUPPORTED, WORKSPACE_TOO_SMALL, HIP.
+ */
+int spexis_token_logprobs(int32_t logits_type, const void* logits, int64_t row_stride,
+                          int32_t num_rows, int32_t vocab, float temperature, int32_t num_items,
+                          const int32_t* row_ids, const int32_t* token_ids, int32_t top_n,
+                          float* logprobs, float* entropy, int32_t* top_ids, float* top_logprobs,
+                          void* workspace, size_t workspace_bytes, void* stream);
 
 /* Bytes of workspace spexis_accept needs. */
 size_t spexis_accept_workspace_size(int32_t num_seqs, int32_t vocab, int32_t max_k);

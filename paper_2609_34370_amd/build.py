@@ -12,7 +12,7 @@ CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 BUILD_DIR = os.path.join(ROOT, "_build")
 LIB_PATH = os.path.join(PKG, "libspexis.so")
-SOURCES = ["append.hip", "rotate.hip", "attention.hip", "attention8.hip", "accept.hip", "lm_head.hip", "select.hip", "lookahead.hip", "linear.hip", "pack.hip", "api.hip"]
+SOURCES = ["append.hip", "rotate.hip", "attention.hip", "attention8.hip", "accept.hip", "logprobs.hip", "lm_head.hip", "select.hip", "lookahead.hip", "linear.hip", "pack.hip", "api.hip"]
 # the benchmark's HBM read-rate probe: a library of its own, never linked into libspexis
 PROBE_LIB_PATH = os.path.join(PKG, "libspexis_probe.so")
 PROBE_SOURCES = ["stream_probe.hip"]

@@ -344,6 +344,60 @@ int spexis_softmax_rows(const float* logits, float* probs, int64_t rows, int32_t
                     "spexis_softmax_rows");
 }
 
+size_t spexis_token_logprobs_workspace_size(int32_t items, int32_t vocab, int32_t top_n) {
+  if (items <= 0 || vocab <= 0 || top_n < 0 || top_n > spexis::kLogprobMaxTop) return 0;
+  const int64_t parts = spexis::logprob_parts(items, vocab);
+  return parts > 1 ? (size_t)(items * parts * (16 + 8 * (int64_t)top_n)) : 0;
+}
+
+int spexis_token_logprobs(int32_t logits_type, const void* logits, int64_t row_stride, int32_t num_rows, int32_t vocab,
+                          float temperature, int32_t num_items, const int32_t* row_ids, const int32_t* token_ids,
+                          int32_t top_n, float* logprobs, float* entropy, int32_t* top_ids, float* top_logprobs,
+                          void* workspace, size_t workspace_bytes, void* stream) {
+  const char* name = "spexis_token_logprobs";
+  if (logits_type != SPEXIS_TYPE_F32 && logits_type != SPEXIS_TYPE_BF16)
+    return fail(SPEXIS_ERR_INVALID_ARGUMENT, "%s: logits type %d", name, logits_type);
+  if (num_rows < 0 || vocab <= 0 || num_items < 0 || top_n < 0 || row_stride < vocab)
+    return fail(SPEXIS_ERR_INVALID_ARGUMENT, "%s: bad size", name);
+  if (!(temperature > 0.f) || !std::isfinite(temperature))
+    return fail(SPEXIS_ERR_INVALID_ARGUMENT, "%s: temperature must be finite and > 0", name);
+  if (!row_ids && num_items > num_rows)
+    return fail(SPEXIS_ERR_INVALID_ARGUMENT, "%s: %d items of %d rows", name, num_items, num_rows);
+  if (vocab > kMaxVocab || top_n > spexis::kLogprobMaxTop)
+    return fail(SPEXIS_ERR_UNSUPPORTED, "%s: vocab %d > %d or top_n %d > %d", name, vocab, kMaxVocab, top_n,
+                spexis::kLogprobMaxTop);
+  const int parts = spexis::logprob_parts(std::max(num_items, 1), vocab);
+  if ((int64_t)num_items * parts >= (1ll << 31)) return fail(SPEXIS_ERR_UNSUPPORTED, "%s: too many items", name);
+  if (num_items == 0) return ok();
+  if (!logits || !token_ids || !logprobs || (top_n > 0 && (!top_ids || !top_logprobs)))
+    return fail(SPEXIS_ERR_INVALID_ARGUMENT, "%s: null pointer", name);
+  if (reinterpret_cast<uintptr_t>(logits) % (logits_type == SPEXIS_TYPE_F32 ? 4 : 2) != 0 || misaligned({workspace}))
+    return fail(SPEXIS_ERR_INVALID_ARGUMENT, "%s: a misaligned pointer", name);
+  const size_t need = spexis_token_logprobs_workspace_size(num_items, vocab, top_n);
+  if (need > 0 && (!workspace || workspace_bytes < need))
+    return fail(SPEXIS_ERR_WORKSPACE_TOO_SMALL, "%s: workspace %zu bytes < %zu needed", name, workspace_bytes, need);
+  spexis::LogprobParams p{};
+  p.logits = logits;
+  p.stride = row_stride;
+  p.row_ids = row_ids;
+  p.tokens = token_ids;
+  p.logprob = logprobs;
+  p.entropy = entropy;
+  p.top_ids = top_ids;
+  p.top_logprobs = top_logprobs;
+  p.part_stats = static_cast<spexis::f32x4*>(workspace);
+  p.part_keys = reinterpret_cast<uint64_t*>(p.part_stats + (int64_t)num_items * parts);
+  p.rows = num_rows;
+  p.items = num_items;
+  p.V = vocab;
+  p.top = top_n;
+  p.in16 = logits_type == SPEXIS_TYPE_BF16;
+  p.parts = parts;
+  p.c = (float)(1.4426950408889634 / (double)temperature);
+  p.inv_t = (float)(1.0 / (double)temperature);
+  return hip_result(spexis::launch_logprobs(p, (hipStream_t)stream), name);
+}
+
 size_t spexis_accept_workspace_size(int32_t num_seqs, int32_t vocab, int32_t max_k) {
   if (num_seqs <= 0 || vocab <= 0 || max_k < 0) return 0;
   return accept_layout(num_seqs, vocab, max_k).total;

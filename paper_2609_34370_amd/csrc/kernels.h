@@ -4,6 +4,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "common.h"
+
 namespace spexis {
 
 struct AppendParams {
@@ -177,6 +179,32 @@ struct LookaheadParams {
 
 constexpr int kLookaheadMaxIters = 1024;
 
+// Token log probabilities: `items` (row, token) pairs over logit rows of V entries, `stride` apart.
+struct LogprobParams {
+  const void* logits;        // [rows] fp32, or bf16 (in16)
+  int64_t stride;
+  const int32_t* row_ids;    // [items], or null: item i's row is i
+  const int32_t* tokens;     // [items]
+  float* logprob;            // [items]
+  float* entropy;            // [items] or null
+  int32_t* top_ids;          // [items][top]
+  float* top_logprobs;       // [items][top]
+  f32x4* part_stats;         // workspace, parts > 1: [items][parts] maximum, Z, U, 0
+  uint64_t* part_keys;       // [items][parts][top]
+  int rows, items, V, top, in16;
+  int parts;                 // a row's workgroups
+  float c, inv_t;            // log2(e) / temperature, 1 / temperature
+};
+
+constexpr int kLogprobMaxTop = 32;
+constexpr int kLogprobMaxParts = 64;   // the merge holds a part a lane
+// Parts of a row.
+inline int logprob_parts(int64_t items, int64_t V) {
+  const int64_t want = (2048 + items - 1) / items, most = (V + 8191) / 8192;
+  const int64_t n = want < most ? want : most;
+  return (int)(n < 1 ? 1 : n > kLogprobMaxParts ? kLogprobMaxParts : n);
+}
+
 struct AcceptParams {
   int kind;              // 0 probs, 1 logits
   int B, V, max_k, T;
@@ -244,6 +272,7 @@ int64_t projection_workgroups(int64_t M, int64_t N);
 int64_t group_rows(int64_t M);
 int64_t launched_workgroups(int64_t N, int64_t groups);
 hipError_t launch_softmax(const float* logits, float* probs, int64_t rows, int V, float c, hipStream_t s);
+hipError_t launch_logprobs(const LogprobParams& p, hipStream_t s);
 hipError_t launch_accept(const AcceptParams& p, hipStream_t s);
 hipError_t launch_gather_columns(const int32_t* qsl, const int32_t* ids, int B, int T, int32_t* cols, hipStream_t s);
 

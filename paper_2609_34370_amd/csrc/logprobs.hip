@@ -1,0 +1,305 @@
+// Log probabilities of given tokens under softmax(logits / T), with the entropy and the top alternatives of
+// their rows.
+//   w_v = (x_v - max x) c, c = log2(e) / T;  Z = sum 2^w;  U = sum 2^w w
+//   log p(v) = (x_v - max x) / T - ln Z;   H = ln Z - ln2 U / Z
+//   (both terms of H are at least 0, as is ln Z: no cancellation)
+// Bound by reading the logits once.
+//
+// Work split.  A workgroup takes one part of one item's row, its four waves every fourth chunk of 2048 logits (in
+// registers, the next one in flight).  Every lane keeps a running maximum, Z and U of its own: no exchange
+// until the end.  With one part per row the workgroup writes the outputs; with more, a second launch combines them.
+//
+// Top alternatives, by (logit, lower index first): a wave's candidates wait in LDS as 64-bit keys, the logit's order in
+// the upper half and the index's complement in the lower, so that no two are equal and every order of work gives the
+// same list.  A logit becomes a candidate when it reaches the threshold; when more than 64 wait they are
+// sorted (one key a lane) and cut to n, and the threshold rises just above the n-th.  A wave meets its indices in
+// ascending order, chunk by chunk and group by group, so a later logit that equals the n-th loses to it.  The first
+// chunk's threshold is the n-th largest of its lanes' maxima: at least n logits reach it, few more do.
+#include "common.h"
+#include "kernels.h"
+
+namespace spexis {
+
+constexpr int kLpElems = 32;                    // logits of a chunk per lane
+constexpr int kLpGroup = 8;                     // of them between two looks at the candidates' count
+constexpr int kLpKeep = 64;                     // candidates that wait without being sorted
+constexpr int kLpCap = kLpKeep + kLpGroup * kWave;
+constexpr float kLowest = -3.402823466e38f;
+constexpr float kLn2 = 0.693147180559945309f;
+
+__device__ __forceinline__ uint32_t order_of(float x) {
+  const uint32_t u = __float_as_uint(x + 0.f);   // -0 counts as 0
+  return u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
+}
+__device__ __forceinline__ float value_of(uint32_t o) {
+  return __uint_as_float(o & 0x80000000u ? o ^ 0x80000000u : ~o);
+}
+
+__device__ __forceinline__ uint64_t shfl_xor_u64(uint64_t v, int mask) {
+  const uint32_t lo = __shfl_xor((int)(uint32_t)v, mask), hi = __shfl_xor((int)(uint32_t)(v >> 32), mask);
+  return ((uint64_t)hi << 32) | lo;
+}
+// Bitonic network over the lanes of a wave; lane 0 ends with the largest key.
+__device__ __forceinline__ uint64_t wave_merge_desc(uint64_t k, int lane) {   // of a bitonic sequence
+#pragma unroll
+  for (int j = 32; j > 0; j >>= 1) {
+    const uint64_t o = shfl_xor_u64(k, j);
+    k = ((lane & j) == 0) == (o > k) ? o : k;
+  }
+  return k;
+}
+__device__ __forceinline__ uint64_t wave_sort_desc(uint64_t k, int lane) {
+#pragma unroll
+  for (int n = 2; n <= kWave; n <<= 1)
+#pragma unroll
+    for (int j = n >> 1; j > 0; j >>= 1) {
+      const uint64_t o = shfl_xor_u64(k, j);
+      const bool desc = (lane & n) == 0;   // n = 64: the whole wave descends
+      k = (((lane & j) == 0) == desc) == (o > k) ? o : k;
+    }
+  return k;
+}
+
+// A wave's candidates: `keys` in LDS, of which `count` wait; `cut` is the least logit that still becomes one.
+struct Candidates {
+  uint64_t* keys;
+  int count;
+  float cut;
+};
+// Sorts what waits and keeps the n largest.
+__device__ __forceinline__ void compact(Candidates& c, int n, int lane) {
+  wave_lds_fence();
+  uint64_t best = wave_sort_desc(lane < c.count ? c.keys[lane] : 0, lane);
+  for (int b = kWave; b < c.count; b += kWave) {
+    const uint64_t k = b + lane < c.count ? c.keys[b + lane] : 0;
+    if (__builtin_amdgcn_ballot_w64(k > readlane_u64(best, n - 1)) == 0) continue;
+    const uint64_t s = wave_sort_desc(k, lane);
+    const uint64_t r = ((uint64_t)(uint32_t)__shfl((int)(uint32_t)(s >> 32), kWave - 1 - lane) << 32) |
+                       (uint32_t)__shfl((int)(uint32_t)s, kWave - 1 - lane);
+    best = wave_merge_desc(best > r ? best : r, lane);
+  }
+  wave_lds_fence();
+  if (lane < n) c.keys[lane] = best;
+  wave_lds_fence();
+  if (c.count >= n) {
+    c.count = n;
+    c.cut = value_of((uint32_t)(readlane_u64(best, n - 1) >> 32) + 1u);   // just above the n-th
+  }
+}
+
+// Running maximum m (a logit), Z and U of the logits seen, relative to m.
+struct RowStats {
+  float m, z, u;
+};
+__device__ __forceinline__ RowStats rebase(RowStats s, float m, float c) {
+  const float d = (s.m - m) * c, a = fast_exp2(d);
+  // a = 0: nothing is left of U (and d may be infinite); a NaN in Z stays
+  return {m, s.z * a, a > 0.f ? a * (s.u + d * s.z) : 0.f};
+}
+__device__ __forceinline__ RowStats wave_combine(RowStats s, float c) {
+  const RowStats r = rebase(s, wave_max(s.m), c);
+  return {r.m, wave_sum(r.z), wave_sum(r.u)};
+}
+
+// Writes an item's outputs, one wave.  best: its keys, the n largest in descending order over the lanes.
+template <typename E>
+__device__ __forceinline__ void write_item(const LogprobParams& p, int item, const E* row, int tok, RowStats s, uint64_t best,
+                                           int found, int lane) {
+  const float nan = __builtin_nanf("");
+  const bool none = row == nullptr, bad = !none && !(s.z > 0.f);   // a NaN, +inf, or nothing above -inf
+  const float lz = kLn2 * __builtin_log2f(s.z);
+  // (not by way of w, which overflows for a masked logit of the type's lowest value)
+  auto logp = [&](float x) { return bad ? nan : (x - s.m) * p.inv_t - lz; };
+  if (lane < p.top) {
+    const bool has = !none && !bad && lane < found;
+    const int64_t at = (int64_t)item * p.top + lane;
+    p.top_ids[at] = has ? (int32_t)~(uint32_t)best : -1;
+    p.top_logprobs[at] = has ? logp(value_of((uint32_t)(best >> 32))) : bad ? nan : -__builtin_inff();
+  }
+  if (lane == 0) {
+    float x = 0.f;
+    if (!none) {
+      if constexpr (sizeof(E) == 2) x = __uint_as_float((uint32_t)row[tok] << 16);
+      else x = row[tok];
+    }
+    p.logprob[item] = none ? 0.f : logp(x);
+    if (p.entropy != nullptr) p.entropy[item] = none ? 0.f : bad ? nan : lz - kLn2 * (s.u / s.z);
+  }
+}
+
+// An item's row (null: the item has no token) and its token.
+template <typename E>
+__device__ __forceinline__ const E* item_row(const LogprobParams& p, int item, int& tok) {
+  tok = p.tokens[item];
+  const int r = p.row_ids != nullptr ? p.row_ids[item] : item;
+  if (tok < 0 || tok >= p.V || r < 0 || r >= p.rows) return nullptr;
+  return reinterpret_cast<const E*>(p.logits) + (int64_t)r * p.stride;
+}
+
+template <typename E, bool kTop>
+__global__ __launch_bounds__(256) void logprobs_kernel(LogprobParams p) {
+  constexpr int kVec = 16 / (int)sizeof(E), kLoads = kLpElems / kVec, kChunkVecs = kLoads * kWave;
+  __shared__ uint64_t sm_keys[4][kTop ? kLpCap : 1];
+  __shared__ RowStats sm_stats[4];
+  __shared__ int sm_count[4];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+  const int item = blockIdx.x / p.parts, part = blockIdx.x % p.parts;
+  int tok;
+  const E* row = item_row<E>(p, item, tok);
+  if (row == nullptr) {
+    if (p.parts == 1 && wave == 0) write_item<E>(p, item, nullptr, 0, {0.f, 1.f, 0.f}, 0, 0, lane);
+    return;
+  }
+  // The row as 16-byte vectors; element e of vector v is logit v * kVec + e - skip.
+  const int skip = (int)(reinterpret_cast<uintptr_t>(row) % 16 / sizeof(E));
+  const E* base = row - skip;
+  const int vecs = (p.V + skip + kVec - 1) / kVec, chunks = (vecs + kChunkVecs - 1) / kChunkVecs;
+  const int c0 = (int)((int64_t)chunks * part / p.parts), c1 = (int)((int64_t)chunks * (part + 1) / p.parts);
+
+  u32x4 raw[kLoads];
+  auto load = [&](int chunk) {
+    const int v0 = chunk * kChunkVecs;
+    if ((v0 > 0 || skip == 0) && (v0 + kChunkVecs) * kVec - skip <= p.V) {
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i)
+        raw[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(base) + v0 + i * kWave + lane);
+      return;
+    }
+    // the row's first and last chunk: logits one by one, -inf outside the row
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i)
+#pragma unroll
+      for (int e = 0; e < kVec; ++e) {
+        const int at = (v0 + i * kWave + lane) * kVec + e - skip;
+        if constexpr (sizeof(E) == 2) {
+          const uint32_t x = at >= 0 && at < p.V ? (uint32_t)row[at] : 0xFF80u;
+          raw[i][e / 2] = e % 2 ? raw[i][e / 2] | (x << 16) : x;
+        } else {
+          raw[i][e] = at >= 0 && at < p.V ? __float_as_uint(row[at]) : 0xFF800000u;
+        }
+      }
+  };
+
+  RowStats s = {kLowest, 0.f, 0.f};
+  Candidates cand = {sm_keys[wave], 0, -__builtin_inff()};
+  int chunk = c0 + wave;
+  if (chunk < c1) load(chunk);
+  for (; chunk < c1; chunk += 4) {
+    float x[kLpElems];
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i)
+#pragma unroll
+      for (int e = 0; e < kVec; ++e) {
+        if constexpr (sizeof(E) == 2) x[i * kVec + e] = __uint_as_float(e % 2 ? raw[i][e / 2] & 0xFFFF0000u : raw[i][e / 2] << 16);
+        else x[i * kVec + e] = __uint_as_float(raw[i][e]);
+      }
+    if (chunk + 4 < c1) load(chunk + 4);
+    float most = x[0];
+#pragma unroll
+    for (int j = 1; j < kLpElems; ++j) most = fmaxf(most, x[j]);
+    if (most > s.m) s = rebase(s, most, p.c);
+#pragma unroll
+    for (int j = 0; j < kLpElems; ++j) {
+      const float w = (x[j] - s.m) * p.c, e = fast_exp2(w);
+      s.z += e;
+      s.u += e * fmaxf(w, kLowest);   // 0 * -inf would be NaN
+    }
+    if constexpr (kTop) {
+      if (chunk == c0 + wave)
+        cand.cut = value_of((uint32_t)(readlane_u64(wave_sort_desc((uint64_t)order_of(most) << 32 | (uint32_t)lane, lane), p.top - 1) >> 32));
+      if (__builtin_amdgcn_ballot_w64(most >= cand.cut) != 0) {
+        const int at = chunk * kChunkVecs * kVec - skip;
+#pragma unroll
+        for (int g = 0; g < kLpElems; g += kLpGroup) {
+#pragma unroll
+          for (int j = g; j < g + kLpGroup; ++j) {
+            const int id = at + (j / kVec * kWave + lane) * kVec + j % kVec;
+            const uint64_t hit = __builtin_amdgcn_ballot_w64(x[j] >= cand.cut && id >= 0 && id < p.V);
+            if (hit == 0) continue;
+            const int before = __builtin_amdgcn_mbcnt_hi((uint32_t)(hit >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)hit, 0));
+            if (hit >> lane & 1) cand.keys[cand.count + before] = (uint64_t)order_of(x[j]) << 32 | ~(uint32_t)id;
+            cand.count += (int)__popcll(hit);
+          }
+          if (cand.count > kLpKeep) compact(cand, p.top, lane);
+        }
+        if (chunk == c0 + wave && cand.count >= p.top) compact(cand, p.top, lane);
+      }
+    }
+  }
+
+  // ---- the four waves' together
+  s = wave_combine(s, p.c);
+  if constexpr (kTop) compact(cand, p.top, lane);
+  if (lane == 0) {
+    sm_stats[wave] = s;
+    sm_count[wave] = cand.count;
+  }
+  __syncthreads();
+  if (wave != 0) return;
+  s = wave_combine(lane < 4 ? sm_stats[lane] : RowStats{kLowest, 0.f, 0.f}, p.c);
+  uint64_t best = 0;
+  if constexpr (kTop) {
+    for (int w = 1; w < 4; ++w) {
+      if (lane < sm_count[w]) cand.keys[cand.count + lane] = sm_keys[w][lane];
+      cand.count += sm_count[w];
+    }
+    compact(cand, p.top, lane);
+    best = lane < cand.count ? cand.keys[lane] : 0;
+  }
+  if (p.parts == 1) {
+    write_item<E>(p, item, row, tok, s, best, cand.count, lane);
+    return;
+  }
+  if (lane == 0) p.part_stats[blockIdx.x] = f32x4{s.m, s.z, s.u, 0.f};
+  if (kTop && lane < p.top) p.part_keys[(int64_t)blockIdx.x * p.top + lane] = best;
+}
+
+// The parts of every item, one wave an item.
+template <typename E, bool kTop>
+__global__ __launch_bounds__(256) void logprobs_merge_kernel(LogprobParams p) {
+  __shared__ uint64_t sm_keys[4][kTop ? kLpCap : 1];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+  const int item = blockIdx.x * 4 + wave;
+  if (item >= p.items) return;
+  int tok;
+  const E* row = item_row<E>(p, item, tok);
+  if (row == nullptr) return write_item<E>(p, item, nullptr, 0, {0.f, 1.f, 0.f}, 0, 0, lane);
+  RowStats s = {kLowest, 0.f, 0.f};
+  if (lane < p.parts) {   // at most a wave's lanes
+    const f32x4 v = p.part_stats[(int64_t)item * p.parts + lane];
+    s = {v[0], v[1], v[2]};
+  }
+  s = wave_combine(s, p.c);
+  uint64_t best = 0;
+  Candidates cand = {sm_keys[wave], 0, 0.f};
+  if constexpr (kTop) {
+    const int total = p.parts * p.top;
+    for (int b = 0; b < total; b += kWave) {
+      const uint64_t k = b + lane < total ? p.part_keys[(int64_t)item * total + b + lane] : 0;   // 0: none
+      const uint64_t hit = __builtin_amdgcn_ballot_w64(k != 0);
+      const int before = __builtin_amdgcn_mbcnt_hi((uint32_t)(hit >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)hit, 0));
+      if (k != 0) cand.keys[cand.count + before] = k;
+      cand.count += (int)__popcll(hit);
+      if (cand.count > kLpCap - kWave) compact(cand, p.top, lane);
+    }
+    compact(cand, p.top, lane);
+    best = lane < cand.count ? cand.keys[lane] : 0;
+  }
+  write_item<E>(p, item, row, tok, s, best, cand.count, lane);
+}
+
+template <typename E, bool kTop>
+static hipError_t launch_logprobs_t(const LogprobParams& p, hipStream_t s) {
+  hipLaunchKernelGGL((logprobs_kernel<E, kTop>), dim3((unsigned)(p.items * p.parts)), dim3(256), 0, s, p);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || p.parts == 1) return e;
+  hipLaunchKernelGGL((logprobs_merge_kernel<E, kTop>), dim3((unsigned)((p.items + 3) / 4)), dim3(256), 0, s, p);
+  return hipGetLastError();
+}
+
+hipError_t launch_logprobs(const LogprobParams& p, hipStream_t s) {
+  if (p.in16) return p.top > 0 ? launch_logprobs_t<uint16_t, true>(p, s) : launch_logprobs_t<uint16_t, false>(p, s);
+  return p.top > 0 ? launch_logprobs_t<float, true>(p, s) : launch_logprobs_t<float, false>(p, s);
+}
+
+}  // namespace spexis

@@ -25,6 +25,7 @@ SPEXIS_ERR_WORKSPACE_TOO_SMALL = -3
 SPEXIS_ERR_HIP = -4
 SPEXIS_INPUT_PROBS = 0
 SPEXIS_INPUT_LOGITS = 1
+SPEXIS_TYPE_F32, SPEXIS_TYPE_BF16 = 0, 1
 SPEXIS_ROTARY_HALVES, SPEXIS_ROTARY_PAIRS = 0, 1
 SPEXIS_ROW_OK, SPEXIS_ROW_EMPTY, SPEXIS_ROW_BAD_VALUE, SPEXIS_ROW_BAD_TOKEN, SPEXIS_ROW_INTERNAL = 0, 1, 2, 3, 4
 
@@ -76,6 +77,10 @@ def lib():
     L.spexis_verify_attention_kv8.restype = ctypes.c_int
     L.spexis_softmax_rows.argtypes = [P, P, i64, i32, f32, P]
     L.spexis_softmax_rows.restype = ctypes.c_int
+    L.spexis_token_logprobs_workspace_size.argtypes = [i32, i32, i32]
+    L.spexis_token_logprobs_workspace_size.restype = sz
+    L.spexis_token_logprobs.argtypes = [i32, P, i64, i32, i32, f32, i32, P, P, i32, P, P, P, P, P, sz, P]
+    L.spexis_token_logprobs.restype = ctypes.c_int
     L.spexis_accept_workspace_size.argtypes = [i32, i32, i32]
     L.spexis_accept_workspace_size.restype = sz
     L.spexis_accept.argtypes = [i32, i32, i32, i32, f32, i32, P, P, P, P, P, P, P, P, P, P, P, sz, P]
@@ -224,6 +229,30 @@ def spexis_softmax_rows(logits, probs, temperature=1.0, stream=None) -> None:
     rows, vocab = logits.shape
     _check(lib().spexis_softmax_rows(_ptr(logits, torch.float32), _ptr(probs, torch.float32), rows, vocab,
                                      ctypes.c_float(temperature), _stream(stream)))
+
+
+def spexis_token_logprobs_workspace_size(num_items, vocab, top_n) -> int:
+    return int(lib().spexis_token_logprobs_workspace_size(num_items, vocab, top_n))
+
+
+def spexis_token_logprobs(logits, token_ids, logprobs, workspace=None, row_ids=None, entropy=None, top_ids=None,
+                          top_logprobs=None, temperature=1.0, stream=None) -> None:
+    """logits [rows][vocab], fp32 or bf16; the rows may lie further apart than vocab.  token_ids, row_ids, logprobs and
+    entropy of any one shape; top_ids and top_logprobs with one more axis, top_n."""
+    if logits.dim() != 2 or logits.stride(1) != 1:
+        raise ValueError("logits must be rows of contiguous entries")
+    if logits.dtype not in (torch.float32, torch.bfloat16):
+        raise ValueError(f"expected torch.float32 or torch.bfloat16, got {logits.dtype}")
+    if not logits.is_cuda:
+        raise ValueError("tensor must be on the GPU")
+    rows, vocab = logits.shape
+    stride = logits.stride(0) if rows > 1 else vocab
+    _check(lib().spexis_token_logprobs(
+        SPEXIS_TYPE_F32 if logits.dtype == torch.float32 else SPEXIS_TYPE_BF16, ctypes.c_void_p(logits.data_ptr()),
+        stride, rows, vocab, temperature, token_ids.numel(), _ptr(row_ids, torch.int32), _ptr(token_ids, torch.int32),
+        0 if top_ids is None else top_ids.shape[-1], _ptr(logprobs, torch.float32), _ptr(entropy, torch.float32),
+        _ptr(top_ids, torch.int32), _ptr(top_logprobs, torch.float32), _ptr(workspace),
+        0 if workspace is None else workspace.numel() * workspace.element_size(), _stream(stream)))
 
 
 def spexis_accept_workspace_size(num_seqs, vocab, max_k) -> int:

@@ -70,3 +70,26 @@ def test_attention_over_the_8_bit_cache():
     assert need > 0 and attend(wsb=need - 1) == SMALL and attend(ws=None) == SMALL
     assert attend(B=0, k=None, ws=None) == 0 and attend(T=0, q=None, ws=None) == 0
     assert sx.spexis_verify_attention_kv8_workspace_size(0, 8, 2, 64, 2, 40) == 0
+
+
+def logprobs(**kw):
+    a = dict(type=0, x=FAKE, stride=1000, rows=8, V=1000, t=1.0, items=8, ids=None, tok=FAKE, top=5, lp=FAKE, h=None,
+             ti=FAKE, tl=FAKE, ws=FAKE, wsb=1 << 30)
+    a.update(kw)
+    return sx.lib().spexis_token_logprobs(a["type"], a["x"], a["stride"], a["rows"], a["V"], a["t"], a["items"], a["ids"],
+                                          a["tok"], a["top"], a["lp"], a["h"], a["ti"], a["tl"], a["ws"], a["wsb"], None)
+
+
+def test_token_logprobs():
+    for kw in (dict(type=2), dict(type=-1), dict(rows=-1), dict(V=0), dict(items=-1), dict(top=-1), dict(stride=999),
+               dict(t=0.0), dict(t=-1.0), dict(t=float("inf")), dict(t=float("nan")), dict(items=9), dict(x=None),
+               dict(tok=None), dict(lp=None), dict(ti=None), dict(tl=None), dict(x=ctypes.c_void_p(258)),
+               dict(x=ctypes.c_void_p(257), type=1), dict(ws=ODD, ids=FAKE, V=200000, stride=200000)):
+        assert logprobs(**kw) == INVALID, kw
+    for kw in (dict(top=33), dict(V=(1 << 22) + 1, stride=1 << 23)):
+        assert logprobs(**kw) == UNSUPPORTED, kw
+    need = sx.spexis_token_logprobs_workspace_size(8, 200000, 5)
+    assert need > 0 and sx.spexis_token_logprobs_workspace_size(8, 200000, 33) == 0
+    big = dict(V=200000, stride=200000)
+    assert logprobs(wsb=need - 1, **big) == SMALL and logprobs(ws=None, **big) == SMALL
+    assert logprobs(items=0, x=None, tok=None, lp=None) == 0
