@@ -13,8 +13,9 @@
 // the upper half and the index's complement in the lower, so that no two are equal and every order of work gives the
 // same list.  A logit becomes a candidate when it reaches the threshold; when more than 64 wait they are
 // sorted (one key a lane) and cut to n, and the threshold rises just above the n-th.  A wave meets its indices in
-// ascending order, chunk by chunk and group by group, so a later logit that equals the n-th loses to it.  The first
-// chunk's threshold is the n-th largest of its lanes' maxima: at least n logits reach it, few more do.
+// ascending order, chunk by chunk and group by group, so a later logit that equals the n-th loses to it.  Until then
+// the threshold is the n-th largest of the lanes' maxima so far (at least n logits reach it, few more do), found
+// again after 1, 2, 4, 8 ... chunks.
 #include "common.h"
 #include "kernels.h"
 
@@ -35,39 +36,61 @@ __device__ __forceinline__ float value_of(uint32_t o) {
   return __uint_as_float(o & 0x80000000u ? o ^ 0x80000000u : ~o);
 }
 
-__device__ __forceinline__ uint64_t shfl_xor_u64(uint64_t v, int mask) {
-  const uint32_t lo = __shfl_xor((int)(uint32_t)v, mask), hi = __shfl_xor((int)(uint32_t)(v >> 32), mask);
-  return ((uint64_t)hi << 32) | lo;
-}
-// Bitonic network over the lanes of a wave; lane 0 ends with the largest key.
-__device__ __forceinline__ uint64_t wave_merge_desc(uint64_t k, int lane) {   // of a bitonic sequence
-#pragma unroll
-  for (int j = 32; j > 0; j >>= 1) {
-    const uint64_t o = shfl_xor_u64(k, j);
-    k = ((lane & j) == 0) == (o > k) ? o : k;
+// The value of lane l ^ J, in lane moves that need no LDS.
+template <int J>
+__device__ __forceinline__ uint32_t lane_xor(uint32_t v, int lane) {
+  if constexpr (J == 1) return dpp_u32<kDppQuadXor1, 0xF>(v, v);
+  if constexpr (J == 2) return dpp_u32<kDppQuadXor2, 0xF>(v, v);
+  if constexpr (J == 4) {   // l ^ 7 in each half of a row, then l ^ 3 in each quad
+    const uint32_t m = dpp_u32<0x141, 0xF>(v, v);
+    return dpp_u32<0x1B, 0xF>(m, m);
   }
+  if constexpr (J == 8) return dpp_u32<0x128, 0xF>(v, v);   // a row of 16 rotated by 8
+  if constexpr (J == 16) {
+    const auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    return lane & 16 ? r[0] : r[1];
+  }
+  if constexpr (J == 32) {
+    const auto r = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    return lane & 32 ? r[0] : r[1];
+  }
+}
+template <int J>
+__device__ __forceinline__ uint64_t lane_xor(uint64_t v, int lane) {
+  return (uint64_t)lane_xor<J>((uint32_t)(v >> 32), lane) << 32 | lane_xor<J>((uint32_t)v, lane);
+}
+// Bitonic network over the lanes of a wave; lane 0 ends with the largest key.  A step exchanges with lane l ^ J
+// inside sorted runs of N lanes, descending where bit N of the lane is clear.
+template <int N, int J, typename K>
+__device__ __forceinline__ K sort_step(K k, int lane) {
+  const K o = lane_xor<J>(k, lane);
+  return (((lane & J) == 0) == ((lane & N) == 0)) == (o > k) ? o : k;
+}
+template <int N, int J, typename K>
+__device__ __forceinline__ K sort_run(K k, int lane) {   // a bitonic run of N lanes sorted
+  k = sort_step<N, J>(k, lane);
+  if constexpr (J > 1) k = sort_run<N, J / 2>(k, lane);
   return k;
 }
-__device__ __forceinline__ uint64_t wave_sort_desc(uint64_t k, int lane) {
-#pragma unroll
-  for (int n = 2; n <= kWave; n <<= 1)
-#pragma unroll
-    for (int j = n >> 1; j > 0; j >>= 1) {
-      const uint64_t o = shfl_xor_u64(k, j);
-      const bool desc = (lane & n) == 0;   // n = 64: the whole wave descends
-      k = (((lane & j) == 0) == desc) == (o > k) ? o : k;
-    }
-  return k;
+template <typename K>
+__device__ __forceinline__ K wave_sort_desc(K k, int lane) {
+  k = sort_run<2, 1>(k, lane);
+  k = sort_run<4, 2>(k, lane);
+  k = sort_run<8, 4>(k, lane);
+  k = sort_run<16, 8>(k, lane);
+  k = sort_run<32, 16>(k, lane);
+  return sort_run<64, 32>(k, lane);
 }
 
 // A wave's candidates: `keys` in LDS, of which `count` wait; `cut` is the least logit that still becomes one.
 struct Candidates {
   uint64_t* keys;
-  int count;
+  int count, sorted;   // the first `sorted` are in order
   float cut;
 };
 // Sorts what waits and keeps the n largest.
 __device__ __forceinline__ void compact(Candidates& c, int n, int lane) {
+  if (c.count == c.sorted) return;
   wave_lds_fence();
   uint64_t best = wave_sort_desc(lane < c.count ? c.keys[lane] : 0, lane);
   for (int b = kWave; b < c.count; b += kWave) {
@@ -76,13 +99,13 @@ __device__ __forceinline__ void compact(Candidates& c, int n, int lane) {
     const uint64_t s = wave_sort_desc(k, lane);
     const uint64_t r = ((uint64_t)(uint32_t)__shfl((int)(uint32_t)(s >> 32), kWave - 1 - lane) << 32) |
                        (uint32_t)__shfl((int)(uint32_t)s, kWave - 1 - lane);
-    best = wave_merge_desc(best > r ? best : r, lane);
+    best = sort_run<64, 32>(best > r ? best : r, lane);
   }
   wave_lds_fence();
   if (lane < n) c.keys[lane] = best;
   wave_lds_fence();
-  if (c.count >= n) {
-    c.count = n;
+  c.count = c.sorted = min(c.count, n);
+  if (c.count == n) {
     c.cut = value_of((uint32_t)(readlane_u64(best, n - 1) >> 32) + 1u);   // just above the n-th
   }
 }
@@ -101,12 +124,11 @@ __device__ __forceinline__ RowStats wave_combine(RowStats s, float c) {
   return {r.m, wave_sum(r.z), wave_sum(r.u)};
 }
 
-// Writes an item's outputs, one wave.  best: its keys, the n largest in descending order over the lanes.
-template <typename E>
-__device__ __forceinline__ void write_item(const LogprobParams& p, int item, const E* row, int tok, RowStats s, uint64_t best,
+// Writes an item's outputs, one wave.  none: it has no token; x: the token's logit; best: its keys, the n largest in descending order over the lanes.
+__device__ __forceinline__ void write_item(const LogprobParams& p, int item, bool none, float x, RowStats s, uint64_t best,
                                            int found, int lane) {
   const float nan = __builtin_nanf("");
-  const bool none = row == nullptr, bad = !none && !(s.z > 0.f);   // a NaN, +inf, or nothing above -inf
+  const bool bad = !none && !(s.z > 0.f);   // a NaN, +inf, or nothing above -inf
   const float lz = kLn2 * __builtin_log2f(s.z);
   // (not by way of w, which overflows for a masked logit of the type's lowest value)
   auto logp = [&](float x) { return bad ? nan : (x - s.m) * p.inv_t - lz; };
@@ -117,23 +139,20 @@ __device__ __forceinline__ void write_item(const LogprobParams& p, int item, con
     p.top_logprobs[at] = has ? logp(value_of((uint32_t)(best >> 32))) : bad ? nan : -__builtin_inff();
   }
   if (lane == 0) {
-    float x = 0.f;
-    if (!none) {
-      if constexpr (sizeof(E) == 2) x = __uint_as_float((uint32_t)row[tok] << 16);
-      else x = row[tok];
-    }
     p.logprob[item] = none ? 0.f : logp(x);
     if (p.entropy != nullptr) p.entropy[item] = none ? 0.f : bad ? nan : lz - kLn2 * (s.u / s.z);
   }
 }
 
-// An item's row (null: the item has no token) and its token.
+// An item's row (null: the item has no token) and its token's logit.
 template <typename E>
-__device__ __forceinline__ const E* item_row(const LogprobParams& p, int item, int& tok) {
-  tok = p.tokens[item];
-  const int r = p.row_ids != nullptr ? p.row_ids[item] : item;
+__device__ __forceinline__ const E* item_row(const LogprobParams& p, int item, float& logit) {
+  const int tok = p.tokens[item], r = p.row_ids != nullptr ? p.row_ids[item] : item;
   if (tok < 0 || tok >= p.V || r < 0 || r >= p.rows) return nullptr;
-  return reinterpret_cast<const E*>(p.logits) + (int64_t)r * p.stride;
+  const E* row = reinterpret_cast<const E*>(p.logits) + (int64_t)r * p.stride;
+  if constexpr (sizeof(E) == 2) logit = __uint_as_float((uint32_t)row[tok] << 16);
+  else logit = row[tok];
+  return row;
 }
 
 template <typename E, bool kTop>
@@ -144,10 +163,10 @@ __global__ __launch_bounds__(256) void logprobs_kernel(LogprobParams p) {
   __shared__ int sm_count[4];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
   const int item = blockIdx.x / p.parts, part = blockIdx.x % p.parts;
-  int tok;
-  const E* row = item_row<E>(p, item, tok);
+  float logit;
+  const E* row = item_row<E>(p, item, logit);
   if (row == nullptr) {
-    if (p.parts == 1 && wave == 0) write_item<E>(p, item, nullptr, 0, {0.f, 1.f, 0.f}, 0, 0, lane);
+    if (p.parts == 1 && wave == 0) write_item(p, item, true, 0.f, {0.f, 1.f, 0.f}, 0, 0, lane);
     return;
   }
   // The row as 16-byte vectors; element e of vector v is logit v * kVec + e - skip.
@@ -181,7 +200,8 @@ __global__ __launch_bounds__(256) void logprobs_kernel(LogprobParams p) {
   };
 
   RowStats s = {kLowest, 0.f, 0.f};
-  Candidates cand = {sm_keys[wave], 0, -__builtin_inff()};
+  Candidates cand = {sm_keys[wave], 0, 0, -__builtin_inff()};
+  float lane_most = -__builtin_inff();   // the lane's maximum over the chunks that were searched
   int chunk = c0 + wave;
   if (chunk < c1) load(chunk);
   for (; chunk < c1; chunk += 4) {
@@ -194,9 +214,14 @@ __global__ __launch_bounds__(256) void logprobs_kernel(LogprobParams p) {
         else x[i * kVec + e] = __uint_as_float(raw[i][e]);
       }
     if (chunk + 4 < c1) load(chunk + 4);
-    float most = x[0];
+    float group[kLpElems / kLpGroup], most = -__builtin_inff();
 #pragma unroll
-    for (int j = 1; j < kLpElems; ++j) most = fmaxf(most, x[j]);
+    for (int g = 0; g < kLpElems / kLpGroup; ++g) {
+      group[g] = x[g * kLpGroup];
+#pragma unroll
+      for (int j = 1; j < kLpGroup; ++j) group[g] = fmaxf(group[g], x[g * kLpGroup + j]);
+      most = fmaxf(most, group[g]);
+    }
     if (most > s.m) s = rebase(s, most, p.c);
 #pragma unroll
     for (int j = 0; j < kLpElems; ++j) {
@@ -205,24 +230,27 @@ __global__ __launch_bounds__(256) void logprobs_kernel(LogprobParams p) {
       s.u += e * fmaxf(w, kLowest);   // 0 * -inf would be NaN
     }
     if constexpr (kTop) {
-      if (chunk == c0 + wave)
-        cand.cut = value_of((uint32_t)(readlane_u64(wave_sort_desc((uint64_t)order_of(most) << 32 | (uint32_t)lane, lane), p.top - 1) >> 32));
       if (__builtin_amdgcn_ballot_w64(most >= cand.cut) != 0) {
+        lane_most = fmaxf(lane_most, most);
+        const int seen = (chunk - c0) / 4;   // chunks of this wave before this one
+        if ((seen & (seen + 1)) == 0)        // 0, 1, 3, 7 ...: the cut is worth a sort
+          cand.cut = fmaxf(cand.cut, value_of((uint32_t)__builtin_amdgcn_readlane((int)wave_sort_desc(order_of(lane_most), lane), p.top - 1)));
         const int at = chunk * kChunkVecs * kVec - skip;
 #pragma unroll
-        for (int g = 0; g < kLpElems; g += kLpGroup) {
+        for (int g = 0; g < kLpElems / kLpGroup; ++g) {
+          if (__builtin_amdgcn_ballot_w64(group[g] >= cand.cut) == 0) continue;
 #pragma unroll
-          for (int j = g; j < g + kLpGroup; ++j) {
+          for (int j = g * kLpGroup; j < (g + 1) * kLpGroup; ++j) {
+            if (__builtin_amdgcn_ballot_w64(x[j] >= cand.cut) == 0) continue;
             const int id = at + (j / kVec * kWave + lane) * kVec + j % kVec;
-            const uint64_t hit = __builtin_amdgcn_ballot_w64(x[j] >= cand.cut && id >= 0 && id < p.V);
-            if (hit == 0) continue;
+            const bool mine = x[j] >= cand.cut && id >= 0 && id < p.V;   // (outside the row lies -inf)
+            const uint64_t hit = __builtin_amdgcn_ballot_w64(mine);
             const int before = __builtin_amdgcn_mbcnt_hi((uint32_t)(hit >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)hit, 0));
-            if (hit >> lane & 1) cand.keys[cand.count + before] = (uint64_t)order_of(x[j]) << 32 | ~(uint32_t)id;
+            if (mine) cand.keys[cand.count + before] = (uint64_t)order_of(x[j]) << 32 | ~(uint32_t)id;
             cand.count += (int)__popcll(hit);
           }
           if (cand.count > kLpKeep) compact(cand, p.top, lane);
         }
-        if (chunk == c0 + wave && cand.count >= p.top) compact(cand, p.top, lane);
       }
     }
   }
@@ -247,7 +275,7 @@ __global__ __launch_bounds__(256) void logprobs_kernel(LogprobParams p) {
     best = lane < cand.count ? cand.keys[lane] : 0;
   }
   if (p.parts == 1) {
-    write_item<E>(p, item, row, tok, s, best, cand.count, lane);
+    write_item(p, item, false, logit, s, best, cand.count, lane);
     return;
   }
   if (lane == 0) p.part_stats[blockIdx.x] = f32x4{s.m, s.z, s.u, 0.f};
@@ -261,9 +289,9 @@ __global__ __launch_bounds__(256) void logprobs_merge_kernel(LogprobParams p) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
   const int item = blockIdx.x * 4 + wave;
   if (item >= p.items) return;
-  int tok;
-  const E* row = item_row<E>(p, item, tok);
-  if (row == nullptr) return write_item<E>(p, item, nullptr, 0, {0.f, 1.f, 0.f}, 0, 0, lane);
+  float logit;
+  const E* row = item_row<E>(p, item, logit);
+  if (row == nullptr) return write_item(p, item, true, 0.f, {0.f, 1.f, 0.f}, 0, 0, lane);
   RowStats s = {kLowest, 0.f, 0.f};
   if (lane < p.parts) {   // at most a wave's lanes
     const f32x4 v = p.part_stats[(int64_t)item * p.parts + lane];
@@ -271,7 +299,7 @@ __global__ __launch_bounds__(256) void logprobs_merge_kernel(LogprobParams p) {
   }
   s = wave_combine(s, p.c);
   uint64_t best = 0;
-  Candidates cand = {sm_keys[wave], 0, 0.f};
+  Candidates cand = {sm_keys[wave], 0, 0, 0.f};
   if constexpr (kTop) {
     const int total = p.parts * p.top;
     for (int b = 0; b < total; b += kWave) {
@@ -285,7 +313,7 @@ __global__ __launch_bounds__(256) void logprobs_merge_kernel(LogprobParams p) {
     compact(cand, p.top, lane);
     best = lane < cand.count ? cand.keys[lane] : 0;
   }
-  write_item<E>(p, item, row, tok, s, best, cand.count, lane);
+  write_item(p, item, false, logit, s, best, cand.count, lane);
 }
 
 template <typename E, bool kTop>

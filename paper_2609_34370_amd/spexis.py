@@ -136,12 +136,14 @@ def _ptr(t: Optional[torch.Tensor], dtype=None):
         raise ValueError("tensor must be contiguous")
     if dtype is not None and t.dtype != dtype:
         raise ValueError(f"expected {dtype}, got {t.dtype}")
-    return ctypes.c_void_p(t.data_ptr())
+    return t.data_ptr()
 
 
-def _stream(stream) -> ctypes.c_void_p:
-    s = torch.cuda.current_stream() if stream is None else stream
-    return ctypes.c_void_p(s.cuda_stream)
+def _stream(stream):
+    if stream is not None:
+        return stream.cuda_stream
+    # the current stream's handle without building a torch.cuda.Stream (4 us a call)
+    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
 
 
 def spexis_version() -> int:
@@ -248,7 +250,7 @@ def spexis_token_logprobs(logits, token_ids, logprobs, workspace=None, row_ids=N
     rows, vocab = logits.shape
     stride = logits.stride(0) if rows > 1 else vocab
     _check(lib().spexis_token_logprobs(
-        SPEXIS_TYPE_F32 if logits.dtype == torch.float32 else SPEXIS_TYPE_BF16, ctypes.c_void_p(logits.data_ptr()),
+        SPEXIS_TYPE_F32 if logits.dtype == torch.float32 else SPEXIS_TYPE_BF16, logits.data_ptr(),
         stride, rows, vocab, temperature, token_ids.numel(), _ptr(row_ids, torch.int32), _ptr(token_ids, torch.int32),
         0 if top_ids is None else top_ids.shape[-1], _ptr(logprobs, torch.float32), _ptr(entropy, torch.float32),
         _ptr(top_ids, torch.int32), _ptr(top_logprobs, torch.float32), _ptr(workspace),
@@ -409,7 +411,7 @@ def spexis_linear_split(x, weight, outputs, workspace, stream=None) -> None:
     assert weight.numel() * 2 == spexis_packed_weight_size(sum(widths), n_in), "weight must be packed"
     m = len(widths)
     w_arr = (ctypes.c_int32 * m)(*widths)
-    o_arr = (ctypes.c_void_p * m)(*[_ptr(o, torch.bfloat16).value for o in outputs])
+    o_arr = (ctypes.c_void_p * m)(*[_ptr(o, torch.bfloat16) for o in outputs])
     ws_bytes = workspace.numel() * workspace.element_size()
     _check(lib().spexis_linear_split(_ptr(x, torch.bfloat16), _ptr(weight, torch.bfloat16), rows, n_in, m, w_arr,
                                      o_arr, _ptr(workspace), ws_bytes, _stream(stream)))
