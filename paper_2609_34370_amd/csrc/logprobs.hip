@@ -13,9 +13,9 @@
 // the upper half and the index's complement in the lower, so that no two are equal and every order of work gives the
 // same list.  A logit becomes a candidate when it reaches the threshold; when more than 64 wait they are
 // sorted (one key a lane) and cut to n, and the threshold rises just above the n-th.  A wave meets its indices in
-// ascending order, chunk by chunk and group by group, so a later logit that equals the n-th loses to it.  Until then
-// the threshold is the n-th largest of the lanes' maxima so far (at least n logits reach it, few more do), found
-// again after 1, 2, 4, 8 ... chunks.
+// ascending order, chunk by chunk and group by group, so a later logit that equals the n-th loses to it.  Before
+// that the threshold is the n-th largest of the workgroup's 256 lanes' maxima so far (at least n logits reach it,
+// few more do), found again after 1, 4, 16 ... chunks.
 #include "common.h"
 #include "kernels.h"
 
@@ -159,6 +159,7 @@ template <typename E, bool kTop>
 __global__ __launch_bounds__(256) void logprobs_kernel(LogprobParams p) {
   constexpr int kVec = 16 / (int)sizeof(E), kLoads = kLpElems / kVec, kChunkVecs = kLoads * kWave;
   __shared__ uint64_t sm_keys[4][kTop ? kLpCap : 1];
+  __shared__ uint32_t sm_most[4][kWave / 2];
   __shared__ RowStats sm_stats[4];
   __shared__ int sm_count[4];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
@@ -201,10 +202,24 @@ __global__ __launch_bounds__(256) void logprobs_kernel(LogprobParams p) {
 
   RowStats s = {kLowest, 0.f, 0.f};
   Candidates cand = {sm_keys[wave], 0, 0, -__builtin_inff()};
-  float lane_most = -__builtin_inff();   // the lane's maximum over the chunks that were searched
+  float lane_most = -__builtin_inff();   // the lane's maximum so far
+  // The threshold of the whole workgroup: the n-th largest (n <= 32) of its 256 lanes' maxima.
+  auto agree = [&]() {
+    const uint32_t mine = wave_sort_desc(order_of(lane_most), lane);
+    __syncthreads();   // the last round's reads
+    if (lane < kWave / 2) sm_most[wave][lane] = mine;
+    __syncthreads();
+    // two pairs of descending halves, each as one bitonic run; the second ends in ascending order
+    const int at = lane < kWave / 2 ? lane : kWave - 1 - lane, up = lane < kWave / 2 ? 0 : 1;
+    const uint32_t a = sort_run<64, 32>(sm_most[up][at], lane), b = ~sort_run<64, 32>(~sm_most[2 + up][at], lane);
+    const uint32_t all = sort_run<64, 32>(a > b ? a : b, lane);
+    cand.cut = fmaxf(cand.cut, value_of((uint32_t)__builtin_amdgcn_readlane((int)all, p.top - 1)));
+  };
   int chunk = c0 + wave;
   if (chunk < c1) load(chunk);
-  for (; chunk < c1; chunk += 4) {
+  const int rounds = (c1 - c0 + 3) / 4;   // the same for the four waves
+  for (int round = 0, next = 0; round < rounds; ++round, chunk += 4) {
+    const bool some = chunk < c1;
     float x[kLpElems];
 #pragma unroll
     for (int i = 0; i < kLoads; ++i)
@@ -222,6 +237,14 @@ __global__ __launch_bounds__(256) void logprobs_kernel(LogprobParams p) {
       for (int j = 1; j < kLpGroup; ++j) group[g] = fmaxf(group[g], x[g * kLpGroup + j]);
       most = fmaxf(most, group[g]);
     }
+    if constexpr (kTop) {
+      if (some) lane_most = fmaxf(lane_most, most);
+      if (round == next) {   // after 1, 4, 16 ... rounds
+        agree();
+        next = 4 * next + 3;
+      }
+    }
+    if (!some) continue;
     if (most > s.m) s = rebase(s, most, p.c);
 #pragma unroll
     for (int j = 0; j < kLpElems; ++j) {
@@ -231,10 +254,6 @@ __global__ __launch_bounds__(256) void logprobs_kernel(LogprobParams p) {
     }
     if constexpr (kTop) {
       if (__builtin_amdgcn_ballot_w64(most >= cand.cut) != 0) {
-        lane_most = fmaxf(lane_most, most);
-        const int seen = (chunk - c0) / 4;   // chunks of this wave before this one
-        if ((seen & (seen + 1)) == 0)        // 0, 1, 3, 7 ...: the cut is worth a sort
-          cand.cut = fmaxf(cand.cut, value_of((uint32_t)__builtin_amdgcn_readlane((int)wave_sort_desc(order_of(lane_most), lane), p.top - 1)));
         const int at = chunk * kChunkVecs * kVec - skip;
 #pragma unroll
         for (int g = 0; g < kLpElems / kLpGroup; ++g) {
@@ -257,7 +276,7 @@ __global__ __launch_bounds__(256) void logprobs_kernel(LogprobParams p) {
 
   // ---- the four waves' together
   s = wave_combine(s, p.c);
-  if constexpr (kTop) compact(cand, p.top, lane);
+  if (kTop && cand.count > 2 * kWave) compact(cand, p.top, lane);
   if (lane == 0) {
     sm_stats[wave] = s;
     sm_count[wave] = cand.count;
@@ -267,8 +286,9 @@ __global__ __launch_bounds__(256) void logprobs_kernel(LogprobParams p) {
   s = wave_combine(lane < 4 ? sm_stats[lane] : RowStats{kLowest, 0.f, 0.f}, p.c);
   uint64_t best = 0;
   if constexpr (kTop) {
+    static_assert(4 * 2 * kWave <= kLpCap, "every wave's candidates fit into the first one's buffer");
     for (int w = 1; w < 4; ++w) {
-      if (lane < sm_count[w]) cand.keys[cand.count + lane] = sm_keys[w][lane];
+      for (int i = lane; i < sm_count[w]; i += kWave) cand.keys[cand.count + i] = sm_keys[w][i];
       cand.count += sm_count[w];
     }
     compact(cand, p.top, lane);
