@@ -140,7 +140,7 @@ int rotate_append(const char* name, const spexis::RotateParams& p, int32_t max_q
       return fail(SPEXIS_ERR_INVALID_ARGUMENT, "%s: style %d", name, p.style);
   }
   if ((p.q || p.q_out) && p.hq <= 0) return fail(SPEXIS_ERR_INVALID_ARGUMENT, "%s: non-positive size", name);
-  if (spexis::rotate_append_waves(p.total_tokens, p.block_size, p.num_seqs, p.hkv) + p.total_tokens >= (1ll << 31) ||
+  if (spexis::rotate_append_groups(p.total_tokens, p.block_size, p.num_seqs, p.hkv) + p.total_tokens >= (1ll << 31) ||
       (int64_t)p.max_blocks * p.block_size >= (1ll << 31))
     return fail(SPEXIS_ERR_UNSUPPORTED, "%s: more than 2^31 rows or slots", name);
   if (p.num_seqs == 0 || p.total_tokens == 0) return ok();
@@ -264,7 +264,7 @@ int spexis_rotate_append_kv(void* k_cache, void* v_cache, int32_t num_blocks, in
   if (max_position <= 0) return fail(SPEXIS_ERR_INVALID_ARGUMENT, "%s: non-positive size", name);
   spexis::RotateParams p{k_cache, v_cache, nullptr, query_start_loc, seq_lens, block_tables, new_k, new_v, q, q_out,
                          cos_sin, positions, num_blocks, num_kv_heads, block_size, head_dim, num_seqs,
-                         max_blocks_per_seq, total_tokens, num_q_heads, rotary_dim, max_position, style, 0, 0};
+                         max_blocks_per_seq, total_tokens, num_q_heads, rotary_dim, max_position, style, 0};
   return rotate_append(name, p, max_query_len, stream);
 }
 
@@ -280,7 +280,7 @@ int spexis_rotate_append_kv8(void* k_cache, void* v_cache, float* scales, int32_
     return fail(SPEXIS_ERR_INVALID_ARGUMENT, "%s: a rotation without a table", name);
   spexis::RotateParams p{k_cache, v_cache, scales, query_start_loc, seq_lens, block_tables, new_k, new_v, q, q_out,
                          cos_sin, positions, num_blocks, num_kv_heads, block_size, head_dim, num_seqs,
-                         max_blocks_per_seq, total_tokens, num_q_heads, rotary_dim, max_position, style, 0, 0};
+                         max_blocks_per_seq, total_tokens, num_q_heads, rotary_dim, max_position, style, 0};
   if (num_seqs > 0 && total_tokens > 0 && !scales) return fail(SPEXIS_ERR_INVALID_ARGUMENT, "%s: null pointer", name);
   return rotate_append(name, p, max_query_len, stream);
 }

@@ -35,10 +35,10 @@ struct RotateParams {
   const int32_t* positions;  // [T], or null: the token's place in its sequence
   int num_blocks, hkv, block_size, head_dim, num_seqs, max_blocks, total_tokens;
   int hq, rot, max_position, style;   // style 0: elements i and i + rot/2 turn together; 1: 2i and 2i+1
-  int append_waves, query_waves;      // set by the launcher
+  int append_groups;                  // set by the launcher
 };
-// Waves that write rows: one per KV head and block index (csrc/rotate.hip).
-inline int64_t rotate_append_waves(int64_t tokens, int64_t block_size, int64_t num_seqs, int64_t hkv) {
+// Workgroups that write rows: one per KV head and block index (csrc/rotate.hip).
+inline int64_t rotate_append_groups(int64_t tokens, int64_t block_size, int64_t num_seqs, int64_t hkv) {
   return (tokens / block_size + 2 * num_seqs) * hkv;
 }
 

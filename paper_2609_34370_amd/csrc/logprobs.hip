@@ -82,24 +82,41 @@ __device__ __forceinline__ K wave_sort_desc(K k, int lane) {
   return sort_run<64, 32>(k, lane);
 }
 
+__device__ __forceinline__ uint64_t max_u64(uint64_t a, uint64_t b) { return a > b ? a : b; }
+__device__ __forceinline__ uint64_t wave_max_u64(uint64_t v) {
+  SPEXIS_DPP_REDUCE(v, dpp_u64_move, max_u64)
+  return readlane_u64(v, kWave - 1);
+}
+
 // A wave's candidates: `keys` in LDS, of which `count` wait; `cut` is the least logit that still becomes one.
 struct Candidates {
   uint64_t* keys;
   int count, sorted;   // the first `sorted` are in order
   float cut;
 };
+__device__ __forceinline__ void push(Candidates& c, bool mine, uint64_t key) {
+  const uint64_t hit = __builtin_amdgcn_ballot_w64(mine);
+  const int before = __builtin_amdgcn_mbcnt_hi((uint32_t)(hit >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)hit, 0));
+  if (mine) c.keys[c.count + before] = key;
+  c.count += (int)__popcll(hit);
+}
 // Sorts what waits and keeps the n largest.
 __device__ __forceinline__ void compact(Candidates& c, int n, int lane) {
   if (c.count == c.sorted) return;
   wave_lds_fence();
-  uint64_t best = wave_sort_desc(lane < c.count ? c.keys[lane] : 0, lane);
-  for (int b = kWave; b < c.count; b += kWave) {
+  uint64_t best = 0;
+#pragma unroll 1
+  for (int b = 0; b < c.count; b += kWave) {
     const uint64_t k = b + lane < c.count ? c.keys[b + lane] : 0;
     if (__builtin_amdgcn_ballot_w64(k > readlane_u64(best, n - 1)) == 0) continue;
     const uint64_t s = wave_sort_desc(k, lane);
-    const uint64_t r = ((uint64_t)(uint32_t)__shfl((int)(uint32_t)(s >> 32), kWave - 1 - lane) << 32) |
-                       (uint32_t)__shfl((int)(uint32_t)s, kWave - 1 - lane);
-    best = sort_run<64, 32>(best > r ? best : r, lane);
+    if (b == 0) {
+      best = s;
+    } else {   // the larger of each and its mirror image in the other: the 64 largest, a bitonic run
+      const uint64_t r = ((uint64_t)(uint32_t)__shfl((int)(uint32_t)(s >> 32), kWave - 1 - lane) << 32) |
+                         (uint32_t)__shfl((int)(uint32_t)s, kWave - 1 - lane);
+      best = sort_run<64, 32>(best > r ? best : r, lane);
+    }
   }
   wave_lds_fence();
   if (lane < n) c.keys[lane] = best;
@@ -144,14 +161,19 @@ __device__ __forceinline__ void write_item(const LogprobParams& p, int item, boo
   }
 }
 
+template <typename E>
+__device__ __forceinline__ float logit_at(const E* row, int v) {
+  if constexpr (sizeof(E) == 2) return __uint_as_float((uint32_t)row[v] << 16);
+  else return row[v];
+}
+
 // An item's row (null: the item has no token) and its token's logit.
 template <typename E>
 __device__ __forceinline__ const E* item_row(const LogprobParams& p, int item, float& logit) {
   const int tok = p.tokens[item], r = p.row_ids != nullptr ? p.row_ids[item] : item;
   if (tok < 0 || tok >= p.V || r < 0 || r >= p.rows) return nullptr;
   const E* row = reinterpret_cast<const E*>(p.logits) + (int64_t)r * p.stride;
-  if constexpr (sizeof(E) == 2) logit = __uint_as_float((uint32_t)row[tok] << 16);
-  else logit = row[tok];
+  logit = logit_at(row, tok);
   return row;
 }
 
@@ -255,20 +277,32 @@ __global__ __launch_bounds__(256) void logprobs_kernel(LogprobParams p) {
     if constexpr (kTop) {
       if (__builtin_amdgcn_ballot_w64(most >= cand.cut) != 0) {
         const int at = chunk * kChunkVecs * kVec - skip;
+        int done = 0;   // groups that were searched
 #pragma unroll
         for (int g = 0; g < kLpElems / kLpGroup; ++g) {
+          if (cand.count > kLpKeep) continue;
+          done = g + 1;
           if (__builtin_amdgcn_ballot_w64(group[g] >= cand.cut) == 0) continue;
 #pragma unroll
           for (int j = g * kLpGroup; j < (g + 1) * kLpGroup; ++j) {
             if (__builtin_amdgcn_ballot_w64(x[j] >= cand.cut) == 0) continue;
             const int id = at + (j / kVec * kWave + lane) * kVec + j % kVec;
-            const bool mine = x[j] >= cand.cut && id >= 0 && id < p.V;   // (outside the row lies -inf)
-            const uint64_t hit = __builtin_amdgcn_ballot_w64(mine);
-            const int before = __builtin_amdgcn_mbcnt_hi((uint32_t)(hit >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)hit, 0));
-            if (mine) cand.keys[cand.count + before] = (uint64_t)order_of(x[j]) << 32 | ~(uint32_t)id;
-            cand.count += (int)__popcll(hit);
+            // (outside the row lies -inf)
+            push(cand, x[j] >= cand.cut && id >= 0 && id < p.V, (uint64_t)order_of(x[j]) << 32 | ~(uint32_t)id);
           }
-          if (cand.count > kLpKeep) compact(cand, p.top, lane);
+        }
+        // Many at once (sorted rows, ties): what is left of the chunk is read again, group by group, between sorts.
+        // One place for the sort, outside the code that holds the chunk in registers.
+        while (cand.count > kLpKeep) {
+          compact(cand, p.top, lane);
+          for (; done < kLpElems / kLpGroup && cand.count <= kLpKeep; ++done)
+#pragma unroll 1
+            for (int j = done * kLpGroup; j < (done + 1) * kLpGroup; ++j) {
+              const int id = at + (j / kVec * kWave + lane) * kVec + j % kVec;
+              float y = -__builtin_inff();
+              if (id >= 0 && id < p.V) y = logit_at(row, id);
+              push(cand, y >= cand.cut && id >= 0 && id < p.V, (uint64_t)order_of(y) << 32 | ~(uint32_t)id);
+            }
         }
       }
     }
@@ -276,7 +310,6 @@ __global__ __launch_bounds__(256) void logprobs_kernel(LogprobParams p) {
 
   // ---- the four waves' together
   s = wave_combine(s, p.c);
-  if (kTop && cand.count > 2 * kWave) compact(cand, p.top, lane);
   if (lane == 0) {
     sm_stats[wave] = s;
     sm_count[wave] = cand.count;
@@ -286,9 +319,9 @@ __global__ __launch_bounds__(256) void logprobs_kernel(LogprobParams p) {
   s = wave_combine(lane < 4 ? sm_stats[lane] : RowStats{kLowest, 0.f, 0.f}, p.c);
   uint64_t best = 0;
   if constexpr (kTop) {
-    static_assert(4 * 2 * kWave <= kLpCap, "every wave's candidates fit into the first one's buffer");
+    static_assert(4 * kLpKeep <= kLpCap, "every wave's candidates fit into the first one's buffer");
     for (int w = 1; w < 4; ++w) {
-      for (int i = lane; i < sm_count[w]; i += kWave) cand.keys[cand.count + i] = sm_keys[w][i];
+      if (lane < sm_count[w]) cand.keys[cand.count + lane] = sm_keys[w][lane];   // at most kLpKeep
       cand.count += sm_count[w];
     }
     compact(cand, p.top, lane);
@@ -321,14 +354,19 @@ __global__ __launch_bounds__(256) void logprobs_merge_kernel(LogprobParams p) {
   uint64_t best = 0;
   Candidates cand = {sm_keys[wave], 0, 0, 0.f};
   if constexpr (kTop) {
+    const uint64_t* keys = p.part_keys + (int64_t)item * p.parts * p.top;
+    // the largest of the parts' n-th keys: n keys reach it, so what is below it is not asked for
+    const uint64_t least = wave_max_u64(lane < p.parts ? keys[lane * p.top + p.top - 1] : 0);   // 0: none
     const int total = p.parts * p.top;
-    for (int b = 0; b < total; b += kWave) {
-      const uint64_t k = b + lane < total ? p.part_keys[(int64_t)item * total + b + lane] : 0;   // 0: none
-      const uint64_t hit = __builtin_amdgcn_ballot_w64(k != 0);
-      const int before = __builtin_amdgcn_mbcnt_hi((uint32_t)(hit >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)hit, 0));
-      if (k != 0) cand.keys[cand.count + before] = k;
-      cand.count += (int)__popcll(hit);
-      if (cand.count > kLpCap - kWave) compact(cand, p.top, lane);
+    constexpr int kAhead = 8;
+    static_assert(kLpKeep + kAhead * kWave <= kLpCap, "a round's candidates fit");
+    for (int b0 = 0; b0 < total; b0 += kAhead * kWave) {
+      uint64_t k[kAhead];
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) k[i] = b0 + i * kWave + lane < total ? keys[b0 + i * kWave + lane] : 0;
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) push(cand, k[i] != 0 && k[i] >= least, k[i]);
+      if (cand.count > kLpKeep) compact(cand, p.top, lane);
     }
     compact(cand, p.top, lane);
     best = lane < cand.count ? cand.keys[lane] : 0;

@@ -6,10 +6,9 @@
 //   y_a = x_a c - x_b s,   y_b = x_b c + x_a s.
 // Memory bound: every row is read once and written once, about three operations an element.
 //
-// Work split.  A wave takes one (block of tokens, KV head) that gets new rows, or one query token with all
-// its heads; the waves of a workgroup share nothing.  A block belongs to one wave because the scale of an
-// 8-bit block needs all its rows, and because V is stored 8 slots to a 16-byte piece: the wave rewrites the
-// pieces it touches whole, so no two waves write into one piece.
+// Work split.  A workgroup takes one (block of tokens, KV head) that gets new rows, or a wave one query token with all
+// its heads.  A block belongs to one workgroup because the scale of an 8-bit block needs all its rows, and
+// because V is stored 8 slots to a 16-byte piece, which is rewritten whole: no two workgroups write into one piece.
 // Which block: sequence b gets the indices from start(b) = floor(qsl[b] / bs) + 2 b.  n new tokens touch at most
 // floor(n / bs) + 2 blocks, which start(b+1) - start(b) is never below, so the launch needs no length
 // on the host and no scan: wave-wide search for the last b with start(b) <= index, two probes for 4096 sequences.
@@ -103,32 +102,46 @@ __device__ __forceinline__ void turn_task(const RotateParams& p, const Task& t, 
   }
 }
 
-// q of one token, every head: the lanes are (head, task), so the token's angles are loaded once.
+// q of one token, every head, one wave: the lanes are (head, task), so the token's angles are loaded once; the rows are
+// in flight while the position is looked up.
 template <int D>
 __device__ __forceinline__ void rotate_query(const RotateParams& p, int tok, int lane) {
-  constexpr int kTasks = D / 16, kHeads = kWave / kTasks;
-  const int t = lane % kTasks;
-  const Task task = row_task(p, t);
+  constexpr int kTasks = D / 16, kHeads = kWave / kTasks, kAhead = 4;
+  const Task task = row_task(p, lane % kTasks);
+  const uint16_t* q = reinterpret_cast<const uint16_t*>(p.q) + (int64_t)tok * p.hq * D;
+  uint16_t* o = reinterpret_cast<uint16_t*>(p.q_out) + (int64_t)tok * p.hq * D;
+  u32x4 a[kAhead], b[kAhead];
+  auto load = [&](int h0) {
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      const int h = min(h0 + i * kHeads, p.hq - 1);
+      a[i] = ld16(q + h * D + task.a);
+      b[i] = ld16(q + h * D + task.b);
+    }
+  };
+  load(lane / kTasks);
   int pos = 0;
   if (p.positions != nullptr) {
     pos = p.positions[tok];
   } else {
-    const int b = wave_search(p.num_seqs, tok, lane, [&](int i) { return seq_start(p, i); });
-    const int q1 = clampi(p.qsl[b + 1], 0, p.total_tokens);
-    pos = p.seq_lens[b] - (q1 - tok);
+    const int s = wave_search(p.num_seqs, tok, lane, [&](int i) { return seq_start(p, i); });
+    pos = p.seq_lens[s] - (clampi(p.qsl[s + 1], 0, p.total_tokens) - tok);
   }
   Angles g;
   if (task.turns) g = load_angles(p, task, pos);
-  const uint16_t* q = reinterpret_cast<const uint16_t*>(p.q) + (int64_t)tok * p.hq * D;
-  uint16_t* o = reinterpret_cast<uint16_t*>(p.q_out) + (int64_t)tok * p.hq * D;
-#pragma unroll 4
-  for (int h = lane / kTasks; h < p.hq; h += kHeads) {
-    float x[8], y[8];
-    widen(ld16(q + h * D + task.a), x);
-    widen(ld16(q + h * D + task.b), y);
-    turn_task<float>(p, task, g, x, y);
-    st16(o + h * D + task.a, narrow(x));
-    st16(o + h * D + task.b, narrow(y));
+  for (int h0 = lane / kTasks; h0 < p.hq; h0 += kAhead * kHeads) {
+    if (h0 != lane / kTasks) load(h0);
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      const int h = h0 + i * kHeads;
+      if (h >= p.hq) break;
+      float x[8], y[8];
+      widen(a[i], x);
+      widen(b[i], y);
+      turn_task<float>(p, task, g, x, y);
+      st16(o + h * D + task.a, narrow(x));
+      st16(o + h * D + task.b, narrow(y));
+    }
   }
 }
 
@@ -171,11 +184,15 @@ __device__ __forceinline__ float most_finite(const float (&x)[8], const float (&
   return m;
 }
 
+// A thread takes one task of K and of V of a block's rows: a workgroup is a (block of tokens, KV head).
+template <int D, int BS>
+constexpr int kThreads = BS * D / 16;
+
 // The new rows of one (block of tokens, KV head).
 template <int D, int BS, bool k8>
-__device__ __forceinline__ void append_block(const RotateParams& p, int index, int h, int lane, u32x4* lds) {
-  constexpr int kTasks = D / 16, kMine = BS * kTasks / kWave;   // tasks of a row; of a lane, at most
-  constexpr int kUnits = BS / 16;
+__device__ __forceinline__ void append_block(const RotateParams& p, int index, int h, int thread) {
+  constexpr int kTasks = D / 16, kWaves = kThreads<D, BS> / kWave;
+  const int lane = thread & 63, wave = thread >> 6;
   const int b = wave_search(p.num_seqs, index, lane, [&](int i) { return seq_start(p, i) / BS + 2 * i; });
   const int q0 = seq_start(p, b), q1 = clampi(p.qsl[b + 1], q0, p.total_tokens);
   const int cap = p.max_blocks * BS;
@@ -186,175 +203,165 @@ __device__ __forceinline__ void append_block(const RotateParams& p, int index, i
   const int first = lo - t * BS;                                  // its slot: the block holds that many rows
   const int blk = clampi(p.block_tables[(int64_t)b * p.max_blocks + t], 0, p.num_blocks - 1);
   const int64_t at = (int64_t)blk * p.hkv + h;
-  const int tok0 = q0 + (lo - L);
 
-  // ---- the new rows: tasks k = row * kTasks + t, the lane's at lane, lane + 64, ...
-  const uint16_t* nk = reinterpret_cast<const uint16_t*>(p.new_k);
-  const uint16_t* nv = reinterpret_cast<const uint16_t*>(p.new_v);
-  const Task task = row_task(p, lane % kTasks);   // 64 is a multiple of kTasks: the same for all of them
-  float kx[kMine][8], ky[kMine][8];
-  u32x4 va[kMine], vb[kMine];
-  float kmost = 0.f, vmost = 0.f;
-#pragma unroll
-  for (int i = 0; i < kMine; ++i) {
-    const int r = (lane + kWave * i) / kTasks;
-    if (r >= m) continue;
-    const int64_t row = ((int64_t)(tok0 + r) * p.hkv + h) * D;
-    const u32x4 a = ld16(nk + row + task.a), c = ld16(nk + row + task.b);
-    va[i] = ld16(nv + row + 16 * (lane % kTasks));
-    vb[i] = ld16(nv + row + 16 * (lane % kTasks) + 8);
-    widen(a, kx[i]);
-    widen(c, ky[i]);
-    if (task.turns) {
-      const Angles g = load_angles(p, task, p.positions != nullptr ? p.positions[tok0 + r] : lo + r);
-      turn_task<std::conditional_t<k8, double, float>>(p, task, g, kx[i], ky[i]);
-    }
-    if constexpr (k8) {
-      kmost = most_finite(kx[i], ky[i], kmost);
-      float x[8], y[8];
-      widen(va[i], x);
-      widen(vb[i], y);
-      vmost = most_finite(x, y, vmost);
-    }
+  // ---- every load: the thread's part of a new row, its token's angles, the V piece that it will write, the scales
+  const int r = thread / kTasks;
+  const bool row = r < m;
+  const Task task = row_task(p, thread % kTasks);
+  u32x4 ka, kb, va, vb;
+  Angles g;
+  if (row) {
+    const int tok = q0 + (lo - L) + r;
+    const int64_t k = ((int64_t)tok * p.hkv + h) * D;
+    const uint16_t* nk = reinterpret_cast<const uint16_t*>(p.new_k) + k;
+    const uint16_t* nv = reinterpret_cast<const uint16_t*>(p.new_v) + k;
+    ka = ld16(nk + task.a);
+    kb = ld16(nk + task.b);
+    va = ld16(nv + 16 * (thread % kTasks));
+    vb = ld16(nv + 16 * (thread % kTasks) + 8);
+    if (task.turns) g = load_angles(p, task, p.positions != nullptr ? p.positions[tok] : lo + r);
   }
-
-  // ---- the scales: never lowered while the block holds earlier rows, whose codes would overflow
-  float kratio = 1.f, vratio = 1.f, kmul = 1.f, vmul = 1.f;
-  if constexpr (k8) {
-    float* sp = p.scales + 2 * at;
-    float ks = exp_float(least_exp(wave_max(kmost))), vs = exp_float(least_exp(wave_max(vmost)));
-    if (first > 0) {
-      const float ko = sp[0], vo = sp[1];
-      ks = fmaxf(ks, ko);
-      vs = fmaxf(vs, vo);
-      kratio = ko / ks;
-      vratio = vo / vs;
-    }
-    if (lane == 0) *reinterpret_cast<f32x2*>(sp) = f32x2{ks, vs};
-    kmul = 1.f / ks;   // exact: a power of two
-    vmul = 1.f / vs;
-  }
-
-  // ---- K: 8 dims of a slot are contiguous (16 in the 8-bit cache)
-  if constexpr (k8) {
-    uint8_t* kc = reinterpret_cast<uint8_t*>(p.k_cache) + at * (BS * D);
-    auto chunk = [&](int slot, int d) { return kc + ((slot / 16 * (D / 16) + d / 16) * 16 + slot % 16) * 16 + d % 16; };
-#pragma unroll
-    for (int i = 0; i < kMine; ++i) {
-      const int r = (lane + kWave * i) / kTasks;
-      if (r >= m) continue;
-      *reinterpret_cast<u32x2*>(chunk(first + r, task.a)) = pack_e4m3x8(kx[i], kmul);
-      *reinterpret_cast<u32x2*>(chunk(first + r, task.b)) = pack_e4m3x8(ky[i], kmul);
-    }
-    if (kratio != 1.f)
-      for (int k = lane; k < first * kTasks; k += kWave) {
-        u32x4* g = reinterpret_cast<u32x4*>(chunk(k / kTasks, 16 * (k % kTasks)));
-        u32x4 w = *g;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) w[e] = rescale_e4m3x4(w[e], kratio);
-        *g = w;
-      }
-  } else {
-    uint16_t* kc = reinterpret_cast<uint16_t*>(p.k_cache) + at * (BS * D);
-#pragma unroll
-    for (int i = 0; i < kMine; ++i) {
-      const int r = (lane + kWave * i) / kTasks;
-      if (r >= m) continue;
-      st16(kc + (task.a / 8 * BS + first + r) * 8, narrow(kx[i]));
-      st16(kc + (task.b / 8 * BS + first + r) * 8, narrow(ky[i]));
-    }
-  }
-
-  // ---- V: transposed through LDS, then the touched units' 16-byte pieces
-#pragma unroll
-  for (int i = 0; i < kMine; ++i) {
-    const int k = lane + kWave * i;
-    if (k / kTasks >= m) continue;
-    if constexpr (k8) {
-      float x[8], y[8];
-      widen(va[i], x);
-      widen(vb[i], y);
-      const u32x2 a = pack_e4m3x8(x, vmul), c = pack_e4m3x8(y, vmul);
-      lds[k] = u32x4{a[0], a[1], c[0], c[1]};
-    } else {
-      lds[2 * k] = va[i];
-      lds[2 * k + 1] = vb[i];
-    }
-  }
-  wave_lds_fence();
   // Piece (unit, part, half): the 8 slots (i / 4) * 8 + half * 4 + i % 4 of a unit of 16, of one dim (bf16) or of
   // dims d and d + 32 (8 bits).
-  constexpr int kPieces = k8 ? D : 2 * D;   // of a unit
-  for (int c = lane; c < kUnits * kPieces; c += kWave) {
-    const int u = c / kPieces, part = c % kPieces, half = part & 1;
-    const int s0 = u * 16 + half * 4;
-    // slots s0 .. s0+3 and s0+8 .. s0+11
-    const int l = first, e = first + m;
-    const bool some = (s0 < e && s0 + 4 > l) || (s0 + 8 < e && s0 + 12 > l);
-    const bool all = s0 >= l && s0 + 12 <= e;
-    const bool again = k8 && vratio != 1.f && s0 < first;
-    if (!some && !again) continue;
-    u32x4* g;
-    int d;
-    if constexpr (k8) {
-      d = part / 64 * 64 + part % 64 / 2;
-      g = reinterpret_cast<u32x4*>(reinterpret_cast<uint8_t*>(p.v_cache) + at * (BS * D) + (u * D + part) * 16);
-    } else {
-      d = part / 2;
-      g = reinterpret_cast<u32x4*>(reinterpret_cast<uint16_t*>(p.v_cache) + at * (BS * D) + d * BS + u * 16 + half * 8);
+  constexpr int kPieces = k8 ? 1 : 2, kUnitPieces = k8 ? D : 2 * D;   // of a thread, of a unit
+  u32x4 piece[kPieces];
+  u32x4* place[kPieces];
+  int slot[kPieces], dim[kPieces];   // the piece's first slot, and dim
+  bool some[kPieces];                // new rows lie in it
+#pragma unroll
+  for (int i = 0; i < kPieces; ++i) {
+    const int c = thread + i * kThreads<D, BS>, u = c / kUnitPieces, part = c % kUnitPieces;
+    const int s0 = slot[i] = u * 16 + (part & 1) * 4;   // slots s0 .. s0+3 and s0+8 .. s0+11
+    dim[i] = k8 ? part / 64 * 64 + part % 64 / 2 : part / 2;
+    place[i] = reinterpret_cast<u32x4*>(reinterpret_cast<uint8_t*>(p.v_cache) + at * (BS * D * (k8 ? 1 : 2)) +
+                                        (k8 ? (u * D + part) * 16 : dim[i] * BS * 2 + u * 32 + (part & 1) * 16));
+    some[i] = (s0 < first + m && s0 + 4 > first) || (s0 + 8 < first + m && s0 + 12 > first);
+    piece[i] = u32x4{0u, 0u, 0u, 0u};
+    if (some[i] && !(s0 >= first && s0 + 12 <= first + m)) piece[i] = *place[i];
+  }
+  float* sp = k8 ? p.scales + 2 * at : nullptr;
+  f32x2 before = {0.f, 0.f};
+  if (k8 && first > 0) before = *reinterpret_cast<const f32x2*>(sp);
+
+  __shared__ u32x4 rows[BS * D * (k8 ? 1 : 2) / 16];   // V's new rows, as they will lie in the cache
+  float kx[8], ky[8];
+  if (row) {
+    widen(ka, kx);
+    widen(kb, ky);
+    turn_task<std::conditional_t<k8, double, float>>(p, task, g, kx, ky);
+  }
+  float kratio = 1.f, vratio = 1.f;
+  if constexpr (k8) {
+    float vx[8], vy[8], kmost = 0.f, vmost = 0.f;
+    if (row) {
+      widen(va, vx);
+      widen(vb, vy);
+      kmost = most_finite(kx, ky, kmost);
+      vmost = most_finite(vx, vy, vmost);
     }
-    u32x4 w = {0u, 0u, 0u, 0u};
-    if (!all) w = *g;
+    kmost = wave_max(kmost);
+    vmost = wave_max(vmost);
+    if constexpr (kWaves > 1) {
+      __shared__ f32x2 most[kWaves];
+      if (lane == 0) most[wave] = f32x2{kmost, vmost};
+      __syncthreads();
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) {
+        kmost = fmaxf(kmost, most[w][0]);
+        vmost = fmaxf(vmost, most[w][1]);
+      }
+    }
+    // the scales: never lowered while the block holds earlier rows, whose codes would overflow
+    float ks = exp_float(least_exp(kmost)), vs = exp_float(least_exp(vmost));
+    if (first > 0) {
+      ks = fmaxf(ks, before[0]);
+      vs = fmaxf(vs, before[1]);
+      kratio = before[0] / ks;
+      vratio = before[1] / vs;
+    }
+    if (thread == 0) *reinterpret_cast<f32x2*>(sp) = f32x2{ks, vs};
+    // K: 16 dims of a slot are contiguous
+    uint8_t* kc = reinterpret_cast<uint8_t*>(p.k_cache) + at * (BS * D);
+    auto chunk = [&](int slot, int d) { return kc + ((slot / 16 * (D / 16) + d / 16) * 16 + slot % 16) * 16 + d % 16; };
+    if (row) {
+      const float kmul = 1.f / ks, vmul = 1.f / vs;   // exact: powers of two
+      *reinterpret_cast<u32x2*>(chunk(first + r, task.a)) = pack_e4m3x8(kx, kmul);
+      *reinterpret_cast<u32x2*>(chunk(first + r, task.b)) = pack_e4m3x8(ky, kmul);
+      const u32x2 a = pack_e4m3x8(vx, vmul), c = pack_e4m3x8(vy, vmul);
+      rows[thread] = u32x4{a[0], a[1], c[0], c[1]};
+    }
+    if (kratio != 1.f && r < first) {
+      u32x4* o = reinterpret_cast<u32x4*>(chunk(r, 16 * (thread % kTasks)));
+      u32x4 w = *o;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) w[e] = rescale_e4m3x4(w[e], kratio);
+      *o = w;
+    }
+  } else if (row) {
+    uint16_t* kc = reinterpret_cast<uint16_t*>(p.k_cache) + at * (BS * D);   // 8 dims of a slot are contiguous
+    st16(kc + (task.a / 8 * BS + first + r) * 8, narrow(kx));
+    st16(kc + (task.b / 8 * BS + first + r) * 8, narrow(ky));
+    rows[2 * thread] = va;
+    rows[2 * thread + 1] = vb;
+  }
+  __syncthreads();
+
+  // ---- V: each piece with its new slots put in
+#pragma unroll
+  for (int i = 0; i < kPieces; ++i) {
+    const bool again = k8 && vratio != 1.f && slot[i] < first;   // it holds earlier rows of another scale
+    if (!some[i] && !again) continue;
+    u32x4 w = piece[i];
+    if (!some[i]) w = *place[i];
     if constexpr (k8) {
-      const uint8_t* rows = reinterpret_cast<const uint8_t*>(lds);
+      const uint8_t* in = reinterpret_cast<const uint8_t*>(rows) + dim[i];
 #pragma unroll
-      for (int j = 0; j < 2; ++j)       // dim d + 32 j: words 2j, 2j+1
+      for (int j = 0; j < 2; ++j)       // dim, dim + 32: words 2j, 2j+1
 #pragma unroll
-        for (int q = 0; q < 2; ++q) {   // slots s0 + 8 q ..
+        for (int q = 0; q < 2; ++q) {   // slots + 8 q ..
           uint32_t x = w[2 * j + q];
           if (vratio != 1.f) {
             const uint32_t y = rescale_e4m3x4(x, vratio);
 #pragma unroll
-            for (int i = 0; i < 4; ++i)   // only rows the sequence holds
-              if (s0 + 8 * q + i < first) x = (x & ~(0xFFu << (8 * i))) | (y & (0xFFu << (8 * i)));
+            for (int e = 0; e < 4; ++e)   // only rows the sequence holds
+              if (slot[i] + 8 * q + e < first) x = (x & ~(0xFFu << (8 * e))) | (y & (0xFFu << (8 * e)));
           }
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int r = s0 + 8 * q + i - first;
-            if (r >= 0 && r < m) x = (x & ~(0xFFu << (8 * i))) | ((uint32_t)rows[r * D + d + 32 * j] << (8 * i));
+          for (int e = 0; e < 4; ++e) {
+            const int k = slot[i] + 8 * q + e - first;
+            if (k >= 0 && k < m) x = (x & ~(0xFFu << (8 * e))) | ((uint32_t)in[k * D + 32 * j] << (8 * e));
           }
           w[2 * j + q] = x;
         }
     } else {
-      const uint16_t* rows = reinterpret_cast<const uint16_t*>(lds);
+      const uint16_t* in = reinterpret_cast<const uint16_t*>(rows) + dim[i];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int r = s0 + (i >> 2) * 8 + (i & 3) - first;
-        if (r < 0 || r >= m) continue;
-        const uint32_t v = rows[r * D + d];
-        w[i >> 1] = (i & 1) ? ((w[i >> 1] & 0x0000FFFFu) | (v << 16)) : ((w[i >> 1] & 0xFFFF0000u) | v);
+      for (int e = 0; e < 8; ++e) {
+        const int k = slot[i] + (e >> 2) * 8 + (e & 3) - first;
+        if (k < 0 || k >= m) continue;
+        const uint32_t v = in[k * D];
+        w[e >> 1] = (e & 1) ? ((w[e >> 1] & 0x0000FFFFu) | (v << 16)) : ((w[e >> 1] & 0xFFFF0000u) | v);
       }
     }
-    *g = w;
+    *place[i] = w;
   }
 }
 
 template <int D, int BS, bool k8>
-__global__ __launch_bounds__(256) void rotate_append_kernel(RotateParams p) {
-  __shared__ u32x4 lds[4][BS * D * (k8 ? 1 : 2) / 16];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int w = __builtin_amdgcn_readfirstlane((int)blockIdx.x * 4 + wave);   // below 2^31 (host)
-  if (w < p.append_waves) {
-    append_block<D, BS, k8>(p, w / p.hkv, w % p.hkv, lane, lds[wave]);
-  } else if (w - p.append_waves < p.query_waves) {
-    rotate_query<D>(p, w - p.append_waves, lane);
-  }
+__global__ __launch_bounds__((kThreads<D, BS>)) void rotate_append_kernel(RotateParams p) {
+  const int w = blockIdx.x;
+  if (w < p.append_groups) return append_block<D, BS, k8>(p, w / p.hkv, w % p.hkv, threadIdx.x);
+  constexpr int kWaves = kThreads<D, BS> / kWave;
+  const int tok = __builtin_amdgcn_readfirstlane((w - p.append_groups) * kWaves + (int)(threadIdx.x >> 6));
+  if (tok < p.total_tokens) rotate_query<D>(p, tok, threadIdx.x & 63);
 }
 
 template <int D, int BS, bool k8>
 static hipError_t launch_rotate_t(const RotateParams& p, hipStream_t s) {
-  const unsigned wgs = ((unsigned)p.append_waves + (unsigned)p.query_waves + 3) / 4;
-  hipLaunchKernelGGL((rotate_append_kernel<D, BS, k8>), dim3(wgs), dim3(256), 0, s, p);
+  constexpr int kWaves = kThreads<D, BS> / kWave;
+  const unsigned queries = p.q != nullptr ? ((unsigned)p.total_tokens + kWaves - 1) / kWaves : 0;
+  hipLaunchKernelGGL((rotate_append_kernel<D, BS, k8>), dim3((unsigned)p.append_groups + queries), dim3(kThreads<D, BS>), 0,
+                     s, p);
   return hipGetLastError();
 }
 template <bool k8>
@@ -364,8 +371,7 @@ static hipError_t launch_rotate_k(const RotateParams& p, hipStream_t s) {
 }
 
 hipError_t launch_rotate_append(RotateParams p, hipStream_t s) {
-  p.append_waves = (int)rotate_append_waves(p.total_tokens, p.block_size, p.num_seqs, p.hkv);
-  p.query_waves = p.q != nullptr ? p.total_tokens : 0;
+  p.append_groups = (int)rotate_append_groups(p.total_tokens, p.block_size, p.num_seqs, p.hkv);
   return p.scales != nullptr ? launch_rotate_k<true>(p, s) : launch_rotate_k<false>(p, s);
 }
 
