@@ -126,9 +126,9 @@ bool misaligned(std::initializer_list<const void*> ps) {
 }
 
 // The checks that both rotating appends share, and the launch.  max_position 0: no rotation (8-bit cache only).
-int rotate_append(const char* name, const spexis::RotateParams& p, int32_t max_query_len, void* stream) {
+int rotate_append(const char* name, const spexis::RotateParams& p, void* stream) {
   if (p.num_blocks <= 0 || p.hkv <= 0 || p.num_seqs < 0 || p.max_blocks <= 0 || p.total_tokens < 0 ||
-      max_query_len <= 0)
+      p.max_query_len <= 0)
     return fail(SPEXIS_ERR_INVALID_ARGUMENT, "%s: non-positive size", name);
   if (bad_cache_shape(p.block_size, p.head_dim))
     return fail(SPEXIS_ERR_UNSUPPORTED, "%s: block_size %d / head_dim %d not in {16,32} x {64,128}", name,
@@ -140,7 +140,8 @@ int rotate_append(const char* name, const spexis::RotateParams& p, int32_t max_q
       return fail(SPEXIS_ERR_INVALID_ARGUMENT, "%s: style %d", name, p.style);
   }
   if ((p.q || p.q_out) && p.hq <= 0) return fail(SPEXIS_ERR_INVALID_ARGUMENT, "%s: non-positive size", name);
-  if (spexis::rotate_append_groups(p.total_tokens, p.block_size, p.num_seqs, p.hkv) + p.total_tokens >= (1ll << 31) ||
+  // every workgroup and query index fits in 32 bits
+  if (((int64_t)p.total_tokens / p.block_size + 2 * (int64_t)p.num_seqs) * p.hkv + 2 * (int64_t)p.total_tokens >= (1ll << 31) ||
       (int64_t)p.max_blocks * p.block_size >= (1ll << 31))
     return fail(SPEXIS_ERR_UNSUPPORTED, "%s: more than 2^31 rows or slots", name);
   if (p.num_seqs == 0 || p.total_tokens == 0) return ok();
@@ -264,8 +265,9 @@ int spexis_rotate_append_kv(void* k_cache, void* v_cache, int32_t num_blocks, in
   if (max_position <= 0) return fail(SPEXIS_ERR_INVALID_ARGUMENT, "%s: non-positive size", name);
   spexis::RotateParams p{k_cache, v_cache, nullptr, query_start_loc, seq_lens, block_tables, new_k, new_v, q, q_out,
                          cos_sin, positions, num_blocks, num_kv_heads, block_size, head_dim, num_seqs,
-                         max_blocks_per_seq, total_tokens, num_q_heads, rotary_dim, max_position, style, 0};
-  return rotate_append(name, p, max_query_len, stream);
+                         max_blocks_per_seq, total_tokens, num_q_heads, rotary_dim, max_position, style, max_query_len, 0, 0, 0,
+                         0};
+  return rotate_append(name, p, stream);
 }
 
 int spexis_rotate_append_kv8(void* k_cache, void* v_cache, float* scales, int32_t num_blocks, int32_t num_kv_heads,
@@ -280,9 +282,10 @@ int spexis_rotate_append_kv8(void* k_cache, void* v_cache, float* scales, int32_
     return fail(SPEXIS_ERR_INVALID_ARGUMENT, "%s: a rotation without a table", name);
   spexis::RotateParams p{k_cache, v_cache, scales, query_start_loc, seq_lens, block_tables, new_k, new_v, q, q_out,
                          cos_sin, positions, num_blocks, num_kv_heads, block_size, head_dim, num_seqs,
-                         max_blocks_per_seq, total_tokens, num_q_heads, rotary_dim, max_position, style, 0};
+                         max_blocks_per_seq, total_tokens, num_q_heads, rotary_dim, max_position, style, max_query_len, 0, 0, 0,
+                         0};
   if (num_seqs > 0 && total_tokens > 0 && !scales) return fail(SPEXIS_ERR_INVALID_ARGUMENT, "%s: null pointer", name);
-  return rotate_append(name, p, max_query_len, stream);
+  return rotate_append(name, p, stream);
 }
 
 size_t spexis_verify_attention_workspace_size(int32_t num_seqs, int32_t num_q_heads, int32_t num_kv_heads,

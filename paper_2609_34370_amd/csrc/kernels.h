@@ -35,13 +35,11 @@ struct RotateParams {
   const int32_t* positions;  // [T], or null: the token's place in its sequence
   int num_blocks, hkv, block_size, head_dim, num_seqs, max_blocks, total_tokens;
   int hq, rot, max_position, style;   // style 0: elements i and i + rot/2 turn together; 1: 2i and 2i+1
-  int append_groups;                  // set by the launcher
+  int max_query_len;
+  // set by the launcher: workgroups that write rows; waves that turn queries; blocks and tokens of each sequence, or
+  // 0: by search
+  int append_groups, queries, seq_blocks, seq_tokens;
 };
-// Workgroups that write rows: one per KV head and block index (csrc/rotate.hip).
-inline int64_t rotate_append_groups(int64_t tokens, int64_t block_size, int64_t num_seqs, int64_t hkv) {
-  return (tokens / block_size + 2 * num_seqs) * hkv;
-}
-
 constexpr int kAttnHdrInts = 8;           // per-wave header of the partial an item's first wave leaves
 constexpr int kAttnMinTilesPerWave = 2;   // floor of the even split (short batches)
 constexpr int kAttnMaxWaves = 1024;       // waves of the even split: one per SIMD of 256 CUs

@@ -10,8 +10,9 @@
 // its heads.  A block belongs to one workgroup because the scale of an 8-bit block needs all its rows, and
 // because V is stored 8 slots to a 16-byte piece, which is rewritten whole: no two workgroups write into one piece.
 // Which block: sequence b gets the indices from start(b) = floor(qsl[b] / bs) + 2 b.  n new tokens touch at most
-// floor(n / bs) + 2 blocks, which start(b+1) - start(b) is never below, so the launch needs no length
-// on the host and no scan: wave-wide search for the last b with start(b) <= index, two probes for 4096 sequences.
+// floor(n / bs) + 2 blocks, which start(b+1) - start(b) is never below, so no scan over the lengths is needed: a
+// wave-wide search for the last b with start(b) <= index, two probes for 4096 sequences.  Where the sequences are of
+// about one length (a step's drafts), index / (blocks of the longest) does without the search.
 #include <type_traits>
 
 #include "common.h"
@@ -83,31 +84,61 @@ __device__ __forceinline__ u32x4 narrow(const float (&x)[8]) {
 // a rounding to bf16, whose half step is 2^15 times larger.
 template <typename T>
 __device__ __forceinline__ void turn(float& a, float& b, float c, float s) {
+  // widened here, pair by pair (no instruction; the compiler would widen a whole task first, 64 more registers)
+  if constexpr (sizeof(T) == 8) asm volatile("" : "+v"(a), "+v"(b), "+v"(c), "+v"(s));
   const T x = a, y = b, cc = c, ss = s;
   a = (float)(x * cc - y * ss);
   b = (float)(y * cc + x * ss);
 }
-template <typename T>
-__device__ __forceinline__ void turn_task(const RotateParams& p, const Task& t, const Angles& g, float (&x)[8], float (&y)[8]) {
-  if (!t.turns) return;
+// A task's elements as pairs (x[i], y[i]), and back.  Halves: x is chunk a, y chunk b; pairs: x the even elements, y the
+// odd ones.
+__device__ __forceinline__ void to_pairs(const RotateParams& p, u32x4 a, u32x4 b, float (&x)[8], float (&y)[8]) {
   if (p.style == 0) {
+    widen(a, x);
+    widen(b, y);
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const uint32_t w = i < 4 ? a[i] : b[i - 4];
+    x[i] = __uint_as_float(w << 16);
+    y[i] = __uint_as_float(w & 0xFFFF0000u);
+  }
+}
+__device__ __forceinline__ void from_pairs(const RotateParams& p, float (&x)[8], float (&y)[8]) {
+  if (p.style == 0) return;
+  const float a[8] = {x[0], y[0], x[1], y[1], x[2], y[2], x[3], y[3]}, b[8] = {x[4], y[4], x[5], y[5], x[6], y[6], x[7], y[7]};
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    x[i] = a[i];
+    y[i] = b[i];
+  }
+}
+// Chunks a and b turned: x and y are theirs.
+template <typename T>
+__device__ __forceinline__ void turn_task(const RotateParams& p, const Task& t, const Angles& g, u32x4 a, u32x4 b, float (&x)[8],
+                                          float (&y)[8]) {
+  to_pairs(p, a, b, x, y);
+  if (t.turns) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) turn<T>(x[i], y[i], g.c[i], g.s[i]);
-  } else {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      turn<T>(x[2 * i], x[2 * i + 1], g.c[i], g.s[i]);
-      turn<T>(y[2 * i], y[2 * i + 1], g.c[4 + i], g.s[4 + i]);
-    }
   }
+  from_pairs(p, x, y);
 }
 
 // q of one token, every head, one wave: the lanes are (head, task), so the token's angles are loaded once; the rows are
 // in flight while the position is looked up.
 template <int D>
-__device__ __forceinline__ void rotate_query(const RotateParams& p, int tok, int lane) {
-  constexpr int kTasks = D / 16, kHeads = kWave / kTasks, kAhead = 4;
+__device__ __forceinline__ void rotate_query(const RotateParams& p, int index, int lane) {
+  constexpr int kTasks = D / 16, kHeads = kWave / kTasks, kAhead = 2;
   const Task task = row_task(p, lane % kTasks);
+  int tok = index, s = 0, q1 = 0;
+  if (p.seq_tokens > 0) {   // token index % seq_tokens of sequence index / seq_tokens
+    s = index / p.seq_tokens;
+    q1 = clampi(p.qsl[s + 1], 0, p.total_tokens);
+    tok = seq_start(p, s) + index % p.seq_tokens;
+    if (tok >= q1) return;
+  }
   const uint16_t* q = reinterpret_cast<const uint16_t*>(p.q) + (int64_t)tok * p.hq * D;
   uint16_t* o = reinterpret_cast<uint16_t*>(p.q_out) + (int64_t)tok * p.hq * D;
   u32x4 a[kAhead], b[kAhead];
@@ -124,8 +155,11 @@ __device__ __forceinline__ void rotate_query(const RotateParams& p, int tok, int
   if (p.positions != nullptr) {
     pos = p.positions[tok];
   } else {
-    const int s = wave_search(p.num_seqs, tok, lane, [&](int i) { return seq_start(p, i); });
-    pos = p.seq_lens[s] - (clampi(p.qsl[s + 1], 0, p.total_tokens) - tok);
+    if (p.seq_tokens == 0) {
+      s = wave_search(p.num_seqs, tok, lane, [&](int i) { return seq_start(p, i); });
+      q1 = clampi(p.qsl[s + 1], 0, p.total_tokens);
+    }
+    pos = p.seq_lens[s] - (q1 - tok);
   }
   Angles g;
   if (task.turns) g = load_angles(p, task, pos);
@@ -136,52 +170,77 @@ __device__ __forceinline__ void rotate_query(const RotateParams& p, int tok, int
       const int h = h0 + i * kHeads;
       if (h >= p.hq) break;
       float x[8], y[8];
-      widen(a[i], x);
-      widen(b[i], y);
-      turn_task<float>(p, task, g, x, y);
+      turn_task<float>(p, task, g, a[i], b[i], x, y);
       st16(o + h * D + task.a, narrow(x));
       st16(o + h * D + task.b, narrow(y));
     }
   }
 }
 
-// Two values of at most 448 to e4m3 codes, to nearest even.  The format has no infinity: what is not finite
-// becomes the NaN 0x7f (put in by hand: the conversion would give a NaN of either sign).
-__device__ __forceinline__ uint32_t pack_e4m3x2(float x, float y) {
-  const bool bx = !(fabsf(x) < __builtin_inff()), by = !(fabsf(y) < __builtin_inff());
-  const uint32_t w = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(bx ? 0.f : x, by ? 0.f : y, 0, false) & 0xFFFFu;
-  return w | (bx ? 0x7Fu : 0u) | (by ? 0x7F00u : 0u);
+// Four values of at most 448 to e4m3 codes, to nearest even.
+__device__ __forceinline__ uint32_t pack_e4m3x4(float a, float b, float c, float d) {
+  const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, lo, true);
 }
 __device__ __forceinline__ u32x2 pack_e4m3x8(const float (&x)[8], float mul) {
-  u32x2 w;
-#pragma unroll
-  for (int i = 0; i < 2; ++i)
-    w[i] = pack_e4m3x2(x[4 * i] * mul, x[4 * i + 1] * mul) | (pack_e4m3x2(x[4 * i + 2] * mul, x[4 * i + 3] * mul) << 16);
-  return w;
+  return u32x2{pack_e4m3x4(x[0] * mul, x[1] * mul, x[2] * mul, x[3] * mul),
+               pack_e4m3x4(x[4] * mul, x[5] * mul, x[6] * mul, x[7] * mul)};
 }
-// Four codes whose scale changes by the factor r.
+// Four codes whose scale changes by the factor r; a NaN becomes 0x7f.
 __device__ __forceinline__ uint32_t rescale_e4m3x4(uint32_t w, float r) {
   const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true);
-  return pack_e4m3x2(lo[0] * r, lo[1] * r) | (pack_e4m3x2(hi[0] * r, hi[1] * r) << 16);
+  const uint32_t nan = ((((w & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u) >> 7) * 0xFFu;
+  return (pack_e4m3x4(lo[0] * r, lo[1] * r, hi[0] * r, hi[1] * r) & ~nan) | (nan & 0x7F7F7F7Fu);
+}
+// The format has no infinity: what is not finite is stored as the NaN 0x7f, written over the conversion's result.
+__device__ __forceinline__ void store_nans(const float (&x)[8], uint8_t* codes, int step) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e)
+    if (!(fabsf(x[e]) < __builtin_inff())) codes[e * step] = 0x7F;
 }
 
 // The exponent of the least power of two, from 2^-100, by which `most` is at most 448 = 1.75 * 2^8.
-__device__ __forceinline__ int least_exp(float most) {
-  const uint32_t u = __float_as_uint(most);
+__device__ __forceinline__ int least_exp(uint32_t u) {   // most's bits
   const int e = (int)(u >> 23) - 127 - 8 + ((u & 0x7FFFFFu) > 0x600000u ? 1 : 0);
   return max(e, -100);
 }
 __device__ __forceinline__ float exp_float(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
 
-// The largest finite magnitude of 16 values, at least m.
-__device__ __forceinline__ float most_finite(const float (&x)[8], const float (&y)[8], float m) {
+constexpr uint32_t kInf = 0x7F800000u;
+// The largest magnitude of 16 values as bits, from kInf up if one is not finite; and the largest of the finite ones.
+__device__ __forceinline__ uint32_t most_bits(const float (&x)[8], const float (&y)[8]) {
+  uint32_t m = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) m = max(m, max(__float_as_uint(x[i]) & 0x7FFFFFFFu, __float_as_uint(y[i]) & 0x7FFFFFFFu));
+  return m;
+}
+__device__ __forceinline__ uint32_t most_finite_bits(const float (&x)[8], const float (&y)[8]) {
+  uint32_t m = 0;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    const float a = fabsf(x[i]), b = fabsf(y[i]);
-    m = fmaxf(m, a < __builtin_inff() ? a : 0.f);
-    m = fmaxf(m, b < __builtin_inff() ? b : 0.f);
+    const uint32_t a = __float_as_uint(x[i]) & 0x7FFFFFFFu, b = __float_as_uint(y[i]) & 0x7FFFFFFFu;
+    m = max(m, max(a < kInf ? a : 0u, b < kInf ? b : 0u));
   }
   return m;
+}
+// The same of one wave's 16 bf16 values a lane, without widening them: the largest 15-bit pattern.
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t most_bits_bf16(u32x4 a, u32x4 b) {
+  u16x2 m = {0, 0};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    m = __builtin_elementwise_max(m, __builtin_bit_cast(u16x2, a[i] & 0x7FFF7FFFu));
+    m = __builtin_elementwise_max(m, __builtin_bit_cast(u16x2, b[i] & 0x7FFF7FFFu));
+  }
+  return (uint32_t)max(m[0], m[1]) << 16;
+}
+
+// Ones in the bytes of the values (of kBytes each) k with lo <= k < hi, of a word that holds values 0 ...
+template <int kBytes>
+__device__ __forceinline__ uint32_t value_mask(int lo, int hi) {
+  constexpr int kValues = 4 / kBytes;
+  auto below = [](int n) { return n <= 0 ? 0u : n >= kValues ? 0xFFFFFFFFu : (1u << (8 * kBytes * n)) - 1u; };
+  return below(hi) & ~below(lo);
 }
 
 // A thread takes one task of K and of V of a block's rows: a workgroup is a (block of tokens, KV head).
@@ -193,11 +252,12 @@ template <int D, int BS, bool k8>
 __device__ __forceinline__ void append_block(const RotateParams& p, int index, int h, int thread) {
   constexpr int kTasks = D / 16, kWaves = kThreads<D, BS> / kWave;
   const int lane = thread & 63, wave = thread >> 6;
-  const int b = wave_search(p.num_seqs, index, lane, [&](int i) { return seq_start(p, i) / BS + 2 * i; });
+  const int b = p.seq_blocks > 0 ? index / p.seq_blocks
+                                 : wave_search(p.num_seqs, index, lane, [&](int i) { return seq_start(p, i) / BS + 2 * i; });
   const int q0 = seq_start(p, b), q1 = clampi(p.qsl[b + 1], q0, p.total_tokens);
   const int cap = p.max_blocks * BS;
   const int n = min(q1 - q0, cap), S = clampi(p.seq_lens[b], n, cap), L = S - n;
-  const int t = L / BS + (index - (q0 / BS + 2 * b));
+  const int t = L / BS + (p.seq_blocks > 0 ? index % p.seq_blocks : index - (q0 / BS + 2 * b));
   if (n == 0 || t < L / BS || t > (S - 1) / BS) return;
   const int lo = max(L, t * BS), m = min(S, (t + 1) * BS) - lo;   // first new position, new rows
   const int first = lo - t * BS;                                  // its slot: the block holds that many rows
@@ -243,32 +303,37 @@ __device__ __forceinline__ void append_block(const RotateParams& p, int index, i
   f32x2 before = {0.f, 0.f};
   if (k8 && first > 0) before = *reinterpret_cast<const f32x2*>(sp);
 
-  __shared__ u32x4 rows[BS * D * (k8 ? 1 : 2) / 16];   // V's new rows, as they will lie in the cache
+  // V's new rows as they will lie in the cache: piece c at image[c], the thread's 16 dims at places 32 bytes apart
+  constexpr int kBytes = k8 ? 1 : 2;
+  __shared__ u32x4 image[BS * D * kBytes / 16];
+  const int at_slot = first + r, us = at_slot & 15, pos = (us >> 3) * 4 + (us & 3), t16 = thread % kTasks;
+  uint8_t* mine = reinterpret_cast<uint8_t*>(image) +
+                  (k8 ? (at_slot >> 4) * 16 * D + ((t16 >> 2) * 32 + (t16 & 1) * 16) * 32 + (t16 >> 1 & 1) * 8
+                      : (at_slot >> 4) * 32 * D + t16 * 16 * 32) +
+                  (us >> 2 & 1) * 16 + pos * kBytes;
   float kx[8], ky[8];
-  if (row) {
-    widen(ka, kx);
-    widen(kb, ky);
-    turn_task<std::conditional_t<k8, double, float>>(p, task, g, kx, ky);
-  }
+  if (row) turn_task<std::conditional_t<k8, double, float>>(p, task, g, ka, kb, kx, ky);
   float kratio = 1.f, vratio = 1.f;
   if constexpr (k8) {
-    float vx[8], vy[8], kmost = 0.f, vmost = 0.f;
-    if (row) {
+    uint32_t kmost = row ? most_bits(kx, ky) : 0u, vmost = row ? most_bits_bf16(va, vb) : 0u;
+    const bool finite = __builtin_amdgcn_ballot_w64(kmost >= kInf || vmost >= kInf) == 0;   // the wave's values
+    if (!finite && row) {
+      float vx[8], vy[8];
       widen(va, vx);
       widen(vb, vy);
-      kmost = most_finite(kx, ky, kmost);
-      vmost = most_finite(vx, vy, vmost);
+      kmost = most_finite_bits(kx, ky);
+      vmost = most_finite_bits(vx, vy);
     }
-    kmost = wave_max(kmost);
-    vmost = wave_max(vmost);
+    kmost = __float_as_uint(wave_max(__uint_as_float(kmost)));
+    vmost = __float_as_uint(wave_max(__uint_as_float(vmost)));
     if constexpr (kWaves > 1) {
-      __shared__ f32x2 most[kWaves];
-      if (lane == 0) most[wave] = f32x2{kmost, vmost};
+      __shared__ u32x2 most[kWaves];
+      if (lane == 0) most[wave] = u32x2{kmost, vmost};
       __syncthreads();
 #pragma unroll
       for (int w = 0; w < kWaves; ++w) {
-        kmost = fmaxf(kmost, most[w][0]);
-        vmost = fmaxf(vmost, most[w][1]);
+        kmost = max(kmost, most[w][0]);
+        vmost = max(vmost, most[w][1]);
       }
     }
     // the scales: never lowered while the block holds earlier rows, whose codes would overflow
@@ -285,13 +350,25 @@ __device__ __forceinline__ void append_block(const RotateParams& p, int index, i
     auto chunk = [&](int slot, int d) { return kc + ((slot / 16 * (D / 16) + d / 16) * 16 + slot % 16) * 16 + d % 16; };
     if (row) {
       const float kmul = 1.f / ks, vmul = 1.f / vs;   // exact: powers of two
-      *reinterpret_cast<u32x2*>(chunk(first + r, task.a)) = pack_e4m3x8(kx, kmul);
-      *reinterpret_cast<u32x2*>(chunk(first + r, task.b)) = pack_e4m3x8(ky, kmul);
-      const u32x2 a = pack_e4m3x8(vx, vmul), c = pack_e4m3x8(vy, vmul);
-      rows[thread] = u32x4{a[0], a[1], c[0], c[1]};
+      *reinterpret_cast<u32x2*>(chunk(at_slot, task.a)) = pack_e4m3x8(kx, kmul);
+      *reinterpret_cast<u32x2*>(chunk(at_slot, task.b)) = pack_e4m3x8(ky, kmul);
+      if (!finite) {
+        store_nans(kx, chunk(at_slot, task.a), 1);
+        store_nans(ky, chunk(at_slot, task.b), 1);
+      }
+      auto values = [&](u32x4 v, uint8_t* to) {
+        float x[8];
+        widen(v, x);
+        const u32x2 c = pack_e4m3x8(x, vmul);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) to[32 * e] = (uint8_t)(c[e / 4] >> (8 * (e % 4)));
+        if (!finite) store_nans(x, to, 32);
+      };
+      values(va, mine);
+      values(vb, mine + 8 * 32);
     }
     if (kratio != 1.f && r < first) {
-      u32x4* o = reinterpret_cast<u32x4*>(chunk(r, 16 * (thread % kTasks)));
+      u32x4* o = reinterpret_cast<u32x4*>(chunk(r, 16 * t16));
       u32x4 w = *o;
 #pragma unroll
       for (int e = 0; e < 4; ++e) w[e] = rescale_e4m3x4(w[e], kratio);
@@ -299,10 +376,11 @@ __device__ __forceinline__ void append_block(const RotateParams& p, int index, i
     }
   } else if (row) {
     uint16_t* kc = reinterpret_cast<uint16_t*>(p.k_cache) + at * (BS * D);   // 8 dims of a slot are contiguous
-    st16(kc + (task.a / 8 * BS + first + r) * 8, narrow(kx));
-    st16(kc + (task.b / 8 * BS + first + r) * 8, narrow(ky));
-    rows[2 * thread] = va;
-    rows[2 * thread + 1] = vb;
+    st16(kc + (task.a / 8 * BS + at_slot) * 8, narrow(kx));
+    st16(kc + (task.b / 8 * BS + at_slot) * 8, narrow(ky));
+#pragma unroll
+    for (int e = 0; e < 16; ++e)
+      *reinterpret_cast<uint16_t*>(mine + 32 * e) = (uint16_t)((e < 8 ? va[e / 2] : vb[e / 2 - 4]) >> (16 * (e % 2)));
   }
   __syncthreads();
 
@@ -312,35 +390,28 @@ __device__ __forceinline__ void append_block(const RotateParams& p, int index, i
     const bool again = k8 && vratio != 1.f && slot[i] < first;   // it holds earlier rows of another scale
     if (!some[i] && !again) continue;
     u32x4 w = piece[i];
-    if (!some[i]) w = *place[i];
+    if (k8 && !some[i]) w = *place[i];
+    const u32x4 in = image[thread + i * kThreads<D, BS>];
     if constexpr (k8) {
-      const uint8_t* in = reinterpret_cast<const uint8_t*>(rows) + dim[i];
+      // words q and q + 2: slots + 8 q .. + 8 q + 3 of dim and of dim + 32
 #pragma unroll
-      for (int j = 0; j < 2; ++j)       // dim, dim + 32: words 2j, 2j+1
-#pragma unroll
-        for (int q = 0; q < 2; ++q) {   // slots + 8 q ..
-          uint32_t x = w[2 * j + q];
-          if (vratio != 1.f) {
-            const uint32_t y = rescale_e4m3x4(x, vratio);
-#pragma unroll
-            for (int e = 0; e < 4; ++e)   // only rows the sequence holds
-              if (slot[i] + 8 * q + e < first) x = (x & ~(0xFFu << (8 * e))) | (y & (0xFFu << (8 * e)));
-          }
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int k = slot[i] + 8 * q + e - first;
-            if (k >= 0 && k < m) x = (x & ~(0xFFu << (8 * e))) | ((uint32_t)in[k * D + 32 * j] << (8 * e));
-          }
-          w[2 * j + q] = x;
+      for (int q = 0; q < 2; ++q) {
+        const int s0 = slot[i] + 8 * q;
+        if (vratio != 1.f) {
+          const uint32_t held = value_mask<1>(0, first - s0);   // only rows the sequence holds
+          w[q] = (w[q] & ~held) | (rescale_e4m3x4(w[q], vratio) & held);
+          w[q + 2] = (w[q + 2] & ~held) | (rescale_e4m3x4(w[q + 2], vratio) & held);
         }
+        const uint32_t fresh = value_mask<1>(first - s0, first + m - s0);
+        w[q] = (w[q] & ~fresh) | (in[q] & fresh);
+        w[q + 2] = (w[q + 2] & ~fresh) | (in[q + 2] & fresh);
+      }
     } else {
-      const uint16_t* in = reinterpret_cast<const uint16_t*>(rows) + dim[i];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const int k = slot[i] + (e >> 2) * 8 + (e & 3) - first;
-        if (k < 0 || k >= m) continue;
-        const uint32_t v = in[k * D];
-        w[e >> 1] = (e & 1) ? ((w[e >> 1] & 0x0000FFFFu) | (v << 16)) : ((w[e >> 1] & 0xFFFF0000u) | v);
+      for (int q = 0; q < 4; ++q) {   // slots s0, s0 + 1
+        const int s0 = slot[i] + q / 2 * 8 + q % 2 * 2;
+        const uint32_t fresh = value_mask<2>(first - s0, first + m - s0);
+        w[q] = (w[q] & ~fresh) | (in[q] & fresh);
       }
     }
     *place[i] = w;
@@ -352,14 +423,14 @@ __global__ __launch_bounds__((kThreads<D, BS>)) void rotate_append_kernel(Rotate
   const int w = blockIdx.x;
   if (w < p.append_groups) return append_block<D, BS, k8>(p, w / p.hkv, w % p.hkv, threadIdx.x);
   constexpr int kWaves = kThreads<D, BS> / kWave;
-  const int tok = __builtin_amdgcn_readfirstlane((w - p.append_groups) * kWaves + (int)(threadIdx.x >> 6));
-  if (tok < p.total_tokens) rotate_query<D>(p, tok, threadIdx.x & 63);
+  const int query = __builtin_amdgcn_readfirstlane((w - p.append_groups) * kWaves + (int)(threadIdx.x >> 6));
+  if (query < p.queries) rotate_query<D>(p, query, threadIdx.x & 63);
 }
 
 template <int D, int BS, bool k8>
 static hipError_t launch_rotate_t(const RotateParams& p, hipStream_t s) {
   constexpr int kWaves = kThreads<D, BS> / kWave;
-  const unsigned queries = p.q != nullptr ? ((unsigned)p.total_tokens + kWaves - 1) / kWaves : 0;
+  const unsigned queries = ((unsigned)p.queries + kWaves - 1) / kWaves;
   hipLaunchKernelGGL((rotate_append_kernel<D, BS, k8>), dim3((unsigned)p.append_groups + queries), dim3(kThreads<D, BS>), 0,
                      s, p);
   return hipGetLastError();
@@ -371,7 +442,13 @@ static hipError_t launch_rotate_k(const RotateParams& p, hipStream_t s) {
 }
 
 hipError_t launch_rotate_append(RotateParams p, hipStream_t s) {
-  p.append_groups = (int)rotate_append_groups(p.total_tokens, p.block_size, p.num_seqs, p.hkv);
+  const int64_t B = p.num_seqs, T = p.total_tokens, bs = p.block_size, n = p.max_query_len;
+  // Sequences of about one length need no search: the longest one's blocks (tokens) for each, where that is no more.
+  const int64_t blocks = B * ((n + bs - 2) / bs + 1), all = T / bs + 2 * B;
+  p.seq_blocks = blocks <= all ? (int)((n + bs - 2) / bs + 1) : 0;
+  p.append_groups = (int)((blocks <= all ? blocks : all) * p.hkv);
+  p.seq_tokens = 4 * B * n <= 5 * T ? (int)n : 0;
+  p.queries = p.q == nullptr ? 0 : p.seq_tokens > 0 ? (int)(B * n) : (int)T;
   return p.scales != nullptr ? launch_rotate_k<true>(p, s) : launch_rotate_k<false>(p, s);
 }
 
