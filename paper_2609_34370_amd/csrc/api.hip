@@ -140,10 +140,12 @@ int rotate_append(const char* name, const spexis::RotateParams& p, void* stream)
       return fail(SPEXIS_ERR_INVALID_ARGUMENT, "%s: style %d", name, p.style);
   }
   if ((p.q || p.q_out) && p.hq <= 0) return fail(SPEXIS_ERR_INVALID_ARGUMENT, "%s: non-positive size", name);
-  // every workgroup and query index fits in 32 bits
-  if (((int64_t)p.total_tokens / p.block_size + 2 * (int64_t)p.num_seqs) * p.hkv + 2 * (int64_t)p.total_tokens >= (1ll << 31) ||
+  // a launch holds fewer than 2^32 threads: at most head_dim * block_size / 16 for a (block, KV head), 64 for a query
+  // token, of which there may be a quarter more than tokens; alternating the two at most doubles their number
+  const int64_t blocks = (int64_t)p.total_tokens / p.block_size + 2 * (int64_t)p.num_seqs;
+  if (2.0 * ((double)blocks * p.hkv * p.head_dim * p.block_size / 16 + 80.0 * p.total_tokens + 512) >= 4294967296.0 ||
       (int64_t)p.max_blocks * p.block_size >= (1ll << 31))
-    return fail(SPEXIS_ERR_UNSUPPORTED, "%s: more than 2^31 rows or slots", name);
+    return fail(SPEXIS_ERR_UNSUPPORTED, "%s: too many tokens or slots", name);
   if (p.num_seqs == 0 || p.total_tokens == 0) return ok();
   if (!p.k_cache || !p.v_cache || !p.qsl || !p.seq_lens || !p.block_tables || !p.new_k || !p.new_v ||
       (p.max_position > 0 && !p.cos_sin) || !p.q != !p.q_out)
@@ -266,7 +268,7 @@ int spexis_rotate_append_kv(void* k_cache, void* v_cache, int32_t num_blocks, in
   spexis::RotateParams p{k_cache, v_cache, nullptr, query_start_loc, seq_lens, block_tables, new_k, new_v, q, q_out,
                          cos_sin, positions, num_blocks, num_kv_heads, block_size, head_dim, num_seqs,
                          max_blocks_per_seq, total_tokens, num_q_heads, rotary_dim, max_position, style, max_query_len, 0, 0, 0,
-                         0};
+                         0, 0, 0};
   return rotate_append(name, p, stream);
 }
 
@@ -283,7 +285,7 @@ int spexis_rotate_append_kv8(void* k_cache, void* v_cache, float* scales, int32_
   spexis::RotateParams p{k_cache, v_cache, scales, query_start_loc, seq_lens, block_tables, new_k, new_v, q, q_out,
                          cos_sin, positions, num_blocks, num_kv_heads, block_size, head_dim, num_seqs,
                          max_blocks_per_seq, total_tokens, num_q_heads, rotary_dim, max_position, style, max_query_len, 0, 0, 0,
-                         0};
+                         0, 0, 0};
   if (num_seqs > 0 && total_tokens > 0 && !scales) return fail(SPEXIS_ERR_INVALID_ARGUMENT, "%s: null pointer", name);
   return rotate_append(name, p, stream);
 }
@@ -370,7 +372,7 @@ int spexis_token_logprobs(int32_t logits_type, const void* logits, int64_t row_s
     return fail(SPEXIS_ERR_UNSUPPORTED, "%s: vocab %d > %d or top_n %d > %d", name, vocab, kMaxVocab, top_n,
                 spexis::kLogprobMaxTop);
   const int parts = spexis::logprob_parts(std::max(num_items, 1), vocab);
-  if ((int64_t)num_items * parts >= (1ll << 31)) return fail(SPEXIS_ERR_UNSUPPORTED, "%s: too many items", name);
+  if ((int64_t)num_items * parts >= (1ll << 24)) return fail(SPEXIS_ERR_UNSUPPORTED, "%s: too many items", name);
   if (num_items == 0) return ok();
   if (!logits || !token_ids || !logprobs || (top_n > 0 && (!top_ids || !top_logprobs)))
     return fail(SPEXIS_ERR_INVALID_ARGUMENT, "%s: null pointer", name);

@@ -37,8 +37,8 @@ struct RotateParams {
   int hq, rot, max_position, style;   // style 0: elements i and i + rot/2 turn together; 1: 2i and 2i+1
   int max_query_len;
   // set by the launcher: workgroups that write rows; waves that turn queries; blocks and tokens of each sequence, or
-  // 0: by search
-  int append_groups, queries, seq_blocks, seq_tokens;
+  // 0: by search; how the two kinds alternate; whether q is too large for the caches
+  int append_groups, queries, seq_blocks, seq_tokens, mix, stream_q;
 };
 constexpr int kAttnHdrInts = 8;           // per-wave header of the partial an item's first wave leaves
 constexpr int kAttnMinTilesPerWave = 2;   // floor of the even split (short batches)

@@ -146,8 +146,10 @@ __device__ __forceinline__ void rotate_query(const RotateParams& p, int index, i
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) {
       const int h = min(h0 + i * kHeads, p.hq - 1);
-      a[i] = ld16(q + h * D + task.a);
-      b[i] = ld16(q + h * D + task.b);
+      const u32x4* pa = reinterpret_cast<const u32x4*>(q + h * D + task.a);
+      const u32x4* pb = reinterpret_cast<const u32x4*>(q + h * D + task.b);
+      a[i] = p.stream_q ? __builtin_nontemporal_load(pa) : *pa;
+      b[i] = p.stream_q ? __builtin_nontemporal_load(pb) : *pb;
     }
   };
   load(lane / kTasks);
@@ -171,8 +173,10 @@ __device__ __forceinline__ void rotate_query(const RotateParams& p, int index, i
       if (h >= p.hq) break;
       float x[8], y[8];
       turn_task<float>(p, task, g, a[i], b[i], x, y);
-      st16(o + h * D + task.a, narrow(x));
-      st16(o + h * D + task.b, narrow(y));
+      // written once, read by a later launch (512 sequences of 9 rows: 19.5 us, plain stores 23.2; 12000 prompt
+      // tokens 52.9 and 54.2)
+      __builtin_nontemporal_store(narrow(x), reinterpret_cast<u32x4*>(o + h * D + task.a));
+      __builtin_nontemporal_store(narrow(y), reinterpret_cast<u32x4*>(o + h * D + task.b));
     }
   }
 }
@@ -243,7 +247,9 @@ __device__ __forceinline__ uint32_t value_mask(int lo, int hi) {
   return below(hi) & ~below(lo);
 }
 
-// A thread takes one task of K and of V of a block's rows: a workgroup is a (block of tokens, KV head).
+// A workgroup is a (block of tokens, KV head); a thread takes one task of K and of V.  (With half the threads where a
+// step has at most 16 new rows, 512 sequences of 9 rows took 14.8 us instead of 17.9 without queries, but 24.0 instead
+// of 22.8 with them.)
 template <int D, int BS>
 constexpr int kThreads = BS * D / 16;
 
@@ -256,7 +262,7 @@ __device__ __forceinline__ void append_block(const RotateParams& p, int index, i
                                  : wave_search(p.num_seqs, index, lane, [&](int i) { return seq_start(p, i) / BS + 2 * i; });
   const int q0 = seq_start(p, b), q1 = clampi(p.qsl[b + 1], q0, p.total_tokens);
   const int cap = p.max_blocks * BS;
-  const int n = min(q1 - q0, cap), S = clampi(p.seq_lens[b], n, cap), L = S - n;
+  const int n = min(min(q1 - q0, p.max_query_len), cap), S = clampi(p.seq_lens[b], n, cap), L = S - n;
   const int t = L / BS + (p.seq_blocks > 0 ? index % p.seq_blocks : index - (q0 / BS + 2 * b));
   if (n == 0 || t < L / BS || t > (S - 1) / BS) return;
   const int lo = max(L, t * BS), m = min(S, (t + 1) * BS) - lo;   // first new position, new rows
@@ -414,25 +420,57 @@ __device__ __forceinline__ void append_block(const RotateParams& p, int index, i
         w[q] = (w[q] & ~fresh) | (in[q] & fresh);
       }
     }
-    *place[i] = w;
+    // whole lines of new slots in the 8-bit cache: 8 prompts of 100 to 3500 tokens 22.6 us without queries, plain
+    // stores 25.5 (bf16, where a piece is part of a line, 16.4 and 14.5)
+    if constexpr (k8) __builtin_nontemporal_store(w, place[i]);
+    else *place[i] = w;
   }
 }
 
 template <int D, int BS, bool k8>
 __global__ __launch_bounds__((kThreads<D, BS>)) void rotate_append_kernel(RotateParams p) {
-  const int w = blockIdx.x;
-  if (w < p.append_groups) return append_block<D, BS, k8>(p, w / p.hkv, w % p.hkv, threadIdx.x);
+  // 8 bits: workgroups of the two kinds alternate, `mix` of one to one of the other: appends compute and wait for one
+  // load after the other, queries keep the memory busy meanwhile (512 sequences of 9 rows: 22.8 us, appends first
+  // 27.0).  bf16 appends are as bound by memory as queries and come first (54.2 us, alternating 58.0, at 12000 tokens).
   constexpr int kWaves = kThreads<D, BS> / kWave;
-  const int query = __builtin_amdgcn_readfirstlane((w - p.append_groups) * kWaves + (int)(threadIdx.x >> 6));
+  const int w = blockIdx.x, m = p.mix < 0 ? -p.mix : p.mix, q = k8 ? w / (m + 1) : 0, r = k8 ? w % (m + 1) : 0;
+  int append, query;   // the index of the one that this workgroup is
+  if constexpr (!k8) {
+    append = w < p.append_groups ? w : -1;
+    query = w - p.append_groups;
+  } else if (p.mix >= 0) {    // r < m: append q m + r, else queries q
+    append = r < m ? q * m + r : -1;
+    query = q;
+  } else {
+    append = r == m ? q : -1;
+    query = q * m + r;
+  }
+  if (append >= 0) {
+    if (append < p.append_groups) append_block<D, BS, k8>(p, append / p.hkv, append % p.hkv, threadIdx.x);
+    return;
+  }
+  query = __builtin_amdgcn_readfirstlane(query * kWaves + (int)(threadIdx.x >> 6));
   if (query < p.queries) rotate_query<D>(p, query, threadIdx.x & 63);
 }
 
 template <int D, int BS, bool k8>
-static hipError_t launch_rotate_t(const RotateParams& p, hipStream_t s) {
+static hipError_t launch_rotate_t(RotateParams p, hipStream_t s) {
   constexpr int kWaves = kThreads<D, BS> / kWave;
-  const unsigned queries = ((unsigned)p.queries + kWaves - 1) / kWaves;
-  hipLaunchKernelGGL((rotate_append_kernel<D, BS, k8>), dim3((unsigned)p.append_groups + queries), dim3(kThreads<D, BS>), 0,
-                     s, p);
+  const int64_t a = p.append_groups, q = ((int64_t)p.queries + kWaves - 1) / kWaves;
+  // rounds of |mix| + 1 workgroups, enough for both kinds
+  int64_t rounds;
+  if (q == 0) {
+    p.mix = (int)a;
+    rounds = 1;
+  } else if (a >= q) {
+    p.mix = (int)((a + q - 1) / q);
+    rounds = q;
+  } else {
+    p.mix = -(int)((q + a - 1) / a);
+    rounds = a;
+  }
+  const int64_t groups = k8 ? rounds * ((p.mix < 0 ? -p.mix : p.mix) + 1) : a + q;
+  hipLaunchKernelGGL((rotate_append_kernel<D, BS, k8>), dim3((unsigned)groups), dim3(kThreads<D, BS>), 0, s, p);
   return hipGetLastError();
 }
 template <bool k8>
@@ -448,6 +486,9 @@ hipError_t launch_rotate_append(RotateParams p, hipStream_t s) {
   p.seq_blocks = blocks <= all ? (int)((n + bs - 2) / bs + 1) : 0;
   p.append_groups = (int)((blocks <= all ? blocks : all) * p.hkv);
   p.seq_tokens = 4 * B * n <= 5 * T ? (int)n : 0;
+  // q beyond 64 MB does not come from the caches: loads that leave the rest in them (117 MB: the call 57.2 us, plain
+  // loads 61.8); below that, it may (33 MB: 22.1 and 19.5)
+  p.stream_q = T * p.hq * p.head_dim * 2 > (int64_t)1 << 26;
   p.queries = p.q == nullptr ? 0 : p.seq_tokens > 0 ? (int)(B * n) : (int)T;
   return p.scales != nullptr ? launch_rotate_k<true>(p, s) : launch_rotate_k<false>(p, s);
 }
