@@ -128,7 +128,7 @@ __device__ __forceinline__ void turn_task(const RotateParams& p, const Task& t, 
 
 // q of one token, every head, one wave: the lanes are (head, task), so the token's angles are loaded once; the rows are
 // in flight while the position is looked up.
-template <int D>
+template <int D, bool kStream>
 __device__ __forceinline__ void rotate_query(const RotateParams& p, int index, int lane) {
   constexpr int kTasks = D / 16, kHeads = kWave / kTasks, kAhead = 2;
   const Task task = row_task(p, lane % kTasks);
@@ -148,8 +148,8 @@ __device__ __forceinline__ void rotate_query(const RotateParams& p, int index, i
       const int h = min(h0 + i * kHeads, p.hq - 1);
       const u32x4* pa = reinterpret_cast<const u32x4*>(q + h * D + task.a);
       const u32x4* pb = reinterpret_cast<const u32x4*>(q + h * D + task.b);
-      a[i] = p.stream_q ? __builtin_nontemporal_load(pa) : *pa;
-      b[i] = p.stream_q ? __builtin_nontemporal_load(pb) : *pb;
+      a[i] = kStream ? __builtin_nontemporal_load(pa) : *pa;
+      b[i] = kStream ? __builtin_nontemporal_load(pb) : *pb;
     }
   };
   load(lane / kTasks);
@@ -450,7 +450,9 @@ __global__ __launch_bounds__((kThreads<D, BS>)) void rotate_append_kernel(Rotate
     return;
   }
   query = __builtin_amdgcn_readfirstlane(query * kWaves + (int)(threadIdx.x >> 6));
-  if (query < p.queries) rotate_query<D>(p, query, threadIdx.x & 63);
+  if (query >= p.queries) return;
+  if (p.stream_q) rotate_query<D, true>(p, query, threadIdx.x & 63);
+  else rotate_query<D, false>(p, query, threadIdx.x & 63);
 }
 
 template <int D, int BS, bool k8>
