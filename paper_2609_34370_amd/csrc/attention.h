@@ -129,27 +129,46 @@ __device__ __forceinline__ bool find_share(const AttnParams& p, int share, int l
     start.S = __builtin_amdgcn_readlane(gl.S, l0);
     start.t = g0 - f0;
   } else {
+    // 512 sequences at a time, eight a lane whose loads are in flight together
+    constexpr int kAhead = 8;
+    int nt[kAhead];
+    const auto sizes = [&](int base) {
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) {
+        const int b = base + k * kWave + lane;
+        nt[k] = seq_geo(p, p.qsl, p.seq_lens, min(b, p.num_seqs - 1)).nt;
+        if (b >= p.num_seqs) nt[k] = 0;
+      }
+    };
     int per_lane = 0;
-    for (int base = 0; base < p.num_seqs; base += kWave)
-      if (base + lane < p.num_seqs) per_lane += seq_geo(p, p.qsl, p.seq_lens, base + lane).nt;
+    for (int base = 0; base < p.num_seqs; base += kAhead * kWave) {
+      sizes(base);
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) per_lane += nt[k];
+    }
     total = __builtin_amdgcn_readfirstlane(wave_sum_i32(per_lane));   // < 2^31 (host)
     P = share_tiles(p, total);
     if (share_first(share, P, share_delta(P, p.skew)) >= total) return false;
     const int g0 = (int)share_first(share, P, share_delta(P, p.skew));
     // the sequence holding tile g0, and the stream index of its first tile
     int before = 0;
-    for (int base = 0; base < p.num_seqs; base += kWave) {
-      const int b = base + lane;
-      const int v = b < p.num_seqs ? seq_geo(p, p.qsl, p.seq_lens, b).nt : 0;
-      const int incl = wave_incl_scan_i32(v, lane);
-      const uint64_t hit = __builtin_amdgcn_ballot_w64(before + incl > g0);
-      if (hit != 0) {
-        const int l0 = __builtin_ctzll(hit);
-        b0 = base + l0;
-        f0 = before + __builtin_amdgcn_readlane(incl - v, l0);
-        break;
+    bool found = false;
+    for (int base = 0; base < p.num_seqs && !found; base += kAhead * kWave) {
+      if (p.num_seqs > kAhead * kWave) sizes(base);   // else they are still there
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) {
+        if (found) continue;
+        const int incl = wave_incl_scan_i32(nt[k], lane);
+        const uint64_t hit = __builtin_amdgcn_ballot_w64(before + incl > g0);
+        if (hit != 0) {
+          const int l0 = __builtin_ctzll(hit);
+          b0 = base + k * kWave + l0;
+          f0 = before + __builtin_amdgcn_readlane(incl - nt[k], l0);
+          found = true;
+        } else {
+          before += __builtin_amdgcn_readlane(incl, kWave - 1);
+        }
       }
-      before += __builtin_amdgcn_readlane(incl, kWave - 1);
     }
     b0 = __builtin_amdgcn_readfirstlane(b0);
     f0 = __builtin_amdgcn_readfirstlane(f0);

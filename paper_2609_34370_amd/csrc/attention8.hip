@@ -20,7 +20,15 @@ __device__ __forceinline__ bf16x8 widen8(uint32_t lo, uint32_t hi, float scale) 
                          __builtin_bit_cast(uint32_t, d)});
 }
 
-typedef const __attribute__((address_space(4))) f32x2 sf32x2;
+// An accumulator where an item ends.  Written out because otherwise the compiler reads every accumulator into a vector
+// register on every tile, for the few tiles that end an item.  The hazard checks do not look inside inline assembly:
+// settle_acc(), in a basic block without an MFMA, gives an accumulator's last MFMA its 18 wait states.
+__device__ __forceinline__ void settle_acc() { asm volatile("s_nop 7\n\ts_nop 7\n\ts_nop 7"); }
+__device__ __forceinline__ float read_acc(float a) {
+  float t;
+  asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(t) : "a"(a));
+  return t;
+}
 
 template <int D, int BS, int NT>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1)))
@@ -29,46 +37,39 @@ void verify_attn8_kernel(AttnParams p) {
   constexpr int KL = D / 32;   // 16-byte loads of K: two k-steps each
   constexpr int VP = D / 64;   // pairs of head-dim tiles: a 16-byte load of V holds both
   constexpr int MT = D / 32;   // 32-wide head-dim tiles of the output
-  // Tiles in flight: the register file of one wave per SIMD holds DEPTH operand buffers.
-  constexpr int DEPTH = NT == 1 ? 5 : 3;
+  constexpr int DEPTH = 2;     // tiles in flight
   const int lane = threadIdx.x & 63, col = lane & 31, half = lane >> 5;
-  // Physical wave qw -> (share s, head h); wid = s * hkv + h names its partial slots and header.
-  // Paired shares (skew > 0): workgroups alternate between the XCDs of even and odd index, and
-  // wave qw = 8m + 4 par + r takes u = 4m + r: share 2 (u / hkv) + par of head u % hkv.  So the
-  // two shares of each pair run on XCDs of opposite parity, and the four waves of a workgroup
-  // take neighbouring heads of one share.  The host makes nwaves a multiple of 8 and of 2 hkv,
-  // which makes the map a bijection of [0, nwaves).
-  const int qw = __builtin_amdgcn_readfirstlane((int)blockIdx.x * 4 + (int)(threadIdx.x >> 6));
-  int s_, h_;
+  const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+  // Wave qw -> (share s, head h); wid = s * hkv + h names its partial slots and header.  Paired shares (skew > 0): wave
+  // qw = 8m + 4 par + r takes u = 4m + r: share 2 (u / hkv) + par of head u % hkv, so the two shares of a pair run on
+  // XCDs of opposite parity, and the waves of a workgroup take neighbouring heads of one share.
+  const int qw = (int)blockIdx.x * 4 + wave;
+  int share, h;
   if (p.skew > 0) {
     const int u = ((qw >> 3) << 2) | (qw & 3);
-    s_ = 2 * (u / p.hkv) + ((qw >> 2) & 1);
-    h_ = u % p.hkv;
+    share = 2 * (u / p.hkv) + ((qw >> 2) & 1);
+    h = u % p.hkv;
   } else {
-    s_ = qw / p.hkv;
-    h_ = qw % p.hkv;
+    share = qw / p.hkv;
+    h = qw % p.hkv;
   }
-  const int wid = s_ * p.hkv + h_;
+  const int wid = share * p.hkv + h;
   const int64_t slot_f = attn_slot_floats(p.rmax, D);
   float* slots = p.ws + (int64_t)wid * 2 * slot_f;
   int32_t* hdr = reinterpret_cast<int32_t*>(p.ws + (int64_t)p.nwaves * 2 * slot_f) + (int64_t)wid * kAttnHdrInts;
-
-  auto no_share = [&]() {
-    if (lane == 0) *reinterpret_cast<u32x4*>(hdr) = u32x4{0u, 0u, 0u, 0u};
-  };
-  const int h = h_, share = s_;
-  if (share >= p.nshares) return no_share();
-
   Share sh;   // this wave's share [g0, g0 + cnt) of head h's tile stream
-  if (!find_share(p, share, lane, sh)) return no_share();
-  const int P = sh.P, dlt = sh.dlt, g0 = sh.g0, cnt = sh.cnt;
-  const Cursor start = sh.start;
+  if (share >= p.nshares || !find_share(p, share, lane, sh)) {
+    if (lane == 0) *reinterpret_cast<u32x4*>(hdr) = u32x4{0u, 0u, 0u, 0u};
+    return;
+  }
+  const int cnt = sh.cnt;
 
+  // ---- loading: the tile being issued (lc, its block ids) and the next one (nc), one step ahead
   const uint8_t* kc = reinterpret_cast<const uint8_t*>(p.k_cache);
   const uint8_t* vc = reinterpret_cast<const uint8_t*>(p.v_cache);
-  const int64_t head_stride = (int64_t)BS * D;   // bytes of one (block, head) chunk
-  // Physical blocks of a tile: keys 0..15 and 16..31 (one block when BS = 32).  The second id
-  // repeats the first past the sequence end; those keys are masked.
+  constexpr int64_t kHead = (int64_t)BS * D;   // bytes of one (block, head) chunk
+  // Physical blocks of a tile: keys 0..15 and 16..31 (one block when BS = 32).  The second id repeats the first past
+  // the sequence end; those keys are masked.
   auto tile_blocks = [&](const Cursor& c, int& ka, int& kb) {
     sint32* row = (sint32*)p.block_tables + (int64_t)c.b * p.max_blocks;
     if (BS == 16) {
@@ -78,187 +79,89 @@ void verify_attn8_kernel(AttnParams p) {
       ka = kb = clampi(row[c.t], 0, p.num_blocks - 1);
     }
   };
+  // An item's tiles are loaded in whole groups of DEPTH, so that every item begins in slot 0: past its last tile the
+  // positions of a group load that tile again (a cache hit).
+  struct Pos {
+    Cursor c;
+    int end, more, left;   // the item's tiles end, its positions after this one, the share's tiles after the item
+  };
+  auto padded = [](int tiles) { return (tiles + DEPTH - 1) / DEPTH * DEPTH; };
+  auto step = [&](Pos& x) {
+    if (x.more > 0) {
+      --x.more;
+      if (x.c.t + 1 < x.end) ++x.c.t;
+    } else if (x.left > 0) {
+      x.c.t = x.c.nt - 1;
+      advance(p, x.c);
+      x.end = min(x.c.nt, x.left);
+      x.left -= x.end;
+      x.more = padded(x.end) - 1;
+    }
+  };
+  Pos now;   // the position being issued and (next) the one after it, whose block ids are on their way
+  now.c = sh.start;
+  now.end = min(now.c.nt, now.c.t + cnt);
+  now.left = cnt - (now.end - now.c.t);
+  now.more = padded(now.end - now.c.t) - 1;
+  Pos next = now;
+  int la, lb, na, nb;
+  step(next);
+  tile_blocks(now.c, la, lb);
+  tile_blocks(next.c, na, nb);
 
-  // load side: the tile being issued (lc, its block ids) and the next one (nc), one step ahead
-  Cursor lc = start, nc = start;
-  int lidx = 0, la, lb, na = 0, nb = 0;
-  // both tiles' block ids fetched together (with one tile, the next cursor is the same one)
-  if (cnt > 1) advance(p, nc);
-  tile_blocks(lc, la, lb);
-  tile_blocks(nc, na, nb);
-
-  // Operand buffers; DEPTH rotate so that DEPTH-1 tiles are in flight while one is computed.
-  // Loads are issued unconditionally -- past the share's end they re-read its last tile (an L2
-  // hit) -- so the count of outstanding loads is the same on every path and waits stay partial.
   struct Buf {
     u32x4 k[KL];
-    u32x4 v[2][VP];      // [unit]
-    f32x2 s[2];          // [unit] the scales of K and V
+    u32x4 v[2][VP];   // [unit]
+    f32x2 s;          // the scales of K and V of the unit of lane col's key
   };
   Buf buf[DEPTH];
-
-  auto load_tile = [&](Buf& B, int i) {
-    if (i < cnt && i > lidx) {
-      lc = nc;
-      la = na;
-      lb = nb;
-      lidx = i;
-      if (i + 1 < cnt) {
-        advance(p, nc);
-        tile_blocks(nc, na, nb);
-      }
-    }
-    // lane col's key lies in unit col / 16
-    const bool second = col >= 16;
-    const int64_t kblk = (int64_t)(BS == 16 && second ? lb : la) * p.hkv + h;
-    const uint8_t* kp = kc + kblk * head_stride + (BS == 32 && second ? 16 * D : 0) + (half * 16 + (col & 15)) * 16;
+  // Loads are issued unconditionally -- past the share's end they re-read its last tile -- so the count of
+  // outstanding loads is the same on every path and waits stay partial.  The scales come by vector loads like the
+  // tiles: a wait for a scalar load waits for every scalar load.
+  auto get = [](const uint8_t* a) { return __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(a)); };
+  auto load_tile = [&](Buf& B) {
+    const int64_t ca = (int64_t)la * p.hkv + h, cb = (int64_t)lb * p.hkv + h;
+    const int64_t ck = BS == 16 && col >= 16 ? cb : ca;   // lane col's key lies in unit col / 16
+    const uint8_t* kp = kc + ck * kHead + (BS == 32 && col >= 16 ? 16 * D : 0) + (half * 16 + (col & 15)) * 16;
+    B.s = reinterpret_cast<const f32x2*>(p.scales)[ck];
 #pragma unroll
-    for (int j = 0; j < KL; ++j) B.k[j] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(kp + j * 512));
+    for (int j = 0; j < KL; ++j) B.k[j] = get(kp + j * 512);
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
-      const int64_t vblk = (int64_t)(BS == 16 && u == 1 ? lb : la) * p.hkv + h;
-      const uint8_t* vp = vc + vblk * head_stride + (BS == 32 ? u * 16 * D : 0) + (col * 2 + half) * 16;
+      const uint8_t* vp = vc + (BS == 16 && u == 1 ? cb : ca) * kHead + (BS == 32 ? u * 16 * D : 0) + (col * 2 + half) * 16;
 #pragma unroll
-      for (int i2 = 0; i2 < VP; ++i2) B.v[u][i2] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(vp + i2 * 1024));
-      B.s[u] = ((sf32x2*)p.scales)[vblk];
+      for (int i2 = 0; i2 < VP; ++i2) B.v[u][i2] = get(vp + i2 * 1024);
     }
+    // to the next position
+    now = next;
+    la = na;
+    lb = nb;
+    step(next);
+    tile_blocks(next.c, na, nb);
   };
 
-  // process side: the item being computed and its online-softmax state
-  Cursor pc = start;
-  int q0 = 0, n = 1, L = 0, R = 0;
-  bool starts_before = false;
-  int head_b = 0, head_f = 0, head_nt = 0, head_q0 = 0, head_n = 0, head_flag = 0;
-  int lim[NT];
-  // Q, the score product's B operand, in operand order: with two row tiles, row tile 0 in this
-  // wave's part of LDS and row tile 1 in registers (both in registers would not fit next to two
-  // tiles' accumulators); one row tile in registers.
-  constexpr bool kQinLds = NT == 2;
-  u32x4 qr[kQinLds ? 1 : NT][KS];
-  const int wave = threadIdx.x >> 6;
-  // Each wave's KS KB of LDS: Q's row tile 0 while an item runs (two row tiles), and the scratch
-  // through which an item's outputs are transposed at its end.
-  __shared__ u32x4 sm_q[4][KS][kWave];
-  u32x4* const scr = &sm_q[wave][0][0];
-  // The partial of the share's first item (its later part, which ends inside the share) waits in
-  // this wave's LDS, its maxima and sums in registers, and goes to memory when the wave ends:
-  // stores issued in the middle of a share cost far more than their bytes (a timing-only copy
-  // without them ran 9% faster at 20 and at 63 rows per item).  With two row tiles of 128-wide
-  // heads the four waves' stashes and row tile 0 of Q fill the 160 KB of LDS exactly.
-  __shared__ f32x4 sm_stash[4][NT * 32 * D / 4];
-  float st_m[NT], st_l[NT];
-  bool stashed = false;
-  int stash_rows = 0;
+  // ---- the item being computed and its online-softmax state
+  // r / group for a row r < 64: (r * magic) >> 16 is exact, since r * (magic - 65536 / group) < 64 <= 65536 / group
+  const int magic = (65536 + p.group - 1) / p.group;
+  Cursor pc = sh.start;
+  int q0 = 0, L = 0, R = 0, lim[NT];
   float m[NT], l[NT];
   f32x16 acc[NT][MT];
-
-  auto begin_item = [&](int i) {
-    const SeqGeo g = seq_geo(p, (sint32*)p.qsl, (sint32*)p.seq_lens, pc.b);
-    q0 = g.q0;
-    n = g.n;
-    L = pc.S - n;
-    R = p.group * n;
-    starts_before = i == 0 && pc.t != 0;
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-      // row r = nt*32 + col is (token j, head g) with r = j*G + g; padding rows repeat a real row
-      const int r = nt * 32 + col;
-      const int j = r < R ? r / p.group : n - 1;
-      const int gq = r < R ? r % p.group : 0;
-      lim[nt] = L + j;   // keys 0..L+j are visible
-      const uint16_t* qrow = reinterpret_cast<const uint16_t*>(p.q) +
-                             ((int64_t)(q0 + j) * p.hq + h * p.group + gq) * D + 16 * half;
-      if (kQinLds && nt == 0) {
-        u32x4 t[KS];
-#pragma unroll
-        for (int s = 0; s < KS; ++s) t[s] = ld16(qrow + s / 2 * 32 + s % 2 * 8);
-#pragma unroll
-        for (int s = 0; s < KS; ++s) sm_q[wave][s][lane] = t[s];
-      } else {
-#pragma unroll
-        for (int s = 0; s < KS; ++s) qr[kQinLds ? 0 : nt][s] = ld16(qrow + s / 2 * 32 + s % 2 * 8);
-      }
-      m[nt] = kNegBig;
-      l[nt] = 0.f;
-#pragma unroll
-      for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) acc[nt][mt][e] = 0.f;
-    }
-    // Wait for Q here, explicitly (this drains the tiles in flight, once per item): the wait
-    // counter then knows Q complete on every path, and the tile loop's waits stay partial.
-    __builtin_amdgcn_s_waitcnt(kWaitVmcnt0);
-  };
-
-  auto end_item = [&](int i) {
-    const bool ends_after = pc.t < pc.nt - 1;
-    const bool whole = !starts_before && !ends_after;
-    if (!whole && !starts_before) {   // this wave holds the item's first tiles
-      head_flag = 1;
-      head_b = pc.b;
-      head_f = g0 + i - pc.t;
-      head_nt = pc.nt;
-      head_q0 = q0;
-      head_n = n;
-    }
-    // Outputs leave through the wave's LDS scratch, transposed, so that each store writes whole
-    // 16-byte chunks of consecutive rows: stored straight from the accumulators, an instruction
-    // writes 8 bytes into each of 32 rows, and a timing-only copy without the output stores ran
-    // 29 us (10%) faster at 63 rows per item.  The scratch holds Q's row tile 0 during the item,
-    // no longer needed here; a wave's LDS operations run in order.
-    constexpr int kOc = D / 8;   // 16-byte chunks of a bf16 output row
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-      const float lt = halves_sum(l[nt]);
-      const int lr = nt * 32 + col;   // row of the item (and of the partial slot)
-      if (whole) {
-        // bf16 rows, chunk c of row col at chunk c ^ (col mod kOc) of the scratch row
-        const float inv = 1.0f / lt;
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-          for (int a = 0; a < 4; ++a) {
-            u32x2 w;
-            w[0] = pack_bf16x2(acc[nt][mt][4 * a] * inv, acc[nt][mt][4 * a + 1] * inv);
-            w[1] = pack_bf16x2(acc[nt][mt][4 * a + 2] * inv, acc[nt][mt][4 * a + 3] * inv);
-            const int c = 4 * mt + a;
-            reinterpret_cast<u32x2*>(scr)[(col * kOc + (c ^ (col & (kOc - 1)))) * 2 + half] = w;
-            __builtin_amdgcn_sched_barrier(0);   // one chunk at a time: few registers live
-          }
-        wave_lds_fence();
-#pragma unroll 1
-        for (int q = lane; q < 32 * kOc; q += kWave) {
-          const int row = q / kOc, c = q % kOc, r = nt * 32 + row;
-          const u32x4 v = scr[row * kOc + (c ^ (row & (kOc - 1)))];
-          if (r < R) {
-            const int j = r / p.group, gq = r % p.group;
-            // written once, read by a later kernel: non-temporal (1-4 us faster at workloads 2-5)
-            __builtin_nontemporal_store(
-                v, reinterpret_cast<u32x4*>(reinterpret_cast<uint16_t*>(p.out) +
-                                            ((int64_t)(q0 + j) * p.hq + h * p.group + gq) * D + 8 * c));
-          }
-        }
-        wave_lds_fence();   // the next row tile's writes, or the next item's Q, follow these reads
-      } else if (starts_before) {
-        if (lr < R) {
-#pragma unroll
-          for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-            for (int a = 0; a < 4; ++a)
-              sm_stash[wave][(lr * D + 32 * mt + 8 * a + 4 * half) / 4] =
-                  f32x4{acc[nt][mt][4 * a], acc[nt][mt][4 * a + 1], acc[nt][mt][4 * a + 2], acc[nt][mt][4 * a + 3]};
-        }
-        st_m[nt] = m[nt];
-        st_l[nt] = lt;
-      }
-      // (an item this wave starts and a later share finishes is the share's last: its partial
-      // is stored after the tile loop, from the accumulators it leaves behind)
-    }
-    if (starts_before) {
-      stashed = true;
-      stash_rows = R;
-    }
-  };
+  // Q, the score product's B operand: with two row tiles, row tile 0 in this wave's part of LDS and row tile 1 in
+  // registers; one row tile in registers.
+  constexpr bool kQinLds = NT == 2;
+  u32x4 qr[KS];
+  // Each wave's KS KB of LDS: Q's row tile 0 while an item runs (two row tiles), and the scratch through which an
+  // item's results are transposed at its end, so that a store instruction writes whole lines of consecutive rows.
+  __shared__ u32x4 sm_q[4][KS][kWave];
+  u32x4* const scr = &sm_q[wave][0][0];
+  // The partial of the share's first item (its later part, which ends inside the share) waits in this wave's LDS, its
+  // maxima and sums in registers, and goes to memory when the wave ends: stores in the middle of a share cost more than
+  // their bytes.  Its 16-byte chunks c of row r lie at c ^ (r mod chunks): lanes hold one chunk of 32 rows.
+  constexpr int kChunks = D / 4;
+  __shared__ f32x4 sm_stash[4][NT * 32 * kChunks];
+  float st_m[NT], st_l[NT];
+  int stash_rows = 0;
 
   // A tile at the causal edge whose V holds NaN codes: a weight of 0 times NaN would reach the rows that do not see
   // the key.  So the codes become 0, and the rows that do see them get their NaN by two products whose factors are
@@ -303,133 +206,235 @@ void verify_attn8_kernel(AttnParams p) {
     }
   };
 
-  auto process = [&](Buf& B, int i) {
-    if (i >= cnt) return;   // padding past the share's end
-    if (i == 0 || pc.t == 0) begin_item(i);
-    const int t0 = pc.t * 32;
-    const int S = pc.S;
-    if (t0 + 32 > S) {
-      // the tile runs past the sequence: zero V rows of keys >= S (they may hold anything)
+  // Tile pc.t of the item (not live: the position only pads the item's last group), then the load of the slot's next
+  // position.
+  auto process = [&](Buf& B, bool live) {
+    const int t0 = pc.t * 32, S = pc.S;
+    const bool need_mask = t0 + 31 > L;   // causal edge (keys >= S are past every row's limit)
+    float vs[2];
+    f32x16 sc[NT];
+    if (live) {
+      if (t0 + 32 > S) {
+        // the tile runs past the sequence: zero V rows of keys >= S (they may hold anything)
 #pragma unroll
-      for (int u = 0; u < 2; ++u)
+        for (int u = 0; u < 2; ++u)
 #pragma unroll
-        for (int w = 0; w < 2; ++w) {
-          // words w and w + 2 hold the same four keys, of two head-dim tiles
-          const int kbase = t0 + 16 * u + 8 * w + 4 * half;
-          uint32_t keep = 0;
+          for (int w = 0; w < 2; ++w) {
+            // words w and w + 2 hold the same four keys, of two head-dim tiles
+            const int kbase = t0 + 16 * u + 8 * w + 4 * half;
+            uint32_t keep = 0;
 #pragma unroll
-          for (int e = 0; e < 4; ++e) keep |= kbase + e < S ? 0xFFu << (8 * e) : 0u;
+            for (int e = 0; e < 4; ++e) keep |= kbase + e < S ? 0xFFu << (8 * e) : 0u;
 #pragma unroll
-          for (int i2 = 0; i2 < VP; ++i2) {
-            B.v[u][i2][w] &= keep;
-            B.v[u][i2][w + 2] &= keep;
+            for (int i2 = 0; i2 < VP; ++i2) {
+              B.v[u][i2][w] &= keep;
+              B.v[u][i2][w + 2] &= keep;
+            }
+          }
+      }
+      if (need_mask) part_nans(B);
+      vs[0] = readlane_f32(B.s[1], 0);
+      vs[1] = readlane_f32(B.s[1], 16);
+      // both row tiles' scores first: the second's products run under the first's softmax
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) sc[nt][e] = 0.f;
+      bf16x8 kop[KS];
+#pragma unroll
+      for (int j = 0; j < KL; ++j) {
+        kop[2 * j] = widen8(B.k[j][0], B.k[j][1], B.s[0]);
+        kop[2 * j + 1] = widen8(B.k[j][2], B.k[j][3], B.s[0]);
+      }
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int s = 0; s < KS; ++s)
+          sc[nt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+              kop[s], as_bf16x8(kQinLds && nt == 0 ? sm_q[wave][s][lane] : qr[s]), sc[nt], 0, 0, 0);
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        float x[16];
+#pragma unroll
+        for (int e = 0; e < 16; ++e) x[e] = sc[nt][e] * p.scale_log2e;
+        if (need_mask) {
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const int key = t0 + (e >> 2) * 8 + 4 * half + (e & 3);
+            if (key > lim[nt]) x[e] = -INFINITY;
           }
         }
-    }
-    const bool need_mask = t0 + 31 > L;   // causal edge (keys >= S are past every row's limit)
-    if (need_mask) part_nans(B);
-    const float ks = col >= 16 ? B.s[1][0] : B.s[0][0];
-    bf16x8 kop[KS];
+        float mx = x[0];
 #pragma unroll
-    for (int j = 0; j < KL; ++j) {
-      kop[2 * j] = widen8(B.k[j][0], B.k[j][1], ks);
-      kop[2 * j + 1] = widen8(B.k[j][2], B.k[j][3], ks);
-    }
-
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-      f32x16 sc;
-#pragma unroll
-      for (int e = 0; e < 16; ++e) sc[e] = 0.f;
-#pragma unroll
-      for (int s = 0; s < KS; ++s)
-        sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-            kop[s],
-            as_bf16x8(kQinLds && nt == 0 ? sm_q[wave][s][lane] : qr[kQinLds ? 0 : nt][s]),
-            sc, 0, 0, 0);
-      float x[16];
-#pragma unroll
-      for (int e = 0; e < 16; ++e) x[e] = sc[e] * p.scale_log2e;
-      if (need_mask) {
+        for (int e = 1; e < 16; ++e) mx = fmaxf(mx, x[e]);
+        mx = halves_max(mx);
+        // Lazy rescaling: the reference maximum moves only when a score exceeds it by more than 2^kLazy, so 2^(x - m)
+        // stays <= 2^kLazy and the accumulators are rescaled rarely.
+        if (__builtin_amdgcn_ballot_w64(mx > m[nt] + kLazy) != 0) {
+          const float mold = m[nt], mnew = fmaxf(mold, mx), alpha = fast_exp2(mold - mnew);
+          m[nt] = mnew;
+          l[nt] *= alpha;
+          // a row still at kNegBig has added nothing yet: the first tile of an item scales nothing
+          if (__builtin_amdgcn_ballot_w64(mold > kNegBig) != 0) scale_acc<MT>(acc[nt], alpha);
+        }
+        float ps = 0.f;
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
-          const int key = t0 + (e >> 2) * 8 + 4 * half + (e & 3);
-          if (key > lim[nt]) x[e] = -INFINITY;
+          x[e] = fast_exp2(x[e] - m[nt]);
+          ps += x[e];
+        }
+        l[nt] += ps;
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          u32x4 pw;
+#pragma unroll
+          for (int w = 0; w < 4; ++w) pw[w] = pack_bf16x2(x[8 * u + 2 * w], x[8 * u + 2 * w + 1]);
+#pragma unroll
+          for (int mt = 0; mt < MT; ++mt)
+            acc[nt][mt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                widen8(B.v[u][mt / 2][2 * (mt % 2)], B.v[u][mt / 2][2 * (mt % 2) + 1], vs[u]), as_bf16x8(pw), acc[nt][mt], 0,
+                0, 0);
         }
       }
-      float mx = x[0];
-#pragma unroll
-      for (int e = 1; e < 16; ++e) mx = fmaxf(mx, x[e]);
-      mx = halves_max(mx);
-      // Lazy rescaling: the reference maximum moves only when a score exceeds it by more than
-      // 2^kLazy, so 2^(x - m) stays <= 2^kLazy and the accumulators are rescaled rarely.
-      if (__builtin_amdgcn_ballot_w64(mx > m[nt] + kLazy) != 0) {
-        const float mold = m[nt];
-        const float mnew = fmaxf(mold, mx);
-        const float alpha = fast_exp2(mold - mnew);
-        m[nt] = mnew;
-        l[nt] *= alpha;
-        // a row still at kNegBig has added nothing yet (its accumulators are zero): the first tile
-        // of an item moves every row's maximum and scales nothing
-        if (__builtin_amdgcn_ballot_w64(mold > kNegBig) != 0) scale_acc<MT>(acc[nt], alpha);
-      }
-      float ps = 0.f;
-#pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        x[e] = fast_exp2(x[e] - m[nt]);
-        ps += x[e];
-      }
-      l[nt] += ps;
-#pragma unroll
-      for (int s2 = 0; s2 < 2; ++s2) {
-        u32x4 pw;
-#pragma unroll
-        for (int w = 0; w < 4; ++w) pw[w] = pack_bf16x2(x[8 * s2 + 2 * w], x[8 * s2 + 2 * w + 1]);
-        const bf16x8 pb = as_bf16x8(pw);
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
-          acc[nt][mt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-              widen8(B.v[s2][mt / 2][2 * (mt % 2)], B.v[s2][mt / 2][2 * (mt % 2) + 1], B.s[s2][1]), pb, acc[nt][mt], 0, 0, 0);
-      }
+      ++pc.t;
     }
-    if (pc.t == pc.nt - 1 || i == cnt - 1) end_item(i);
-    if (i + 1 < cnt) advance(p, pc);
+    load_tile(B);
   };
 
-  // Wait counts retire in issue order, so the loop is shaped for them: every pass runs a whole
-  // group of DEPTH tiles with no exit inside it (an exit edge back to the loop head would make
-  // one buffer look younger than the next, and each wait for it would drain the prefetched
-  // tiles); the share is padded to a multiple of DEPTH with tiles that are loaded but skipped.
+  // An item that this wave computed whole: normalised, bf16, row by row.  Chunk c of row col at chunk c ^ (col mod kOc)
+  // of the scratch row.
+  auto write_whole = [&]() {
+    constexpr int kOc = D / 8;   // 16-byte chunks of an output row
+    uint16_t* out = reinterpret_cast<uint16_t*>(p.out) + ((int64_t)q0 * p.hq + h * p.group) * D;
 #pragma unroll
-  for (int d = 0; d < DEPTH; ++d) load_tile(buf[d], d);
-  for (int i = 0; i < cnt; i += DEPTH) {
+    for (int nt = 0; nt < NT; ++nt) {
+      const float inv = 1.0f / halves_sum(l[nt]);
 #pragma unroll
-    for (int d = 0; d < DEPTH; ++d) {
-      process(buf[d], i + d);
-      load_tile(buf[d], i + d + DEPTH);
+      for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+        for (int a = 0; a < 4; ++a) {
+          const u32x2 w = {pack_bf16x2(read_acc(acc[nt][mt][4 * a]) * inv, read_acc(acc[nt][mt][4 * a + 1]) * inv),
+                           pack_bf16x2(read_acc(acc[nt][mt][4 * a + 2]) * inv, read_acc(acc[nt][mt][4 * a + 3]) * inv)};
+          const int c = 4 * mt + a;
+          reinterpret_cast<u32x2*>(scr)[(col * kOc + (c ^ (col & (kOc - 1)))) * 2 + half] = w;
+        }
+      wave_lds_fence();
+#pragma unroll 4
+      for (int x = 0; x < 32 * kOc / kWave; ++x) {
+        const int row = (x * kWave + lane) / kOc, c = lane % kOc, r = nt * 32 + row;
+        const u32x4 v = scr[row * kOc + (c ^ (row & (kOc - 1)))];
+        // row r is (token j, head g) with r = j * G + g: at (j * Hq + g) * D
+        const int j = (r * magic) >> 16;
+        if (r < R)
+          __builtin_nontemporal_store(v, reinterpret_cast<u32x4*>(out + ((int64_t)j * (p.hq - p.group) + r) * D + 8 * c));
+      }
+      wave_lds_fence();   // the next row tile's writes follow these reads
     }
-  }
-
-  // The share's last item, if a later share finishes it: its partial to slot 1, through the LDS
-  // scratch in two halves of the head dimension (32 rows x D/2 columns each), so that each store
-  // writes 16-byte chunks of consecutive rows.  Here, past the tile loop, the transpose costs no
-  // registers the loop needs (inside it, it spilled).
-  // Partials are written once and read by the merge launch.  With two row tiles (33 to 64 rows:
-  // large partials) they are stored non-temporally, like the outputs, so that the end of this
-  // launch does not wait for them to be written back from the caches (the call 11.6 us faster at
-  // 63 rows per item, 99 MB of partials); with one row tile plain stores leave the merge's reads
-  // to the caches (at 20 rows per item the merge ran 6.0 against 7.6 us, the call 1 us faster).
+  };
   auto put4 = [](float* a, u32x4 v) {
+    // two row tiles: large partials, streamed; one: the merge reads them from the caches
     if (NT == 2) __builtin_nontemporal_store(v, reinterpret_cast<u32x4*>(a));
     else *reinterpret_cast<u32x4*>(a) = v;
   };
-  auto put1 = [](float* a, float v) {
-    if (NT == 2) __builtin_nontemporal_store(v, a);
-    else *a = v;
-  };
-  if (head_flag) {
+
+  int i = 0;                // tiles computed
+  int first_i = 0;          // the item's first tile in the share
+  Cursor item = sh.start;   // the item, at that tile
+  bool head = false;        // the share's last item is finished by a later share
+#pragma unroll
+  for (int d = 0; d < DEPTH; ++d) load_tile(buf[d]);
+  for (;;) {
+    // ---- between two items.  With one row tile the next one's Q is in flight while the last one's results are written
+    // (two row tiles: there are no registers for it).
+    const bool more = i < cnt;
+    SeqGeo g = {0, 1, 0, 0};
+    u32x4 qn[NT][KS];
+    auto load_q = [&]() {
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        // padding rows repeat a real row
+        const int r = nt * 32 + col, rr = r < p.group * g.n ? r : p.group * g.n - 1, j = (rr * magic) >> 16;
+        const uint16_t* qrow = reinterpret_cast<const uint16_t*>(p.q) +
+                               ((int64_t)(g.q0 + j) * p.hq + h * p.group + rr - j * p.group) * D + 16 * half;
+#pragma unroll
+        for (int s = 0; s < KS; ++s) qn[nt][s] = ld16(qrow + s / 2 * 32 + s % 2 * 8);
+      }
+    };
+    if (more) {
+      g = seq_geo(p, (sint32*)p.qsl, (sint32*)p.seq_lens, pc.b);
+      if (NT == 1) load_q();
+    }
+    if (i > 0) {
+      const bool starts_before = first_i == 0 && item.t != 0, ends_after = item.t + (i - first_i) < item.nt;
+      settle_acc();
+      if (starts_before) {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          const int lr = nt * 32 + col;
+          if (lr < R) {
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+              for (int a = 0; a < 4; ++a)
+                sm_stash[wave][lr * kChunks + ((8 * mt + 2 * a + half) ^ (lr & (kChunks - 1)))] =
+                    f32x4{read_acc(acc[nt][mt][4 * a]), read_acc(acc[nt][mt][4 * a + 1]), read_acc(acc[nt][mt][4 * a + 2]),
+                          read_acc(acc[nt][mt][4 * a + 3])};
+          }
+          st_m[nt] = m[nt];
+          st_l[nt] = halves_sum(l[nt]);
+        }
+        stash_rows = R;
+      } else if (!ends_after) {
+        write_whole();
+      } else {
+        head = true;   // its partial stays in the accumulators
+      }
+    }
+    if (!more) break;
+    item = pc;
+    first_i = i;
+    q0 = g.q0;
+    L = pc.S - g.n;
+    R = p.group * g.n;
+    if (NT == 2) load_q();
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      const int r = nt * 32 + col, rr = r < R ? r : R - 1;
+      lim[nt] = L + ((rr * magic) >> 16);   // keys 0 .. L + j are visible
+#pragma unroll
+      for (int s = 0; s < KS; ++s) {
+        if (kQinLds && nt == 0) sm_q[wave][s][lane] = qn[nt][s];
+        else qr[s] = qn[nt][s];
+      }
+      m[nt] = kNegBig;
+      l[nt] = 0.f;
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[nt][mt][e] = 0.f;
+    }
+    // Everything in flight has arrived past this point (Q was issued last): entering the loop here changes none of its
+    // wait counts.
+    __builtin_amdgcn_s_waitcnt(kWaitVmcnt0);
+    const int tiles = min(cnt - i, pc.nt - pc.t);
+    for (int t = 0; t < tiles; t += DEPTH) {
+#pragma unroll
+      for (int d = 0; d < DEPTH; ++d) {
+        process(buf[d], t + d < tiles);
+      }
+    }
+    i += tiles;
+    if (pc.t == pc.nt && i < cnt) {
+      pc.t = pc.nt - 1;
+      advance(p, pc);
+    }
+  }
+
+  // ---- the share's last item, if a later share finishes it: its partial to slot 1, half of the head dimension at a time
+  if (head) {
     constexpr int kHc = D / 8;   // 16-byte chunks of half an fp32 row
     float* slot1 = slots + slot_f;
+    settle_acc();
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
       const float lt = halves_sum(l[nt]);
@@ -442,46 +447,46 @@ void verify_attn8_kernel(AttnParams p) {
           for (int a = 0; a < 4; ++a) {
             const int c = 8 * (mt - hm * MT / 2) + 2 * a + half;
             scr[col * kHc + (c ^ (col & (kHc - 1)))] =
-                u32x4{__float_as_uint(acc[nt][mt][4 * a]), __float_as_uint(acc[nt][mt][4 * a + 1]),
-                      __float_as_uint(acc[nt][mt][4 * a + 2]), __float_as_uint(acc[nt][mt][4 * a + 3])};
+                u32x4{__float_as_uint(read_acc(acc[nt][mt][4 * a])), __float_as_uint(read_acc(acc[nt][mt][4 * a + 1])),
+                      __float_as_uint(read_acc(acc[nt][mt][4 * a + 2])), __float_as_uint(read_acc(acc[nt][mt][4 * a + 3]))};
           }
         wave_lds_fence();
-        for (int q = lane; q < 32 * kHc; q += kWave) {
-          const int row = q / kHc, c = q % kHc, r = nt * 32 + row;
+#pragma unroll 4
+        for (int x = 0; x < 32 * kHc / kWave; ++x) {
+          const int row = (x * kWave + lane) / kHc, c = lane % kHc, r = nt * 32 + row;
           const u32x4 v = scr[row * kHc + (c ^ (row & (kHc - 1)))];
           if (r < R) put4(slot1 + (int64_t)r * D + hm * (D / 2) + 4 * c, v);
         }
         wave_lds_fence();
       }
       if (half == 0 && lr < R) {
-        put1(slot1 + (int64_t)p.rmax * D + lr, m[nt]);
-        put1(slot1 + (int64_t)p.rmax * D + p.rmax + lr, lt);
+        slot1[(int64_t)p.rmax * D + lr] = m[nt];
+        slot1[(int64_t)p.rmax * D + p.rmax + lr] = lt;
       }
     }
   }
-
-  // the stashed partial to slot 0, 16 bytes per lane and step, stored as above (the wave's own
-  // LDS writes are complete before its reads).  (Issued instead right after the share's last tile load, so that
-  // the stores drain under the last tiles' compute, it needed the loop split in two, and the
-  // kernel ran slower.)
-  if (stashed) {
+  // the stashed partial to slot 0
+  if (stash_rows > 0) {
     wave_lds_fence();
-    for (int idx = lane; idx < stash_rows * D / 4; idx += kWave)
-      put4(slots + 4 * (int64_t)idx, __builtin_bit_cast(u32x4, sm_stash[wave][idx]));
+#pragma unroll 4
+    for (int x = lane; x < stash_rows * kChunks; x += kWave) {
+      const int row = x / kChunks;
+      put4(slots + 4 * (int64_t)x, __builtin_bit_cast(u32x4, sm_stash[wave][row * kChunks + ((x % kChunks) ^ (row & (kChunks - 1)))]));
+    }
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
       const int r = nt * 32 + col;
       if (half == 0 && r < stash_rows) {
-        put1(slots + (int64_t)p.rmax * D + r, st_m[nt]);
-        put1(slots + (int64_t)p.rmax * D + p.rmax + r, st_l[nt]);
+        slots[(int64_t)p.rmax * D + r] = st_m[nt];
+        slots[(int64_t)p.rmax * D + p.rmax + r] = st_l[nt];
       }
     }
   }
-
   // header of the slot-1 partial: the item this wave starts and a later share finishes
   if (lane == 0) {
-    *reinterpret_cast<u32x4*>(hdr) = u32x4{(uint32_t)head_flag, (uint32_t)head_b, (uint32_t)head_f, (uint32_t)head_nt};
-    *reinterpret_cast<u32x4*>(hdr + 4) = u32x4{(uint32_t)P, (uint32_t)head_q0, (uint32_t)head_n, (uint32_t)dlt};
+    *reinterpret_cast<u32x4*>(hdr) =
+        u32x4{head ? 1u : 0u, (uint32_t)item.b, (uint32_t)(sh.g0 + first_i - item.t), (uint32_t)item.nt};
+    *reinterpret_cast<u32x4*>(hdr + 4) = u32x4{(uint32_t)sh.P, (uint32_t)q0, (uint32_t)(R / p.group), (uint32_t)sh.dlt};
   }
 }
 
