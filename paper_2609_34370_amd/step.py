@@ -2,22 +2,30 @@
 
 Holds the device buffers of a batch (metadata, pools, outputs, workspaces sized once from the
 library's queries) and calls the three entry points of libspexis in order on one stream.
+
+Options: a cache held in 8 bits (AttentionInputs8 in place of AttentionInputs), q and keys that the append
+rotates by position (rotary), and the emitted tokens' log probabilities behind the acceptance (top_logprobs).
 """
 from __future__ import annotations
 
 import math
-from typing import Optional
+from typing import Optional, Union
 
 import numpy as np
 import torch
 
 from . import spexis as sx
-from .workloads import AcceptInputs, AttentionInputs, Batch
+from .workloads import AcceptInputs, AttentionInputs, AttentionInputs8, Batch, RotaryInputs
 
 
 class VerifyStep:
-    def __init__(self, batch: Batch, attn: AttentionInputs, acc: Optional[AcceptInputs], kv_chunk_tokens: int = 0,
-                 kind: int = sx.SPEXIS_INPUT_LOGITS, device="cuda"):
+    def __init__(self, batch: Batch, attn: Union[AttentionInputs, AttentionInputs8], acc: Optional[AcceptInputs],
+                 kv_chunk_tokens: int = 0, kind: int = sx.SPEXIS_INPUT_LOGITS, device="cuda",
+                 rotary: Optional[RotaryInputs] = None, top_logprobs: Optional[int] = None):
+        """rotary: attn's q and new_k are not rotated yet; the append does it (the rotated q is self.q).
+        top_logprobs: with acceptance from logits, the emitted tokens' log probabilities and entropies, and that many
+        alternatives of each (0: none); self.logprob, entropy [B][max_k+1], top_ids, top_logprob
+        [B][max_k+1][top_logprobs]."""
         spec = batch.spec
         self.batch, self.spec, self.kind = batch, spec, kind
         self.kv_chunk_tokens = kv_chunk_tokens
@@ -26,10 +34,14 @@ class VerifyStep:
         self.seq_lens = torch.as_tensor(batch.seq_lens, device=dev)
         self.tables = torch.as_tensor(batch.block_tables, device=dev)
         self.attn = attn
+        self.in8 = isinstance(attn, AttentionInputs8)
+        self.rotary = rotary
+        self.q = attn.q if rotary is None else torch.empty_like(attn.q)
         self.out = torch.empty_like(attn.q)
         self.scale = 1.0 / math.sqrt(spec.head_dim)
-        ws = sx.spexis_verify_attention_workspace_size(batch.B, spec.num_q_heads, spec.num_kv_heads, spec.head_dim,
-                                                      batch.max_query_len, batch.max_seq_len, kv_chunk_tokens)
+        size = sx.spexis_verify_attention_kv8_workspace_size if self.in8 else sx.spexis_verify_attention_workspace_size
+        ws = size(batch.B, spec.num_q_heads, spec.num_kv_heads, spec.head_dim, batch.max_query_len, batch.max_seq_len,
+                  kv_chunk_tokens)
         self.attn_ws = torch.empty(max(ws, 16), dtype=torch.uint8, device=dev)
         self.acc = acc
         self.max_k = batch.max_k
@@ -39,19 +51,44 @@ class VerifyStep:
             self.accepted_len = torch.empty(batch.B, dtype=torch.int32, device=dev)
             self.out_tokens = torch.empty((batch.B, self.max_k + 1), dtype=torch.int32, device=dev)
             self.row_status = torch.empty(batch.B, dtype=torch.int32, device=dev)
+        self.top_logprobs = top_logprobs
+        if top_logprobs is not None:
+            if acc is None or kind != sx.SPEXIS_INPUT_LOGITS:
+                raise ValueError("log probabilities need acceptance from logits")
+            items = (batch.B, self.max_k + 1)
+            # the logit row of every place in out_tokens (places past a sequence's drafts hold no token)
+            j = np.minimum(np.arange(self.max_k + 1)[None, :], np.asarray(batch.k)[:, None])
+            self.rows = torch.as_tensor((batch.qsl[:-1, None] + j).astype(np.int32), device=dev)
+            self.logprob = torch.empty(items, device=dev)
+            self.entropy = torch.empty(items, device=dev)
+            self.top_ids = torch.empty((*items, top_logprobs), dtype=torch.int32, device=dev)
+            self.top_logprob = torch.empty((*items, top_logprobs), device=dev)
+            lw = sx.spexis_token_logprobs_workspace_size(items[0] * items[1], spec.vocab, top_logprobs)
+            self.lp_ws = torch.empty(max(lw, 16), dtype=torch.uint8, device=dev)
+
+    def _cache(self):
+        """The cache's pools (and scales), and where the batch lies in it."""
+        s, b, a = self.spec, self.batch, self.attn
+        pools = (a.k_pool, a.v_pool, a.scales) if self.in8 else (a.k_pool, a.v_pool)
+        return (*pools, b.num_blocks, s.num_kv_heads, s.block_size, s.head_dim, self.qsl, self.seq_lens, self.tables, b.T,
+                b.max_query_len)
 
     def append(self, stream=None):
-        s, b = self.spec, self.batch
-        sx.spexis_append_kv(self.attn.k_pool, self.attn.v_pool, b.num_blocks, s.num_kv_heads, s.block_size,
-                            s.head_dim, self.qsl, self.seq_lens, self.tables, b.T, b.max_query_len,
-                            self.attn.new_k, self.attn.new_v, stream=stream)
+        new = (self.attn.new_k, self.attn.new_v)
+        rotation = {}
+        if self.rotary is not None:
+            rotation = dict(cos_sin=self.rotary.cos_sin, style=self.rotary.style, q=self.attn.q, q_out=self.q)
+        if self.in8:
+            sx.spexis_rotate_append_kv8(*self._cache(), *new, **rotation, stream=stream)
+        elif rotation:
+            sx.spexis_rotate_append_kv(*self._cache(), *new, **rotation, stream=stream)
+        else:
+            sx.spexis_append_kv(*self._cache(), *new, stream=stream)
 
     def attention(self, stream=None):
-        s, b = self.spec, self.batch
-        sx.spexis_verify_attention(self.attn.k_pool, self.attn.v_pool, b.num_blocks, s.num_kv_heads, s.block_size,
-                                   s.head_dim, self.qsl, self.seq_lens, self.tables, b.T, b.max_query_len,
-                                   b.max_seq_len, self.attn.q, s.num_q_heads, self.scale, self.out, self.attn_ws,
-                                   kv_chunk_tokens=self.kv_chunk_tokens, stream=stream)
+        f = sx.spexis_verify_attention_kv8 if self.in8 else sx.spexis_verify_attention
+        f(*self._cache(), self.batch.max_seq_len, self.q, self.spec.num_q_heads, self.scale, self.out, self.attn_ws,
+          kv_chunk_tokens=self.kv_chunk_tokens, stream=stream)
 
     def accept(self, target=None, draft=None, kind=None, stream=None, seq_lens_inout=None):
         a = self.acc
@@ -62,11 +99,19 @@ class VerifyStep:
                          self.accepted_len, self.out_tokens, self.row_status, self.acc_ws,
                          temperature=a.temperature, seq_lens_inout=seq_lens_inout, stream=stream)
 
+    def logprobs(self, stream=None):
+        """Of the tokens that the acceptance emitted."""
+        sx.spexis_token_logprobs(self.acc.target_logits, self.out_tokens, self.logprob, self.lp_ws, row_ids=self.rows,
+                                 entropy=self.entropy, top_ids=self.top_ids, top_logprobs=self.top_logprob,
+                                 temperature=self.acc.temperature, stream=stream)
+
     def run(self, stream=None):
         self.append(stream)
         self.attention(stream)
         if self.acc is not None:
             self.accept(stream=stream)
+        if self.top_logprobs is not None:
+            self.logprobs(stream)
 
     def capture(self, warmup: int = 1):
         """Records run() into a HIP graph (torch.cuda.CUDAGraph); replay() then launches the whole

@@ -199,6 +199,51 @@ def make_attention_inputs(spec: WorkloadSpec, batch: Batch, device="cpu", seed: 
 
 
 @dataclasses.dataclass
+class AttentionInputs8:
+    """The same with a cache held in 8 bits (the layout of include/spexis.h)."""
+    k_pool: torch.Tensor   # [num_blocks * Hkv * bs * D] float8_e4m3fn (flat)
+    v_pool: torch.Tensor
+    scales: torch.Tensor   # [num_blocks, Hkv, 2] fp32, powers of two
+    q: torch.Tensor
+    new_k: torch.Tensor
+    new_v: torch.Tensor
+
+
+def make_attention_inputs8(spec: WorkloadSpec, batch: Batch, device="cpu", seed: Optional[int] = None) -> AttentionInputs8:
+    """Codes of N(0, 64^2), scales of 2^-7 .. 2^-5 by block, head and pool."""
+    seed = BASE_SEED + spec.wid if seed is None else seed
+    hkv, D, bs = spec.num_kv_heads, spec.head_dim, spec.block_size
+    gp = _gen(device, seed + _S_POOL)
+    pools = []
+    for _ in range(2):
+        pool = torch.empty(batch.num_blocks * hkv * bs * D, dtype=torch.float8_e4m3fn, device=device)
+        for s in range(0, pool.numel(), 1 << 26):
+            e = min(pool.numel(), s + (1 << 26))
+            pool[s:e] = (torch.randn(e - s, generator=gp, device=device) * 64).clamp_(-448, 448).to(pool.dtype)
+        pools.append(pool)
+    e = torch.randint(-7, -4, (batch.num_blocks, hkv, 2), generator=gp, device=device)
+    q = _randn_bf16((batch.T, spec.num_q_heads, D), _gen(device, seed + _S_Q), device)
+    gn = _gen(device, seed + _S_NEWKV)
+    new_k = _randn_bf16((batch.T, hkv, D), gn, device)
+    new_v = _randn_bf16((batch.T, hkv, D), gn, device)
+    return AttentionInputs8(*pools, torch.exp2(e.float()), q, new_k, new_v)
+
+
+@dataclasses.dataclass
+class RotaryInputs:
+    cos_sin: torch.Tensor  # [max_position, rotary_dim] fp32: cosines, then sines
+    style: int = 0         # 0: elements i and i + rotary_dim/2 turn together; 1: 2i and 2i+1
+
+
+def make_rotary_inputs(positions: int, rotary_dim: int, device="cpu", theta: float = 500000.0, style: int = 0) -> RotaryInputs:
+    """The table of angles position * theta^(-2i / rotary_dim)."""
+    half = rotary_dim // 2
+    ang = np.arange(positions)[:, None] * theta ** (-np.arange(half) / half)[None, :]
+    table = np.concatenate([np.cos(ang), np.sin(ang)], axis=1).astype(np.float32)
+    return RotaryInputs(torch.as_tensor(table, device=device), style)
+
+
+@dataclasses.dataclass
 class AcceptInputs:
     target_logits: torch.Tensor  # [T, V] fp32; row qsl[b]+i is target position i of b
     draft_logits: torch.Tensor   # [T-B, V] fp32; row qsl[b]-b+i is draft position i of b

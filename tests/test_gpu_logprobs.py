@@ -38,9 +38,13 @@ def call(logits, tokens, rows, temperature, top, stream=None):
 
 
 def check(logits, tokens, rows, temperature, top):
+    compare(call(logits, tokens, rows, temperature, top), logits, tokens, rows, temperature, top)
+
+
+def compare(got, logits, tokens, rows, temperature, top):
     x = logits.double().cpu().numpy()
     V, u = x.shape[1], 2.0 ** -24
-    lp, h, ids, alt = call(logits, tokens, rows, temperature, top)
+    lp, h, ids, alt = got
     with np.errstate(invalid="ignore"):
         wlp, wh, wids, walt = osv.token_logprobs(x, rows, tokens, temperature, top)
     assert np.array_equal(ids, wids)
