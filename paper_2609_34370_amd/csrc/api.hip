@@ -390,8 +390,8 @@ int spexis_token_logprobs(int32_t logits_type, const void* logits, int64_t row_s
   p.entropy = entropy;
   p.top_ids = top_ids;
   p.top_logprobs = top_logprobs;
-  p.part_stats = static_cast<spexis::f32x4*>(workspace);
-  p.part_keys = reinterpret_cast<uint64_t*>(p.part_stats + (int64_t)num_items * parts);
+  p.part_stats = static_cast<float*>(workspace);
+  p.part_keys = reinterpret_cast<uint64_t*>(p.part_stats + 4 * (int64_t)num_items * parts);
   p.rows = num_rows;
   p.items = num_items;
   p.V = vocab;

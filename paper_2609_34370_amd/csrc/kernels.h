@@ -4,8 +4,6 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
-#include "common.h"
-
 namespace spexis {
 
 struct AppendParams {
@@ -187,7 +185,7 @@ struct LogprobParams {
   float* entropy;            // [items] or null
   int32_t* top_ids;          // [items][top]
   float* top_logprobs;       // [items][top]
-  f32x4* part_stats;         // workspace, parts > 1: [items][parts] maximum, Z, U, 0
+  float* part_stats;         // workspace, parts > 1: [items][parts][4] maximum, Z, U, 0
   uint64_t* part_keys;       // [items][parts][top]
   int rows, items, V, top, in16;
   int parts;                 // a row's workgroups

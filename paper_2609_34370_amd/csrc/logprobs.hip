@@ -331,7 +331,7 @@ __global__ __launch_bounds__(256) void logprobs_kernel(LogprobParams p) {
     write_item(p, item, false, logit, s, best, cand.count, lane);
     return;
   }
-  if (lane == 0) p.part_stats[blockIdx.x] = f32x4{s.m, s.z, s.u, 0.f};
+  if (lane == 0) reinterpret_cast<f32x4*>(p.part_stats)[blockIdx.x] = f32x4{s.m, s.z, s.u, 0.f};
   if (kTop && lane < p.top) p.part_keys[(int64_t)blockIdx.x * p.top + lane] = best;
 }
 
@@ -347,7 +347,7 @@ __global__ __launch_bounds__(256) void logprobs_merge_kernel(LogprobParams p) {
   if (row == nullptr) return write_item(p, item, true, 0.f, {0.f, 1.f, 0.f}, 0, 0, lane);
   RowStats s = {kLowest, 0.f, 0.f};
   if (lane < p.parts) {   // at most a wave's lanes
-    const f32x4 v = p.part_stats[(int64_t)item * p.parts + lane];
+    const f32x4 v = reinterpret_cast<const f32x4*>(p.part_stats)[(int64_t)item * p.parts + lane];
     s = {v[0], v[1], v[2]};
   }
   s = wave_combine(s, p.c);
