@@ -15,7 +15,8 @@
 // sorted (one key a lane) and cut to n, and the threshold rises just above the n-th.  A wave meets its indices in
 // ascending order, chunk by chunk and group by group, so a later logit that equals the n-th loses to it.  Before
 // that the threshold is the n-th largest of the workgroup's 256 lanes' maxima so far (at least n logits reach it,
-// few more do), found again after 1, 4, 16 ... chunks.
+// few more do), found again after 1, 4, 16 ... chunks while
+// at least as many are to come (a search costs about one chunk's work).
 #include "common.h"
 #include "kernels.h"
 
@@ -261,9 +262,10 @@ __global__ __launch_bounds__(256) void logprobs_kernel(LogprobParams p) {
     }
     if constexpr (kTop) {
       if (some) lane_most = fmaxf(lane_most, most);
-      if (round == next) {   // after 1, 4, 16 ... rounds
+      if (round == next) {   // after 1, 4, 16 ... rounds, the later times only where as many follow
         agree();
         next = 4 * next + 3;
+        if (2 * (next + 1) > rounds) next = rounds;
       }
     }
     if (!some) continue;
