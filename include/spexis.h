@@ -162,7 +162,8 @@ int spexis_append_kv(void* k_cache, void* v_cache, int32_t num_blocks, int32_t n
  *   positions     [total_tokens] int32: the row of cos_sin of every token, or NULL: the token's place in its
  *                 sequence, L_b + j.  (It does not change where rows are stored.)
  *   q, q_out      [total_tokens][Hq][head_dim] bf16, read and written; q_out may be q.  Both NULL: keys only
- *                 (num_q_heads is then not read)
+ *                 (num_q_heads is then not read).  In a padded batch, total_tokens > qsl[B], the rows from qsl[B] on
+ *                 are left as they were
  * Other arguments as spexis_append_kv; pools, rows and table 16-byte aligned.  Any number of new tokens a
  * sequence, prompts included; a sequence's blocks that receive rows must be its own.
  * Supported: rotary_dim a multiple of 16, 16 .. head_dim; head_dim in {64, 128}, block_size in {16, 32}.
@@ -311,6 +312,7 @@ size_t spexis_token_logprobs_workspace_size(int32_t num_items, int32_t vocab, in
  *   logits        num_rows rows of vocab entries, row_stride >= vocab entries apart, aligned to an entry (read)
  *   row_ids       [num_items] int32 or NULL (then num_items <= num_rows);  token_ids  [num_items] int32
  *   top_n         host: 0 .. 32;  top_ids [num_items][top_n] int32, top_logprobs fp32 (not used with top_n = 0)
+ *   temperature   host: T, finite, > 0 and not subnormal
  *   logprobs      [num_items] fp32;  entropy [num_items] fp32 or NULL
  *   workspace     >= spexis_token_logprobs_workspace_size(num_items, vocab, top_n) bytes, 16-byte aligned (may be
  *                 NULL where that is 0)

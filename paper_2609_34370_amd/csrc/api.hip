@@ -364,8 +364,8 @@ int spexis_token_logprobs(int32_t logits_type, const void* logits, int64_t row_s
     return fail(SPEXIS_ERR_INVALID_ARGUMENT, "%s: logits type %d", name, logits_type);
   if (num_rows < 0 || vocab <= 0 || num_items < 0 || top_n < 0 || row_stride < vocab)
     return fail(SPEXIS_ERR_INVALID_ARGUMENT, "%s: bad size", name);
-  if (!(temperature > 0.f) || !std::isfinite(temperature))
-    return fail(SPEXIS_ERR_INVALID_ARGUMENT, "%s: temperature must be finite and > 0", name);
+  if (!std::isnormal(temperature) || temperature < 0.f)   // (a subnormal's reciprocal overflows)
+    return fail(SPEXIS_ERR_INVALID_ARGUMENT, "%s: temperature must be finite, > 0 and not subnormal", name);
   if (!row_ids && num_items > num_rows)
     return fail(SPEXIS_ERR_INVALID_ARGUMENT, "%s: %d items of %d rows", name, num_items, num_rows);
   if (vocab > kMaxVocab || top_n > spexis::kLogprobMaxTop)

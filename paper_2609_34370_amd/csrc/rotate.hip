@@ -138,6 +138,8 @@ __device__ __forceinline__ void rotate_query(const RotateParams& p, int index, i
     q1 = clampi(p.qsl[s + 1], 0, p.total_tokens);
     tok = seq_start(p, s) + index % p.seq_tokens;
     if (tok >= q1) return;
+  } else if (tok >= clampi(p.qsl[p.num_seqs], 0, p.total_tokens)) {
+    return;   // a row behind the last sequence: left as it is
   }
   const uint16_t* q = reinterpret_cast<const uint16_t*>(p.q) + (int64_t)tok * p.hq * D;
   uint16_t* o = reinterpret_cast<uint16_t*>(p.q_out) + (int64_t)tok * p.hq * D;

@@ -93,3 +93,7 @@ def test_token_logprobs():
     big = dict(V=200000, stride=200000)
     assert logprobs(wsb=need - 1, **big) == SMALL and logprobs(ws=None, **big) == SMALL
     assert logprobs(items=0, x=None, tok=None, lp=None) == 0
+
+
+def test_a_temperature_whose_reciprocal_overflows():
+    assert logprobs(t=1e-39) == INVALID

@@ -157,3 +157,18 @@ def test_an_offset_past_31_bits():
     assert torch.equal(ssc, sc[-own:])
     for f, s in zip(big, small):
         assert torch.equal(f[-s.numel():], s.view(torch.uint8)) and not f[: -s.numel()].any()
+
+
+@pytest.mark.parametrize("chunk", [0, 32])
+def test_a_padded_batch(chunk):
+    """More rows than the sequences have, and sequences without rows at the end: the same bits, nothing written behind."""
+    hq, hkv, D, bs, n, pad = 8, 2, 64, 16, [2, 1, 5, 0, 0], 3
+    r = np.random.default_rng(8)
+    qsl, S, tables, blocks = batch(n, [300, 0, 44, 0, 0], bs, 8)
+    T = int(qsl[-1])
+    codes, scales = cache(blocks, bs, hkv, D, r)
+    q = torch.from_numpy(r.standard_normal((T + pad, hq, D)).astype(np.float32)).to(torch.bfloat16).cuda()
+    pool, sc = pools(codes, bs), dev(scales)
+    say(f"[attention 8 bit] padded, chunk {chunk}")
+    got, want = (attend(pool, sc, blocks, hkv, bs, D, qsl, S, tables, x, 0.125, chunk) for x in (q, q[:T]))
+    assert torch.equal(got[:T], want) and (got[T:] == 777.0).all()

@@ -156,3 +156,20 @@ def test_no_items():
     with pytest.raises(ValueError):
         sx.spexis_token_logprobs(torch.empty((2, 50), device="cuda").t(), torch.empty(1, dtype=torch.int32, device="cuda"),
                                  torch.empty(1, device="cuda"))
+
+
+def test_shapes_and_devices_that_are_refused(monkeypatch):
+    """What the number of items is taken from, and the buffers that have to be as long."""
+    x, three = torch.zeros((4, 50), device="cuda"), torch.zeros(3, dtype=torch.int32, device="cuda")
+    out = torch.zeros(3, device="cuda")
+    top = (torch.zeros((3, 5), dtype=torch.int32, device="cuda"), torch.zeros((3, 5), device="cuda"))
+    for kw in (dict(logprobs=out[:2]), dict(row_ids=three[:2]), dict(entropy=out[:1]), dict(top_ids=top[0]),
+               dict(top_logprobs=top[1]), dict(top_ids=top[0][:2], top_logprobs=top[1][:2]),
+               dict(top_ids=top[0], top_logprobs=top[1][:, :4].contiguous())):
+        with pytest.raises(ValueError):
+            sx.spexis_token_logprobs(x, three, **dict(dict(logprobs=out), **kw))
+    sx.spexis_token_logprobs(x, three, out, top_ids=top[0], top_logprobs=top[1])
+    torch.cuda.synchronize()
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 1)
+    with pytest.raises(ValueError):
+        sx.spexis_token_logprobs(x, three, out)

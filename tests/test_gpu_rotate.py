@@ -205,3 +205,48 @@ def test_without_new_tokens_nothing_is_touched():
                                 0, 1, None, None)
     sx.spexis_rotate_append_kv(None, None, 4, 2, 16, 64, dev(np.zeros(3, np.int32)), None, dev(np.zeros((2, 1), np.int32)),
                                0, 1, None, None, dev(table(1, 16)))
+
+
+@pytest.mark.parametrize("n", [[3, 3, 3, 3], [1, 0, 7, 1]])   # places found directly, and by a search
+@pytest.mark.parametrize("given", [False, True])
+@pytest.mark.parametrize("in8", [False, True])
+def test_rows_behind_the_last_sequence_stay(n, given, in8):
+    """A batch padded to more rows than its sequences have: the same as without the padding, nothing written there."""
+    hq, hkv, D, bs, rot, pad = 6, 2, 64, 16, 32, 2
+    r = np.random.default_rng(3)
+    qsl, S, tables, blocks = batch(n, [20, 3, 16, 31], bs, 4)
+    T = int(qsl[-1])
+    new_k, new_v, q = (bf16((T + pad, h, D), r).cuda() for h in (hkv, hkv, hq))
+    cs = dev(table(64, rot))
+    pos = dev(r.integers(0, 64, T + pad), torch.int32) if given else None
+    say(f"[rotate padded] {n} given {given} 8 bit {in8}")
+    results = []
+    for rows in (T, T + pad):
+        if in8:
+            f, pools = sx.spexis_rotate_append_kv8, [torch.zeros(blocks * hkv * bs * D, dtype=torch.uint8, device="cuda").view(
+                torch.float8_e4m3fn) for _ in range(2)] + [torch.ones((blocks, hkv, 2), device="cuda")]
+        else:
+            f, pools = sx.spexis_rotate_append_kv, [torch.zeros(blocks * hkv * bs * D, dtype=torch.bfloat16, device="cuda")
+                                                    for _ in range(2)]
+        out = torch.full((T + pad, hq, D), 777.0, dtype=torch.bfloat16, device="cuda")
+        f(*pools, blocks, hkv, bs, D, dev(qsl), dev(S), dev(tables), rows, max(n), new_k[:rows], new_v[:rows], cs,
+          positions=pos, q=q[:rows], q_out=out[:rows])
+        torch.cuda.synchronize()
+        assert (out[T:] == 777.0).all() and not (out[:T] == 777.0).any()
+        results.append([out] + pools)
+    for a, b in zip(*results):
+        assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
+
+
+def test_shapes_and_devices_that_are_refused(monkeypatch):
+    pool, one = torch.zeros(2 * 16 * 64, dtype=torch.bfloat16, device="cuda"), dev([0, 1], torch.int32)
+    new = torch.zeros((1, 1, 64), dtype=torch.bfloat16, device="cuda")
+    args = (pool, pool.clone(), 2, 1, 16, 64, one, one[1:], one[:1].view(1, 1), 1, 1, new, new, dev(table(4, 16)))
+    for q, out in ((new.view(1, 64), new.view(1, 64)), (new.view(1, 2, 32), new.view(1, 2, 32)), (new, new.view(1, 2, 32))):
+        with pytest.raises(ValueError):
+            sx.spexis_rotate_append_kv(*args, q=q, q_out=out)
+    with pytest.raises(sx.SpexisError):
+        sx.spexis_rotate_append_kv(*args, q=new)
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 1)
+    with pytest.raises(ValueError):
+        sx.spexis_rotate_append_kv(*args)
