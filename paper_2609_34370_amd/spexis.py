@@ -139,19 +139,17 @@ def _ptr(t: Optional[torch.Tensor], dtype=None):
     return t.data_ptr()
 
 
-def _here(t, stream) -> None:
-    """Kernels are launched on the current device: a tensor or a stream of another one is refused."""
-    if t is not None and t.is_cuda:
+def _stream(stream, t=None):
+    """The stream's handle.  Kernels are launched on the current device: t, or a stream, of another one is refused."""
+    if stream is None:
+        # the current stream's handle without building a torch.cuda.Stream (4 us a call)
         here = torch._C._cuda_getDevice()
-        if t.get_device() != here or (stream is not None and stream.device_index != here):
-            raise ValueError("tensors and stream must be on the current device")
-
-
-def _stream(stream):
-    if stream is not None:
-        return stream.cuda_stream
-    # the current stream's handle without building a torch.cuda.Stream (4 us a call)
-    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+        if t is not None and t.get_device() != here:
+            raise ValueError("tensors must be on the current device")
+        return torch._C._cuda_getCurrentRawStream(here)
+    if t is not None and not t.get_device() == stream.device_index == torch._C._cuda_getDevice():
+        raise ValueError("tensors and stream must be on the current device")
+    return stream.cuda_stream
 
 
 def spexis_version() -> int:
@@ -185,14 +183,13 @@ def spexis_rotate_append_kv(k_cache, v_cache, num_blocks, num_kv_heads, block_si
                             seq_lens, block_tables, total_tokens, max_query_len, new_k, new_v, cos_sin,
                             style=SPEXIS_ROTARY_HALVES, positions=None, q=None, q_out=None, stream=None) -> None:
     """cos_sin [max_position][rotary_dim] fp32; q and q_out [T][Hq][head_dim] bf16 (q_out may be q)."""
-    _here(k_cache, stream)
     _check(lib().spexis_rotate_append_kv(
         _ptr(k_cache, torch.bfloat16), _ptr(v_cache, torch.bfloat16), num_blocks, num_kv_heads, block_size,
         head_dim, query_start_loc.shape[0] - 1, _ptr(query_start_loc, torch.int32), _ptr(seq_lens, torch.int32),
         _ptr(block_tables, torch.int32), block_tables.shape[1], total_tokens, max_query_len,
         _ptr(new_k, torch.bfloat16), _ptr(new_v, torch.bfloat16), _ptr(cos_sin, torch.float32), *_table(cos_sin), style,
         _ptr(positions, torch.int32), _ptr(q, torch.bfloat16), _heads(q, q_out, head_dim),
-        _ptr(q_out, torch.bfloat16), _stream(stream)))
+        _ptr(q_out, torch.bfloat16), _stream(stream, k_cache)))
 
 
 def spexis_rotate_append_kv8(k_cache, v_cache, scales, num_blocks, num_kv_heads, block_size, head_dim,
@@ -200,14 +197,13 @@ def spexis_rotate_append_kv8(k_cache, v_cache, scales, num_blocks, num_kv_heads,
                              cos_sin=None, style=SPEXIS_ROTARY_HALVES, positions=None, q=None, q_out=None,
                              stream=None) -> None:
     """Pools torch.float8_e4m3fn, scales [num_blocks][Hkv][2] fp32; without cos_sin nothing is rotated."""
-    _here(k_cache, stream)
     _check(lib().spexis_rotate_append_kv8(
         _ptr(k_cache, torch.float8_e4m3fn), _ptr(v_cache, torch.float8_e4m3fn), _ptr(scales, torch.float32), num_blocks,
         num_kv_heads, block_size, head_dim, query_start_loc.shape[0] - 1, _ptr(query_start_loc, torch.int32),
         _ptr(seq_lens, torch.int32), _ptr(block_tables, torch.int32), block_tables.shape[1], total_tokens,
         max_query_len, _ptr(new_k, torch.bfloat16), _ptr(new_v, torch.bfloat16), _ptr(cos_sin, torch.float32),
         *_table(cos_sin), style, _ptr(positions, torch.int32), _ptr(q, torch.bfloat16), _heads(q, q_out, head_dim),
-        _ptr(q_out, torch.bfloat16), _stream(stream)))
+        _ptr(q_out, torch.bfloat16), _stream(stream, k_cache)))
 
 
 def spexis_verify_attention_workspace_size(num_seqs, num_q_heads, num_kv_heads, head_dim, max_query_len, max_seq_len,
@@ -238,18 +234,18 @@ def spexis_verify_attention_kv8(k_cache, v_cache, scales, num_blocks, num_kv_hea
                                 query_start_loc, seq_lens, block_tables, total_tokens, max_query_len, max_seq_len, q,
                                 num_q_heads, scale, out, workspace, kv_chunk_tokens=0, stream=None) -> None:
     """Pools torch.float8_e4m3fn, scales [num_blocks][Hkv][2] fp32 (powers of two)."""
-    _here(k_cache, stream)
     _check(lib().spexis_verify_attention_kv8(
         _ptr(k_cache, torch.float8_e4m3fn), _ptr(v_cache, torch.float8_e4m3fn), _ptr(scales, torch.float32), num_blocks,
         num_kv_heads, block_size, head_dim, query_start_loc.shape[0] - 1, _ptr(query_start_loc, torch.int32),
         _ptr(seq_lens, torch.int32), _ptr(block_tables, torch.int32), block_tables.shape[1], total_tokens, max_query_len,
         max_seq_len, _ptr(q, torch.bfloat16), num_q_heads, scale, _ptr(out, torch.bfloat16), kv_chunk_tokens,
-        _ptr(workspace), workspace.numel() * workspace.element_size(), _stream(stream)))
+        _ptr(workspace), workspace.numel() * workspace.element_size(), _stream(stream, k_cache)))
 
 
 def spexis_softmax_rows(logits, probs, temperature=1.0, stream=None) -> None:
     n = token_ids.numel()
-    if logprobs.numel() != n or any(t is not None and t.numel() != n for t in (row_ids, entropy)):
+    if (logprobs.numel() != n or (row_ids is not None and row_ids.numel() != n) or
+            (entropy is not None and entropy.numel() != n)):
         raise ValueError("token_ids, row_ids, logprobs and entropy must have one shape")
     if (top_ids is None) != (top_logprobs is None) or (top_ids is not None and (
             top_ids.shape != top_logprobs.shape or top_ids.numel() != n * top_ids.shape[-1])):
@@ -274,20 +270,20 @@ def spexis_token_logprobs(logits, token_ids, logprobs, workspace=None, row_ids=N
     if not logits.is_cuda:
         raise ValueError("tensor must be on the GPU")
     n = token_ids.numel()
-    if logprobs.numel() != n or any(t is not None and t.numel() != n for t in (row_ids, entropy)):
+    if (logprobs.numel() != n or (row_ids is not None and row_ids.numel() != n) or
+            (entropy is not None and entropy.numel() != n)):
         raise ValueError("token_ids, row_ids, logprobs and entropy must have one shape")
     if (top_ids is None) != (top_logprobs is None) or (top_ids is not None and (
             top_ids.shape != top_logprobs.shape or top_ids.numel() != n * top_ids.shape[-1])):
         raise ValueError("top_ids and top_logprobs must have token_ids' shape and one more axis")
     rows, vocab = logits.shape
     stride = logits.stride(0) if rows > 1 else vocab
-    _here(logits, stream)
     _check(lib().spexis_token_logprobs(
         SPEXIS_TYPE_F32 if logits.dtype == torch.float32 else SPEXIS_TYPE_BF16, logits.data_ptr(),
         stride, rows, vocab, temperature, n, _ptr(row_ids, torch.int32), _ptr(token_ids, torch.int32),
         0 if top_ids is None else top_ids.shape[-1], _ptr(logprobs, torch.float32), _ptr(entropy, torch.float32),
         _ptr(top_ids, torch.int32), _ptr(top_logprobs, torch.float32), _ptr(workspace),
-        0 if workspace is None else workspace.numel() * workspace.element_size(), _stream(stream)))
+        0 if workspace is None else workspace.numel() * workspace.element_size(), _stream(stream, logits)))
 
 
 def spexis_accept_workspace_size(num_seqs, vocab, max_k) -> int:
