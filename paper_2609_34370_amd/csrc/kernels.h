@@ -194,7 +194,9 @@ struct LogprobParams {
 
 constexpr int kLogprobMaxTop = 32;
 constexpr int kLogprobMaxParts = 64;   // the merge holds a part a lane
-// Parts of a row.
+// Parts of a row: about 2048 workgroups, eight for each CU, as items without a token leave at once (576 items, 221 with a
+// token, of 128256 logits: 34.6 us; 512 workgroups 39.5, 8192 42.2), of at least 8192 logits, one round of a workgroup (one
+// row of 128256: 11.0 us; 32768 logits 13.9, and 64 rows, where the starts weigh more, 20.7 and 19.8).
 inline int logprob_parts(int64_t items, int64_t V) {
   const int64_t want = (2048 + items - 1) / items, most = (V + 8191) / 8192;
   const int64_t n = want < most ? want : most;

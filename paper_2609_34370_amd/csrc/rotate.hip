@@ -13,6 +13,11 @@
 // floor(n / bs) + 2 blocks, which start(b+1) - start(b) is never below, so no scan over the lengths is needed: a
 // wave-wide search for the last b with start(b) <= index, two probes for 4096 sequences.  Where the sequences are of
 // about one length (a step's drafts), index / (blocks of the longest) does without the search.
+//
+// Measured (reads and writes of 5.3 TB/s are what a large copy reaches): q and keys of 14420 prompt tokens (28 + 4 heads
+// of 128) into the bf16 cache 48.2 us, 5.6 TB/s with what the last-level cache holds; of 15060 (32 + 8) into the 8-bit
+// cache 57 us, 6.0 TB/s; a step of 512 sequences of 9 rows in 8 bits 18.1 us, 4.5 TB/s.  A step of 64 sequences is a
+// launch and two dependent loads, 5.4 us.
 #include <type_traits>
 
 #include "common.h"
@@ -175,7 +180,7 @@ __device__ __forceinline__ void rotate_query(const RotateParams& p, int index, i
       if (h >= p.hq) break;
       float x[8], y[8];
       turn_task<float>(p, task, g, a[i], b[i], x, y);
-      // written once, read by a later launch (512 sequences of 9 rows: 19.5 us, plain stores 23.2; 12000 prompt
+      // written once, read by a later launch (512 sequences of 9 rows: 19.5 us, plain stores 23.2; 14420 prompt
       // tokens 52.9 and 54.2)
       __builtin_nontemporal_store(narrow(x), reinterpret_cast<u32x4*>(o + h * D + task.a));
       __builtin_nontemporal_store(narrow(y), reinterpret_cast<u32x4*>(o + h * D + task.b));
@@ -433,7 +438,7 @@ template <int D, int BS, bool k8>
 __global__ __launch_bounds__((kThreads<D, BS>)) void rotate_append_kernel(RotateParams p) {
   // 8 bits: workgroups of the two kinds alternate, `mix` of one to one of the other: appends compute and wait for one
   // load after the other, queries keep the memory busy meanwhile (512 sequences of 9 rows: 22.8 us, appends first
-  // 27.0).  bf16 appends are as bound by memory as queries and come first (54.2 us, alternating 58.0, at 12000 tokens).
+  // 27.0).  bf16 appends are as bound by memory as queries and come first (54.2 us, alternating 58.0, at 14420 tokens).
   constexpr int kWaves = kThreads<D, BS> / kWave;
   const int w = blockIdx.x, m = p.mix < 0 ? -p.mix : p.mix, q = k8 ? w / (m + 1) : 0, r = k8 ? w % (m + 1) : 0;
   int append, query;   // the index of the one that this workgroup is
@@ -485,7 +490,9 @@ static hipError_t launch_rotate_k(const RotateParams& p, hipStream_t s) {
 
 hipError_t launch_rotate_append(RotateParams p, hipStream_t s) {
   const int64_t B = p.num_seqs, T = p.total_tokens, bs = p.block_size, n = p.max_query_len;
-  // Sequences of about one length need no search: the longest one's blocks (tokens) for each, where that is no more.
+  // Sequences of about one length need no search: the longest one's blocks for each, where that is no more (8 bits, 512
+  // sequences of 9 rows: 19.3 us, by search 22.3), and its tokens where at most a quarter of the waves find none (512 of
+  // 9: 29.5 us, by search 30.2; 512 of 1 to 9, half of the waves idle: 20.7 and 20.6).
   const int64_t blocks = B * ((n + bs - 2) / bs + 1), all = T / bs + 2 * B;
   p.seq_blocks = blocks <= all ? (int)((n + bs - 2) / bs + 1) : 0;
   p.append_groups = (int)((blocks <= all ? blocks : all) * p.hkv);
