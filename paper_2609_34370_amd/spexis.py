@@ -243,13 +243,6 @@ def spexis_verify_attention_kv8(k_cache, v_cache, scales, num_blocks, num_kv_hea
 
 
 def spexis_softmax_rows(logits, probs, temperature=1.0, stream=None) -> None:
-    n = token_ids.numel()
-    if (logprobs.numel() != n or (row_ids is not None and row_ids.numel() != n) or
-            (entropy is not None and entropy.numel() != n)):
-        raise ValueError("token_ids, row_ids, logprobs and entropy must have one shape")
-    if (top_ids is None) != (top_logprobs is None) or (top_ids is not None and (
-            top_ids.shape != top_logprobs.shape or top_ids.numel() != n * top_ids.shape[-1])):
-        raise ValueError("top_ids and top_logprobs must have token_ids' shape and one more axis")
     rows, vocab = logits.shape
     _check(lib().spexis_softmax_rows(_ptr(logits, torch.float32), _ptr(probs, torch.float32), rows, vocab,
                                      ctypes.c_float(temperature), _stream(stream)))
