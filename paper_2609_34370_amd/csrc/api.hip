@@ -181,8 +181,9 @@ int verify_attention(const char* name, bool in8, const void* k_cache, const void
                 name, group * max_query_len, kMaxRows);
   if ((int64_t)max_blocks_per_seq * block_size < max_query_len)
     return fail(SPEXIS_ERR_INVALID_ARGUMENT, "%s: block tables hold fewer slots than a query", name);
-  // every tile index of the stream fits in 32 bits
-  if ((int64_t)num_seqs * (((int64_t)max_blocks_per_seq * block_size + 31) / 32) >= (1ll << 31))
+  // every tile index of the stream fits in 32 bits, with what the items cost
+  if ((int64_t)num_seqs * (((int64_t)max_blocks_per_seq * block_size + 31) / 32 + (in8 ? spexis::kAttn8ItemCost : 0)) >=
+      (1ll << 31))
     return fail(SPEXIS_ERR_UNSUPPORTED, "%s: more than 2^31 key tiles", name);
   if (num_seqs == 0 || total_tokens == 0) return ok();
   if (!k_cache || !v_cache || !query_start_loc || !seq_lens || !block_tables || !q || !out || (in8 && !scales))
@@ -225,6 +226,7 @@ int verify_attention(const char* name, bool in8, const void* k_cache, const void
   p.skew = skew;
   p.scale_log2e = (float)((double)scale * 1.4426950408889634);
   p.scales = scales;
+  p.item_cost = in8 && kv_chunk_tokens == 0 && !spexis::attn_merges_wide(p) ? spexis::kAttn8ItemCost : 0;
   return hip_result(in8 ? spexis::launch_attention8(p, (hipStream_t)stream) : spexis::launch_attention(p, (hipStream_t)stream), name);
 }
 

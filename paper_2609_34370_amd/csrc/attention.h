@@ -101,20 +101,23 @@ __device__ __forceinline__ int share_of(int g, int P, int dlt) {
   return 2 * j + (g - 2 * P * j >= P + dlt ? 1 : 0);
 }
 
-// A share of a head's tile stream: tiles [g0, g0 + cnt), where it starts, and the geometry it was cut by.
+// A share of a head's stream of positions: [g0, g0 + cnt), where it starts, and the geometry it was cut by.  A position is
+// a tile, or one of the `tail` positions behind every sequence's last tile, which stand for what an item costs besides
+// its tiles; the share starts at a tile.
 struct Share {
-  int P, dlt, g0, cnt;   // the tiles of a share (paired: P + dlt and P - dlt)
+  int P, dlt, g0, cnt, tail;   // the positions of a share (paired: P + dlt and P - dlt)
   Cursor start;
 };
 
-// Share `share` of a head (the same for all of a wave's lanes); false where it holds no tile.
-__device__ __forceinline__ bool find_share(const AttnParams& p, int share, int lane, Share& o) {
-  int total, P, b0 = 0, f0 = 0;   // P: the tiles of a share
+// Share `share` of a head (the same for all of a wave's lanes); false where it holds no tile.  tail: what an
+// item costs, in tiles.
+__device__ __forceinline__ bool find_share(const AttnParams& p, int share, int lane, Share& o, int tail) {
+  int total, P, b0 = 0, f0 = 0;   // P: the positions of a share
   Cursor start;
   if (p.num_seqs <= kWave) {
     // one pass: lane b holds sequence b's geometry; the share start is read from the lanes
     const SeqGeo gl = lane < p.num_seqs ? seq_geo(p, p.qsl, p.seq_lens, lane) : SeqGeo{0, 0, 0, 0};
-    const int incl = wave_incl_scan_i32(gl.nt, lane);
+    const int size = gl.nt > 0 ? gl.nt + tail : 0, incl = wave_incl_scan_i32(size, lane);
     total = __builtin_amdgcn_readlane(incl, kWave - 1);   // < 2^31 (host)
     P = share_tiles(p, total);
     if (share_first(share, P, share_delta(P, p.skew)) >= total) return false;
@@ -123,7 +126,7 @@ __device__ __forceinline__ bool find_share(const AttnParams& p, int share, int l
     if (hit == 0) return false;
     const int l0 = __builtin_ctzll(hit);
     b0 = l0;
-    f0 = __builtin_amdgcn_readlane(incl - gl.nt, l0);
+    f0 = __builtin_amdgcn_readlane(incl - size, l0);
     start.b = b0;
     start.nt = __builtin_amdgcn_readlane(gl.nt, l0);
     start.S = __builtin_amdgcn_readlane(gl.S, l0);
@@ -144,13 +147,13 @@ __device__ __forceinline__ bool find_share(const AttnParams& p, int share, int l
     for (int base = 0; base < p.num_seqs; base += kAhead * kWave) {
       sizes(base);
 #pragma unroll
-      for (int k = 0; k < kAhead; ++k) per_lane += nt[k];
+      for (int k = 0; k < kAhead; ++k) per_lane += nt[k] > 0 ? nt[k] + tail : 0;
     }
     total = __builtin_amdgcn_readfirstlane(wave_sum_i32(per_lane));   // < 2^31 (host)
     P = share_tiles(p, total);
     if (share_first(share, P, share_delta(P, p.skew)) >= total) return false;
     const int g0 = (int)share_first(share, P, share_delta(P, p.skew));
-    // the sequence holding tile g0, and the stream index of its first tile
+    // the sequence holding position g0, and the stream index of its first tile
     int before = 0;
     bool found = false;
     for (int base = 0; base < p.num_seqs && !found; base += kAhead * kWave) {
@@ -158,12 +161,12 @@ __device__ __forceinline__ bool find_share(const AttnParams& p, int share, int l
 #pragma unroll
       for (int k = 0; k < kAhead; ++k) {
         if (found) continue;
-        const int incl = wave_incl_scan_i32(nt[k], lane);
+        const int size = nt[k] > 0 ? nt[k] + tail : 0, incl = wave_incl_scan_i32(size, lane);
         const uint64_t hit = __builtin_amdgcn_ballot_w64(before + incl > g0);
         if (hit != 0) {
           const int l0 = __builtin_ctzll(hit);
           b0 = base + k * kWave + l0;
-          f0 = before + __builtin_amdgcn_readlane(incl - nt[k], l0);
+          f0 = before + __builtin_amdgcn_readlane(incl - size, l0);
           found = true;
         } else {
           before += __builtin_amdgcn_readlane(incl, kWave - 1);
@@ -173,15 +176,23 @@ __device__ __forceinline__ bool find_share(const AttnParams& p, int share, int l
     b0 = __builtin_amdgcn_readfirstlane(b0);
     f0 = __builtin_amdgcn_readfirstlane(f0);
     const SeqGeo g = seq_geo(p, (sint32*)p.qsl, (sint32*)p.seq_lens, b0);
-    if (g.nt == 0 || g0 < f0 || g0 - f0 >= g.nt) return false;   // inputs changed under us
+    if (g.nt == 0 || g0 < f0 || g0 - f0 >= g.nt + tail) return false;   // inputs changed under us
     start.b = b0;
     start.nt = g.nt;
     start.S = g.S;
     start.t = g0 - f0;
   }
   const int dlt = share_delta(P, p.skew);
-  const int g0 = (int)share_first(share, P, dlt);
-  o = {P, dlt, g0, min(share_size(share, P, dlt), total - g0), start};
+  int g0 = (int)share_first(share, P, dlt), cnt = min(share_size(share, P, dlt), total - g0);
+  if (tail > 0 && start.t >= start.nt) {   // it starts behind a sequence's tiles: with the next one
+    const int skip = start.nt + tail - start.t;
+    if (skip >= cnt) return false;
+    g0 += skip;
+    cnt -= skip;
+    start.t = start.nt - 1;
+    advance(p, start);
+  }
+  o = {P, dlt, g0, cnt, tail, start};
   return true;
 }
 

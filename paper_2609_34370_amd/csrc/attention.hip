@@ -68,7 +68,7 @@ void verify_attn_kernel(AttnParams p) {
   if (share >= p.nshares) return no_share();
 
   Share sh;   // this wave's share [g0, g0 + cnt) of head h's tile stream
-  if (!find_share(p, share, lane, sh)) return no_share();
+  if (!find_share(p, share, lane, sh, 0)) return no_share();
   const int P = sh.P, dlt = sh.dlt, g0 = sh.g0, cnt = sh.cnt;
   const Cursor start = sh.start;
 
@@ -612,15 +612,19 @@ __global__ __launch_bounds__(512) void attn_merge_wide_kernel(AttnParams p, int 
   __builtin_nontemporal_store(w, reinterpret_cast<u32x4*>(orow));
 }
 
+// Few, long items: at least kMergeWideShares shares per sequence (the call, wide merge against
+// attn_merge_kernel: 30.3 against 60.7 us at one sequence of 16384 keys, 25.7 against 30.8 at 4 of
+// 1000-4096, 30.2 against 32.0 at 8 of them, where there are 16 shares a sequence; 45.4 against 43.0
+// at 16 of them).  At just that many, items of up to 8 rows of 64 take attn_merge_kernel as few round
+// trips, without the combination through LDS (12.2 against 12.9 us at one sequence of 1024 keys).
+bool attn_merges_wide(const AttnParams& p) {
+  const bool small = p.head_dim == 64 && p.rmax <= 8;
+  return p.nshares / (kMergeWideShares + (small ? 1 : 0)) >= p.num_seqs;
+}
+
 template <int D>
 static hipError_t launch_merge_t(const AttnParams& p, hipStream_t s) {
-  // Few, long items: at least kMergeWideShares shares per sequence (the call, wide merge against
-  // attn_merge_kernel: 30.3 against 60.7 us at one sequence of 16384 keys, 25.7 against 30.8 at 4 of
-  // 1000-4096, 30.2 against 32.0 at 8 of them, where there are 16 shares a sequence; 45.4 against 43.0
-  // at 16 of them).  At just that many, items of up to 8 rows of 64 take attn_merge_kernel as few round
-  // trips, without the combination through LDS (12.2 against 12.9 us at one sequence of 1024 keys).
-  const bool small = D == 64 && p.rmax <= 8;
-  if (p.nshares / (kMergeWideShares + (small ? 1 : 0)) >= p.num_seqs) {
+  if (attn_merges_wide(p)) {
     const int rg = (p.rmax + kMergeRows - 1) / kMergeRows;
     hipLaunchKernelGGL((attn_merge_wide_kernel<D>), dim3((unsigned)(p.num_seqs * p.hkv * rg)), dim3(512), 0, s, p, rg);
     return hipGetLastError();

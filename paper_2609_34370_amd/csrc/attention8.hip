@@ -66,7 +66,7 @@ void verify_attn8_kernel(AttnParams p) {
   float* slots = p.ws + (int64_t)wid * 2 * slot_f;
   int32_t* hdr = reinterpret_cast<int32_t*>(p.ws + (int64_t)p.nwaves * 2 * slot_f) + (int64_t)wid * kAttnHdrInts;
   Share sh;   // this wave's share [g0, g0 + cnt) of head h's tile stream
-  if (share >= p.nshares || !find_share(p, share, lane, sh)) {
+  if (share >= p.nshares || !find_share(p, share, lane, sh, p.item_cost)) {
     if (lane == 0) *reinterpret_cast<u32x4*>(hdr) = u32x4{0u, 0u, 0u, 0u};
     return;
   }
@@ -91,14 +91,15 @@ void verify_attn8_kernel(AttnParams p) {
   // positions of a group load that tile again (a cache hit).
   struct Pos {
     Cursor c;
-    int end, more, left;   // the item's tiles end, its positions after this one, the share's tiles after the item
+    int end, more, left;   // the item's tiles end, its loads after this one, the share's positions after those tiles
   };
   auto padded = [](int tiles) { return (tiles + DEPTH - 1) / DEPTH * DEPTH; };
   auto step = [&](Pos& x) {
     if (x.more > 0) {
       --x.more;
       if (x.c.t + 1 < x.end) ++x.c.t;
-    } else if (x.left > 0) {
+    } else if (x.left > sh.tail) {
+      x.left -= sh.tail;
       x.c.t = x.c.nt - 1;
       advance(p, x.c);
       x.end = min(x.c.nt, x.left);
@@ -345,16 +346,16 @@ void verify_attn8_kernel(AttnParams p) {
     else *reinterpret_cast<u32x4*>(a) = v;
   };
 
-  int i = 0;                // tiles computed
-  int first_i = 0;          // the item's first tile in the share
-  Cursor item = sh.start;   // the item, at that tile
+  int done = 0;             // positions of the share that are done
+  int at = 0, ran = 0;      // the item's first one, and its tiles in the share
+  Cursor item = sh.start;   // the item, at its first tile in the share
   bool head = false;        // the share's last item is finished by a later share
 #pragma unroll
   for (int d = 0; d < DEPTH; ++d) load_tile(buf[d]);
   for (;;) {
     // ---- between two items.  With one row tile the next one's Q is in flight while the last one's results are written
     // (two row tiles: there are no registers for it).
-    const bool more = i < cnt;
+    const bool more = done < cnt;
     SeqGeo g = {0, 1, 0, 0};
     u32x4 qn[NT][KS];
     auto load_q = [&]() {
@@ -372,8 +373,8 @@ void verify_attn8_kernel(AttnParams p) {
       g = seq_geo(p, (sint32*)p.qsl, (sint32*)p.seq_lens, pc.b);
       if (NT == 1) load_q();
     }
-    if (i > 0) {
-      const bool starts_before = first_i == 0 && item.t != 0, ends_after = item.t + (i - first_i) < item.nt;
+    if (ran > 0) {
+      const bool starts_before = at == 0 && item.t != 0, ends_after = item.t + ran < item.nt;
       settle_acc();
       if (starts_before) {
 #pragma unroll
@@ -400,7 +401,7 @@ void verify_attn8_kernel(AttnParams p) {
     }
     if (!more) break;
     item = pc;
-    first_i = i;
+    at = done;
     q0 = g.q0;
     L = pc.S - g.n;
     R = p.group * g.n;
@@ -424,17 +425,20 @@ void verify_attn8_kernel(AttnParams p) {
     // Everything in flight has arrived past this point (Q was issued last): entering the loop here changes none of its
     // wait counts.
     __builtin_amdgcn_s_waitcnt(kWaitVmcnt0);
-    const int tiles = min(cnt - i, pc.nt - pc.t);
-    for (int t = 0; t < tiles; t += DEPTH) {
+    ran = min(cnt - done, pc.nt - pc.t);
+    for (int t = 0; t < ran; t += DEPTH) {
 #pragma unroll
       for (int d = 0; d < DEPTH; ++d) {
-        process(buf[d], t + d < tiles);
+        process(buf[d], t + d < ran);
       }
     }
-    i += tiles;
-    if (pc.t == pc.nt && i < cnt) {
-      pc.t = pc.nt - 1;
-      advance(p, pc);
+    done += ran;
+    if (pc.t == pc.nt) {
+      done += sh.tail;
+      if (done < cnt) {
+        pc.t = pc.nt - 1;
+        advance(p, pc);
+      }
     }
   }
 
@@ -493,7 +497,7 @@ void verify_attn8_kernel(AttnParams p) {
   // header of the slot-1 partial: the item this wave starts and a later share finishes
   if (lane == 0) {
     *reinterpret_cast<u32x4*>(hdr) =
-        u32x4{head ? 1u : 0u, (uint32_t)item.b, (uint32_t)(sh.g0 + first_i - item.t), (uint32_t)item.nt};
+        u32x4{head ? 1u : 0u, (uint32_t)item.b, (uint32_t)(sh.g0 + at - item.t), (uint32_t)item.nt};
     *reinterpret_cast<u32x4*>(hdr + 4) = u32x4{(uint32_t)sh.P, (uint32_t)q0, (uint32_t)(R / p.group), (uint32_t)sh.dlt};
   }
 }

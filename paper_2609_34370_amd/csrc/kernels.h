@@ -104,7 +104,14 @@ struct AttnParams {
   int skew;              // 0: equal shares; else paired shares, the even-XCD one skew/1024 longer
   float scale_log2e;     // scale * log2(e): scores live in the base-2 domain
   const float* scales;   // 8-bit cache: [num_blocks][hkv][2], K and V
+  int item_cost;         // what an item costs besides its tiles, in tiles (0: shares of as many tiles)
 };
+
+// The 8-bit kernel's shares count every (sequence, KV head) as so many tiles more: its Q, its outputs or partials and the
+// waits around them.  Against shares of as many tiles: 512 sequences of 512 to 2048 keys, 63 rows a head, 173.0 us for
+// 178.3; 512 of 100 to 400 67.0 for 75.2; 64 of 20 to 200 keys, 20 rows, 18.3 for 23.2; 64 of 1024 to 4096 69.3 for
+// 70.7.  (2: 176.2, 70.2, 19.5, 69.7; 3: 174.2, 67.9, 18.5, 69.9; 5: 172.1, 66.1, 18.3, 70.2.)
+constexpr int kAttn8ItemCost = 4;
 
 // One partial slot: [rmax][D] unnormalised output, then rmax reference maxima and rmax sums.
 // Rounded up to 16 floats so that every slot starts 64-byte aligned.
@@ -254,6 +261,7 @@ hipError_t launch_attention(const AttnParams& p, hipStream_t s);
 hipError_t launch_attention8(const AttnParams& p, hipStream_t s);   // 8-bit cache (p.scales)
 // The partials of the items cut between shares, combined (after either attention kernel).
 hipError_t launch_attn_merge(const AttnParams& p, hipStream_t s);
+bool attn_merges_wide(const AttnParams& p);   // by a kernel that cuts the stream of tiles again itself
 
 hipError_t launch_select(const SelectParams& p, hipStream_t s);
 hipError_t launch_lookahead(const LookaheadParams& p, hipStream_t s);

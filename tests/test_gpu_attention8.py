@@ -172,3 +172,18 @@ def test_a_padded_batch(chunk):
     say(f"[attention 8 bit] padded, chunk {chunk}")
     got, want = (attend(pool, sc, blocks, hkv, bs, D, qsl, S, tables, x, 0.125, chunk) for x in (q, q[:T]))
     assert torch.equal(got[:T], want) and (got[T:] == 777.0).all()
+
+
+@pytest.mark.parametrize("B,hq,hkv,bs,most", [(20, 8, 8, 16, 90), (65, 4, 1, 32, 700), (300, 2, 2, 16, 300), (600, 6, 1, 16, 120)])
+def test_many_items_of_any_length(B, hq, hkv, bs, most):
+    """Shares that begin behind a sequence's last tile, hold several sequences or a part of one; sequences without rows."""
+    r = np.random.default_rng(B)
+    n = r.integers(0, 6, B)
+    ctx = (most * r.random(B) ** 3).astype(np.int32)
+    n[-1] = 0
+    qsl, S, tables, blocks = batch(n, ctx, bs, B)
+    codes, scales = cache(blocks, bs, hkv, 64, r, False)
+    q = torch.from_numpy(r.standard_normal((int(qsl[-1]), hq, 64)).astype(np.float32)).to(torch.bfloat16).cuda()
+    say(f"[attention 8 bit] {B} sequences of up to {most} keys")
+    got = attend(pools(codes, bs), dev(scales), blocks, hkv, bs, 64, qsl, S, tables, q, 0.125)
+    check(got, codes, scales, qsl, S, tables, q, 0.125)
