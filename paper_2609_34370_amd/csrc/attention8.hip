@@ -1,5 +1,5 @@
 // Verification attention over the cache held in 8 bits: attention.hip's work split (a head's 32-key tiles cut into
-// equal shares, one wave a share, partials merged), on tiles of half the bytes.
+// shares, one wave a share, partials merged), on tiles of half the bytes, in which shares an item costs more than its tiles.
 //
 // A tile is 32 keys: two units of 16 slots, which in blocks of 16 are two blocks.  Codes come from HBM straight into
 // registers, 16 bytes a lane, and are widened there to the bf16 operands of v_mfma_f32_32x32x16_bf16 by
@@ -10,9 +10,9 @@
 //     score tile holds keys, so they feed the products of two head-dim tiles.
 //
 // Bound by the cache's bytes up to 32 query rows a head: 64 sequences of 1024 to 4096 keys (32 query heads over 8 of 128,
-// 5 tokens; 357 MB) take 62.5 us, 5.7 TB/s, and 7.6 us of merge behind them.  With 33 to 64 rows by its own
+// 5 tokens; 357 MB) take 61.5 us, 5.8 TB/s, and 7.6 us of merge behind them.  With 33 to 64 rows by its own
 // instructions (two softmaxes a tile, 64 exponentials and 32 conversions a lane): 512 sequences of 512 to 2048 keys (63
-// rows, 762 MB) 157 us, 4.8 TB/s, and 18.6 us of merge.  One sequence of 16384 keys: 13.2 us for 32 MB, a chain of share
+// rows, 762 MB) 153 us, 5.0 TB/s, and 18.4 us of merge.  One sequence of 16384 keys: 13.2 us for 32 MB, a chain of share
 // search, block ids, codes and products; 6.8 us of merge.
 // One wave a SIMD holds everything in registers; two (half the registers each, twice the shares and partials) took 78
 // and 197 us where one takes 71 and 180.  Three tiles in flight took 72 us instead of 71, the loads of two being enough.

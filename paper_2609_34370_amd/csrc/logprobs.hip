@@ -3,8 +3,8 @@
 //   w_v = (x_v - max x) c, c = log2(e) / T;  Z = sum 2^w;  U = sum 2^w w
 //   log p(v) = (x_v - max x) / T - ln Z;   H = ln Z - ln2 U / Z
 //   (both terms of H are at least 0, as is ln Z: no cancellation)
-// Bound by reading the logits once: 4608 rows of 152064 fp32 with 5 alternatives 412 us, 6.8 TB/s, what a large read
-// reaches.  221 rows of 128256 (64 sequences' emitted tokens) with 20 alternatives 33 us, 3.4 TB/s: four rounds of loads a
+// Bound by reading the logits once: 4608 rows of 152064 fp32 with 5 alternatives 413 us, 6.8 TB/s, what a large read
+// reaches.  221 rows of 128256 (64 sequences' emitted tokens) with 20 alternatives 34 us, 3.3 TB/s: four rounds of loads a
 // workgroup, of which the first has to find a threshold and to sort (with none 24 us), and 4.7 us of merge.
 //
 // Work split.  A workgroup takes one part of one item's row, its four waves every fourth chunk of 2048 logits (in
