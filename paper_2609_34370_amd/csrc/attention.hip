@@ -617,7 +617,11 @@ __global__ __launch_bounds__(512) void attn_merge_wide_kernel(AttnParams p, int 
 // 1000-4096, 30.2 against 32.0 at 8 of them, where there are 16 shares a sequence; 45.4 against 43.0
 // at 16 of them).  At just that many, items of up to 8 rows of 64 take attn_merge_kernel as few round
 // trips, without the combination through LDS (12.2 against 12.9 us at one sequence of 1024 keys).
+// The 8-bit kernel's items of more than 32 rows from 8 shares a sequence on: their partials, up to 32 KB each, want more
+// workgroups (one sequence of 500 keys, 63 rows, 17.5 us, attn_merge_kernel 28.3; 16 of 300 to 1000 31.9 and 43.8; at 4
+// shares 32 of 100 to 300 take 36.2 and 27.6).
 bool attn_merges_wide(const AttnParams& p) {
+  if (p.scales != nullptr && p.rmax > 32) return p.nshares / 8 >= p.num_seqs;
   const bool small = p.head_dim == 64 && p.rmax <= 8;
   return p.nshares / (kMergeWideShares + (small ? 1 : 0)) >= p.num_seqs;
 }

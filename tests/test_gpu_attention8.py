@@ -187,3 +187,14 @@ def test_many_items_of_any_length(B, hq, hkv, bs, most):
     say(f"[attention 8 bit] {B} sequences of up to {most} keys")
     got = attend(pools(codes, bs), dev(scales), blocks, hkv, bs, 64, qsl, S, tables, q, 0.125)
     check(got, codes, scales, qsl, S, tables, q, 0.125)
+
+
+@pytest.mark.parametrize("B,most", [(1, 500), (3, 900), (16, 1000), (40, 300)])   # either merge of 63-row items
+def test_tall_items_in_many_shares(B, most):
+    r = np.random.default_rng(B)
+    qsl, S, tables, blocks = batch([9] * B, r.integers(most // 3, most + 1, B), 32, B)
+    codes, scales = cache(blocks, 32, 2, 128, r, False)
+    q = torch.from_numpy(r.standard_normal((9 * B, 14, 128)).astype(np.float32)).to(torch.bfloat16).cuda()
+    scale = float(np.float32(128 ** -0.5))
+    say(f"[attention 8 bit] {B} sequences of up to {most} keys, 63 rows")
+    check(attend(pools(codes, 32), dev(scales), blocks, 2, 32, 128, qsl, S, tables, q, scale), codes, scales, qsl, S, tables, q, scale)
