@@ -353,7 +353,7 @@ int spexis_softmax_rows(const float* logits, float* probs, int64_t rows, int32_t
 
 size_t spexis_token_logprobs_workspace_size(int32_t items, int32_t vocab, int32_t top_n) {
   if (items <= 0 || vocab <= 0 || top_n < 0 || top_n > spexis::kLogprobMaxTop) return 0;
-  const int64_t parts = spexis::logprob_parts(items, vocab);
+  const int64_t parts = spexis::logprob_parts(items, vocab, true);   // the more of the two
   return parts > 1 ? (size_t)(items * parts * (16 + 8 * (int64_t)top_n)) : 0;
 }
 
@@ -373,7 +373,7 @@ int spexis_token_logprobs(int32_t logits_type, const void* logits, int64_t row_s
   if (vocab > kMaxVocab || top_n > spexis::kLogprobMaxTop)
     return fail(SPEXIS_ERR_UNSUPPORTED, "%s: vocab %d > %d or top_n %d > %d", name, vocab, kMaxVocab, top_n,
                 spexis::kLogprobMaxTop);
-  const int parts = spexis::logprob_parts(std::max(num_items, 1), vocab);
+  const int parts = spexis::logprob_parts(std::max(num_items, 1), vocab, num_items > num_rows);
   if ((int64_t)num_items * parts >= (1ll << 24)) return fail(SPEXIS_ERR_UNSUPPORTED, "%s: too many items", name);
   if (num_items == 0) return ok();
   if (!logits || !token_ids || !logprobs || (top_n > 0 && (!top_ids || !top_logprobs)))

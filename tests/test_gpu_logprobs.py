@@ -173,3 +173,23 @@ def test_shapes_and_devices_that_are_refused(monkeypatch):
     monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 1)
     with pytest.raises(ValueError):
         sx.spexis_token_logprobs(x, three, out)
+
+
+@pytest.mark.parametrize("items", [1, 9, 100, 300, 600])
+def test_every_number_of_parts(items):
+    """Long rows: cut into many parts, a few, none; as many items as rows, and more (some without a token)."""
+    r = np.random.default_rng(items)
+    V, n = 50021, min(items, 40)
+    x = torch.from_numpy((r.standard_normal((n, V)) * 3).astype(np.float32)).cuda()
+    x[:, 17:900:5] = x[:, 40000:40001]   # equal logits in several parts
+    rows = r.integers(0, n, items)
+    tokens = r.integers(0, V, items)
+    say(f"[logprobs] {items} items of {n} rows of {V}")
+    check(x, tokens.tolist(), rows.tolist(), 1.3, 12)
+    if items <= n:
+        check(x, tokens.tolist(), None, 1.3, 12)
+    else:
+        wide = x.repeat(-(-items // n), 1)[:items]
+        check(wide, tokens.tolist(), None, 1.3, 12)
+        tokens[::2] = -1
+        check(x, tokens.tolist(), rows.tolist(), 1.3, 0)
