@@ -373,7 +373,7 @@ int spexis_token_logprobs(int32_t logits_type, const void* logits, int64_t row_s
   if (vocab > kMaxVocab || top_n > spexis::kLogprobMaxTop)
     return fail(SPEXIS_ERR_UNSUPPORTED, "%s: vocab %d > %d or top_n %d > %d", name, vocab, kMaxVocab, top_n,
                 spexis::kLogprobMaxTop);
-  const int parts = spexis::logprob_parts(std::max(num_items, 1), vocab, num_items > num_rows);
+  const int parts = spexis::logprob_parts(std::max(num_items, 1), vocab, row_ids && num_items >= num_rows);
   if ((int64_t)num_items * parts >= (1ll << 24)) return fail(SPEXIS_ERR_UNSUPPORTED, "%s: too many items", name);
   if (num_items == 0) return ok();
   if (!logits || !token_ids || !logprobs || (top_n > 0 && (!top_ids || !top_logprobs)))

@@ -204,8 +204,9 @@ constexpr int kLogprobMaxParts = 64;   // the merge holds a part a lane
 // Parts of a row: the search for the alternatives and the sorts cost a workgroup as much as several rounds of loads, and a
 // second part the merge's launch, so a row is cut for less than two workgroups a CU only (128256 logits, 5 alternatives:
 // 256 rows in 2 parts 29.5 us, in 8 37.4; 500 rows whole 43.0, in 5 parts 50.0), and short rows never (40000 logits:
-// 200 rows 13.8 us, in 2 parts 17.5; 8 rows 12.1 and 11.7 in 5).  Where there are more items than rows some have no
-// token, and their workgroups leave at once (sparse: 576 items, 221 with a token, 20 alternatives, 34.6 us, in one part 39.4).
+// 200 rows 13.8 us, in 2 parts 17.5; 8 rows 12.1 and 11.7 in 5).  Items that pick their rows, no fewer than there are
+// rows, are a step's places, many without a token, whose workgroups leave at once (sparse: 576 items, 221 with a token, 20
+// alternatives, 34.6 us, in one part 39.4; 320 items of 320 rows 33.8 and 36.5).
 // A part has at least 8192 logits, one round of a workgroup (one row of 128256: 11.1 us, with 32768 13.9).
 inline int logprob_parts(int64_t items, int64_t V, bool sparse) {
   if (V <= 49152) return 1;
