@@ -19,6 +19,8 @@
 // that the threshold is the n-th largest of the workgroup's 256 lanes' maxima so far (at least n logits reach it,
 // few more do), found again after 1, 4, 16 ... chunks while
 // at least as many are to come (a search costs about one chunk's work).
+// 600 rows of 128256 with 20 alternatives take 59 us; masked but for four logits, or of one value, 64 to 66; ascending,
+// where every logit is a candidate, 761.
 #include "common.h"
 #include "kernels.h"
 
