@@ -186,7 +186,8 @@ int spexis_rotate_append_kv(void* k_cache, void* v_cache, int32_t num_blocks, in
  *   scale = need where the block holds no earlier row of the sequence (slots before the first new one),
  *           else max(old scale, need): a scale is never lowered under rows that use it
  *   new rows:      code = e4m3(x / scale), x the fp32 value (rotated: the sum rounded once to fp32),
- *                  to nearest even; a NaN or an infinity is stored as NaN
+ *                  to nearest even; a NaN or an infinity is stored as NaN, a finite x beyond 240 * 2^120
+ *                  (3.19e38) as that value, so that code * scale is finite in bf16
  *   earlier rows of a block whose scale grew: code = e4m3(code * old scale / scale)
  * Slots behind the sequence's last token keep their codes, other blocks and scales are not touched.  A power of
  * two costs no precision (codes are floating point) and re-coding earlier rows is exact but for the format's
@@ -264,8 +265,8 @@ size_t spexis_verify_attention_kv8_workspace_size(int32_t num_seqs, int32_t num_
  * code * scales[block][g][K or V].  Codes are widened to bf16, which holds them and their scale exactly; products
  * accumulate in fp32, the softmax weights are rounded to bf16 in front of the product with V as there.
  *   scales  [num_blocks][Hkv][2] fp32, positive powers of two (spexis_rotate_append_kv8 writes no others; of any
- *           other value only the exponent counts); 8-byte entries, 16-byte aligned like the pools, q, out and
- *           workspace
+ *           other value only the exponent counts) by which every code of the block is finite in bf16; 8-byte
+ *           entries, 16-byte aligned like the pools, q, out and workspace
  *   workspace >= spexis_verify_attention_kv8_workspace_size(...) bytes
  * A NaN code of a key that a query token sees makes its output NaN; slots behind the sequence may hold anything.
  * Other arguments, supported shapes and errors as spexis_verify_attention.

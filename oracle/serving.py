@@ -9,6 +9,7 @@ import numpy as np
 
 E4M3_MAX = 448.0
 LEAST_EXP = -100
+MOST = 240 * 2.0 ** 120   # the largest magnitude stored: the next code at that scale, 256, times 2^120 is infinity in bf16
 
 
 # ------------------------------------------------------------------ e4m3 codes
@@ -84,6 +85,7 @@ def append8(codes, scales, qsl, seq_lens, tables, rows):
     place; one of K and V."""
     bs, hkv = codes.shape[1], codes.shape[2]
     rows = np.asarray(rows, dtype=np.float64)
+    rows = np.where(np.isfinite(rows), np.clip(rows, -MOST, MOST), rows)
     for b in range(len(seq_lens)):
         L = int(seq_lens[b]) - int(qsl[b + 1] - qsl[b])
         for t in range(L // bs, (int(seq_lens[b]) - 1) // bs + 1):

@@ -203,6 +203,15 @@ __device__ __forceinline__ uint32_t rescale_e4m3x4(uint32_t w, float r) {
   const uint32_t nan = ((((w & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u) >> 7) * 0xFFu;
   return (pack_e4m3x4(lo[0] * r, lo[1] * r, hi[0] * r, hi[1] * r) & ~nan) | (nan & 0x7F7F7F7Fu);
 }
+// The largest magnitude that is stored, 240 * 2^120: values beyond it (the largest bf16 is 255 * 2^120) would round up
+// to the code of 256, and 256 * 2^120 is infinity in bf16, where the attention widens codes.
+constexpr uint32_t kMostBits = 0x7F700000u;
+__device__ __forceinline__ void limit_finite(float (&x)[8]) {
+  const float most = __uint_as_float(kMostBits);
+#pragma unroll
+  for (int e = 0; e < 8; ++e)
+    if (fabsf(x[e]) < __builtin_inff()) x[e] = fminf(fmaxf(x[e], -most), most);
+}
 // The format has no infinity: what is not finite is stored as the NaN 0x7f, written over the conversion's result.
 __device__ __forceinline__ void store_nans(const float (&x)[8], uint8_t* codes, int step) {
 #pragma unroll
@@ -329,8 +338,10 @@ __device__ __forceinline__ void append_block(const RotateParams& p, int index, i
   float kratio = 1.f, vratio = 1.f;
   if constexpr (k8) {
     uint32_t kmost = row ? most_bits(kx, ky) : 0u, vmost = row ? most_bits_bf16(va, vb) : 0u;
-    const bool finite = __builtin_amdgcn_ballot_w64(kmost >= kInf || vmost >= kInf) == 0;   // the wave's values
-    if (!finite && row) {
+    const bool usual = __builtin_amdgcn_ballot_w64(kmost > kMostBits || vmost > kMostBits) == 0;   // the wave's values
+    if (!usual && row) {
+      limit_finite(kx);
+      limit_finite(ky);
       float vx[8], vy[8];
       widen(va, vx);
       widen(vb, vy);
@@ -365,17 +376,18 @@ __device__ __forceinline__ void append_block(const RotateParams& p, int index, i
       const float kmul = 1.f / ks, vmul = 1.f / vs;   // exact: powers of two
       *reinterpret_cast<u32x2*>(chunk(at_slot, task.a)) = pack_e4m3x8(kx, kmul);
       *reinterpret_cast<u32x2*>(chunk(at_slot, task.b)) = pack_e4m3x8(ky, kmul);
-      if (!finite) {
+      if (!usual) {
         store_nans(kx, chunk(at_slot, task.a), 1);
         store_nans(ky, chunk(at_slot, task.b), 1);
       }
       auto values = [&](u32x4 v, uint8_t* to) {
         float x[8];
         widen(v, x);
+        if (!usual) limit_finite(x);
         const u32x2 c = pack_e4m3x8(x, vmul);
 #pragma unroll
         for (int e = 0; e < 8; ++e) to[32 * e] = (uint8_t)(c[e / 4] >> (8 * (e % 4)));
-        if (!finite) store_nans(x, to, 32);
+        if (!usual) store_nans(x, to, 32);
       };
       values(va, mine);
       values(vb, mine + 8 * 32);
