@@ -193,7 +193,7 @@ int spexis_rotate_append_kv(void* k_cache, void* v_cache, int32_t num_blocks, in
  * two costs no precision (codes are floating point) and re-coding earlier rows is exact but for the format's
  * subnormal codes, those below 2^-6.  Scales of blocks that hold rows must be positive
  * and finite; a caller that fills blocks by other means uses powers of two.
- *   scales  [num_blocks][Hkv][2] fp32 (read and written)
+ *   scales  [num_blocks][Hkv][2] fp32, 16-byte aligned (read and written)
  *   cos_sin NULL with max_position 0: nothing is rotated (style and rotary_dim are not read; q, q_out and
  *           positions NULL)
  * Other arguments and errors as spexis_rotate_append_kv.

@@ -150,7 +150,7 @@ int rotate_append(const char* name, const spexis::RotateParams& p, void* stream)
   if (!p.k_cache || !p.v_cache || !p.qsl || !p.seq_lens || !p.block_tables || !p.new_k || !p.new_v ||
       (p.max_position > 0 && !p.cos_sin) || !p.q != !p.q_out)
     return fail(SPEXIS_ERR_INVALID_ARGUMENT, "%s: null pointer", name);
-  if (misaligned({p.k_cache, p.v_cache, p.new_k, p.new_v, p.q, p.q_out, p.cos_sin}))
+  if (misaligned({p.k_cache, p.v_cache, p.scales, p.new_k, p.new_v, p.q, p.q_out, p.cos_sin}))
     return fail(SPEXIS_ERR_INVALID_ARGUMENT, "%s: a pointer that is not 16-byte aligned", name);
   return hip_result(spexis::launch_rotate_append(p, (hipStream_t)stream), name);
 }
