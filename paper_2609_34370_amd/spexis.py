@@ -139,16 +139,20 @@ def _ptr(t: Optional[torch.Tensor], dtype=None):
     return t.data_ptr()
 
 
-def _stream(stream, t=None):
-    """The stream's handle.  Kernels are launched on the current device: t, or a stream, of another one is refused."""
-    if stream is None:
-        # the current stream's handle without building a torch.cuda.Stream (4 us a call)
-        here = torch._C._cuda_getDevice()
+def _stream(stream, *tensors):
+    """The stream's handle.  Kernels are launched on the current device: tensors, or a stream beside them, of another
+    one are refused."""
+    if stream is not None and not tensors:
+        return stream.cuda_stream
+    here = torch._C._cuda_getDevice()
+    for t in tensors:
         if t is not None and t.get_device() != here:
             raise ValueError("tensors must be on the current device")
+    if stream is None:
+        # the current stream's handle without building a torch.cuda.Stream (4 us a call)
         return torch._C._cuda_getCurrentRawStream(here)
-    if t is not None and not t.get_device() == stream.device_index == torch._C._cuda_getDevice():
-        raise ValueError("tensors and stream must be on the current device")
+    if stream.device_index != here:
+        raise ValueError("the stream must be of the current device")
     return stream.cuda_stream
 
 
@@ -188,8 +192,9 @@ def spexis_rotate_append_kv(k_cache, v_cache, num_blocks, num_kv_heads, block_si
         head_dim, query_start_loc.shape[0] - 1, _ptr(query_start_loc, torch.int32), _ptr(seq_lens, torch.int32),
         _ptr(block_tables, torch.int32), block_tables.shape[1], total_tokens, max_query_len,
         _ptr(new_k, torch.bfloat16), _ptr(new_v, torch.bfloat16), _ptr(cos_sin, torch.float32), *_table(cos_sin), style,
-        _ptr(positions, torch.int32), _ptr(q, torch.bfloat16), _heads(q, q_out, head_dim),
-        _ptr(q_out, torch.bfloat16), _stream(stream, k_cache)))
+        _ptr(positions, torch.int32), _ptr(q, torch.bfloat16), _heads(q, q_out, head_dim), _ptr(q_out, torch.bfloat16),
+        _stream(stream, k_cache, v_cache, query_start_loc, seq_lens, block_tables, new_k, new_v, cos_sin, positions, q,
+                q_out)))
 
 
 def spexis_rotate_append_kv8(k_cache, v_cache, scales, num_blocks, num_kv_heads, block_size, head_dim,
@@ -203,7 +208,9 @@ def spexis_rotate_append_kv8(k_cache, v_cache, scales, num_blocks, num_kv_heads,
         _ptr(seq_lens, torch.int32), _ptr(block_tables, torch.int32), block_tables.shape[1], total_tokens,
         max_query_len, _ptr(new_k, torch.bfloat16), _ptr(new_v, torch.bfloat16), _ptr(cos_sin, torch.float32),
         *_table(cos_sin), style, _ptr(positions, torch.int32), _ptr(q, torch.bfloat16), _heads(q, q_out, head_dim),
-        _ptr(q_out, torch.bfloat16), _stream(stream, k_cache)))
+        _ptr(q_out, torch.bfloat16),
+        _stream(stream, k_cache, v_cache, scales, query_start_loc, seq_lens, block_tables, new_k, new_v, cos_sin,
+                positions, q, q_out)))
 
 
 def spexis_verify_attention_workspace_size(num_seqs, num_q_heads, num_kv_heads, head_dim, max_query_len, max_seq_len,
@@ -239,7 +246,8 @@ def spexis_verify_attention_kv8(k_cache, v_cache, scales, num_blocks, num_kv_hea
         num_kv_heads, block_size, head_dim, query_start_loc.shape[0] - 1, _ptr(query_start_loc, torch.int32),
         _ptr(seq_lens, torch.int32), _ptr(block_tables, torch.int32), block_tables.shape[1], total_tokens, max_query_len,
         max_seq_len, _ptr(q, torch.bfloat16), num_q_heads, scale, _ptr(out, torch.bfloat16), kv_chunk_tokens,
-        _ptr(workspace), workspace.numel() * workspace.element_size(), _stream(stream, k_cache)))
+        _ptr(workspace), workspace.numel() * workspace.element_size(),
+        _stream(stream, k_cache, v_cache, scales, query_start_loc, seq_lens, block_tables, q, out, workspace)))
 
 
 def spexis_softmax_rows(logits, probs, temperature=1.0, stream=None) -> None:
@@ -276,7 +284,8 @@ def spexis_token_logprobs(logits, token_ids, logprobs, workspace=None, row_ids=N
         stride, rows, vocab, temperature, n, _ptr(row_ids, torch.int32), _ptr(token_ids, torch.int32),
         0 if top_ids is None else top_ids.shape[-1], _ptr(logprobs, torch.float32), _ptr(entropy, torch.float32),
         _ptr(top_ids, torch.int32), _ptr(top_logprobs, torch.float32), _ptr(workspace),
-        0 if workspace is None else workspace.numel() * workspace.element_size(), _stream(stream, logits)))
+        0 if workspace is None else workspace.numel() * workspace.element_size(),
+        _stream(stream, logits, token_ids, logprobs, workspace, row_ids, entropy, top_ids, top_logprobs)))
 
 
 def spexis_accept_workspace_size(num_seqs, vocab, max_k) -> int:

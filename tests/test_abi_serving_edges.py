@@ -20,3 +20,71 @@ def marked(f):
 @marked
 def test_scales_that_the_attention_refuses_are_refused_by_the_append():
     assert rotate(True, sc=ODD) == INVALID and b"16-byte aligned" in sx.lib().spexis_last_error()
+
+
+class Placed(torch.Tensor):
+    """A tensor in host memory that says it lies on a GPU."""
+    on = 0
+
+    @property
+    def is_cuda(self):
+        return True
+
+    def get_device(self):
+        return self.on
+
+
+def placed(shape, dtype, on=0):
+    t = torch.zeros(shape, dtype=dtype).as_subclass(Placed)
+    t.on = on
+    return t
+
+
+class Recorder:
+    """In place of the library: every call succeeds."""
+    def __init__(self):
+        self.calls = []
+
+    def __getattr__(self, name):
+        return lambda *a: self.calls.append((name, a)) or 0
+
+
+@pytest.fixture
+def recorded(monkeypatch):
+    r = Recorder()
+    monkeypatch.setattr(sx, "lib", lambda: r)
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda device: 77, raising=False)
+    return r
+
+
+BF, F32, I32, E4 = torch.bfloat16, torch.float32, torch.int32, torch.float8_e4m3fn
+B, T, HQ, HKV, D, BS, NB, MB = 2, 5, 4, 2, 64, 16, 6, 3   # sequences, tokens, heads, head_dim, block size, blocks, table width
+WHERE = dict(query_start_loc=((B + 1,), I32), seq_lens=((B,), I32), block_tables=((B, MB), I32))
+POOLS = dict(k_cache=((NB * HKV * BS * D,), BF), v_cache=((NB * HKV * BS * D,), BF))
+POOLS8 = dict(k_cache=((NB * HKV * BS * D,), E4), v_cache=((NB * HKV * BS * D,), E4), scales=((NB, HKV, 2), F32))
+ROWS = dict(new_k=((T, HKV, D), BF), new_v=((T, HKV, D), BF), cos_sin=((40, 32), F32), positions=((T,), I32),
+            q=((T, HQ, D), BF), q_out=((T, HQ, D), BF))
+LIKE = dict(num_blocks=NB, num_kv_heads=HKV, block_size=BS, head_dim=D, total_tokens=T, max_query_len=3)
+CALLS = {
+    "spexis_rotate_append_kv": (dict(POOLS, **WHERE, **ROWS), LIKE),
+    "spexis_rotate_append_kv8": (dict(POOLS8, **WHERE, **ROWS), LIKE),
+    "spexis_verify_attention_kv8": (dict(POOLS8, **WHERE, q=((T, HQ, D), BF), out=((T, HQ, D), BF), workspace=((1 << 20,), torch.uint8)),
+                                    dict(LIKE, max_seq_len=40, num_q_heads=HQ, scale=0.125)),
+    "spexis_token_logprobs": (dict(logits=((4, 50), F32), token_ids=((3,), I32), logprobs=((3,), F32), row_ids=((3,), I32),
+                                   entropy=((3,), F32), top_ids=((3, 5), I32), top_logprobs=((3, 5), F32),
+                                   workspace=((64,), torch.uint8)), {}),
+}
+
+
+@pytest.mark.parametrize("call", CALLS)
+def test_every_tensor_has_to_be_on_the_current_device(call, recorded):
+    """Kernels run on the current device: a tensor of another one, whichever argument, is refused before the call."""
+    shapes, scalars = CALLS[call]
+    f = getattr(sx, call)
+    f(**{k: placed(*v) for k, v in shapes.items()}, **scalars)
+    assert [name for name, _ in recorded.calls] == [call] and recorded.calls[0][1][-1] == 77
+    for other in shapes:
+        with pytest.raises(ValueError, match="current device"):
+            f(**{k: placed(*v, on=int(k == other)) for k, v in shapes.items()}, **scalars)
+    assert len(recorded.calls) == 1
