@@ -139,17 +139,33 @@ def _ptr(t: Optional[torch.Tensor], dtype=None):
     return t.data_ptr()
 
 
-def _stream(stream, *tensors):
-    """The stream's handle.  Kernels are launched on the current device: tensors, or a stream beside them, of another
-    one are refused."""
-    if stream is not None and not tensors:
-        return stream.cuda_stream
-    here = torch._C._cuda_getDevice()
-    for t in tensors:
-        if t is not None and t.get_device() != here:
-            raise ValueError("tensors must be on the current device")
+def _stream(stream):
     if stream is None:
         # the current stream's handle without building a torch.cuda.Stream (4 us a call)
+        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+    return stream.cuda_stream
+
+
+# The serving operators' arguments.  Kernels are launched on the current device, `here`: a tensor or a stream of another
+# one is refused, and a tensor with fewer entries than the call takes.
+
+
+def _on(t: Optional[torch.Tensor], dtype, here, entries=0, name=""):
+    if t is None:
+        return None
+    if t.get_device() != here:
+        raise ValueError("tensors must be on the current device" if t.is_cuda else "tensor must be on the GPU")
+    if not t.is_contiguous():
+        raise ValueError("tensor must be contiguous")
+    if t.dtype != dtype:
+        raise ValueError(f"expected {dtype}, got {t.dtype}")
+    if t.numel() < entries:
+        raise ValueError(f"{name} holds {t.numel()} entries, the call takes {entries}")
+    return t.data_ptr()
+
+
+def _stream_on(stream, here):
+    if stream is None:
         return torch._C._cuda_getCurrentRawStream(here)
     if stream.device_index != here:
         raise ValueError("the stream must be of the current device")
@@ -169,32 +185,48 @@ def spexis_append_kv(k_cache, v_cache, num_blocks, num_kv_heads, block_size, hea
         _ptr(new_k, torch.bfloat16), _ptr(new_v, torch.bfloat16), _stream(stream)))
 
 
-def _table(cos_sin):
-    """(rows, width) of a rotation table."""
-    return (0, 0) if cos_sin is None else tuple(cos_sin.shape)
+_BF16, _F32, _I32, _E4M3 = torch.bfloat16, torch.float32, torch.int32, torch.float8_e4m3fn
 
 
-def _heads(q, q_out, head_dim) -> int:
+def _batch_args(here, query_start_loc, seq_lens, block_tables):
+    """num_seqs, query_start_loc, seq_lens, block_tables, their width."""
+    seqs, (rows, width) = query_start_loc.numel() - 1, block_tables.shape
+    if rows < seqs:
+        raise ValueError(f"block_tables holds {rows} sequences, the call takes {seqs}")
+    return (seqs, _on(query_start_loc, _I32, here), _on(seq_lens, _I32, here, seqs, "seq_lens"),
+            _on(block_tables, _I32, here), width)
+
+
+def _heads(q, q_out, head_dim, tokens) -> int:
     """Query heads of q, whose shape q_out has as well."""
     if q is None:
         return 0
-    if q.dim() != 3 or q.shape[2] != head_dim or (q_out is not None and q_out.shape != q.shape):
+    shape = q.shape
+    if len(shape) != 3 or shape[2] != head_dim or (q_out is not None and q_out is not q and q_out.shape != shape):
         raise ValueError("q and q_out must be [tokens][query heads][head_dim]")
-    return q.shape[1]
+    if shape[0] < tokens:
+        raise ValueError(f"q holds {shape[0]} tokens, the call takes {tokens}")
+    return shape[1]
+
+
+def _row_args(here, tokens, heads, head_dim, new_k, new_v, cos_sin, style, positions, q, q_out):
+    """What the rotating appends take from new_k on."""
+    rows = tokens * heads * head_dim
+    return (_on(new_k, _BF16, here, rows, "new_k"), _on(new_v, _BF16, here, rows, "new_v"), _on(cos_sin, _F32, here),
+            *((0, 0) if cos_sin is None else cos_sin.shape), style, _on(positions, _I32, here, tokens, "positions"),
+            _on(q, _BF16, here), _heads(q, q_out, head_dim, tokens), _on(q_out, _BF16, here))
 
 
 def spexis_rotate_append_kv(k_cache, v_cache, num_blocks, num_kv_heads, block_size, head_dim, query_start_loc,
                             seq_lens, block_tables, total_tokens, max_query_len, new_k, new_v, cos_sin,
                             style=SPEXIS_ROTARY_HALVES, positions=None, q=None, q_out=None, stream=None) -> None:
     """cos_sin [max_position][rotary_dim] fp32; q and q_out [T][Hq][head_dim] bf16 (q_out may be q)."""
+    here, pool = torch._C._cuda_getDevice(), num_blocks * num_kv_heads * block_size * head_dim
     _check(lib().spexis_rotate_append_kv(
-        _ptr(k_cache, torch.bfloat16), _ptr(v_cache, torch.bfloat16), num_blocks, num_kv_heads, block_size,
-        head_dim, query_start_loc.shape[0] - 1, _ptr(query_start_loc, torch.int32), _ptr(seq_lens, torch.int32),
-        _ptr(block_tables, torch.int32), block_tables.shape[1], total_tokens, max_query_len,
-        _ptr(new_k, torch.bfloat16), _ptr(new_v, torch.bfloat16), _ptr(cos_sin, torch.float32), *_table(cos_sin), style,
-        _ptr(positions, torch.int32), _ptr(q, torch.bfloat16), _heads(q, q_out, head_dim), _ptr(q_out, torch.bfloat16),
-        _stream(stream, k_cache, v_cache, query_start_loc, seq_lens, block_tables, new_k, new_v, cos_sin, positions, q,
-                q_out)))
+        _on(k_cache, _BF16, here, pool, "k_cache"), _on(v_cache, _BF16, here, pool, "v_cache"), num_blocks, num_kv_heads,
+        block_size, head_dim, *_batch_args(here, query_start_loc, seq_lens, block_tables), total_tokens, max_query_len,
+        *_row_args(here, total_tokens, num_kv_heads, head_dim, new_k, new_v, cos_sin, style, positions, q, q_out),
+        _stream_on(stream, here)))
 
 
 def spexis_rotate_append_kv8(k_cache, v_cache, scales, num_blocks, num_kv_heads, block_size, head_dim,
@@ -202,15 +234,13 @@ def spexis_rotate_append_kv8(k_cache, v_cache, scales, num_blocks, num_kv_heads,
                              cos_sin=None, style=SPEXIS_ROTARY_HALVES, positions=None, q=None, q_out=None,
                              stream=None) -> None:
     """Pools torch.float8_e4m3fn, scales [num_blocks][Hkv][2] fp32; without cos_sin nothing is rotated."""
+    here, pool = torch._C._cuda_getDevice(), num_blocks * num_kv_heads * block_size * head_dim
     _check(lib().spexis_rotate_append_kv8(
-        _ptr(k_cache, torch.float8_e4m3fn), _ptr(v_cache, torch.float8_e4m3fn), _ptr(scales, torch.float32), num_blocks,
-        num_kv_heads, block_size, head_dim, query_start_loc.shape[0] - 1, _ptr(query_start_loc, torch.int32),
-        _ptr(seq_lens, torch.int32), _ptr(block_tables, torch.int32), block_tables.shape[1], total_tokens,
-        max_query_len, _ptr(new_k, torch.bfloat16), _ptr(new_v, torch.bfloat16), _ptr(cos_sin, torch.float32),
-        *_table(cos_sin), style, _ptr(positions, torch.int32), _ptr(q, torch.bfloat16), _heads(q, q_out, head_dim),
-        _ptr(q_out, torch.bfloat16),
-        _stream(stream, k_cache, v_cache, scales, query_start_loc, seq_lens, block_tables, new_k, new_v, cos_sin,
-                positions, q, q_out)))
+        _on(k_cache, _E4M3, here, pool, "k_cache"), _on(v_cache, _E4M3, here, pool, "v_cache"),
+        _on(scales, _F32, here, num_blocks * num_kv_heads * 2, "scales"), num_blocks, num_kv_heads, block_size, head_dim,
+        *_batch_args(here, query_start_loc, seq_lens, block_tables), total_tokens, max_query_len,
+        *_row_args(here, total_tokens, num_kv_heads, head_dim, new_k, new_v, cos_sin, style, positions, q, q_out),
+        _stream_on(stream, here)))
 
 
 def spexis_verify_attention_workspace_size(num_seqs, num_q_heads, num_kv_heads, head_dim, max_query_len, max_seq_len,
@@ -241,13 +271,14 @@ def spexis_verify_attention_kv8(k_cache, v_cache, scales, num_blocks, num_kv_hea
                                 query_start_loc, seq_lens, block_tables, total_tokens, max_query_len, max_seq_len, q,
                                 num_q_heads, scale, out, workspace, kv_chunk_tokens=0, stream=None) -> None:
     """Pools torch.float8_e4m3fn, scales [num_blocks][Hkv][2] fp32 (powers of two)."""
+    here, pool = torch._C._cuda_getDevice(), num_blocks * num_kv_heads * block_size * head_dim
+    rows = total_tokens * num_q_heads * head_dim
     _check(lib().spexis_verify_attention_kv8(
-        _ptr(k_cache, torch.float8_e4m3fn), _ptr(v_cache, torch.float8_e4m3fn), _ptr(scales, torch.float32), num_blocks,
-        num_kv_heads, block_size, head_dim, query_start_loc.shape[0] - 1, _ptr(query_start_loc, torch.int32),
-        _ptr(seq_lens, torch.int32), _ptr(block_tables, torch.int32), block_tables.shape[1], total_tokens, max_query_len,
-        max_seq_len, _ptr(q, torch.bfloat16), num_q_heads, scale, _ptr(out, torch.bfloat16), kv_chunk_tokens,
-        _ptr(workspace), workspace.numel() * workspace.element_size(),
-        _stream(stream, k_cache, v_cache, scales, query_start_loc, seq_lens, block_tables, q, out, workspace)))
+        _on(k_cache, _E4M3, here, pool, "k_cache"), _on(v_cache, _E4M3, here, pool, "v_cache"),
+        _on(scales, _F32, here, num_blocks * num_kv_heads * 2, "scales"), num_blocks, num_kv_heads, block_size, head_dim,
+        *_batch_args(here, query_start_loc, seq_lens, block_tables), total_tokens, max_query_len, max_seq_len,
+        _on(q, _BF16, here, rows, "q"), num_q_heads, scale, _on(out, _BF16, here, rows, "out"), kv_chunk_tokens,
+        _on(workspace, workspace.dtype, here), workspace.nbytes, _stream_on(stream, here)))
 
 
 def spexis_softmax_rows(logits, probs, temperature=1.0, stream=None) -> None:
@@ -279,13 +310,16 @@ def spexis_token_logprobs(logits, token_ids, logprobs, workspace=None, row_ids=N
         raise ValueError("top_ids and top_logprobs must have token_ids' shape and one more axis")
     rows, vocab = logits.shape
     stride = logits.stride(0) if rows > 1 else vocab
+    here = torch._C._cuda_getDevice()
+    if logits.get_device() != here:
+        raise ValueError("tensors must be on the current device")
     _check(lib().spexis_token_logprobs(
         SPEXIS_TYPE_F32 if logits.dtype == torch.float32 else SPEXIS_TYPE_BF16, logits.data_ptr(),
-        stride, rows, vocab, temperature, n, _ptr(row_ids, torch.int32), _ptr(token_ids, torch.int32),
-        0 if top_ids is None else top_ids.shape[-1], _ptr(logprobs, torch.float32), _ptr(entropy, torch.float32),
-        _ptr(top_ids, torch.int32), _ptr(top_logprobs, torch.float32), _ptr(workspace),
-        0 if workspace is None else workspace.numel() * workspace.element_size(),
-        _stream(stream, logits, token_ids, logprobs, workspace, row_ids, entropy, top_ids, top_logprobs)))
+        stride, rows, vocab, temperature, n, _on(row_ids, _I32, here), _on(token_ids, _I32, here),
+        0 if top_ids is None else top_ids.shape[-1], _on(logprobs, _F32, here), _on(entropy, _F32, here),
+        _on(top_ids, _I32, here), _on(top_logprobs, _F32, here),
+        *((None, 0) if workspace is None else (_on(workspace, workspace.dtype, here), workspace.nbytes)),
+        _stream_on(stream, here)))
 
 
 def spexis_accept_workspace_size(num_seqs, vocab, max_k) -> int:

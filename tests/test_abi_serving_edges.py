@@ -88,3 +88,39 @@ def test_every_tensor_has_to_be_on_the_current_device(call, recorded):
         with pytest.raises(ValueError, match="current device"):
             f(**{k: placed(*v, on=int(k == other)) for k, v in shapes.items()}, **scalars)
     assert len(recorded.calls) == 1
+
+
+# per call, tensors that hold less than the other arguments say
+SHORT = {
+    "spexis_rotate_append_kv": dict(k_cache=(NB * HKV * BS * D - 1,), v_cache=(NB * HKV * BS * D - 1,), seq_lens=(B - 1,),
+                                    block_tables=(B - 1, MB), new_k=(T - 1, HKV, D), new_v=(T, HKV - 1, D), positions=(T - 1,)),
+    "spexis_rotate_append_kv8": dict(k_cache=((NB - 1) * HKV * BS * D,), v_cache=((NB - 1) * HKV * BS * D,), scales=(NB, HKV),
+                                     seq_lens=(0,), block_tables=(B - 1, MB), new_k=(T, HKV, D - 1), new_v=(T - 1, HKV, D),
+                                     positions=(1,)),
+    "spexis_verify_attention_kv8": dict(k_cache=((NB - 1) * HKV * BS * D,), v_cache=((NB - 1) * HKV * BS * D,),
+                                        scales=(NB, HKV, 1), seq_lens=(B - 1,), block_tables=(B - 1, MB), q=(T - 1, HQ, D),
+                                        out=(T, HQ - 1, D)),
+}
+
+
+@pytest.mark.parametrize("call,name", [(c, n) for c, names in SHORT.items() for n in names])
+def test_tensors_that_are_too_short(call, name, recorded):
+    shapes, scalars = CALLS[call]
+    tensors = {k: placed(*v) for k, v in shapes.items()}
+    tensors[name] = placed(SHORT[call][name], shapes[name][1])
+    with pytest.raises(ValueError, match=name):
+        getattr(sx, call)(**tensors, **scalars)
+    assert not recorded.calls
+
+
+@pytest.mark.parametrize("call", ["spexis_rotate_append_kv", "spexis_rotate_append_kv8"])
+def test_q_with_fewer_rows_than_tokens(call, recorded):
+    shapes, scalars = CALLS[call]
+    tensors = {k: placed(*v) for k, v in shapes.items()}
+    tensors.update(q=placed((T - 1, HQ, D), BF), q_out=placed((T - 1, HQ, D), BF))
+    with pytest.raises(ValueError, match="q"):
+        getattr(sx, call)(**tensors, **scalars)
+    # longer buffers than the call takes, as a program keeps them, are fine
+    more = {k: placed((s[0] + 3, *s[1:]) if k != "query_start_loc" and k != "cos_sin" else s, d) for k, (s, d) in shapes.items()}
+    getattr(sx, call)(**more, **scalars)
+    assert len(recorded.calls) == 1
