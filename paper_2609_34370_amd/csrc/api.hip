@@ -376,7 +376,7 @@ int spexis_token_logprobs(int32_t logits_type, const void* logits, int64_t row_s
   const int parts = spexis::logprob_parts(std::max(num_items, 1), vocab, row_ids && num_items >= num_rows);
   if ((int64_t)num_items * parts >= (1ll << 24)) return fail(SPEXIS_ERR_UNSUPPORTED, "%s: too many items", name);
   if (num_items == 0) return ok();
-  if (!logits || !token_ids || !logprobs || (top_n > 0 && (!top_ids || !top_logprobs)))
+  if ((num_rows > 0 && !logits) || !token_ids || !logprobs || (top_n > 0 && (!top_ids || !top_logprobs)))
     return fail(SPEXIS_ERR_INVALID_ARGUMENT, "%s: null pointer", name);
   if (reinterpret_cast<uintptr_t>(logits) % (logits_type == SPEXIS_TYPE_F32 ? 4 : 2) != 0 || misaligned({workspace}))
     return fail(SPEXIS_ERR_INVALID_ARGUMENT, "%s: a misaligned pointer", name);
