@@ -35,6 +35,9 @@ class VerifyStep:
         self.tables = torch.as_tensor(batch.block_tables, device=dev)
         self.attn = attn
         self.in8 = isinstance(attn, AttentionInputs8)
+        if rotary is not None and rotary.cos_sin.shape[0] < batch.max_seq_len:
+            raise ValueError(f"the rotation's table ends at position {rotary.cos_sin.shape[0]}, "
+                             f"the longest sequence at {batch.max_seq_len}")
         self.rotary = rotary
         self.q = attn.q if rotary is None else torch.empty_like(attn.q)
         self.out = torch.empty_like(attn.q)

@@ -124,3 +124,17 @@ def test_q_with_fewer_rows_than_tokens(call, recorded):
     more = {k: placed((s[0] + 3, *s[1:]) if k != "query_start_loc" and k != "cos_sin" else s, d) for k, (s, d) in shapes.items()}
     getattr(sx, call)(**more, **scalars)
     assert len(recorded.calls) == 1
+
+
+@pytest.mark.skipif(not os.path.exists(sx.LIB_PATH), reason="libspexis.so not built")
+def test_a_step_whose_rotation_table_is_shorter_than_its_sequences():
+    """The library clamps positions for memory safety: the keys behind the table's end would all turn alike."""
+    from paper_2609_34370_amd import workloads as wl
+    from paper_2609_34370_amd.step import VerifyStep
+    spec = wl.spec_with(1, batch=2)
+    batch = wl.make_batch(spec, ctx_lens=[30, 70], k=[4, 2])
+    attn = wl.make_attention_inputs(spec, batch)
+    most = int(batch.max_seq_len)
+    VerifyStep(batch, attn, None, device="cpu", rotary=wl.make_rotary_inputs(most, 32))
+    with pytest.raises(ValueError, match=str(most)):
+        VerifyStep(batch, attn, None, device="cpu", rotary=wl.make_rotary_inputs(most - 1, 32))
