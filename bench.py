@@ -813,14 +813,19 @@ def stored_traffic(workload: int, call: str):
 
 
 def _kernel_digest(sources=("attention.hip",)) -> str:
-    """Digest of the sources a call's kernels are built from (their code, the shared device
-    helpers, and the header with their parameters and launch constants): a stored traffic figure
+    """Digest of the sources a call's kernels are built from (their code, and the headers of csrc that they include,
+    themselves or through another: shared device code, parameters and launch constants): a stored traffic figure
     is used only while they are unchanged."""
     import hashlib
+    import re
     h = hashlib.sha256()
-    for name in tuple(sources) + ("common.h", "kernels.h"):
-        with open(os.path.join(ROOT, "paper_2609_34370_amd", "csrc", name), "rb") as f:
-            h.update(f.read())
+    csrc, names = os.path.join(ROOT, "paper_2609_34370_amd", "csrc"), list(sources)
+    for name in names:   # grows on the way
+        with open(os.path.join(csrc, name), "rb") as f:
+            text = f.read()
+        h.update(text)
+        names += [n for n in re.findall(r'^#include "([^"]+)"', text.decode(), re.M)
+                  if n not in names and os.path.exists(os.path.join(csrc, n))]
     return h.hexdigest()[:16]
 
 
