@@ -87,10 +87,6 @@ __device__ __forceinline__ void advance(const AttnParams& p, Cursor& c) {
 // Share geometry of a head's tile stream: shares pair up, shares 2j and 2j+1 covering tiles
 // [2jP, 2(j+1)P), the first (the wave on an even XCD) P + dlt of them and the second P - dlt.
 // dlt = 0 gives equal shares of P.
-// P of a head's `total` tiles: an even split over its shares, but at least attn_least_tiles each.
-__device__ __forceinline__ int share_tiles(const AttnParams& p, int total) {
-  return max(attn_least_tiles(p.least, total), (total + p.nshares - 1) / p.nshares);
-}
 __device__ __forceinline__ int share_delta(int P, int skew) { return (int)(((int64_t)P * skew) >> 10); }
 __device__ __forceinline__ int64_t share_first(int s, int P, int dlt) {
   return (int64_t)(s >> 1) * 2 * P + (s & 1) * (P + dlt);
@@ -117,9 +113,12 @@ __device__ __forceinline__ bool find_share(const AttnParams& p, int share, int l
   if (p.num_seqs <= kWave) {
     // one pass: lane b holds sequence b's geometry; the share start is read from the lanes
     const SeqGeo gl = lane < p.num_seqs ? seq_geo(p, p.qsl, p.seq_lens, lane) : SeqGeo{0, 0, 0, 0};
-    const int size = gl.nt > 0 ? gl.nt + tail : 0, incl = wave_incl_scan_i32(size, lane);
-    total = __builtin_amdgcn_readlane(incl, kWave - 1);   // < 2^31 (host)
-    P = share_tiles(p, total);
+    const uint64_t some = __builtin_amdgcn_ballot_w64(gl.nt > 0);   // the sequences with tiles, and those before a lane's
+    const int before = __builtin_amdgcn_mbcnt_hi((uint32_t)(some >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)some, 0));
+    const int scan = wave_incl_scan_i32(gl.nt, lane), tiles = __builtin_amdgcn_readlane(scan, kWave - 1);
+    const int size = gl.nt > 0 ? gl.nt + tail : 0, incl = scan + tail * (before + (gl.nt > 0 ? 1 : 0));
+    total = tiles + tail * (int)__popcll(some);   // < 2^31 (host)
+    P = attn_share_positions(p.least, tiles, (int)__popcll(some), tail, p.nshares);
     if (share_first(share, P, share_delta(P, p.skew)) >= total) return false;
     const int g0 = (int)share_first(share, P, share_delta(P, p.skew));
     const uint64_t hit = __builtin_amdgcn_ballot_w64(incl > g0);
@@ -132,7 +131,8 @@ __device__ __forceinline__ bool find_share(const AttnParams& p, int share, int l
     start.S = __builtin_amdgcn_readlane(gl.S, l0);
     start.t = g0 - f0;
   } else {
-    // 512 sequences at a time, eight a lane whose loads are in flight together
+    // 512 sequences at a time, eight a lane whose loads are in flight together (the bf16 kernel against a search of 64 at a
+    // time: 512 sequences of 20 to 200 keys 17.5 us for 19.8, 64-wide, 74.3 for 76.9, 128-wide; from 65 to 150 the same)
     constexpr int kAhead = 8;
     int nt[kAhead];
     const auto sizes = [&](int base) {
@@ -143,14 +143,18 @@ __device__ __forceinline__ bool find_share(const AttnParams& p, int share, int l
         if (b >= p.num_seqs) nt[k] = 0;
       }
     };
-    int per_lane = 0;
+    int per_lane = 0, items = 0;
     for (int base = 0; base < p.num_seqs; base += kAhead * kWave) {
       sizes(base);
 #pragma unroll
-      for (int k = 0; k < kAhead; ++k) per_lane += nt[k] > 0 ? nt[k] + tail : 0;
+      for (int k = 0; k < kAhead; ++k) {
+        per_lane += nt[k];
+        items += (int)__popcll(__builtin_amdgcn_ballot_w64(nt[k] > 0));
+      }
     }
-    total = __builtin_amdgcn_readfirstlane(wave_sum_i32(per_lane));   // < 2^31 (host)
-    P = share_tiles(p, total);
+    const int tiles = __builtin_amdgcn_readfirstlane(wave_sum_i32(per_lane));
+    total = tiles + tail * items;   // < 2^31 (host)
+    P = attn_share_positions(p.least, tiles, items, tail, p.nshares);
     if (share_first(share, P, share_delta(P, p.skew)) >= total) return false;
     const int g0 = (int)share_first(share, P, share_delta(P, p.skew));
     // the sequence holding position g0, and the stream index of its first tile

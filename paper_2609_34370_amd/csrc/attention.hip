@@ -551,7 +551,7 @@ __global__ __launch_bounds__(512) void attn_merge_wide_kernel(AttnParams p, int 
   const int total = wave_sum_i32(all), f = wave_sum_i32(before);   // < 2^31 (host)
   const int R = p.group * g.n;
   if (g.nt == 0 || rg * kMergeRows >= R) return;
-  const int P = share_tiles(p, total);
+  const int P = attn_share_positions(p.least, total, 0, 0, p.nshares);   // (no item costs more: launch)
   const int dlt = share_delta(P, p.skew);
   const int s0 = share_of(f, P, dlt);
   const int C = min(share_of(f + g.nt - 1, P, dlt), p.nshares - 1) - s0 + 1;

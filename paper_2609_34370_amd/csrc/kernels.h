@@ -82,6 +82,15 @@ inline AttnLeast attn_least(int64_t num_seqs, int64_t hkv, int head_dim, int R) 
 __host__ __device__ inline int attn_least_tiles(const AttnLeast& l, int total) {
   return total >= l.from6 ? 6 : total >= l.from4 || (total >= l.lo4 && total < l.hi4) ? 4 : l.tiles;
 }
+// The positions of a share: an even split of a head's tiles and of the `item_cost` positions that each of its `items` counts
+// besides, but at least attn_least_tiles, a rule on tiles alone.  (Shown the item cost of the 8-bit kernel too, it took
+// sequences of four tiles for eight: 64 over 8 heads, 20 rows, 17.2 us for 13.7; 512 over one 19.7 for 14.7.  Without the
+// cost where that floor decides, 256 sequences of three tiles over 4 heads took 23.2 us for 14.9, and 256 of eight over 8
+// as long as with it.)
+__host__ __device__ inline int attn_share_positions(const AttnLeast& l, int tiles, int items, int item_cost, int nshares) {
+  const int least = attn_least_tiles(l, tiles), even = (tiles + item_cost * items + nshares - 1) / nshares;
+  return least > even ? least : even;
+}
 // Tiles moved, per 1024, from the share of each pair on an odd XCD to the one on an even XCD:
 // waves on odd XCDs stream the cache a few per cent slower.
 constexpr int kAttnXcdSkew = 28;
