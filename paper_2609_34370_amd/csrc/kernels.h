@@ -38,6 +38,33 @@ struct RotateParams {
   // 0: by search; how the two kinds alternate; whether q is too large for the caches
   int append_groups, queries, seq_blocks, seq_tokens, mix, stream_q;
 };
+// Workgroups of the rotating appends for that many appends and workgroups of queries; `mix`: 0, appends come first, or they
+// alternate, mix appends to a query, -mix queries to an append.
+inline int64_t rotate_groups(int64_t appends, int64_t queries, bool alternate, int* mix) {
+  *mix = 0;
+  if (!alternate || queries == 0) return appends + queries;
+  // rounds of |mix| + 1 workgroups, enough for both kinds
+  const int64_t many = appends >= queries ? appends : queries, rounds = appends >= queries ? queries : appends;
+  const int64_t m = (many + rounds - 1) / rounds;
+  *mix = (int)(appends >= queries ? m : -m);
+  return (rounds * (m + 1) + 7) / 8 * 8;
+}
+// What workgroup w is: an append or a workgroup of queries, and which (past their number: nothing).
+struct RotatePlace {
+  bool append;
+  int index;
+};
+__host__ __device__ inline RotatePlace rotate_place(int w, int mix, int appends) {
+  if (mix == 0) return w < appends ? RotatePlace{true, w} : RotatePlace{false, w - appends};
+  // Workgroup w runs on XCD w mod 8: each eight turn by one place more than the eight before, so that rounds of an even
+  // length do not put a kind on the same XCDs every time (512 sequences of 5 rows, 32 + 8 heads, seven appends to a query:
+  // 35.6 us with every query on one XCD, 19.3 us).
+  w = (w & ~7) | ((w + (w >> 3)) & 7);
+  const int m = mix < 0 ? -mix : mix, round = w / (m + 1), r = w % (m + 1);
+  if (mix > 0) return r < m ? RotatePlace{true, round * m + r} : RotatePlace{false, round};
+  return r == m ? RotatePlace{true, round} : RotatePlace{false, round * m + r};
+}
+
 constexpr int kAttnHdrInts = 8;           // per-wave header of the partial an item's first wave leaves
 constexpr int kAttnMinTilesPerWave = 2;   // floor of the even split (short batches)
 constexpr int kAttnMaxWaves = 1024;       // waves of the even split: one per SIMD of 256 CUs
@@ -85,8 +112,7 @@ __host__ __device__ inline int attn_least_tiles(const AttnLeast& l, int total) {
 // The positions of a share: an even split of a head's tiles and of the `item_cost` positions that each of its `items` counts
 // besides, but at least attn_least_tiles, a rule on tiles alone.  (Shown the item cost of the 8-bit kernel too, it took
 // sequences of four tiles for eight: 64 over 8 heads, 20 rows, 17.2 us for 13.7; 512 over one 19.7 for 14.7.  Without the
-// cost where that floor decides, 256 sequences of three tiles over 4 heads took 23.2 us for 14.9, and 256 of eight over 8
-// as long as with it.)
+// cost where that floor decides, 256 sequences of three tiles over 4 heads took 23.2 us for 14.9.)
 __host__ __device__ inline int attn_share_positions(const AttnLeast& l, int tiles, int items, int item_cost, int nshares) {
   const int least = attn_least_tiles(l, tiles), even = (tiles + item_cost * items + nshares - 1) / nshares;
   return least > even ? least : even;

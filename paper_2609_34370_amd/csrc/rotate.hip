@@ -448,27 +448,13 @@ __device__ __forceinline__ void append_block(const RotateParams& p, int index, i
 
 template <int D, int BS, bool k8>
 __global__ __launch_bounds__((kThreads<D, BS>)) void rotate_append_kernel(RotateParams p) {
-  // 8 bits: workgroups of the two kinds alternate, `mix` of one to one of the other: appends compute and wait for one
-  // load after the other, queries keep the memory busy meanwhile (512 sequences of 9 rows: 22.8 us, appends first
-  // 27.0).  bf16 appends are as bound by memory as queries and come first (54.2 us, alternating 58.0, at 14420 tokens).
   constexpr int kWaves = kThreads<D, BS> / kWave;
-  const int w = blockIdx.x, m = p.mix < 0 ? -p.mix : p.mix, q = k8 ? w / (m + 1) : 0, r = k8 ? w % (m + 1) : 0;
-  int append, query;   // the index of the one that this workgroup is
-  if constexpr (!k8) {
-    append = w < p.append_groups ? w : -1;
-    query = w - p.append_groups;
-  } else if (p.mix >= 0) {    // r < m: append q m + r, else queries q
-    append = r < m ? q * m + r : -1;
-    query = q;
-  } else {
-    append = r == m ? q : -1;
-    query = q * m + r;
-  }
-  if (append >= 0) {
-    if (append < p.append_groups) append_block<D, BS, k8>(p, append / p.hkv, append % p.hkv, threadIdx.x);
+  const RotatePlace place = rotate_place(blockIdx.x, k8 ? p.mix : 0, p.append_groups);
+  if (place.append) {
+    if (place.index < p.append_groups) append_block<D, BS, k8>(p, place.index / p.hkv, place.index % p.hkv, threadIdx.x);
     return;
   }
-  query = __builtin_amdgcn_readfirstlane(query * kWaves + (int)(threadIdx.x >> 6));
+  const int query = __builtin_amdgcn_readfirstlane(place.index * kWaves + (int)(threadIdx.x >> 6));
   if (query >= p.queries) return;
   if (p.stream_q) rotate_query<D, true>(p, query, threadIdx.x & 63);
   else rotate_query<D, false>(p, query, threadIdx.x & 63);
@@ -477,20 +463,10 @@ __global__ __launch_bounds__((kThreads<D, BS>)) void rotate_append_kernel(Rotate
 template <int D, int BS, bool k8>
 static hipError_t launch_rotate_t(RotateParams p, hipStream_t s) {
   constexpr int kWaves = kThreads<D, BS> / kWave;
-  const int64_t a = p.append_groups, q = ((int64_t)p.queries + kWaves - 1) / kWaves;
-  // rounds of |mix| + 1 workgroups, enough for both kinds
-  int64_t rounds;
-  if (q == 0) {
-    p.mix = (int)a;
-    rounds = 1;
-  } else if (a >= q) {
-    p.mix = (int)((a + q - 1) / q);
-    rounds = q;
-  } else {
-    p.mix = -(int)((q + a - 1) / a);
-    rounds = a;
-  }
-  const int64_t groups = k8 ? rounds * ((p.mix < 0 ? -p.mix : p.mix) + 1) : a + q;
+  // 8 bits: workgroups of the two kinds alternate: appends compute and wait for one load after the other, queries keep the
+  // memory busy meanwhile.
+  const int64_t queries = ((int64_t)p.queries + kWaves - 1) / kWaves;
+  const int64_t groups = rotate_groups(p.append_groups, queries, k8, &p.mix);
   hipLaunchKernelGGL((rotate_append_kernel<D, BS, k8>), dim3((unsigned)groups), dim3(kThreads<D, BS>), 0, s, p);
   return hipGetLastError();
 }
