@@ -446,10 +446,20 @@ __device__ __forceinline__ void append_block(const RotateParams& p, int index, i
   }
 }
 
+// 8 bits, 128-wide heads: appends and queries alternate: appends compute and wait for one load after the other, queries keep
+// the memory busy meanwhile (512 sequences of 9 rows, 28 + 4 heads, 19.3 us, appends first 23.0; of 5, 32 + 8 heads, 19.4
+// and 22.4; 15060 prompt tokens 58.4 and 61.0; below 50 MB the order decides little: 64 sequences of 5 6.3 and 5.7, 42 MB of
+// prompts 10.3 and 9.0).  Appends of 64-wide heads are one wave each and as short as the queries: first (512 of 9, 8 + 2
+// heads, 7.8 us, alternating 12.7; 14420 prompt tokens 12.2 and 14.7).  bf16 appends are as bound by memory as queries and
+// come first, too (512 sequences of 5, 28 + 4 heads, 20.8 us, alternating 22.9; 128 of 5 8.1 and 9.4; but 14420 prompt
+// tokens 49.5 and 46.0).
+template <int D, bool k8>
+constexpr bool kAlternate = k8 && D == 128;
+
 template <int D, int BS, bool k8>
 __global__ __launch_bounds__((kThreads<D, BS>)) void rotate_append_kernel(RotateParams p) {
   constexpr int kWaves = kThreads<D, BS> / kWave;
-  const RotatePlace place = rotate_place(blockIdx.x, k8 ? p.mix : 0, p.append_groups);
+  const RotatePlace place = rotate_place(blockIdx.x, kAlternate<D, k8> ? p.mix : 0, p.append_groups);
   if (place.append) {
     if (place.index < p.append_groups) append_block<D, BS, k8>(p, place.index / p.hkv, place.index % p.hkv, threadIdx.x);
     return;
@@ -463,10 +473,8 @@ __global__ __launch_bounds__((kThreads<D, BS>)) void rotate_append_kernel(Rotate
 template <int D, int BS, bool k8>
 static hipError_t launch_rotate_t(RotateParams p, hipStream_t s) {
   constexpr int kWaves = kThreads<D, BS> / kWave;
-  // 8 bits: workgroups of the two kinds alternate: appends compute and wait for one load after the other, queries keep the
-  // memory busy meanwhile.
   const int64_t queries = ((int64_t)p.queries + kWaves - 1) / kWaves;
-  const int64_t groups = rotate_groups(p.append_groups, queries, k8, &p.mix);
+  const int64_t groups = rotate_groups(p.append_groups, queries, kAlternate<D, k8>, &p.mix);
   hipLaunchKernelGGL((rotate_append_kernel<D, BS, k8>), dim3((unsigned)groups), dim3(kThreads<D, BS>), 0, s, p);
   return hipGetLastError();
 }
