@@ -12,7 +12,7 @@
 // Which block: sequence b gets the indices from start(b) = floor(qsl[b] / bs) + 2 b.  n new tokens touch at most
 // floor(n / bs) + 2 blocks, which start(b+1) - start(b) is never below, so no scan over the lengths is needed: a
 // wave-wide search for the last b with start(b) <= index, two probes for 4096 sequences.  Where the sequences are of
-// about one length (a step's drafts), index / (blocks of the longest) does without the search.
+// about one length (a step's drafts), every one gets the blocks of the longest, without the search.
 //
 // Measured (reads and writes of 5.3 TB/s are what a large copy reaches): q and keys of 14420 prompt tokens (28 + 4 heads
 // of 128) into the bf16 cache 48.2 us, 5.6 TB/s with what the last-level cache holds; of 15060 (32 + 8) into the 8-bit
@@ -274,12 +274,12 @@ template <int D, int BS, bool k8>
 __device__ __forceinline__ void append_block(const RotateParams& p, int index, int h, int thread) {
   constexpr int kTasks = D / 16, kWaves = kThreads<D, BS> / kWave;
   const int lane = thread & 63, wave = thread >> 6;
-  const int b = p.seq_blocks > 0 ? index / p.seq_blocks
+  const int b = p.seq_blocks > 0 ? rotate_block(index, p.num_seqs).seq
                                  : wave_search(p.num_seqs, index, lane, [&](int i) { return seq_start(p, i) / BS + 2 * i; });
   const int q0 = seq_start(p, b), q1 = clampi(p.qsl[b + 1], q0, p.total_tokens);
   const int cap = p.max_blocks * BS;
   const int n = min(min(q1 - q0, p.max_query_len), cap), S = clampi(p.seq_lens[b], n, cap), L = S - n;
-  const int t = L / BS + (p.seq_blocks > 0 ? index % p.seq_blocks : index - (q0 / BS + 2 * b));
+  const int t = L / BS + (p.seq_blocks > 0 ? rotate_block(index, p.num_seqs).nth : index - (q0 / BS + 2 * b));
   if (n == 0 || t < L / BS || t > (S - 1) / BS) return;
   const int lo = max(L, t * BS), m = min(S, (t + 1) * BS) - lo;   // first new position, new rows
   const int first = lo - t * BS;                                  // its slot: the block holds that many rows

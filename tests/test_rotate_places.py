@@ -70,3 +70,38 @@ def test_both_kinds_lie_on_every_xcd_alike(places, appends, queries):
         last = max(w for w, (k, i) in enumerate(got) if k == kind and i < n) + 1
         quarters = [sum(k == kind and i < n for k, i in got[last * j // 4: last * (j + 1) // 4]) for j in range(4)]
         assert max(quarters) <= n / 4 * 1.25 + 8, (kind, quarters)
+
+
+BLOCKS = r"""
+#include <cstdio>
+#include "kernels.h"
+int main() {
+  int seqs, blocks;
+  while (std::scanf("%d %d", &seqs, &blocks) == 2) {
+    for (int i = 0; i < seqs * blocks; ++i) {
+      const spexis::RotateBlock b = spexis::rotate_block(i, seqs);
+      std::printf("%d %d ", b.seq, b.nth);
+    }
+    std::printf("\n");
+  }
+}
+"""
+
+
+@pytest.mark.parametrize("seqs,blocks,heads", [(64, 2, 4), (128, 2, 4), (64, 2, 2), (100, 2, 1), (37, 4, 2), (512, 2, 8), (3, 40, 4)])
+def test_the_blocks_that_get_rows_lie_on_every_xcd_alike(tmp_path, seqs, blocks, heads):
+    """A step's few rows touch one block of a sequence, of the two that it has places for: with four heads the one used to
+    be on XCDs 0 to 3 and the empty one on 4 to 7."""
+    (tmp_path / "b.cpp").write_text(BLOCKS)
+    r = subprocess.run(["g++", "-std=c++17", "-D__HIP_PLATFORM_AMD__", "-I/opt/rocm/include",
+                        "-I" + os.path.join(ROOT, "paper_2609_34370_amd", "csrc"), str(tmp_path / "b.cpp"), "-o", str(tmp_path / "b")],
+                       capture_output=True, text=True)
+    assert r.returncode == 0, r.stderr
+    out = subprocess.run([str(tmp_path / "b")], input=f"{seqs} {blocks}", capture_output=True, text=True, check=True).stdout
+    v = [int(x) for x in out.split()]
+    got = list(zip(v[::2], v[1::2]))
+    assert sorted(got) == [(s, n) for s in range(seqs) for n in range(blocks)]
+    for nth in range(blocks):
+        at = [(i * heads + h) % 8 for i, g in enumerate(got) if g[1] == nth for h in range(heads)]
+        by = [at.count(x) for x in range(8)]
+        assert max(by) - min(by) <= 1, by
