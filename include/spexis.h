@@ -312,7 +312,9 @@ size_t spexis_token_logprobs_workspace_size(int32_t num_items, int32_t vocab, in
  *   logits_type   SPEXIS_TYPE_F32 or SPEXIS_TYPE_BF16 (fp32 arithmetic)
  *   logits        num_rows rows of vocab entries, row_stride >= vocab entries apart, aligned to an entry (read)
  *                 (with num_rows 0, where every item is without a row, it may be NULL)
- *   row_ids       [num_items] int32 or NULL (then num_items <= num_rows);  token_ids  [num_items] int32
+ *   row_ids       [num_items] int32 or NULL (then num_items <= num_rows);  token_ids  [num_items] int32.  Items that
+ *                 pick rows, no fewer than there are rows, are taken for a step's places, many without a token; to
+ *                 score every row NULL is the quicker call
  *   top_n         host: 0 .. 32;  top_ids [num_items][top_n] int32, top_logprobs fp32 (not used with top_n = 0)
  *   temperature   host: T, finite, > 0 and not subnormal
  *   logprobs      [num_items] fp32;  entropy [num_items] fp32 or NULL

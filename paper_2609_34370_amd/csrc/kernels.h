@@ -245,17 +245,19 @@ struct LogprobParams {
 constexpr int kLogprobMaxTop = 32;
 constexpr int kLogprobMaxParts = 64;   // the merge holds a part a lane
 // Parts of a row: the search for the alternatives and the sorts cost a workgroup as much as several rounds of loads, and a
-// second part the merge's launch, so a row is cut for less than two workgroups a CU only (128256 logits, 5 alternatives:
-// 256 rows in 2 parts 29.5 us, in 8 37.4; 500 rows whole 43.0, in 5 parts 50.0), and short rows never (40000 logits:
-// 200 rows 13.8 us, in 2 parts 17.5; 8 rows 12.1 and 11.7 in 5).  Items that pick their rows, no fewer than there are
-// rows, are a step's places, many without a token, whose workgroups leave at once (sparse: 576 items, 221 with a token, 20
-// alternatives, 34.6 us, in one part 39.4; 320 items of 320 rows 33.8 and 36.5).
-// A part has at least 8192 logits, one round of a workgroup (one row of 128256: 11.1 us, with 32768 13.9).
+// second part the merge's launch.  So a row is cut where four parts or more leave no CU with more than two workgroups
+// (128256 logits, 5 alternatives: one row in 16 parts 11.2 us, whole 20.9; 128 rows in 4 21.6, whole 24.7; but 200 rows in 2
+// 28.1, whole 25.6, 256 in 2 30.0, in 8 37.7, whole 28.0), and not where it is short (5 and 20 alternatives: one row of
+// 32000 10.7 and 13.5 us, in 6 parts 11.3 and 12.9; of 41000 11.9 and 15.5, in 6 11.3 and 12.4; in fewer than 8 parts 128 of
+// 49152 14.7 and 20.2, in 4 16.4 and 17.4).  A part has at least 8192 logits, one round of a workgroup.
+// Items that pick their rows, no fewer than there are rows, are taken for a step's places (sparse), many of them without a
+// token, whose workgroups leave at once: four times the parts (128256, 20 alternatives: 495 items, 168 with a token, 31.9
+// us, whole 36.3; 252, 83 with, 24.4 and 30.3).  Where all have one, that costs: 500 56.0 us, whole 48.8.
 inline int logprob_parts(int64_t items, int64_t V, bool sparse) {
-  if (V <= 49152) return 1;
   const int64_t want = sparse ? (2048 + items - 1) / items : 512 / items, most = (V + 8191) / 8192;
+  if (V <= (want >= 8 ? 36864 : 49152) || (!sparse && want < 4)) return 1;
   const int64_t n = want < most ? want : most;
-  return (int)(n < 1 ? 1 : n > kLogprobMaxParts ? kLogprobMaxParts : n);
+  return (int)(n > kLogprobMaxParts ? kLogprobMaxParts : n);
 }
 
 struct AcceptParams {
