@@ -15,9 +15,10 @@
 // about one length (a step's drafts), every one gets the blocks of the longest, without the search.
 //
 // Measured (reads and writes of 5.3 TB/s are what a large copy reaches): q and keys of 14420 prompt tokens (28 + 4 heads
-// of 128) into the bf16 cache 48.2 us, 5.6 TB/s with what the last-level cache holds; of 15060 (32 + 8) into the 8-bit
-// cache 57 us, 6.0 TB/s; a step of 512 sequences of 9 rows in 8 bits 18.1 us, 4.5 TB/s.  A step of 64 sequences is a
-// launch and two dependent loads, 5.4 us.
+// of 128) into the bf16 cache 48.5 us, 5.5 TB/s with what the last-level cache holds; of 15060 (32 + 8) into the 8-bit
+// cache 58 us, 5.9 TB/s; a step of 512 sequences of 9 rows in 8 bits 19.5 us, 4.2 TB/s.  A step of 64 sequences is a
+// launch and two dependent loads, 5.6 us.  (Figures below: the whole call in a replayed graph, on three sets of buffers in
+// turn.)
 #include <type_traits>
 
 #include "common.h"
@@ -180,8 +181,8 @@ __device__ __forceinline__ void rotate_query(const RotateParams& p, int index, i
       if (h >= p.hq) break;
       float x[8], y[8];
       turn_task<float>(p, task, g, a[i], b[i], x, y);
-      // written once, read by a later launch (512 sequences of 9 rows: 19.5 us, plain stores 23.2; 14420 prompt
-      // tokens 52.9 and 54.2)
+      // written once, read by a later launch (512 sequences of 9 rows, 8 bits, 19.8 us, plain stores 23.3; 14420 prompt
+      // tokens, bf16, 49.7 and 52.7)
       __builtin_nontemporal_store(narrow(x), reinterpret_cast<u32x4*>(o + h * D + task.a));
       __builtin_nontemporal_store(narrow(y), reinterpret_cast<u32x4*>(o + h * D + task.b));
     }
@@ -263,9 +264,7 @@ __device__ __forceinline__ uint32_t value_mask(int lo, int hi) {
   return below(hi) & ~below(lo);
 }
 
-// A workgroup is a (block of tokens, KV head); a thread takes one task of K and of V.  (With half the threads where a
-// step has at most 16 new rows, 512 sequences of 9 rows took 14.8 us instead of 17.9 without queries, but 24.0 instead
-// of 22.8 with them.)
+// A workgroup is a (block of tokens, KV head); a thread takes one task of K and of V.
 template <int D, int BS>
 constexpr int kThreads = BS * D / 16;
 
@@ -439,20 +438,19 @@ __device__ __forceinline__ void append_block(const RotateParams& p, int index, i
         w[q] = (w[q] & ~fresh) | (in[q] & fresh);
       }
     }
-    // whole lines of new slots in the 8-bit cache: 8 prompts of 100 to 3500 tokens 22.6 us without queries, plain
-    // stores 25.5 (bf16, where a piece is part of a line, 16.4 and 14.5)
+    // whole lines of new slots in the 8-bit cache: 15060 prompt tokens 58.8 us, plain stores 62.1 (bf16, where a piece is
+    // part of a line: 14420 49.7, streamed 52.8)
     if constexpr (k8) __builtin_nontemporal_store(w, place[i]);
     else *place[i] = w;
   }
 }
 
 // 8 bits, 128-wide heads: appends and queries alternate: appends compute and wait for one load after the other, queries keep
-// the memory busy meanwhile (512 sequences of 9 rows, 28 + 4 heads, 19.3 us, appends first 23.0; of 5, 32 + 8 heads, 19.4
-// and 22.4; 15060 prompt tokens 58.4 and 61.0; below 50 MB the order decides little: 64 sequences of 5 6.3 and 5.7, 42 MB of
-// prompts 10.3 and 9.0).  Appends of 64-wide heads are one wave each and as short as the queries: first (512 of 9, 8 + 2
-// heads, 7.8 us, alternating 12.7; 14420 prompt tokens 12.2 and 14.7).  bf16 appends are as bound by memory as queries and
-// come first, too (512 sequences of 5, 28 + 4 heads, 20.8 us, alternating 22.9; 128 of 5 8.1 and 9.4; but 14420 prompt
-// tokens 49.5 and 46.0).
+// the memory busy meanwhile (28 + 4 heads: 512 sequences of 9 rows 19.8 us, appends first 22.7; 15060 prompt tokens, 32 + 8
+// heads, 58.8 and 61.1; below 50 MB the order decides less and rather for appends first: 512 of 5 17.9 and 17.3, 64 of 5 5.8
+// and 5.4, 128 of 5 7.9 and 6.9).  Appends of 64-wide heads are one wave each and as short as the queries: first (512 of 9,
+// 8 + 2 heads, 7.5 us, alternating 11.6; 14420 prompt tokens 12.0 and 15.2).  bf16 appends are as bound by memory as queries
+// and come first, too (512 of 5 18.9 us, alternating 22.2; 128 of 5 7.3 and 8.9; but 14420 prompt tokens 49.7 and 46.2).
 template <int D, bool k8>
 constexpr bool kAlternate = k8 && D == 128;
 
@@ -486,15 +484,16 @@ static hipError_t launch_rotate_k(const RotateParams& p, hipStream_t s) {
 
 hipError_t launch_rotate_append(RotateParams p, hipStream_t s) {
   const int64_t B = p.num_seqs, T = p.total_tokens, bs = p.block_size, n = p.max_query_len;
-  // Sequences of about one length need no search: the longest one's blocks for each, where that is no more (8 bits, 512
-  // sequences of 9 rows: 19.3 us, by search 22.3), and its tokens where at most a quarter of the waves find none (512 of
-  // 9: 29.5 us, by search 30.2; 512 of 1 to 9, half of the waves idle: 20.7 and 20.6).
+  // Sequences of about one length need no search: the longest one's blocks for each, where that is no more (512 sequences
+  // of 9 rows, 8 bits, 19.8 us, by search 22.4; of one 11.7 and 15.5; of 5, bf16, 18.9 and 20.4), and its tokens where at
+  // most half of the waves find none in a step (512 of 1 to 9, 8 bits, 17.4 us, by search 20.6; of 9, 64-wide, bf16, 7.2 and
+  // 8.3), a fifth among prompts, whose search costs less (8 of 100 to 1000 20.8 us, by search 19.3).
   const int64_t blocks = B * ((n + bs - 2) / bs + 1), all = T / bs + 2 * B;
   p.seq_blocks = blocks <= all ? (int)((n + bs - 2) / bs + 1) : 0;
   p.append_groups = (int)((blocks <= all ? blocks : all) * p.hkv);
-  p.seq_tokens = 4 * B * n <= 5 * T ? (int)n : 0;
-  // q beyond 64 MB does not come from the caches: loads that leave the rest in them (117 MB: the call 57.2 us, plain
-  // loads 61.8); below that, it may (33 MB: 22.1 and 19.5)
+  p.seq_tokens = (n <= 64 ? 5 : 8) * B * n <= 10 * T ? (int)n : 0;
+  // q beyond 64 MB does not come from the caches: loads that leave the rest in them (prompts, 103 MB of q, 8 bits, the
+  // call 45.9 us, plain loads 51.9); below that, it may (21 MB: 20.3, streamed 26.0)
   p.stream_q = T * p.hq * p.head_dim * 2 > (int64_t)1 << 26;
   p.queries = p.q == nullptr ? 0 : p.seq_tokens > 0 ? (int)(B * n) : (int)T;
   return p.scales != nullptr ? launch_rotate_k<true>(p, s) : launch_rotate_k<false>(p, s);
