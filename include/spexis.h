@@ -166,7 +166,9 @@ int spexis_append_kv(void* k_cache, void* v_cache, int32_t num_blocks, int32_t n
  *                 are left as they were
  * Other arguments as spexis_append_kv; pools, rows and table 16-byte aligned.  Any number of new tokens a
  * sequence, prompts included; a sequence's blocks that receive rows must be its own.
- * Supported: rotary_dim a multiple of 16, 16 .. head_dim; head_dim in {64, 128}, block_size in {16, 32}.
+ * Supported: rotary_dim a multiple of 16, 16 .. head_dim; head_dim in {64, 128}, block_size in {16, 32};
+ * max_blocks_per_seq * block_size < 2^31, and tokens for one launch: (total_tokens / block_size + 2 num_seqs) * Hkv *
+ * head_dim * block_size / 16 + 128 total_tokens up to about 2^31.
  * Errors: INVALID_ARGUMENT, UNSUPPORTED, HIP.
  */
 int spexis_rotate_append_kv(void* k_cache, void* v_cache, int32_t num_blocks, int32_t num_kv_heads,
@@ -193,6 +195,9 @@ int spexis_rotate_append_kv(void* k_cache, void* v_cache, int32_t num_blocks, in
  * two costs no precision (codes are floating point) and re-coding earlier rows is exact but for the format's
  * subnormal codes, those below 2^-6.  Scales of blocks that hold rows must be positive
  * and finite; a caller that fills blocks by other means uses powers of two.
+ * Drafts that acceptance then rejects count as rows: where one was much larger than the rows before it in its
+ * block, those keep the coarser codes (values below 2^-10 of the larger scale are 0 from then on), until the
+ * block is begun anew.  So what this cache holds depends on rejected drafts too; a bf16 cache does not.
  *   scales  [num_blocks][Hkv][2] fp32, 16-byte aligned (read and written)
  *   cos_sin NULL with max_position 0: nothing is rotated (style and rotary_dim are not read; q, q_out and
  *           positions NULL)
@@ -269,7 +274,7 @@ size_t spexis_verify_attention_kv8_workspace_size(int32_t num_seqs, int32_t num_
  *           entries, 16-byte aligned like the pools, q, out and workspace
  *   workspace >= spexis_verify_attention_kv8_workspace_size(...) bytes
  * A NaN code of a key that a query token sees makes its output NaN; slots behind the sequence may hold anything.
- * Other arguments, supported shapes and errors as spexis_verify_attention.
+ * Other arguments, supported shapes and errors as spexis_verify_attention, every sequence counting four tiles more.
  */
 int spexis_verify_attention_kv8(const void* k_cache, const void* v_cache, const float* scales,
                                 int32_t num_blocks, int32_t num_kv_heads, int32_t block_size,
@@ -320,7 +325,7 @@ size_t spexis_token_logprobs_workspace_size(int32_t num_items, int32_t vocab, in
  *   logprobs      [num_items] fp32;  entropy [num_items] fp32 or NULL
  *   workspace     >= spexis_token_logprobs_workspace_size(num_items, vocab, top_n) bytes, 16-byte aligned (may be
  *                 NULL where that is 0)
- * Supported: vocab <= 4194304.  Errors: INVALID_ARGUMENT, UNSUPPORTED, WORKSPACE_TOO_SMALL, HIP.
+ * Supported: vocab <= 4194304, num_items < 2^24.  Errors: INVALID_ARGUMENT, UNSUPPORTED, WORKSPACE_TOO_SMALL, HIP.
  */
 int spexis_token_logprobs(int32_t logits_type, const void* logits, int64_t row_stride,
                           int32_t num_rows, int32_t vocab, float temperature, int32_t num_items,

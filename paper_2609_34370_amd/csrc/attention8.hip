@@ -10,12 +10,16 @@
 //     score tile holds keys, so they feed the products of two head-dim tiles.
 //
 // Bound by the cache's bytes up to 32 query rows a head: 64 sequences of 1024 to 4096 keys (32 query heads over 8 of 128,
-// 5 tokens; 357 MB) take 61.5 us, 5.8 TB/s, and 7.6 us of merge behind them.  With 33 to 64 rows by its own
-// instructions (two softmaxes a tile, 64 exponentials and 32 conversions a lane): 512 sequences of 512 to 2048 keys (63
-// rows, 762 MB) 153 us, 5.0 TB/s, and 18.4 us of merge.  One sequence of 16384 keys: 13.2 us for 32 MB, a chain of share
-// search, block ids, codes and products; 6.8 us of merge.
+// 5 tokens; 357 MB) take 62 to 65 us (two cards), 5.5 to 5.8 TB/s, and 7.8 us of merge behind them.  With 33 to 64 rows by
+// one wave's chain: 512 sequences of 512 to 2048 keys (63 rows, 762 MB) 154 to 158 us, 4.9 TB/s, and 18.4 us of merge.  There
+// a wave lives 302 thousand cycles, 3600 for each of its 84 tiles, at about 2.1 GHz: 352 vector instructions a tile (32
+// exponentials, 64 conversions of codes and 16 of weights among them) and 32 matrix products, which are busy for 28% of the
+// time; for 57% of it an instruction issues, for 28% the wave waits for loads, for 15% for earlier results.  One sequence of
+// 16384 keys: 13 to 15 us for 32 MB, a chain of share search, block ids, codes and products, whose partials (10.6 MB) are
+// written and read again, and 6.9 us of merge.
 // One wave a SIMD holds everything in registers; two (half the registers each, twice the shares and partials) took 78
-// and 197 us where one takes 71 and 180.  Three tiles in flight took 72 us instead of 71, the loads of two being enough.
+// and 197 us a call where one took 71 and 180.  Three tiles in flight took 72 us instead of 71 (one row tile; two have no
+// registers for a third).
 #include "attention.h"
 
 namespace spexis {

@@ -151,9 +151,9 @@ struct AttnParams {
 };
 
 // The 8-bit kernel's shares count every (sequence, KV head) as so many tiles more: its Q, its outputs or partials and the
-// waits around them.  Against shares of as many tiles: 512 sequences of 512 to 2048 keys, 63 rows a head, 173.0 us for
-// 178.3; 512 of 100 to 400 67.0 for 75.2; 64 of 20 to 200 keys, 20 rows, 18.3 for 23.2; 64 of 1024 to 4096 69.3 for
-// 70.7.  (2: 176.2, 70.2, 19.5, 69.7; 3: 174.2, 67.9, 18.5, 69.9; 5: 172.1, 66.1, 18.3, 70.2.)
+// waits around them.  Against shares of as many tiles: 512 sequences of 512 to 2048 keys, 63 rows a head, 173.3 us for
+// 178.9; 512 of 100 to 400 68.2 for 77.3; 64 of 20 to 200 keys, 20 rows, 20.0 for 24.3; 64 of 1024 to 4096 70.9 for 72.9;
+// 128 of 100 to 1000 44.7 for 46.0.  (3: 172.9, 69.5, 19.8, 70.8, 44.2; 5: 172.6, 67.9, 20.3, 70.9, 45.1.)
 constexpr int kAttn8ItemCost = 4;
 
 // One partial slot: [rmax][D] unnormalised output, then rmax reference maxima and rmax sums.

@@ -5,7 +5,8 @@
 //   (both terms of H are at least 0, as is ln Z: no cancellation)
 // Bound by reading the logits once: 4608 rows of 152064 fp32 with 5 alternatives 413 us, 6.8 TB/s, what a large read
 // reaches.  221 rows of 128256 (64 sequences' emitted tokens) with 20 alternatives 34 us, 3.3 TB/s: four rounds of loads a
-// workgroup, of which the first has to find a threshold and to sort (with none 24 us), and 4.7 us of merge.
+// workgroup, of which the first has to find a threshold and to sort (with none 24 us), and 4.8 us of merge.  bf16 rows are
+// bound by instructions, as many a logit on half the bytes: 266 us, 5.3 TB/s, and 31 us.
 //
 // Work split.  A workgroup takes one part of one item's row, its four waves every fourth chunk of 2048 logits (in
 // registers, the next one in flight).  Every lane keeps a running maximum, Z and U of its own: no exchange
