@@ -15,7 +15,7 @@
 // a wave lives 302 thousand cycles, 3600 for each of its 84 tiles, at about 2.1 GHz: 352 vector instructions a tile (32
 // exponentials, 64 conversions of codes and 16 of weights among them) and 32 matrix products, which are busy for 28% of the
 // time; for 57% of it an instruction issues, for 28% the wave waits for loads, for 15% for earlier results.  One sequence of
-// 16384 keys: 13 to 15 us for 32 MB, a chain of share search, block ids, codes and products, whose partials (10.6 MB) are
+// 16384 keys: 13 to 15 us for 32 MB, a chain of share search, block ids, codes and products, whose partials (7.1 MB) are
 // written and read again, and 6.9 us of merge.
 // One wave a SIMD holds everything in registers; two (half the registers each, twice the shares and partials) took 78
 // and 197 us a call where one took 71 and 180.  Three tiles in flight took 72 us instead of 71 (one row tile; two have no
