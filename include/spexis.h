@@ -168,7 +168,7 @@ int spexis_append_kv(void* k_cache, void* v_cache, int32_t num_blocks, int32_t n
  * sequence, prompts included; a sequence's blocks that receive rows must be its own.
  * Supported: rotary_dim a multiple of 16, 16 .. head_dim; head_dim in {64, 128}, block_size in {16, 32};
  * max_blocks_per_seq * block_size < 2^31, and tokens for one launch: (total_tokens / block_size + 2 num_seqs) * Hkv *
- * head_dim * block_size / 16 + 128 total_tokens up to about 2^31.
+ * head_dim * block_size / 16 + 80 total_tokens up to about 2^31.
  * Errors: INVALID_ARGUMENT, UNSUPPORTED, HIP.
  */
 int spexis_rotate_append_kv(void* k_cache, void* v_cache, int32_t num_blocks, int32_t num_kv_heads,

@@ -141,9 +141,10 @@ int rotate_append(const char* name, const spexis::RotateParams& p, void* stream)
   }
   if ((p.q || p.q_out) && p.hq <= 0) return fail(SPEXIS_ERR_INVALID_ARGUMENT, "%s: non-positive size", name);
   // a launch holds fewer than 2^32 threads: at most head_dim * block_size / 16 for a (block, KV head), 64 for a query
-  // token, of which there may be twice as many as tokens; alternating the two at most doubles their number (and rounds up)
+  // token, of which there may be a quarter more than tokens (twice as many where that is far from the limit); alternating
+  // the two at most doubles their number and rounds up
   const int64_t blocks = (int64_t)p.total_tokens / p.block_size + 2 * (int64_t)p.num_seqs;
-  if (2.0 * ((double)blocks * p.hkv * p.head_dim * p.block_size / 16 + 128.0 * p.total_tokens + 1536) >= 4294967296.0 ||
+  if (2.0 * ((double)blocks * p.hkv * p.head_dim * p.block_size / 16 + 80.0 * p.total_tokens + 1536) >= 4294967296.0 ||
       (int64_t)p.max_blocks * p.block_size >= (1ll << 31))
     return fail(SPEXIS_ERR_UNSUPPORTED, "%s: too many tokens or slots", name);
   if (p.num_seqs == 0 || p.total_tokens == 0) return ok();

@@ -491,7 +491,8 @@ hipError_t launch_rotate_append(RotateParams p, hipStream_t s) {
   const int64_t blocks = B * ((n + bs - 2) / bs + 1), all = T / bs + 2 * B;
   p.seq_blocks = blocks <= all ? (int)((n + bs - 2) / bs + 1) : 0;
   p.append_groups = (int)((blocks <= all ? blocks : all) * p.hkv);
-  p.seq_tokens = (n <= 64 ? 5 : 8) * B * n <= 10 * T ? (int)n : 0;
+  const bool step = n <= 64 && T <= 1 << 20 && (int64_t)p.append_groups * p.head_dim * bs / 16 <= 1 << 30;   // far from a launch's limit
+  p.seq_tokens = (step ? 5 : 8) * B * n <= 10 * T ? (int)n : 0;
   // q beyond 64 MB does not come from the caches: loads that leave the rest in them (prompts, 103 MB of q, 8 bits, the
   // call 45.9 us, plain loads 51.9); below that, it may (21 MB: 20.3, streamed 26.0)
   p.stream_q = T * p.hq * p.head_dim * 2 > (int64_t)1 << 26;

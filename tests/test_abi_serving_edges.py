@@ -138,3 +138,12 @@ def test_a_step_whose_rotation_table_is_shorter_than_its_sequences():
     VerifyStep(batch, attn, None, device="cpu", rotary=wl.make_rotary_inputs(most, 32))
     with pytest.raises(ValueError, match=str(most)):
         VerifyStep(batch, attn, None, device="cpu", rotary=wl.make_rotary_inputs(most - 1, 32))
+
+
+@marked
+@pytest.mark.parametrize("in8", [False, True])
+def test_a_launch_as_large_as_may_be(in8):
+    """25 million tokens in one call are a launch (refused here only for want of a GPU); 27 million are not."""
+    big = dict(hkv=1, d=64, bs=16, mb=2**21, mq=2**21, B=12)
+    assert rotate(in8, T=25_000_000, **big) not in (INVALID, sx.SPEXIS_ERR_UNSUPPORTED)
+    assert rotate(in8, T=27_000_000, **big) == sx.SPEXIS_ERR_UNSUPPORTED
