@@ -274,6 +274,8 @@ size_t spexis_verify_attention_kv8_workspace_size(int32_t num_seqs, int32_t num_
  *           entries, 16-byte aligned like the pools, q, out and workspace
  *   workspace >= spexis_verify_attention_kv8_workspace_size(...) bytes
  * A NaN code of a key that a query token sees makes its output NaN; slots behind the sequence may hold anything.
+ * Scores and the sums of weights times v, the weights up to 2^8 each until they are normalised, are fp32 and have to
+ * stay in its range (so has spexis_verify_attention's).
  * Other arguments, supported shapes and errors as spexis_verify_attention, every sequence counting four tiles more.
  */
 int spexis_verify_attention_kv8(const void* k_cache, const void* v_cache, const float* scales,
