@@ -13,6 +13,10 @@
  *   spexis_rotate_append_kv8  the same into a cache held in 8 bits with a scale per block and head
  *   spexis_verify_attention  causal grouped-query attention of those rows over the cache
  *   spexis_verify_attention_kv8  the same over the 8-bit cache
+ *   spexis_prompt_attention  causal attention of whole prompts (also _kv8)
+ *   spexis_shared_attention  attention of a batch that shares prefixes, each read once (also _kv8)
+ *   spexis_attention_weights the softmax weight of every cached key, summed up for evictions
+ *   spexis_evict_kv          drop the cached keys of least weight, move the others together
  *   spexis_accept            ratio tests, residual / bonus sampling, outputs
  *   spexis_lm_head           logits = h W^T with fused softmax statistics (next to accept)
  *   spexis_lm_head_gather    the same, also gathering each row's logit at a given column
@@ -287,6 +291,143 @@ int spexis_verify_attention_kv8(const void* k_cache, const void* v_cache, const 
                                 int32_t num_q_heads, float scale, void* out,
                                 int32_t kv_chunk_tokens, void* workspace, size_t workspace_bytes,
                                 void* stream);
+
+/*
+ * Bytes of workspace spexis_prompt_attention and spexis_prompt_attention_kv8 need (> 0 whenever the sizes are valid, else
+ * 0): 16 where rows fill the chip without cutting their keys, at most about 120 MB (head_dim 128) where they do not.
+ */
+size_t spexis_prompt_attention_workspace_size(int32_t num_seqs, int32_t num_q_heads, int32_t num_kv_heads,
+                                              int32_t head_dim, int32_t total_tokens, int32_t max_query_len,
+                                              int32_t max_seq_len);
+
+/*
+ * spexis_prompt_attention -- causal attention of any number of query tokens a sequence: of the prompts whose rows an append
+ * has written (spexis_verify_attention takes up to 64 rows a KV head), packed without padding, behind cached tokens or
+ * not.  The function is spexis_verify_attention's:
+ *   out[qsl[b]+j][h][:] = sum_{t <= L_b + j} softmax_t(scale * <q[qsl[b]+j][h], k[b,t,g]>) * v[b,t,g][:],  g = h / G
+ * bf16 inputs, fp32 scores, sums and accumulation; the softmax weights, up to 2^8 each until they are normalised, are
+ * rounded to bf16 in front of the product with V; bf16 output.
+ *   q, out  [total_tokens][Hq][head_dim] bf16 (read; written; they must not overlap).  In a padded batch, total_tokens > qsl[B],
+ *           the rows from qsl[B] on are left as they were
+ *   lse     [total_tokens][Hq] fp32 (written) or NULL: ln sum_{t <= L_b + j} exp(scale * <q, k>)
+ * Sequences without query tokens are skipped.  What lies in the slots behind a sequence does not matter; a V that is not
+ * finite makes the outputs of the tokens that see its key, in its element, not finite, and no others.
+ * Pools, q, out and workspace 16-byte aligned.
+ * Supported: head_dim in {64, 128}, block_size in {16, 32}, any Hq / Hkv; total_tokens * Hq < 2^31,
+ * max_blocks_per_seq * block_size < 2^30.
+ * Errors: INVALID_ARGUMENT, UNSUPPORTED, WORKSPACE_TOO_SMALL, HIP.
+ */
+int spexis_prompt_attention(const void* k_cache, const void* v_cache, int32_t num_blocks,
+                            int32_t num_kv_heads, int32_t block_size, int32_t head_dim,
+                            int32_t num_seqs, const int32_t* query_start_loc,
+                            const int32_t* seq_lens, const int32_t* block_tables,
+                            int32_t max_blocks_per_seq, int32_t total_tokens, int32_t max_query_len,
+                            int32_t max_seq_len, const void* q, int32_t num_q_heads, float scale,
+                            void* out, float* lse, void* workspace, size_t workspace_bytes,
+                            void* stream);
+
+/* The same over the 8-bit cache (scales as in spexis_verify_attention_kv8). */
+int spexis_prompt_attention_kv8(const void* k_cache, const void* v_cache, const float* scales,
+                                int32_t num_blocks, int32_t num_kv_heads, int32_t block_size,
+                                int32_t head_dim, int32_t num_seqs, const int32_t* query_start_loc,
+                                const int32_t* seq_lens, const int32_t* block_tables,
+                                int32_t max_blocks_per_seq, int32_t total_tokens,
+                                int32_t max_query_len, int32_t max_seq_len, const void* q,
+                                int32_t num_q_heads, float scale, void* out, float* lse,
+                                void* workspace, size_t workspace_bytes, void* stream);
+
+/* Bytes of workspace spexis_shared_attention and spexis_shared_attention_kv8 need (> 0 whenever the sizes are valid, else 0). */
+size_t spexis_shared_attention_workspace_size(int32_t num_seqs, int32_t num_groups, int32_t num_q_heads,
+                                              int32_t num_kv_heads, int32_t head_dim, int32_t total_tokens,
+                                              int32_t max_query_len, int32_t max_seq_len);
+
+/*
+ * spexis_shared_attention -- spexis_prompt_attention of a batch in which groups of sequences begin with the same cached
+ * blocks (one instruction in front of every request; many answers to one problem): every group's prefix is read once, by the
+ * query rows of all its sequences together, each sequence's own keys by its rows, and the two are joined.  The outputs are
+ * spexis_prompt_attention's but for the order in which fp32 sums are taken.
+ *   group_start_loc  [num_groups+1] int32 ascending: group i is the sequences group_start_loc[i] .. group_start_loc[i+1]-1;
+ *                    sequences in front of the first group or behind the last share nothing
+ *   prefix_lens      [num_groups] int32: tokens that the group's sequences share, taken in whole blocks (what is behind the
+ *                    last multiple of block_size counts as each sequence's own), at most L_b of each of them (the new
+ *                    tokens are never shared); 0: nothing.  The prefix's blocks are those of the group's first sequence
+ *   num_groups       0: nothing is shared (the two arrays may be NULL)
+ * Any number of query tokens a sequence.  Other arguments, supported shapes and errors as spexis_prompt_attention.
+ */
+int spexis_shared_attention(const void* k_cache, const void* v_cache, int32_t num_blocks,
+                            int32_t num_kv_heads, int32_t block_size, int32_t head_dim,
+                            int32_t num_seqs, const int32_t* query_start_loc,
+                            const int32_t* seq_lens, const int32_t* block_tables,
+                            int32_t max_blocks_per_seq, int32_t total_tokens, int32_t max_query_len,
+                            int32_t max_seq_len, int32_t num_groups, const int32_t* group_start_loc,
+                            const int32_t* prefix_lens, const void* q, int32_t num_q_heads,
+                            float scale, void* out, float* lse, void* workspace,
+                            size_t workspace_bytes, void* stream);
+
+/* The same over the 8-bit cache (scales as in spexis_verify_attention_kv8). */
+int spexis_shared_attention_kv8(const void* k_cache, const void* v_cache, const float* scales,
+                                int32_t num_blocks, int32_t num_kv_heads, int32_t block_size,
+                                int32_t head_dim, int32_t num_seqs, const int32_t* query_start_loc,
+                                const int32_t* seq_lens, const int32_t* block_tables,
+                                int32_t max_blocks_per_seq, int32_t total_tokens,
+                                int32_t max_query_len, int32_t max_seq_len, int32_t num_groups,
+                                const int32_t* group_start_loc, const int32_t* prefix_lens,
+                                const void* q, int32_t num_q_heads, float scale, void* out,
+                                float* lse, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * spexis_attention_weights -- the softmax weight that every cached key gets from a call's query tokens, summed over them and
+ * over the query heads of its KV head: what tells, added up over steps, which keys an eviction may drop.
+ *   weights[blk][g][slot] = (t < L_b ? weights_in[blk][g][slot] : 0)
+ *                           + sum over j < n_b, L_b + j >= t, and the G heads h of g of exp(scale * <q[qsl[b]+j][h], k[b,t,g]>
+ *                             - lse[qsl[b]+j][h])
+ * for every key t < S_b (blk, slot: its place); fp32, the order of the sums is fixed.  A key's first call, which brings its
+ * own token, begins its sum, so arrays need no clearing when tokens are appended; other places are left as they were.
+ *   lse           [total_tokens][Hq] fp32 (read), as spexis_prompt_attention and spexis_shared_attention write it for the
+ *                 same q, keys and scale
+ *   accepted_len  [num_seqs] int32 or NULL: only the first accepted_len[b] + 1 tokens of a sequence count (clamped to
+ *                 [0, n_b]), and S_b is its length with them: spexis_accept's accepted_len and seq_lens_inout after it
+ *   weights_in    [num_blocks][Hkv][block_size] fp32 (read), which may be `weights`, or NULL: all sums begin here
+ *   weights       the same shape (written)
+ *   max_seq_len   host: >= max_b S_b (keys from it on are left out)
+ * A block that several sequences share gets the sums of one of them.
+ * Supported shapes as spexis_prompt_attention; num_seqs * Hkv * ceil(max_seq_len / 128) < 2^24.  k_cache, q, weights and
+ * weights_in 16-byte aligned.
+ * Errors: INVALID_ARGUMENT, UNSUPPORTED, HIP.
+ */
+int spexis_attention_weights(const void* k_cache, int32_t num_blocks, int32_t num_kv_heads, int32_t block_size,
+                             int32_t head_dim, int32_t num_seqs, const int32_t* query_start_loc,
+                             const int32_t* seq_lens, const int32_t* block_tables, int32_t max_blocks_per_seq,
+                             int32_t total_tokens, int32_t max_query_len, int32_t max_seq_len, const void* q,
+                             int32_t num_q_heads, float scale, const float* lse, const int32_t* accepted_len,
+                             const float* weights_in, float* weights, void* stream);
+
+/* Bytes of workspace spexis_evict_kv needs (> 0 whenever the sizes are valid, else 0). */
+size_t spexis_evict_kv_workspace_size(int32_t num_seqs, int32_t num_kv_heads, int32_t max_seq_len);
+
+/*
+ * spexis_evict_kv -- drops the keys of least accumulated weight from a bf16 cache, for every sequence and KV head apart.
+ * With m = min(keep_lens[b], S_b), f = min(first_keys[b], m) and l = min(keep_last, m - f), the first f and the last l
+ * keys stay, and of those between the m - f - l of largest weight (of equal ones the earlier; a NaN counts as less than any
+ * number); they move together, in their order, to the places of tokens 0 .. m-1, their weights with them, and
+ * new_seq_lens[b] = m.  Every head keeps as many keys, each its own.  Keys were rotated by the positions that they had, so
+ * attention over what is left is what it was without the dropped keys; later tokens are appended at place m and rotated by
+ * positions that the caller counts (spexis_rotate_append_kv's `positions`).  Places from m on hold anything.
+ *   weights       [num_blocks][Hkv][block_size] fp32 (read)
+ *   weights_out   the same shape (written at the places below m); may be `weights`
+ *   keep_lens     [num_seqs] int32 (negative: 0);  first_keys [num_seqs] int32 or NULL (0): keys at the front that stay, at
+ *                 least those of blocks that other sequences share;  keep_last host, >= 0
+ *   seq_lens      [num_seqs] int32 (read);  new_seq_lens [num_seqs] int32 (written); may be seq_lens
+ *   max_seq_len   host: >= max_b S_b (keys from it on are dropped)
+ * The blocks of a sequence from the first key that moves on must be its own.  Pools, weights and workspace 16-byte aligned.
+ * Supported: head_dim in {64, 128}, block_size in {16, 32}; num_seqs * Hkv < 2^21.
+ * Errors: INVALID_ARGUMENT, UNSUPPORTED, WORKSPACE_TOO_SMALL, HIP.
+ */
+int spexis_evict_kv(void* k_cache, void* v_cache, const float* weights, int32_t num_blocks, int32_t num_kv_heads,
+                    int32_t block_size, int32_t head_dim, int32_t num_seqs, const int32_t* seq_lens,
+                    const int32_t* block_tables, int32_t max_blocks_per_seq, int32_t max_seq_len,
+                    const int32_t* keep_lens, const int32_t* first_keys, int32_t keep_last, float* weights_out,
+                    int32_t* new_seq_lens, void* workspace, size_t workspace_bytes, void* stream);
 
 /*
  * spexis_softmax_rows -- the probabilities p = softmax(logits / T) and q that the acceptance

@@ -231,6 +231,136 @@ int verify_attention(const char* name, bool in8, const void* k_cache, const void
   return hip_result(in8 ? spexis::launch_attention8(p, (hipStream_t)stream) : spexis::launch_attention(p, (hipStream_t)stream), name);
 }
 
+// ---- attention of many rows at once
+
+// The most row tiles a head of sequences whose tokens come to total_tokens: each may end with a tile that is not full.
+int64_t most_row_tiles(int64_t seqs, int64_t group, int64_t total_tokens, int64_t longest) {
+  const int64_t all = (total_tokens * group + seqs * (spexis::kTileRows - 1)) / spexis::kTileRows;
+  const int64_t each = (group * longest + spexis::kTileRows - 1) / spexis::kTileRows;
+  return std::min(all, seqs * each);
+}
+
+struct TileLayout {
+  int64_t units, prefix_units, groups_hdr, ws_prefix, ws_seq, total;   // offsets in bytes
+  int shares, pitch;
+  bool partial;
+};
+
+// Units, and where their partials lie.  Tiles are cut into parts where prefixes are shared (few tiles with many keys beside
+// many with few), and where one tile a workgroup would not fill the chip.
+TileLayout tile_layout(int64_t seqs, int64_t groups, int64_t hq, int64_t hkv, int64_t head_dim, int64_t total_tokens,
+                       int64_t max_query_len) {
+  TileLayout l{};
+  const int64_t group = hq / hkv;
+  const int64_t pre = groups > 0 ? most_row_tiles(groups, group, total_tokens, total_tokens) : 0;
+  const int64_t own = most_row_tiles(seqs, group, total_tokens, max_query_len);
+  l.partial = groups > 0 || own * hkv <= spexis::kTileSlots;
+  l.shares = l.partial ? (int)std::max<int64_t>(1, spexis::kTileSlots / hkv) : 0;
+  l.prefix_units = groups > 0 ? pre + l.shares : 0;
+  l.units = pre + own + l.shares;
+  l.pitch = (int)std::min<int64_t>(spexis::kTileRows, group * max_query_len);
+  int64_t off = 0;
+  auto take = [&](int64_t bytes) {
+    const int64_t at = off;
+    off += round_up(bytes, 256);
+    return at;
+  };
+  if (l.partial) {
+    take(l.units * spexis::kTileHdrInts * 4);
+    l.groups_hdr = take(groups * 16);
+    l.ws_prefix = take(l.prefix_units * hkv * spexis::tile_slot_floats(spexis::kTileRows, (int)head_dim) * 4);
+    l.ws_seq = take(l.units * hkv * spexis::tile_slot_floats(l.pitch, (int)head_dim) * 4);
+  }
+  l.total = std::max<int64_t>(off, 16);
+  return l;
+}
+
+size_t tile_workspace_size(int32_t num_seqs, int32_t num_groups, int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim,
+                           int32_t total_tokens, int32_t max_query_len, int32_t max_seq_len) {
+  if (num_seqs <= 0 || num_groups < 0 || num_kv_heads <= 0 || num_q_heads <= 0 || num_q_heads % num_kv_heads != 0 ||
+      head_dim <= 0 || total_tokens <= 0 || max_query_len <= 0 || max_seq_len <= 0 ||
+      (int64_t)total_tokens * num_q_heads >= (1ll << 31))
+    return 0;
+  return (size_t)tile_layout(num_seqs, num_groups, num_q_heads, num_kv_heads, head_dim, total_tokens, max_query_len).total;
+}
+
+// The four attention calls over many rows: their checks and the launch.  groups < 0: a call without shared prefixes.
+int tile_attention(const char* name, bool in8, const void* k_cache, const void* v_cache, const float* scales,
+                   int32_t num_blocks, int32_t num_kv_heads, int32_t block_size, int32_t head_dim, int32_t num_seqs,
+                   const int32_t* query_start_loc, const int32_t* seq_lens, const int32_t* block_tables,
+                   int32_t max_blocks_per_seq, int32_t total_tokens, int32_t max_query_len, int32_t max_seq_len,
+                   int32_t num_groups, const int32_t* group_start_loc, const int32_t* prefix_lens, const void* q,
+                   int32_t num_q_heads, float scale, void* out, float* lse, void* workspace, size_t workspace_bytes,
+                   void* stream) {
+  if (num_blocks <= 0 || num_kv_heads <= 0 || num_q_heads <= 0 || num_seqs < 0 || max_blocks_per_seq <= 0 ||
+      total_tokens < 0 || max_query_len <= 0 || max_seq_len <= 0 || num_groups < 0)
+    return fail(SPEXIS_ERR_INVALID_ARGUMENT, "%s: non-positive size", name);
+  if (num_q_heads % num_kv_heads != 0)
+    return fail(SPEXIS_ERR_INVALID_ARGUMENT, "%s: %d query heads not a multiple of %d KV heads", name, num_q_heads,
+                num_kv_heads);
+  if (!std::isfinite(scale)) return fail(SPEXIS_ERR_INVALID_ARGUMENT, "%s: scale not finite", name);
+  if (bad_cache_shape(block_size, head_dim))
+    return fail(SPEXIS_ERR_UNSUPPORTED, "%s: block_size %d / head_dim %d not in {16,32} x {64,128}", name, block_size,
+                head_dim);
+  if ((int64_t)max_blocks_per_seq * block_size < max_query_len)
+    return fail(SPEXIS_ERR_INVALID_ARGUMENT, "%s: block tables hold fewer slots than a query", name);
+  if ((int64_t)total_tokens * num_q_heads >= (1ll << 31) || (int64_t)max_blocks_per_seq * block_size >= (1ll << 30) ||
+      (int64_t)num_seqs + num_groups >= (1ll << 30))
+    return fail(SPEXIS_ERR_UNSUPPORTED, "%s: too many tokens or slots", name);
+  if (num_seqs == 0 || total_tokens == 0) return ok();
+  if (!k_cache || !v_cache || !query_start_loc || !seq_lens || !block_tables || !q || !out || (in8 && !scales) ||
+      (num_groups > 0 && (!group_start_loc || !prefix_lens)))
+    return fail(SPEXIS_ERR_INVALID_ARGUMENT, "%s: null pointer", name);
+  if (misaligned({k_cache, v_cache, scales, q, out, workspace}))
+    return fail(SPEXIS_ERR_INVALID_ARGUMENT, "%s: a pointer that is not 16-byte aligned", name);
+  if (q == out) return fail(SPEXIS_ERR_INVALID_ARGUMENT, "%s: out aliases q", name);
+  const TileLayout l = tile_layout(num_seqs, num_groups, num_q_heads, num_kv_heads, head_dim, total_tokens, max_query_len);
+  // a launch holds fewer than 2^32 threads
+  if (l.units * num_kv_heads * 256 >= (1ll << 32)) return fail(SPEXIS_ERR_UNSUPPORTED, "%s: too many tokens or slots", name);
+  if (!workspace || workspace_bytes < (size_t)l.total)
+    return fail(SPEXIS_ERR_WORKSPACE_TOO_SMALL, "%s: workspace %zu bytes < %zu needed", name, workspace_bytes,
+                (size_t)l.total);
+  spexis::TileAttnParams p{};
+  p.k_cache = k_cache;
+  p.v_cache = v_cache;
+  p.scales = scales;
+  p.qsl = query_start_loc;
+  p.seq_lens = seq_lens;
+  p.block_tables = block_tables;
+  p.group_start = group_start_loc;
+  p.prefix_lens = prefix_lens;
+  p.q = q;
+  p.out = out;
+  p.lse = lse;
+  uint8_t* ws = static_cast<uint8_t*>(workspace);
+  p.units_hdr = reinterpret_cast<int32_t*>(ws);
+  p.groups_hdr = reinterpret_cast<int32_t*>(ws + l.groups_hdr);
+  p.ws_prefix = reinterpret_cast<float*>(ws + l.ws_prefix);
+  p.ws_seq = reinterpret_cast<float*>(ws + l.ws_seq);
+  p.num_blocks = num_blocks;
+  p.hkv = num_kv_heads;
+  p.block_size = block_size;
+  p.head_dim = head_dim;
+  p.num_seqs = num_seqs;
+  p.num_groups = num_groups;
+  p.max_blocks = max_blocks_per_seq;
+  p.total_tokens = total_tokens;
+  p.max_query_len = max_query_len;
+  p.hq = num_q_heads;
+  p.group = num_q_heads / num_kv_heads;
+  p.pitch = l.pitch;
+  p.shares = l.shares;
+  p.units = (int)l.units;
+  p.prefix_units = (int)l.prefix_units;
+  p.partial = l.partial ? 1 : 0;
+  // the kernel takes maxima of scores before their scale, which is positive there: a negative one turns q's signs over, and
+  // 0 counts as the least that a masked score (minus infinity) can be multiplied with
+  p.q_sign = scale < 0.f ? 0x80008000u : 0u;
+  p.scale_log2e = (float)std::max(std::fabs((double)scale) * 1.4426950408889634, 1e-37);
+  p.lazy = (float)(8.0 / (double)p.scale_log2e);
+  return hip_result(spexis::launch_tile_attention(p, (hipStream_t)stream), name);
+}
+
 }  // namespace
 
 extern "C" {
@@ -337,6 +467,150 @@ int spexis_verify_attention_kv8(const void* k_cache, const void* v_cache, const 
   return verify_attention("spexis_verify_attention_kv8", true, k_cache, v_cache, scales, num_blocks, num_kv_heads, block_size, head_dim, num_seqs,
                           query_start_loc, seq_lens, block_tables, max_blocks_per_seq, total_tokens, max_query_len,
                           max_seq_len, q, num_q_heads, scale, out, kv_chunk_tokens, workspace, workspace_bytes, stream);
+}
+
+size_t spexis_prompt_attention_workspace_size(int32_t num_seqs, int32_t num_q_heads, int32_t num_kv_heads,
+                                              int32_t head_dim, int32_t total_tokens, int32_t max_query_len,
+                                              int32_t max_seq_len) {
+  return tile_workspace_size(num_seqs, 0, num_q_heads, num_kv_heads, head_dim, total_tokens, max_query_len,
+                             max_seq_len);
+}
+
+int spexis_prompt_attention(const void* k_cache, const void* v_cache, int32_t num_blocks,
+                            int32_t num_kv_heads, int32_t block_size, int32_t head_dim,
+                            int32_t num_seqs, const int32_t* query_start_loc,
+                            const int32_t* seq_lens, const int32_t* block_tables,
+                            int32_t max_blocks_per_seq, int32_t total_tokens, int32_t max_query_len,
+                            int32_t max_seq_len, const void* q, int32_t num_q_heads, float scale,
+                            void* out, float* lse, void* workspace, size_t workspace_bytes,
+                            void* stream) {
+  return tile_attention("spexis_prompt_attention", false, k_cache, v_cache, nullptr, num_blocks, num_kv_heads, block_size,
+                        head_dim, num_seqs, query_start_loc, seq_lens, block_tables, max_blocks_per_seq, total_tokens,
+                        max_query_len, max_seq_len, 0, nullptr, nullptr, q, num_q_heads, scale, out, lse,
+                        workspace, workspace_bytes, stream);
+}
+
+int spexis_prompt_attention_kv8(const void* k_cache, const void* v_cache, const float* scales,
+                                int32_t num_blocks, int32_t num_kv_heads, int32_t block_size,
+                                int32_t head_dim, int32_t num_seqs, const int32_t* query_start_loc,
+                                const int32_t* seq_lens, const int32_t* block_tables,
+                                int32_t max_blocks_per_seq, int32_t total_tokens,
+                                int32_t max_query_len, int32_t max_seq_len, const void* q,
+                                int32_t num_q_heads, float scale, void* out, float* lse,
+                                void* workspace, size_t workspace_bytes, void* stream) {
+  return tile_attention("spexis_prompt_attention_kv8", true, k_cache, v_cache, scales, num_blocks, num_kv_heads, block_size,
+                        head_dim, num_seqs, query_start_loc, seq_lens, block_tables, max_blocks_per_seq, total_tokens,
+                        max_query_len, max_seq_len, 0, nullptr, nullptr, q, num_q_heads, scale, out, lse,
+                        workspace, workspace_bytes, stream);
+}
+
+size_t spexis_shared_attention_workspace_size(int32_t num_seqs, int32_t num_groups, int32_t num_q_heads, int32_t num_kv_heads,
+                                              int32_t head_dim, int32_t total_tokens, int32_t max_query_len,
+                                              int32_t max_seq_len) {
+  if (num_groups < 0) return 0;
+  return tile_workspace_size(num_seqs, num_groups, num_q_heads, num_kv_heads, head_dim, total_tokens, max_query_len,
+                             max_seq_len);
+}
+
+int spexis_shared_attention(const void* k_cache, const void* v_cache, int32_t num_blocks,
+                            int32_t num_kv_heads, int32_t block_size, int32_t head_dim,
+                            int32_t num_seqs, const int32_t* query_start_loc,
+                            const int32_t* seq_lens, const int32_t* block_tables,
+                            int32_t max_blocks_per_seq, int32_t total_tokens, int32_t max_query_len,
+                            int32_t max_seq_len, int32_t num_groups, const int32_t* group_start_loc,
+                            const int32_t* prefix_lens, const void* q, int32_t num_q_heads,
+                            float scale, void* out, float* lse, void* workspace,
+                            size_t workspace_bytes, void* stream) {
+  return tile_attention("spexis_shared_attention", false, k_cache, v_cache, nullptr, num_blocks, num_kv_heads, block_size,
+                        head_dim, num_seqs, query_start_loc, seq_lens, block_tables, max_blocks_per_seq, total_tokens,
+                        max_query_len, max_seq_len, num_groups, group_start_loc, prefix_lens, q, num_q_heads, scale, out, lse,
+                        workspace, workspace_bytes, stream);
+}
+
+int spexis_shared_attention_kv8(const void* k_cache, const void* v_cache, const float* scales,
+                                int32_t num_blocks, int32_t num_kv_heads, int32_t block_size,
+                                int32_t head_dim, int32_t num_seqs, const int32_t* query_start_loc,
+                                const int32_t* seq_lens, const int32_t* block_tables,
+                                int32_t max_blocks_per_seq, int32_t total_tokens,
+                                int32_t max_query_len, int32_t max_seq_len, int32_t num_groups,
+                                const int32_t* group_start_loc, const int32_t* prefix_lens,
+                                const void* q, int32_t num_q_heads, float scale, void* out,
+                                float* lse, void* workspace, size_t workspace_bytes, void* stream) {
+  return tile_attention("spexis_shared_attention_kv8", true, k_cache, v_cache, scales, num_blocks, num_kv_heads, block_size,
+                        head_dim, num_seqs, query_start_loc, seq_lens, block_tables, max_blocks_per_seq, total_tokens,
+                        max_query_len, max_seq_len, num_groups, group_start_loc, prefix_lens, q, num_q_heads, scale, out, lse,
+                        workspace, workspace_bytes, stream);
+}
+
+int spexis_attention_weights(const void* k_cache, int32_t num_blocks, int32_t num_kv_heads, int32_t block_size,
+                             int32_t head_dim, int32_t num_seqs, const int32_t* query_start_loc, const int32_t* seq_lens,
+                             const int32_t* block_tables, int32_t max_blocks_per_seq, int32_t total_tokens,
+                             int32_t max_query_len, int32_t max_seq_len, const void* q, int32_t num_q_heads, float scale,
+                             const float* lse, const int32_t* accepted_len, const float* weights_in, float* weights,
+                             void* stream) {
+  const char* name = "spexis_attention_weights";
+  if (num_blocks <= 0 || num_kv_heads <= 0 || num_q_heads <= 0 || num_seqs < 0 || max_blocks_per_seq <= 0 ||
+      total_tokens < 0 || max_query_len <= 0 || max_seq_len <= 0)
+    return fail(SPEXIS_ERR_INVALID_ARGUMENT, "%s: non-positive size", name);
+  if (num_q_heads % num_kv_heads != 0)
+    return fail(SPEXIS_ERR_INVALID_ARGUMENT, "%s: %d query heads not a multiple of %d KV heads", name, num_q_heads,
+                num_kv_heads);
+  if (!std::isfinite(scale)) return fail(SPEXIS_ERR_INVALID_ARGUMENT, "%s: scale not finite", name);
+  if (bad_cache_shape(block_size, head_dim))
+    return fail(SPEXIS_ERR_UNSUPPORTED, "%s: block_size %d / head_dim %d not in {16,32} x {64,128}", name, block_size,
+                head_dim);
+  if ((int64_t)max_blocks_per_seq * block_size < max_query_len)
+    return fail(SPEXIS_ERR_INVALID_ARGUMENT, "%s: block tables hold fewer slots than a query", name);
+  // a launch holds fewer than 2^32 threads: 256 for 128 keys of a (sequence, KV head)
+  if ((int64_t)total_tokens * num_q_heads >= (1ll << 31) || (int64_t)max_blocks_per_seq * block_size >= (1ll << 30) ||
+      (double)num_seqs * num_kv_heads * (((int64_t)max_seq_len + 127) / 128) * 256.0 >= 4294967296.0)
+    return fail(SPEXIS_ERR_UNSUPPORTED, "%s: too many tokens or slots", name);
+  if (num_seqs == 0 || total_tokens == 0) return ok();
+  if (!k_cache || !query_start_loc || !seq_lens || !block_tables || !q || !lse || !weights)
+    return fail(SPEXIS_ERR_INVALID_ARGUMENT, "%s: null pointer", name);
+  if (misaligned({k_cache, q, weights, weights_in}))
+    return fail(SPEXIS_ERR_INVALID_ARGUMENT, "%s: a pointer that is not 16-byte aligned", name);
+  spexis::WeightParams p{k_cache, query_start_loc, seq_lens, block_tables, q, lse, accepted_len, weights_in, weights,
+                         num_blocks, num_kv_heads, block_size, head_dim, num_seqs, max_blocks_per_seq, total_tokens,
+                         max_query_len, max_seq_len, num_q_heads, num_q_heads / num_kv_heads,
+                         (float)((double)scale * 1.4426950408889634)};
+  return hip_result(spexis::launch_weights(p, (hipStream_t)stream), name);
+}
+
+size_t spexis_evict_kv_workspace_size(int32_t num_seqs, int32_t num_kv_heads, int32_t max_seq_len) {
+  if (num_seqs <= 0 || num_kv_heads <= 0 || max_seq_len <= 0) return 0;
+  const int64_t items = (int64_t)num_seqs * num_kv_heads;
+  return (size_t)(round_up(items * 8, 256) + round_up(items * max_seq_len * 4, 256));
+}
+
+int spexis_evict_kv(void* k_cache, void* v_cache, const float* weights, int32_t num_blocks, int32_t num_kv_heads,
+                    int32_t block_size, int32_t head_dim, int32_t num_seqs, const int32_t* seq_lens,
+                    const int32_t* block_tables, int32_t max_blocks_per_seq, int32_t max_seq_len, const int32_t* keep_lens,
+                    const int32_t* first_keys, int32_t keep_last, float* weights_out, int32_t* new_seq_lens, void* workspace,
+                    size_t workspace_bytes, void* stream) {
+  const char* name = "spexis_evict_kv";
+  if (num_blocks <= 0 || num_kv_heads <= 0 || num_seqs < 0 || max_blocks_per_seq <= 0 || max_seq_len <= 0 || keep_last < 0)
+    return fail(SPEXIS_ERR_INVALID_ARGUMENT, "%s: non-positive size", name);
+  if (bad_cache_shape(block_size, head_dim))
+    return fail(SPEXIS_ERR_UNSUPPORTED, "%s: block_size %d / head_dim %d not in {16,32} x {64,128}", name, block_size,
+                head_dim);
+  // a launch holds fewer than 2^32 threads: at most 2048 for a (sequence, KV head)
+  if ((int64_t)num_seqs * num_kv_heads >= (1ll << 21) || (int64_t)max_blocks_per_seq * block_size >= (1ll << 30) ||
+      max_seq_len >= (1 << 30))
+    return fail(SPEXIS_ERR_UNSUPPORTED, "%s: too many sequences or slots", name);
+  if (num_seqs == 0) return ok();
+  if (!k_cache || !v_cache || !weights || !seq_lens || !block_tables || !keep_lens || !weights_out || !new_seq_lens)
+    return fail(SPEXIS_ERR_INVALID_ARGUMENT, "%s: null pointer", name);
+  if (misaligned({k_cache, v_cache, weights, weights_out, workspace}))
+    return fail(SPEXIS_ERR_INVALID_ARGUMENT, "%s: a pointer that is not 16-byte aligned", name);
+  const size_t need = spexis_evict_kv_workspace_size(num_seqs, num_kv_heads, max_seq_len);
+  if (!workspace || workspace_bytes < need)
+    return fail(SPEXIS_ERR_WORKSPACE_TOO_SMALL, "%s: workspace %zu bytes < %zu needed", name, workspace_bytes, need);
+  int32_t* ws = static_cast<int32_t*>(workspace);
+  spexis::EvictParams p{k_cache, v_cache, weights, weights_out, seq_lens, block_tables, keep_lens, first_keys, new_seq_lens, ws,
+                        ws + round_up((int64_t)num_seqs * num_kv_heads * 8, 256) / 4, num_blocks, num_kv_heads, block_size,
+                        head_dim, num_seqs, max_blocks_per_seq, max_seq_len, keep_last};
+  return hip_result(spexis::launch_evict(p, (hipStream_t)stream), name);
 }
 
 int spexis_softmax_rows(const float* logits, float* probs, int64_t rows, int32_t vocab, float temperature,

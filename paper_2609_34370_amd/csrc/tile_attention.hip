@@ -1,0 +1,548 @@
+// Attention of many query rows at once over the paged cache: whole prompts (any number of new tokens a sequence), and
+// batches whose sequences begin with a prefix that they share.
+//
+// Work decomposition.  A segment is a run of query tokens against a run of keys: a sequence against the keys that are its
+// own, causally; and, where a group of sequences shares a prefix, all tokens of the group against that prefix, once.  With
+// G query heads a KV head, a segment has G rows a token, in tiles of 128: row r is (token r / G, head r % G), so every row
+// of a tile reads the same K and V.  A unit, one workgroup, is a tile against the keys that any of its rows sees, or, where
+// there are too few tiles to fill the chip, against one of several equal parts of them.  A unit that is the whole of its
+// rows writes outputs; the others leave fp32 partials (reference maximum, sum, unnormalised output) in the workspace,
+// which tile_merge_kernel joins.
+//
+// Each of the four waves owns 32 rows.  The 64 keys of a step pass through LDS, where all waves read them: fetched into
+// registers one step ahead, widened there from the 8-bit cache, and stored in the order in which a wave reads matrix
+// operands, 1 KB a fragment, so that no two lanes meet in a bank.  With v_mfma_f32_32x32x16_bf16 (operand A: lane l holds
+// row l%32, k-slice 8*(l/32)..+7; B: column l%32, same k-slice; C: lane l, value i holds row 8*(i/4) + 4*(l/32) + i%4,
+// column l%32):
+//   S^T[key][row] = K Q^T: lane l owns query row l%32, so a row's maximum is one over 32 values and one lane exchange;
+//   O^T[d][row] += V^T P^T: the V layouts hold slots in the order in which the score tile leaves them, so P^T is the
+//   lane's own values.
+#include "attention.h"
+
+namespace spexis {
+
+namespace {
+
+constexpr int kRows = kTileRows, kKeys = kTileKeys;
+
+// Eight e4m3 codes times a power of two, as a matrix operand.
+__device__ __forceinline__ u32x4 widen_codes(uint32_t lo, uint32_t hi, float scale) {
+  const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true);
+  const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true);
+  return u32x4{__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b), __builtin_bit_cast(uint32_t, c),
+               __builtin_bit_cast(uint32_t, d)};
+}
+
+// Keys that sequence b shares with its group (a multiple of the block size), and the group.
+__device__ __forceinline__ int prefix_of(const TileAttnParams& p, int b, int* group) {
+  *group = -1;
+  if (p.num_groups == 0) return 0;
+  int lo = 0, hi = p.num_groups;   // the last group that starts at or before b
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (p.group_start[mid] <= b) lo = mid;
+    else hi = mid;
+  }
+  if (p.group_start[lo] > b || p.group_start[lo + 1] <= b) return 0;
+  *group = lo;
+  return clampi(p.prefix_lens[lo], 0, p.max_blocks * p.block_size) & ~(p.block_size - 1);
+}
+
+// Segment s: the groups' prefixes, then the sequences.  Clamped so that every address derived from it stays in its buffer.
+struct Segment {
+  int q0, rows;      // first query token, query rows a KV head
+  int seq;           // the row of the block tables
+  int base, end;     // keys [base, end)
+  int last;          // token j sees the keys up to last + j (a prefix: all of them)
+  int group;         // of a sequence with a shared prefix: its group, else -1
+};
+
+__device__ __forceinline__ Segment segment(const TileAttnParams& p, int s) {
+  Segment g;
+  if (s < p.num_groups) {
+    const int b0 = clampi(p.group_start[s], 0, p.num_seqs), b1 = clampi(p.group_start[s + 1], b0, p.num_seqs);
+    g.q0 = clampi(p.qsl[b0], 0, p.total_tokens);
+    const int n = clampi(p.qsl[b1], g.q0, p.total_tokens) - g.q0;
+    g.seq = min(b0, p.num_seqs - 1);
+    g.base = 0;
+    g.end = clampi(p.prefix_lens[s], 0, p.max_blocks * p.block_size) & ~(p.block_size - 1);
+    g.rows = g.end > 0 ? n * p.group : 0;
+    g.last = INT32_MAX / 2;
+    g.group = -1;
+    return g;
+  }
+  const int b = s - p.num_groups;
+  g.q0 = clampi(p.qsl[b], 0, p.total_tokens);
+  const int n = min(clampi(p.qsl[b + 1], g.q0, p.total_tokens) - g.q0, p.max_query_len);
+  g.rows = n * p.group;
+  g.seq = b;
+  g.end = clampi(p.seq_lens[b], max(n, 1), p.max_blocks * p.block_size);
+  g.last = g.end - n;
+  g.base = min(prefix_of(p, b, &g.group), g.last & ~(p.block_size - 1));
+  if (g.base == 0) g.group = -1;
+  return g;
+}
+
+__device__ __forceinline__ int row_tiles(const Segment& g) { return (g.rows + kRows - 1) / kRows; }
+__device__ __forceinline__ int key_tiles(const Segment& g) { return (g.end - g.base + kKeys - 1) / kKeys; }
+// The keys of a segment's row tile end in front of this one.
+__device__ __forceinline__ int tile_end(const TileAttnParams& p, const Segment& g, int tile) {
+  const int r = min(g.rows, (tile + 1) * kRows) - 1;
+  return min((int64_t)g.end, (int64_t)g.last + r / p.group + 1);
+}
+
+struct Unit {
+  int seg, tile, part, parts, first;   // part of `parts` equal ones of the tile's keys; `first`: the unit of part 0
+};
+
+// The unit u of a head (false: there are fewer).  All threads of the workgroup call it; they look at 256 segments at a
+// time.  Where units are parts of tiles, a part is about `share` key tiles: sum(ceil(nt / share)) units.
+__device__ __forceinline__ bool find_unit(const TileAttnParams& p, int u, Unit& o) {
+  __shared__ int64_t sm_total[4];
+  __shared__ int sm_scan[4], sm_unit[5];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int ns = p.num_groups + p.num_seqs;
+  int tiles = 0, nt = 0;
+  auto load = [&](int base) {
+    const int s = base + tid;
+    tiles = nt = 0;
+    if (s < ns) {
+      const Segment g = segment(p, s);
+      tiles = row_tiles(g);
+      nt = key_tiles(g);
+    }
+  };
+  int share = INT32_MAX;
+  if (p.shares > 0) {
+    int64_t sum = 0;   // key tiles of all row tiles; row tiles
+    int rows = 0;
+    for (int base = 0; base < ns; base += 256) {
+      load(base);
+      sum += (int64_t)tiles * nt;
+      rows += tiles;
+    }
+    sum = (int64_t)wave_sum_u64((uint64_t)sum);
+    rows = wave_sum_i32(rows);
+    if (lane == 0) {
+      sm_total[wave] = sum;
+      sm_scan[wave] = rows;
+    }
+    __syncthreads();
+    sum = sm_total[0] + sm_total[1] + sm_total[2] + sm_total[3];
+    rows = sm_scan[0] + sm_scan[1] + sm_scan[2] + sm_scan[3];
+    const int64_t goal = tile_attn_parts(p.shares, rows);
+    share = (int)min((int64_t)INT32_MAX, max((sum + goal - 1) / goal, (int64_t)kTileLeast));
+    __syncthreads();
+  }
+  int before = 0;
+  if (tid == 0) sm_unit[0] = -1;
+  __syncthreads();
+  for (int base = 0; base < ns; base += 256) {
+    if (p.shares == 0 || ns > 256) load(base);
+    const int parts = (int)min((int64_t)1 << 20, ((int64_t)nt + share - 1) / share), mine = tiles * max(parts, 1);
+    const int incl = wave_incl_scan_i32(mine, lane);
+    if (lane == 63) sm_scan[wave] = incl;
+    __syncthreads();
+    int at = before + incl - mine, all = 0;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      if (w < wave) at += sm_scan[w];
+      all += sm_scan[w];
+    }
+    if (u >= at && u < at + mine) {
+      const int n = max(parts, 1), t = (u - at) / n;
+      sm_unit[0] = base + tid;
+      sm_unit[1] = t;
+      sm_unit[2] = (u - at) % n;
+      sm_unit[3] = n;
+      sm_unit[4] = at + t * n;
+    }
+    before += all;
+    __syncthreads();
+    if (before > u) break;   // (the same for all threads)
+  }
+  o.seg = __builtin_amdgcn_readfirstlane(sm_unit[0]);
+  o.tile = __builtin_amdgcn_readfirstlane(sm_unit[1]);
+  o.part = __builtin_amdgcn_readfirstlane(sm_unit[2]);
+  o.parts = __builtin_amdgcn_readfirstlane(sm_unit[3]);
+  o.first = __builtin_amdgcn_readfirstlane(sm_unit[4]);
+  return o.seg >= 0;
+}
+
+}  // namespace
+
+template <int D, int BS, bool IN8>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2)))
+void tile_attn_kernel(TileAttnParams p) {
+  constexpr int KS = D / 16;              // k-steps of the score product
+  constexpr int MT = D / 32;              // 32-wide head-dim tiles of the output
+  constexpr int NL = IN8 ? D / 64 : D / 32;   // 16-byte loads of K, and of V, a thread and step
+  constexpr int kFrags = 2 * KS;          // fragments of 1 KB of K, and of V (= 4 * MT)
+  __shared__ u32x4 sm[2][2][kFrags][kWave];   // [buffer][K, V]
+  const int tid = threadIdx.x, lane = tid & 63, col = lane & 31, half = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  // the heads alternate over the XCDs: with 8 of them each XCD's L2 holds one head's keys
+  const int h = (int)blockIdx.x % p.hkv, u = (int)blockIdx.x / p.hkv;
+
+  Unit un;
+  bool some = find_unit(p, u, un);
+  if (un.seg < p.num_groups && u >= p.prefix_units) some = false;   // groups that overlap
+  Segment g{};
+  if (some) g = segment(p, un.seg);
+  // the tiles of a sequence that see most keys first
+  const int tile = some ? row_tiles(g) - 1 - un.tile : 0;
+  const bool is_prefix = un.seg < p.num_groups;
+  const bool whole = !is_prefix && un.parts == 1 && g.group < 0;
+  if (p.partial && h == 0 && tid == 0) {   // what the merge needs to know
+    int32_t* hdr = p.units_hdr + (int64_t)u * kTileHdrInts;
+    const bool joins = some && !is_prefix && un.part == 0 && !whole;
+    *reinterpret_cast<u32x4*>(hdr) =
+        u32x4{joins ? 1u : 0u, (uint32_t)g.q0, (uint32_t)(joins ? g.rows - tile * kRows : 0), (uint32_t)tile};
+    *reinterpret_cast<u32x4*>(hdr + 4) = u32x4{(uint32_t)un.parts, (uint32_t)un.first, (uint32_t)g.group, 0u};
+    if (some && is_prefix && un.tile == 0 && un.part == 0)
+      *reinterpret_cast<u32x4*>(p.groups_hdr + (int64_t)un.seg * 4) =
+          u32x4{(uint32_t)g.q0, (uint32_t)row_tiles(g), (uint32_t)un.parts, (uint32_t)un.first};
+  }
+  if (!some) return;
+
+  const int row0 = tile * kRows;
+  const int end = tile_end(p, g, tile);                      // keys [g.base, end)
+  const int nt = (end - g.base + kKeys - 1) / kKeys;
+  const int k0 = (int)((int64_t)nt * un.part / un.parts), k1 = (int)((int64_t)nt * (un.part + 1) / un.parts);
+
+  // ---- staging: this thread's part of a step's keys, global memory -> registers -> LDS
+  const uint8_t* kc = reinterpret_cast<const uint8_t*>(p.k_cache);
+  const uint8_t* vc = reinterpret_cast<const uint8_t*>(p.v_cache);
+  constexpr int64_t kHead = (int64_t)BS * D * (IN8 ? 1 : 2);   // bytes of one (block, head) chunk
+  sint32* table = (sint32*)p.block_tables + (int64_t)g.seq * p.max_blocks;
+  const int last_block = (g.end - 1) / BS;
+  // K: wave w stages keys 32 (w & 1) + col, half of the head dim; V: the 16 keys of unit w, all of it
+  const int k_key = (wave & 1) * 32 + col;
+  int k_slot = (k_key % BS), v_slot = (wave * 16) % BS;
+  u32x4 kr[NL], vr[NL];
+  float ks = 0.f, vs = 0.f;
+  auto block_of = [&](int t, int key) {   // the block of step t's key
+    const int i = min((g.base + t * kKeys + key) / BS, last_block);
+    return (int64_t)clampi(table[i], 0, p.num_blocks - 1);
+  };
+  auto load_k = [&](int t) {
+    const int ka = BS == 16 ? (wave & 1) * 32 : k_key & ~31;
+    const int64_t b0 = block_of(t, ka), b1 = BS == 16 ? block_of(t, ka + 16) : b0;
+    const int64_t c = (col < 16 ? b0 : b1) * p.hkv + h;
+    if (IN8) {
+      const uint8_t* a = kc + c * kHead + (k_slot / 16) * 16 * D + (((wave >> 1) * (KS / 2) + half) * 16 + k_slot % 16) * 16;
+#pragma unroll
+      for (int i = 0; i < NL; ++i) kr[i] = ld16(a + i * 2 * 256);
+      ks = p.scales[2 * c];
+    } else {
+      const uint8_t* a = kc + c * kHead + ((2 * ((wave >> 1) * (KS / 2)) + half) * BS + k_slot) * 16;
+#pragma unroll
+      for (int i = 0; i < NL; ++i) kr[i] = ld16(a + i * 2 * BS * 16);
+    }
+  };
+  auto load_v = [&](int t) {
+    const int64_t c = block_of(t, wave * 16) * p.hkv + h;
+    if (IN8) {
+      const uint8_t* a = vc + c * kHead + (v_slot / 16) * 16 * D + (col * 2 + half) * 16;
+#pragma unroll
+      for (int i = 0; i < NL; ++i) vr[i] = ld16(a + i * 1024);
+      vs = p.scales[2 * c + 1];
+    } else {
+      const uint8_t* a = vc + c * kHead + (col * BS + v_slot + 8 * half) * 2;
+#pragma unroll
+      for (int i = 0; i < NL; ++i) vr[i] = ld16(a + i * 32 * BS * 2);
+    }
+  };
+  auto store_k = [&](int buf) {
+#pragma unroll
+    for (int i = 0; i < NL; ++i) {
+      if (IN8) {
+        u32x4* f = &sm[buf][0][(wave & 1) * KS + (wave >> 1) * (KS / 2) + 2 * i + half][col];
+        f[0] = widen_codes(kr[i][0], kr[i][1], ks);
+        f[32] = widen_codes(kr[i][2], kr[i][3], ks);
+      } else {
+        sm[buf][0][(wave & 1) * KS + (wave >> 1) * (KS / 2) + i][lane] = kr[i];
+      }
+    }
+  };
+  auto store_v = [&](int buf, int t) {
+    // 32-bit word w of a fragment holds this lane's keys 8 (w / 2) + 4 half + 2 (w % 2) and the next of unit `wave`
+    uint32_t keep[4] = {~0u, ~0u, ~0u, ~0u};
+    const int over = g.end - (g.base + t * kKeys + wave * 16);   // keys of the unit in front of the sequence's end
+    if (over < 16) {   // what lies behind it may be anything
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        const int key = 8 * (w >> 1) + 4 * half + 2 * (w & 1);
+        keep[w] = (key < over ? 0x0000FFFFu : 0u) | (key + 1 < over ? 0xFFFF0000u : 0u);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < NL; ++i) {
+      if (IN8) {
+        u32x4 a = widen_codes(vr[i][0], vr[i][1], vs), b = widen_codes(vr[i][2], vr[i][3], vs);
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          a[w] &= keep[w];
+          b[w] &= keep[w];
+        }
+        sm[buf][1][wave * MT + 2 * i][lane] = a;
+        sm[buf][1][wave * MT + 2 * i + 1][lane] = b;
+      } else {
+#pragma unroll
+        for (int w = 0; w < 4; ++w) vr[i][w] &= keep[w];
+        sm[buf][1][wave * MT + i][lane] = vr[i];
+      }
+    }
+  };
+
+  // ---- this wave's rows
+  const int rw = row0 + wave * 32;
+  const bool active = rw < g.rows;
+  const int r = min(rw + col, g.rows - 1), j = r / p.group;   // rows behind the last repeat it
+  const int lim = min((int64_t)g.end - 1, (int64_t)g.last + j);   // the last key the lane's row sees
+  const int64_t qrow = (int64_t)(g.q0 + j) * p.hq + h * p.group + r % p.group;
+  u32x4 qf[KS];
+  {
+    const uint16_t* q = reinterpret_cast<const uint16_t*>(p.q) + qrow * D + 8 * half;
+#pragma unroll
+    for (int s = 0; s < KS; ++s) qf[s] = ld16(q + 16 * s) ^ p.q_sign;
+  }
+  // every row of the wave sees the keys up to this one
+  const int sure = min((int64_t)g.end - 1, (int64_t)g.last + min(rw, g.rows - 1) / p.group);
+  float m = kNegBig, l = 0.f;   // in units of a score before its scale
+  f32x16 acc[MT];
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) acc[mt][e] = 0.f;
+
+  if (k0 < k1) {
+    load_k(k0);
+    load_v(k0);
+    store_k(0);
+    store_v(0, k0);
+  }
+  for (int t = k0; t < k1; ++t) {
+    const int buf = (t - k0) & 1;
+    __syncthreads();
+    const bool more = t + 1 < k1;
+    if (more) load_k(t + 1);
+    const int t0 = g.base + t * kKeys;
+    f32x16 sc[2];
+    if (active) {
+#pragma unroll
+      for (int kt = 0; kt < 2; ++kt) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) sc[kt][e] = 0.f;
+#pragma unroll
+        for (int s = 0; s < KS; ++s)
+          sc[kt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(sm[buf][0][kt * KS + s][lane]), as_bf16x8(qf[s]), sc[kt], 0, 0, 0);
+      }
+    }
+    if (more) {
+      store_k(buf ^ 1);
+      load_v(t + 1);
+    }
+    if (active) {
+      const bool need_mask = t0 + kKeys - 1 > sure;
+      if (need_mask) {
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+          for (int e = 0; e < 16; ++e)
+            if (t0 + kt * 32 + (e >> 2) * 8 + 4 * half + (e & 3) > lim) sc[kt][e] = -INFINITY;
+      }
+      float mx = sc[0][0];
+#pragma unroll
+      for (int e = 1; e < 16; ++e) mx = fmaxf(mx, sc[0][e]);
+#pragma unroll
+      for (int e = 0; e < 16; ++e) mx = fmaxf(mx, sc[1][e]);
+      mx = halves_max(mx);
+      // Lazy rescaling: the reference maximum moves only when a score exceeds it by more than 2^kLazy, so 2^(x - m)
+      // stays <= 2^kLazy and the accumulators are rescaled rarely.
+      if (__builtin_amdgcn_ballot_w64(mx > m + p.lazy) != 0) {
+        const float mnew = fmaxf(m, mx), alpha = fast_exp2((m - mnew) * p.scale_log2e);
+        m = mnew;
+        l *= alpha;
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) acc[mt][e] *= alpha;
+      }
+      const float mc = -m * p.scale_log2e;
+      float ps = 0.f;
+      u32x4 pw[4];
+#pragma unroll
+      for (int kt = 0; kt < 2; ++kt) {
+        float x[16];
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          x[e] = fast_exp2(fmaf(sc[kt][e], p.scale_log2e, mc));
+          ps += x[e];
+        }
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          pw[2 * kt][w] = pack_bf16x2(x[2 * w], x[2 * w + 1]);
+          pw[2 * kt + 1][w] = pack_bf16x2(x[8 + 2 * w], x[8 + 2 * w + 1]);
+        }
+      }
+      l += ps;
+      // A V that is not finite, of a key that some of the rows do not see: 0 times it would reach them.
+      bool odd = false;
+      if (need_mask) {
+        uint32_t any = 0;
+#pragma unroll 1
+        for (int f = 0; f < 4 * MT; ++f) {
+          const u32x4 v = sm[buf][1][f][lane];
+#pragma unroll
+          for (int w = 0; w < 4; ++w) any |= ((v[w] & 0x7F807F80u) + 0x00800080u) & 0x80008000u;
+        }
+        odd = __builtin_amdgcn_ballot_w64(any != 0) != 0;
+      }
+      if (!odd) {
+#pragma unroll
+        for (int s2 = 0; s2 < 4; ++s2)
+#pragma unroll
+          for (int mt = 0; mt < MT; ++mt)
+            acc[mt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(sm[buf][1][s2 * MT + mt][lane]), as_bf16x8(pw[s2]), acc[mt], 0, 0, 0);
+      } else {
+        // Such values become 0, and the rows that see them get a NaN by two products whose factors are finite: 2^127
+        // times 2^127 overflows to infinity, and infinity minus infinity is NaN.
+#pragma unroll
+        for (int s2 = 0; s2 < 4; ++s2) {
+          u32x4 sees;   // bf16 2^127 (0x7F00) for the keys that the lane's row sees
+#pragma unroll
+          for (int w = 0; w < 4; ++w) {
+            const int key = t0 + 16 * s2 + (w >> 1) * 8 + 4 * half + 2 * (w & 1);
+            sees[w] = (key <= lim ? 0x7F00u : 0u) | (key + 1 <= lim ? 0x7F000000u : 0u);
+          }
+#pragma unroll
+          for (int mt = 0; mt < MT; ++mt) {
+            u32x4 v = sm[buf][1][s2 * MT + mt][lane], big;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+              const uint32_t bad = (((v[w] & 0x7F807F80u) + 0x00800080u) & 0x80008000u) >> 15;   // 1 in a half
+              big[w] = bad * 0x7F00u;
+              v[w] &= ~(bad * 0xFFFFu);
+            }
+            acc[mt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(v), as_bf16x8(pw[s2]), acc[mt], 0, 0, 0);
+            acc[mt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(big), as_bf16x8(sees), acc[mt], 0, 0, 0);
+            acc[mt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(big), as_bf16x8(sees | 0x80008000u), acc[mt], 0, 0, 0);
+          }
+        }
+      }
+    }
+    if (more) store_v(buf ^ 1, t + 1);
+  }
+
+  // ---- outputs, through LDS (each wave its own quarter), so that a store instruction writes whole lines
+  __syncthreads();
+  if (!active) return;
+  const float lt = halves_sum(l);
+  u32x4* const scr = &sm[0][0][0][0] + wave * kFrags * kWave;
+  const int left = g.rows - rw;   // rows of this wave
+  if (whole) {
+    constexpr int kOc = D / 8;   // 16-byte chunks of an output row; chunk c of row col at chunk c ^ (col mod kOc)
+    const float inv = 1.0f / lt;
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+      for (int a = 0; a < 4; ++a) {
+        const u32x2 w = {pack_bf16x2(acc[mt][4 * a] * inv, acc[mt][4 * a + 1] * inv),
+                         pack_bf16x2(acc[mt][4 * a + 2] * inv, acc[mt][4 * a + 3] * inv)};
+        reinterpret_cast<u32x2*>(scr)[(col * kOc + ((4 * mt + a) ^ (col & (kOc - 1)))) * 2 + half] = w;
+      }
+    wave_lds_fence();
+#pragma unroll 1
+    for (int i = lane; i < 32 * kOc; i += kWave) {
+      const int row = i / kOc, c = i % kOc, rr = rw + row;
+      if (row < left)
+        st16(reinterpret_cast<uint16_t*>(p.out) + ((int64_t)(g.q0 + rr / p.group) * p.hq + h * p.group + rr % p.group) * D + 8 * c,
+             scr[row * kOc + (c ^ (row & (kOc - 1)))]);
+    }
+    if (p.lse && half == 0 && col < left) p.lse[qrow] = (m * p.scale_log2e + __builtin_amdgcn_logf(lt)) * kLn2;
+  } else {
+    // the partial: [pitch][D], then maxima (in the base-2 domain) and sums
+    const int pitch = is_prefix ? kRows : p.pitch;
+    float* slot = is_prefix ? p.ws_prefix + ((int64_t)u * p.hkv + h) * tile_slot_floats(kRows, D)
+                            : p.ws_seq + ((int64_t)u * p.hkv + h) * tile_slot_floats(p.pitch, D);
+    constexpr int kFc = D / 4;   // 16-byte chunks of an fp32 row; chunk c of row col at chunk c ^ (col mod kFc)
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+      for (int a = 0; a < 4; ++a) {
+        const int c = 8 * mt + 2 * a + half;
+        scr[col * kFc + (c ^ (col & (kFc - 1)))] =
+            u32x4{__float_as_uint(acc[mt][4 * a]), __float_as_uint(acc[mt][4 * a + 1]), __float_as_uint(acc[mt][4 * a + 2]),
+                  __float_as_uint(acc[mt][4 * a + 3])};
+      }
+    wave_lds_fence();
+#pragma unroll 1
+    for (int i = lane; i < 32 * kFc; i += kWave) {
+      const int row = i / kFc, c = i % kFc;
+      if (row < left) st16(slot + (int64_t)(wave * 32 + row) * D + 4 * c, scr[row * kFc + (c ^ (row & (kFc - 1)))]);
+    }
+    if (half == 0 && col < left) {
+      slot[(int64_t)pitch * D + wave * 32 + col] = m * p.scale_log2e;
+      slot[(int64_t)pitch * (D + 1) + wave * 32 + col] = lt;
+    }
+  }
+}
+
+// Joins the partials of the rows that are no unit's whole: workgroup (unit, head, 16 rows) for the first unit of a
+// sequence's tile; the tile's other parts follow it, and the parts of the shared prefix are found by the group.
+//   o = sum_c acc_c 2^(m_c - M) / sum_c l_c 2^(m_c - M),   M = max_c m_c
+template <int D>
+__global__ __launch_bounds__(16 * D / 8) void tile_merge_kernel(TileAttnParams p) {
+  const int h = (int)blockIdx.x % p.hkv, u = (int)blockIdx.x / p.hkv;
+  const int32_t* hdr = p.units_hdr + (int64_t)u * kTileHdrInts;
+  const u32x4 h0 = *reinterpret_cast<const u32x4*>(hdr), h1 = *reinterpret_cast<const u32x4*>(hdr + 4);
+  const int left = (int)h0[2], lr = (int)blockIdx.y * 16 + threadIdx.x / (D / 8), d = (threadIdx.x % (D / 8)) * 8;
+  if (h0[0] != 1u || lr >= min(left, kRows)) return;
+  const int q0 = (int)h0[1], r = (int)h0[3] * kRows + lr, parts = (int)h1[0], first = (int)h1[1], group = (int)h1[2];
+  const int j = r / p.group;
+  float M = kNegBig, den = 0.f;
+  f32x4 o0 = {0.f, 0.f, 0.f, 0.f}, o1 = o0;
+  auto add = [&](const float* slot, int pitch, int row) {
+    const float mc = slot[(int64_t)pitch * D + row], lc = slot[(int64_t)pitch * (D + 1) + row];
+    const f32x4 a0 = *reinterpret_cast<const f32x4*>(slot + (int64_t)row * D + d);
+    const f32x4 a1 = *reinterpret_cast<const f32x4*>(slot + (int64_t)row * D + d + 4);
+    const float mn = fmaxf(M, mc), x = fast_exp2(M - mn), e = fast_exp2(mc - mn);
+    den = den * x + lc * e;
+    o0 = o0 * x + a0 * e;
+    o1 = o1 * x + a1 * e;
+    M = mn;
+  };
+  for (int c = 0; c < parts && first + c < p.units; ++c)
+    add(p.ws_seq + ((int64_t)(first + c) * p.hkv + h) * tile_slot_floats(p.pitch, D), p.pitch, lr);
+  if (group >= 0) {
+    const u32x4 g = *reinterpret_cast<const u32x4*>(p.groups_hdr + (int64_t)group * 4);
+    const int rg = max(q0 - (int)g[0], 0) * p.group + r, tile = rg / kRows, n = (int)g[2];
+    const int pf = max((int)g[3] + ((int)g[1] - 1 - tile) * n, 0);   // units count tiles from the last
+    for (int c = 0; c < n && pf + c < p.prefix_units; ++c) add(p.ws_prefix + ((int64_t)(pf + c) * p.hkv + h) * tile_slot_floats(kRows, D), kRows, rg % kRows);
+  }
+  const float inv = 1.0f / den;
+  const int64_t row = (int64_t)(q0 + j) * p.hq + h * p.group + r % p.group;
+  st16(reinterpret_cast<uint16_t*>(p.out) + row * D + d,
+       u32x4{pack_bf16x2(o0[0] * inv, o0[1] * inv), pack_bf16x2(o0[2] * inv, o0[3] * inv), pack_bf16x2(o1[0] * inv, o1[1] * inv),
+             pack_bf16x2(o1[2] * inv, o1[3] * inv)});
+  if (p.lse && d == 0) p.lse[row] = (M + __builtin_amdgcn_logf(den)) * kLn2;
+}
+
+template <int D, int BS>
+static hipError_t launch_tiles_t(const TileAttnParams& p, hipStream_t s) {
+  const dim3 grid((unsigned)((int64_t)p.units * p.hkv));
+  if (p.scales) hipLaunchKernelGGL((tile_attn_kernel<D, BS, true>), grid, dim3(256), 0, s, p);
+  else hipLaunchKernelGGL((tile_attn_kernel<D, BS, false>), grid, dim3(256), 0, s, p);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || !p.partial) return e;
+  hipLaunchKernelGGL((tile_merge_kernel<D>), dim3(grid.x, (unsigned)((p.pitch + 15) / 16)), dim3(16 * D / 8), 0, s, p);
+  return hipGetLastError();
+}
+
+hipError_t launch_tile_attention(const TileAttnParams& p, hipStream_t s) {
+  if (p.head_dim == 128) return p.block_size == 16 ? launch_tiles_t<128, 16>(p, s) : launch_tiles_t<128, 32>(p, s);
+  return p.block_size == 16 ? launch_tiles_t<64, 16>(p, s) : launch_tiles_t<64, 32>(p, s);
+}
+
+}  // namespace spexis

@@ -75,6 +75,18 @@ def lib():
     L.spexis_verify_attention_kv8.argtypes = [P, P, P, i32, i32, i32, i32, i32, P, P, P, i32, i32, i32, i32, P, i32, f32,
                                               P, i32, P, sz, P]
     L.spexis_verify_attention_kv8.restype = ctypes.c_int
+    for kind, groups in (("prompt", []), ("shared", [i32, P, P])):
+        size = getattr(L, f"spexis_{kind}_attention_workspace_size")
+        size.argtypes, size.restype = [i32] * (8 if groups else 7), sz
+        for end, scales in (("", []), ("_kv8", [P])):
+            f = getattr(L, f"spexis_{kind}_attention{end}")
+            f.argtypes = [P, P, *scales, i32, i32, i32, i32, i32, P, P, P, i32, i32, i32, i32, *groups, P, i32, f32, P, P, P, sz, P]
+            f.restype = ctypes.c_int
+    L.spexis_attention_weights.argtypes = [P, i32, i32, i32, i32, i32, P, P, P, i32, i32, i32, i32, P, i32, f32, P, P, P, P, P]
+    L.spexis_attention_weights.restype = ctypes.c_int
+    L.spexis_evict_kv_workspace_size.argtypes, L.spexis_evict_kv_workspace_size.restype = [i32, i32, i32], sz
+    L.spexis_evict_kv.argtypes = [P, P, P, i32, i32, i32, i32, i32, P, P, i32, i32, P, P, i32, P, P, P, sz, P]
+    L.spexis_evict_kv.restype = ctypes.c_int
     L.spexis_softmax_rows.argtypes = [P, P, i64, i32, f32, P]
     L.spexis_softmax_rows.restype = ctypes.c_int
     L.spexis_token_logprobs_workspace_size.argtypes = [i32, i32, i32]
@@ -278,6 +290,109 @@ def spexis_verify_attention_kv8(k_cache, v_cache, scales, num_blocks, num_kv_hea
         _on(scales, _F32, here, num_blocks * num_kv_heads * 2, "scales"), num_blocks, num_kv_heads, block_size, head_dim,
         *_batch_args(here, query_start_loc, seq_lens, block_tables), total_tokens, max_query_len, max_seq_len,
         _on(q, _BF16, here, rows, "q"), num_q_heads, scale, _on(out, _BF16, here, rows, "out"), kv_chunk_tokens,
+        _on(workspace, workspace.dtype, here), workspace.nbytes, _stream_on(stream, here)))
+
+
+def spexis_prompt_attention_workspace_size(num_seqs, num_q_heads, num_kv_heads, head_dim, total_tokens, max_query_len,
+                                           max_seq_len) -> int:
+    return int(lib().spexis_prompt_attention_workspace_size(num_seqs, num_q_heads, num_kv_heads, head_dim, total_tokens,
+                                                            max_query_len, max_seq_len))
+
+
+def spexis_shared_attention_workspace_size(num_seqs, num_groups, num_q_heads, num_kv_heads, head_dim, total_tokens,
+                                           max_query_len, max_seq_len) -> int:
+    return int(lib().spexis_shared_attention_workspace_size(num_seqs, num_groups, num_q_heads, num_kv_heads, head_dim,
+                                                            total_tokens, max_query_len, max_seq_len))
+
+
+def _tile_attention(f, pools, num_blocks, num_kv_heads, block_size, head_dim, query_start_loc, seq_lens, block_tables,
+                    total_tokens, max_query_len, max_seq_len, groups, q, num_q_heads, scale, out, workspace, lse, stream):
+    """The calls over many rows.  pools: k_cache, v_cache and, of the 8-bit cache, scales; groups: none, or group_start_loc
+    and prefix_lens."""
+    here, pool = torch._C._cuda_getDevice(), num_blocks * num_kv_heads * block_size * head_dim
+    rows, kind = total_tokens * num_q_heads, _E4M3 if len(pools) == 3 else _BF16
+    args = [_on(pools[0], kind, here, pool, "k_cache"), _on(pools[1], kind, here, pool, "v_cache")]
+    if len(pools) == 3:
+        args.append(_on(pools[2], _F32, here, num_blocks * num_kv_heads * 2, "scales"))
+    shared = ()
+    if groups:
+        start, prefix = groups
+        n = 0 if prefix is None else prefix.numel()
+        shared = (n, _on(start, _I32, here, n + 1, "group_start_loc"), _on(prefix, _I32, here))
+    _check(f(*args, num_blocks, num_kv_heads, block_size, head_dim,
+             *_batch_args(here, query_start_loc, seq_lens, block_tables), total_tokens, max_query_len, max_seq_len, *shared,
+             _on(q, _BF16, here, rows * head_dim, "q"), num_q_heads, scale, _on(out, _BF16, here, rows * head_dim, "out"),
+             _on(lse, _F32, here, rows, "lse"), _on(workspace, workspace.dtype, here), workspace.nbytes,
+             _stream_on(stream, here)))
+
+
+def spexis_prompt_attention(k_cache, v_cache, num_blocks, num_kv_heads, block_size, head_dim, query_start_loc, seq_lens,
+                            block_tables, total_tokens, max_query_len, max_seq_len, q, num_q_heads, scale, out, workspace,
+                            lse=None, stream=None) -> None:
+    """q and out [T][Hq][head_dim] bf16, lse [T][Hq] fp32."""
+    _tile_attention(lib().spexis_prompt_attention, (k_cache, v_cache), num_blocks, num_kv_heads, block_size, head_dim,
+                    query_start_loc, seq_lens, block_tables, total_tokens, max_query_len, max_seq_len, (), q, num_q_heads,
+                    scale, out, workspace, lse, stream)
+
+
+def spexis_prompt_attention_kv8(k_cache, v_cache, scales, num_blocks, num_kv_heads, block_size, head_dim, query_start_loc,
+                                seq_lens, block_tables, total_tokens, max_query_len, max_seq_len, q, num_q_heads, scale, out,
+                                workspace, lse=None, stream=None) -> None:
+    """Pools torch.float8_e4m3fn, scales [num_blocks][Hkv][2] fp32 (powers of two)."""
+    _tile_attention(lib().spexis_prompt_attention_kv8, (k_cache, v_cache, scales), num_blocks, num_kv_heads, block_size,
+                    head_dim, query_start_loc, seq_lens, block_tables, total_tokens, max_query_len, max_seq_len, (), q,
+                    num_q_heads, scale, out, workspace, lse, stream)
+
+
+def spexis_shared_attention(k_cache, v_cache, num_blocks, num_kv_heads, block_size, head_dim, query_start_loc, seq_lens,
+                            block_tables, total_tokens, max_query_len, max_seq_len, group_start_loc, prefix_lens, q,
+                            num_q_heads, scale, out, workspace, lse=None, stream=None) -> None:
+    """group_start_loc [groups + 1] and prefix_lens [groups] int32 (or both None)."""
+    _tile_attention(lib().spexis_shared_attention, (k_cache, v_cache), num_blocks, num_kv_heads, block_size, head_dim,
+                    query_start_loc, seq_lens, block_tables, total_tokens, max_query_len, max_seq_len,
+                    (group_start_loc, prefix_lens), q, num_q_heads, scale, out, workspace, lse, stream)
+
+
+def spexis_shared_attention_kv8(k_cache, v_cache, scales, num_blocks, num_kv_heads, block_size, head_dim, query_start_loc,
+                                seq_lens, block_tables, total_tokens, max_query_len, max_seq_len, group_start_loc,
+                                prefix_lens, q, num_q_heads, scale, out, workspace, lse=None, stream=None) -> None:
+    _tile_attention(lib().spexis_shared_attention_kv8, (k_cache, v_cache, scales), num_blocks, num_kv_heads, block_size,
+                    head_dim, query_start_loc, seq_lens, block_tables, total_tokens, max_query_len, max_seq_len,
+                    (group_start_loc, prefix_lens), q, num_q_heads, scale, out, workspace, lse, stream)
+
+
+def spexis_attention_weights(k_cache, num_blocks, num_kv_heads, block_size, head_dim, query_start_loc, seq_lens,
+                             block_tables, total_tokens, max_query_len, max_seq_len, q, num_q_heads, scale, lse, weights,
+                             weights_in=None, accepted_len=None, stream=None) -> None:
+    """weights and weights_in [num_blocks][Hkv][block_size] fp32 (weights_in may be weights)."""
+    here, slots = torch._C._cuda_getDevice(), num_blocks * num_kv_heads * block_size
+    rows, batch = total_tokens * num_q_heads, _batch_args(here, query_start_loc, seq_lens, block_tables)
+    _check(lib().spexis_attention_weights(
+        _on(k_cache, _BF16, here, slots * head_dim, "k_cache"), num_blocks, num_kv_heads, block_size, head_dim, *batch,
+        total_tokens, max_query_len, max_seq_len, _on(q, _BF16, here, rows * head_dim, "q"), num_q_heads, scale,
+        _on(lse, _F32, here, rows, "lse"), _on(accepted_len, _I32, here, batch[0], "accepted_len"),
+        _on(weights_in, _F32, here, slots, "weights_in"), _on(weights, _F32, here, slots, "weights"),
+        _stream_on(stream, here)))
+
+
+def spexis_evict_kv_workspace_size(num_seqs, num_kv_heads, max_seq_len) -> int:
+    return int(lib().spexis_evict_kv_workspace_size(num_seqs, num_kv_heads, max_seq_len))
+
+
+def spexis_evict_kv(k_cache, v_cache, weights, num_blocks, num_kv_heads, block_size, head_dim, seq_lens, block_tables,
+                    max_seq_len, keep_lens, keep_last, weights_out, new_seq_lens, workspace, first_keys=None,
+                    stream=None) -> None:
+    """weights_out may be weights, new_seq_lens seq_lens."""
+    here, slots = torch._C._cuda_getDevice(), num_blocks * num_kv_heads * block_size
+    seqs, (rows, width) = seq_lens.numel(), block_tables.shape
+    if rows < seqs:
+        raise ValueError(f"block_tables holds {rows} sequences, the call takes {seqs}")
+    _check(lib().spexis_evict_kv(
+        _on(k_cache, _BF16, here, slots * head_dim, "k_cache"), _on(v_cache, _BF16, here, slots * head_dim, "v_cache"),
+        _on(weights, _F32, here, slots, "weights"), num_blocks, num_kv_heads, block_size, head_dim, seqs,
+        _on(seq_lens, _I32, here), _on(block_tables, _I32, here), width, max_seq_len,
+        _on(keep_lens, _I32, here, seqs, "keep_lens"), _on(first_keys, _I32, here, seqs, "first_keys"), keep_last,
+        _on(weights_out, _F32, here, slots, "weights_out"), _on(new_seq_lens, _I32, here, seqs, "new_seq_lens"),
         _on(workspace, workspace.dtype, here), workspace.nbytes, _stream_on(stream, here)))
 
 
