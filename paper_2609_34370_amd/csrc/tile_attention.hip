@@ -179,11 +179,13 @@ void tile_attn_kernel(TileAttnParams p) {
   constexpr int NL = IN8 ? D / 64 : D / 32;   // 16-byte loads of K, and of V, a thread and step
   constexpr int kFrags = 2 * KS;          // fragments of 1 KB of K, and of V (= 4 * MT)
   __shared__ u32x4 sm[2][2][kFrags][kWave];   // [buffer][K, V]
+  __shared__ int sm_odd[D];
   const int tid = threadIdx.x, lane = tid & 63, col = lane & 31, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   // the heads alternate over the XCDs: with 8 of them each XCD's L2 holds one head's keys
   const int h = (int)blockIdx.x % p.hkv, u = (int)blockIdx.x / p.hkv;
 
+  if (tid < D) sm_odd[tid] = INT32_MAX;
   Unit un;
   bool some = find_unit(p, u, un);
   if (un.seg < p.num_groups && u >= p.prefix_units) some = false;   // groups that overlap
@@ -206,6 +208,7 @@ void tile_attn_kernel(TileAttnParams p) {
   if (!some) return;
 
   const int row0 = tile * kRows;
+  const int sure0 = min((int64_t)g.end - 1, (int64_t)g.last + row0 / p.group);   // every row sees the keys up to this one
   const int end = tile_end(p, g, tile);                      // keys [g.base, end)
   const int nt = (end - g.base + kKeys - 1) / kKeys;
   const int k0 = (int)((int64_t)nt * un.part / un.parts), k1 = (int)((int64_t)nt * (un.part + 1) / un.parts);
@@ -265,6 +268,21 @@ void tile_attn_kernel(TileAttnParams p) {
       }
     }
   };
+  // A V that is not finite, of a key that some of the tile's rows do not see: 0 times it would reach them.  It becomes 0, and
+  // sm_odd[d] the first such key of its element, from which on rows get a NaN there at the end.
+  auto part_odd = [&](u32x4& v, int d, int key0) {
+    uint32_t bad[4], any = 0;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) any |= bad[w] = ((v[w] & 0x7F807F80u) + 0x00800080u) & 0x80008000u;
+    if (__builtin_amdgcn_ballot_w64(any != 0) == 0) return;
+#pragma unroll
+    for (int w = 3; w >= 0; --w) {
+      const int key = key0 + 8 * (w >> 1) + 4 * half + 2 * (w & 1);
+      if (bad[w] >> 31) atomicMin(&sm_odd[d], key + 1);
+      if (bad[w] & 0x8000u) atomicMin(&sm_odd[d], key);
+      v[w] &= ~((bad[w] >> 15) * 0xFFFFu);
+    }
+  };
   auto store_v = [&](int buf, int t) {
     // 32-bit word w of a fragment holds this lane's keys 8 (w / 2) + 4 half + 2 (w % 2) and the next of unit `wave`
     uint32_t keep[4] = {~0u, ~0u, ~0u, ~0u};
@@ -276,21 +294,23 @@ void tile_attn_kernel(TileAttnParams p) {
         keep[w] = (key < over ? 0x0000FFFFu : 0u) | (key + 1 < over ? 0xFFFF0000u : 0u);
       }
     }
+    const bool edge = t * kKeys + g.base + kKeys - 1 > sure0;   // some row does not see all of the step's keys
 #pragma unroll
     for (int i = 0; i < NL; ++i) {
+      u32x4 v[IN8 ? 2 : 1];
       if (IN8) {
-        u32x4 a = widen_codes(vr[i][0], vr[i][1], vs), b = widen_codes(vr[i][2], vr[i][3], vs);
-#pragma unroll
-        for (int w = 0; w < 4; ++w) {
-          a[w] &= keep[w];
-          b[w] &= keep[w];
-        }
-        sm[buf][1][wave * MT + 2 * i][lane] = a;
-        sm[buf][1][wave * MT + 2 * i + 1][lane] = b;
+        v[0] = widen_codes(vr[i][0], vr[i][1], vs);
+        v[IN8 ? 1 : 0] = widen_codes(vr[i][2], vr[i][3], vs);
       } else {
+        v[0] = vr[i];
+      }
 #pragma unroll
-        for (int w = 0; w < 4; ++w) vr[i][w] &= keep[w];
-        sm[buf][1][wave * MT + i][lane] = vr[i];
+      for (int x = 0; x < (IN8 ? 2 : 1); ++x) {
+        const int mt = IN8 ? 2 * i + x : i;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) v[x][w] &= keep[w];
+        if (edge) part_odd(v[x], 32 * mt + col, g.base + t * kKeys + wave * 16);
+        sm[buf][1][wave * MT + mt][lane] = v[x];
       }
     }
   };
@@ -387,50 +407,11 @@ void tile_attn_kernel(TileAttnParams p) {
         }
       }
       l += ps;
-      // A V that is not finite, of a key that some of the rows do not see: 0 times it would reach them.
-      bool odd = false;
-      if (need_mask) {
-        uint32_t any = 0;
-#pragma unroll 1
-        for (int f = 0; f < 4 * MT; ++f) {
-          const u32x4 v = sm[buf][1][f][lane];
 #pragma unroll
-          for (int w = 0; w < 4; ++w) any |= ((v[w] & 0x7F807F80u) + 0x00800080u) & 0x80008000u;
-        }
-        odd = __builtin_amdgcn_ballot_w64(any != 0) != 0;
-      }
-      if (!odd) {
+      for (int s2 = 0; s2 < 4; ++s2)
 #pragma unroll
-        for (int s2 = 0; s2 < 4; ++s2)
-#pragma unroll
-          for (int mt = 0; mt < MT; ++mt)
-            acc[mt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(sm[buf][1][s2 * MT + mt][lane]), as_bf16x8(pw[s2]), acc[mt], 0, 0, 0);
-      } else {
-        // Such values become 0, and the rows that see them get a NaN by two products whose factors are finite: 2^127
-        // times 2^127 overflows to infinity, and infinity minus infinity is NaN.
-#pragma unroll
-        for (int s2 = 0; s2 < 4; ++s2) {
-          u32x4 sees;   // bf16 2^127 (0x7F00) for the keys that the lane's row sees
-#pragma unroll
-          for (int w = 0; w < 4; ++w) {
-            const int key = t0 + 16 * s2 + (w >> 1) * 8 + 4 * half + 2 * (w & 1);
-            sees[w] = (key <= lim ? 0x7F00u : 0u) | (key + 1 <= lim ? 0x7F000000u : 0u);
-          }
-#pragma unroll
-          for (int mt = 0; mt < MT; ++mt) {
-            u32x4 v = sm[buf][1][s2 * MT + mt][lane], big;
-#pragma unroll
-            for (int w = 0; w < 4; ++w) {
-              const uint32_t bad = (((v[w] & 0x7F807F80u) + 0x00800080u) & 0x80008000u) >> 15;   // 1 in a half
-              big[w] = bad * 0x7F00u;
-              v[w] &= ~(bad * 0xFFFFu);
-            }
-            acc[mt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(v), as_bf16x8(pw[s2]), acc[mt], 0, 0, 0);
-            acc[mt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(big), as_bf16x8(sees), acc[mt], 0, 0, 0);
-            acc[mt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(big), as_bf16x8(sees | 0x80008000u), acc[mt], 0, 0, 0);
-          }
-        }
-      }
+        for (int mt = 0; mt < MT; ++mt)
+          acc[mt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(sm[buf][1][s2 * MT + mt][lane]), as_bf16x8(pw[s2]), acc[mt], 0, 0, 0);
     }
     if (more) store_v(buf ^ 1, t + 1);
   }
@@ -438,6 +419,17 @@ void tile_attn_kernel(TileAttnParams p) {
   // ---- outputs, through LDS (each wave its own quarter), so that a store instruction writes whole lines
   __syncthreads();
   if (!active) return;
+  if (g.base + k1 * kKeys - 1 > sure0) {
+    int first = sm_odd[lane];
+    if (D == 128) first = min(first, sm_odd[D - kWave + lane]);
+    if (__builtin_amdgcn_ballot_w64(first < INT32_MAX) != 0) {
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          if (lim >= sm_odd[32 * mt + 8 * (e >> 2) + 4 * half + (e & 3)]) acc[mt][e] = __builtin_nanf("");
+    }
+  }
   const float lt = halves_sum(l);
   u32x4* const scr = &sm[0][0][0][0] + wave * kFrags * kWave;
   const int left = g.rows - rw;   // rows of this wave
