@@ -167,3 +167,86 @@ def token_logprobs(logits, rows, tokens, temperature, top):
         order = np.argsort(-x, kind="stable")[:top]
         ids[i, : len(order)], alt[i, : len(order)] = order, z[order] - ln
     return lp, entropy, ids, alt
+
+
+# ------------------------------------------------------------------ prompts, shared prefixes, weights, eviction
+# over logical caches k, v [block][slot][KV head][dim] (values, not codes)
+
+
+def attention_rows(k, v, qsl, seq_lens, tables, q, scale):
+    """Causal attention of every query token over its sequence, any number of tokens: outputs, the weighted mean of |v|,
+    the largest sum of |q_d k_d| |scale| of a key, and the logarithm of the sum of exponentials."""
+    bs, hkv, D = k.shape[1:]
+    q = np.asarray(q, dtype=np.float64)
+    out, mean, most, lse = np.zeros(q.shape), np.zeros(q.shape), np.zeros(q.shape[:2]), np.zeros(q.shape[:2])
+    G = q.shape[1] // hkv
+    for b in range(len(seq_lens)):
+        S, n = int(seq_lens[b]), int(qsl[b + 1] - qsl[b])
+        if n == 0:
+            continue
+        t = np.arange(S)
+        kb, vb = k[tables[b, t // bs], t % bs], v[tables[b, t // bs], t % bs]
+        sees = t[None, :] <= (S - n + np.arange(n))[:, None]
+        rows = slice(int(qsl[b]), int(qsl[b]) + n)
+        for h in range(q.shape[1]):
+            keys = kb[:, h // G]
+            x = np.where(sees, q[rows, h] @ keys.T * scale, -np.inf)
+            m = x.max(axis=1, keepdims=True)
+            p = np.exp(x - m)
+            total = p.sum(axis=1, keepdims=True)
+            out[rows, h] = p @ vb[:, h // G] / total
+            mean[rows, h] = p @ np.abs(vb[:, h // G]) / total
+            most[rows, h] = np.where(sees, np.abs(q[rows, h]) @ np.abs(keys).T * abs(scale), 0).max(axis=1)
+            lse[rows, h] = (m + np.log(total))[:, 0]
+    return out, mean, most, lse
+
+
+def attention_weights(k, qsl, seq_lens, tables, q, scale, lse, before, accepted=None):
+    """`before` [block][KV head][slot] (None: zeros) with the sums of the step's weights; and the sums of the weights'
+    relative errors in units of fp32's: what an exponent's rounding amounts to."""
+    bs, hkv, D = k.shape[1:]
+    q = np.asarray(q, dtype=np.float64)
+    out = np.zeros((k.shape[0], hkv, bs)) if before is None else np.array(before, dtype=np.float64)
+    size = np.zeros(out.shape)
+    G = q.shape[1] // hkv
+    for b in range(len(seq_lens)):
+        S, n = int(seq_lens[b]), int(qsl[b + 1] - qsl[b])
+        if accepted is not None:
+            n = min(n, int(accepted[b]) + 1)
+        t = np.arange(S)
+        place = tables[b, t // bs], slice(None), t % bs
+        kb = k[tables[b, t // bs], t % bs]
+        total, err = np.zeros((S, hkv)), np.zeros((S, hkv))
+        for j in range(n):
+            row, seen = int(qsl[b]) + j, S - n + j + 1
+            for h in range(q.shape[1]):
+                e = lse[row, h]
+                w = np.exp(kb[:seen, h // G] @ q[row, h] * scale - e)
+                total[:seen, h // G] += w
+                err[:seen, h // G] += w * ((D + 8) * (np.abs(kb[:seen, h // G]) @ np.abs(q[row, h]) * abs(scale)) + 4 * abs(e) + 16)
+        old = np.where(t[:, None] < S - n, out[place] if before is not None else 0.0, 0.0)
+        out[place] = old + total
+        size[place] = err + (n * G + 8) * total + 2 * np.abs(old)
+    return out, size
+
+
+def evict(k, v, weights, seq_lens, tables, keep, first, last):
+    """Caches, weights and lengths with all but `keep` keys of each sequence and KV head gone (copies)."""
+    bs, hkv = k.shape[1:3]
+    k2, v2, w2, lens = k.copy(), v.copy(), weights.copy(), []
+    for b in range(len(seq_lens)):
+        S = int(seq_lens[b])
+        m = min(max(int(keep[b]), 0), S)
+        f = min(max(int(first[b]), 0), m) if first is not None else 0
+        le = min(int(last), m - f)
+        lens.append(m)
+        t = np.arange(S)
+        blk, slot = tables[b, t // bs], t % bs
+        for h in range(hkv):
+            w = weights[blk, h, slot].astype(np.float64)
+            order = sorted(range(f, S - le), key=lambda i: (np.isnan(w[i]), -w[i] if not np.isnan(w[i]) else 0.0, i))
+            src = np.array(sorted([*range(f), *order[: m - f - le], *range(S - le, S)]), dtype=np.int64)
+            k2[blk[:m], slot[:m], h] = k[blk[src], slot[src], h]
+            v2[blk[:m], slot[:m], h] = v[blk[src], slot[src], h]
+            w2[blk[:m], h, slot[:m]] = weights[blk[src], h, slot[src]]
+    return k2, v2, w2, np.array(lens, np.int32)

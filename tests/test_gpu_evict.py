@@ -1,0 +1,267 @@
+"""The cached keys' attention weights, and eviction by them.
+
+Weights: of a weight exp(scale <q, k> - lse), with u = 2^-24, the exponent is an fp32 sum of D exact products, scaled, minus
+lse, each side rounded a few times: (D + 8) u sum |q k| scale + 4 u |lse| and 16 u for exp2 and the factors of base 2, times
+the weight; the sum over a KV head's rows adds as many units of u of itself, the sum of before two.  Eviction moves bits: exact.
+"""
+import sys
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import serving as osv
+from paper_2609_34370_amd import spexis as sx
+from tests import layout_ref
+from tests.test_gpu_rotate import batch, dev
+from tests.test_gpu_tile_attention import Cache, attend, queries
+
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -24
+
+
+def say(*a):
+    print(*a, file=sys.stderr, flush=True)
+
+
+def weigh(c, k_pool, qsl, S, tables, q, scale, lse, before, accepted=None, out=None, max_s=None):
+    n = max(int(np.diff(qsl).max()), 1)
+    w = torch.full((c.blocks, c.hkv, c.bs), 777.0, device="cuda") if out is None else out
+    sx.spexis_attention_weights(k_pool, c.blocks, c.hkv, c.bs, c.D, dev(qsl), dev(S), dev(tables), q.shape[0], n,
+                                max_s or int(max(S.max(), 1)), q, q.shape[1], scale, lse, w, weights_in=before,
+                                accepted_len=None if accepted is None else dev(np.asarray(accepted, np.int32)))
+    torch.cuda.synchronize()
+    return w
+
+
+def used_places(S, tables, blocks, bs):
+    used = np.zeros((blocks, bs), bool)
+    for b in range(len(S)):
+        t = np.arange(S[b])
+        used[tables[b, t // bs], t % bs] = True
+    return used
+
+
+WEIGHTS = [
+    # hq, hkv, D, bs, new tokens, cached tokens, accepted
+    (8, 2, 64, 16, [5, 5, 1, 5], [0, 31, 15, 200], None),
+    (32, 8, 128, 16, [5, 1, 0, 5], [100, 16, 40, 1], [2, 0, 3, -1]),
+    (28, 4, 128, 32, [9, 70], [500, 129], None),
+    (7, 1, 128, 16, [300], [1000], None),
+    (4, 4, 64, 32, [1] * 70, list(range(70)), None),
+    (6, 3, 128, 32, [9, 9, 9], [31, 32, 0], [8, 0, 4]),
+    (2, 1, 64, 16, [400, 1], [0, 0], [250, 0]),
+]
+
+
+@pytest.mark.parametrize("add", [False, True])
+@pytest.mark.parametrize("shape", range(len(WEIGHTS)))
+def test_weights_against_64_bits(shape, add):
+    hq, hkv, D, bs, n, ctx, accepted = WEIGHTS[shape]
+    r = np.random.default_rng(shape)
+    qsl, S, tables, blocks = batch(n, ctx, bs, shape)
+    c = Cache(blocks, bs, hkv, D, r, False)
+    q = queries(int(qsl[-1]), hq, D, r)
+    scale = float(np.float32(D ** -0.5))
+    k, v = c.pools()
+    _, lse = attend(c, (k, v), qsl, S, tables, q, scale)
+    if accepted is not None:
+        S = (S - n + np.minimum(n, np.asarray(accepted) + 1)).astype(np.int32)
+    before = torch.rand((blocks, hkv, bs), device="cuda") if add else None
+    got = weigh(c, k, qsl, S, tables, q, scale, lse, before, accepted).double().cpu().numpy()
+    want, size = osv.attention_weights(c.k, qsl, S, tables, q.double().cpu().numpy(), scale, lse.double().cpu().numpy(),
+                                       before.double().cpu().numpy() if add else None, accepted)
+    used = used_places(S, tables, blocks, bs)
+    err, bound = np.abs(got - want), U * size + 1e-30
+    mask = np.broadcast_to(used[:, None, :], got.shape)
+    say(f"[weights] {WEIGHTS[shape][:4]} max err/bound {(err / bound)[mask].max():.3f}")
+    assert (err <= bound)[mask].all() and (got[~mask] == 777.0).all()
+    if add:   # in place: the same bits
+        own = before.clone()
+        weigh(c, k, qsl, S, tables, q, scale, lse, own, accepted, out=own)
+        assert np.array_equal(own.double().cpu().numpy()[mask], got[mask])
+
+
+def test_weights_of_a_row_sum_to_its_heads():
+    """Every query token's weights sum to 1 a head."""
+    r = np.random.default_rng(2)
+    qsl, S, tables, blocks = batch([37, 4], [900, 12], 16, 2)
+    c = Cache(blocks, 16, 2, 128, r, False)
+    q = queries(41, 8, 128, r)
+    k, v = c.pools()
+    _, lse = attend(c, (k, v), qsl, S, tables, q, 0.1)
+    w = weigh(c, k, qsl, S, tables, q, 0.1, lse, None, out=torch.zeros((blocks, 2, 16), device="cuda"))
+    assert torch.allclose(w.sum(dim=(0, 2)), torch.full((2,), 41.0 * 4, device="cuda"), rtol=1e-5)
+
+
+def evict(c, pools, weights, S, tables, keep, first, last, out=None, lens=None):
+    w = torch.full_like(weights, 777.0) if out is None else out
+    S_d = dev(S)
+    new = torch.full_like(S_d, -5) if lens is None else S_d
+    ws = torch.full((sx.spexis_evict_kv_workspace_size(len(S), c.hkv, int(max(S.max(), 1))),), 0x7F, dtype=torch.uint8, device="cuda")
+    sx.spexis_evict_kv(*pools, weights, c.blocks, c.hkv, c.bs, c.D, S_d, dev(tables), int(max(S.max(), 1)),
+                       dev(np.asarray(keep, np.int32)), last, w, new, ws,
+                       first_keys=None if first is None else dev(np.asarray(first, np.int32)))
+    torch.cuda.synchronize()
+    return w, new.cpu().numpy()
+
+
+def logical(pool, c, which):
+    f = layout_ref.k_offsets if which == "k" else layout_ref.v_offsets
+    blk, slot, h, d = np.ogrid[:c.blocks, :c.bs, :c.hkv, :c.D]
+    return pool.double().cpu().numpy()[f(blk, h, slot, d, c.hkv, c.bs, c.D)]
+
+
+EVICT = [
+    # hkv, D, bs, lengths, kept, first, last
+    (2, 64, 16, [100, 37, 16, 1], [50, 36, 1, 1], [4, 0, 0, 0], 8),
+    (8, 128, 16, [1000, 17, 0, 333], [200, 17, 0, 400], None, 32),
+    (4, 128, 32, [2500, 64, 65], [1250, 63, 1], [64, 100, 0], 0),
+    (1, 64, 32, [5000], [4999], [1], 1),
+    (3, 128, 16, [700, 300], [0, -3], [5, 5], 7),
+    (2, 128, 32, [1024, 2048, 1025], [10, 2000, 1024], [3, 16, 1], 2000),
+    (1, 128, 16, [40] * 90, list(range(90)), [i % 9 for i in range(90)], 3),
+]
+
+
+@pytest.mark.parametrize("kind", ["spread", "ties", "odd"])
+@pytest.mark.parametrize("shape", range(len(EVICT)))
+def test_eviction(shape, kind):
+    hkv, D, bs, S, keep, first, last = EVICT[shape]
+    r = np.random.default_rng(shape)
+    _, S, tables, blocks = batch([0] * len(S), S, bs, shape)
+    c = Cache(blocks, bs, hkv, D, r, False)
+    w = r.exponential(size=(blocks, hkv, bs)).astype(np.float32)
+    if kind == "ties":
+        w = np.floor(w * 2).astype(np.float32)
+        w[r.random(w.shape) < 0.2] = -0.0
+    if kind == "odd":
+        for x in (np.nan, -np.nan, np.inf, -np.inf, -1.0, 1e-40):
+            w[r.random(w.shape) < 0.1] = x
+    for same in (False, True):   # into other arrays, and in place
+        pools, weights = c.pools(), dev(w)
+        got, lens = evict(c, pools, weights, S, tables, keep, first, last, out=weights if same else None, lens=same or None)
+        k, v, w2, m = osv.evict(c.k, c.v, w, S, tables, keep, first, last)
+        assert np.array_equal(lens, m)
+        kept = used_places(m, tables, blocks, bs)
+        free = used_places(S, tables, blocks, bs) & ~kept
+        got = got.cpu().numpy()
+        assert np.array_equal(got.transpose(0, 2, 1)[kept], w2.transpose(0, 2, 1)[kept], equal_nan=True)
+        if not same:
+            assert (got.transpose(0, 2, 1)[~kept] == 777.0).all()
+        for pool, want, which in zip(pools, (k, v), "kv"):
+            x = logical(pool, c, which)
+            assert np.array_equal(x[~free], want[~free]), which
+
+
+def test_a_shared_block_at_the_front_is_left_alone():
+    """Two sequences that begin with the same blocks: first_keys keeps them."""
+    r = np.random.default_rng(21)
+    _, S, tables, blocks = batch([0, 0], [200, 150], 16, 21)
+    tables[1, :3] = tables[0, :3]
+    c = Cache(blocks, 16, 2, 64, r, False)
+    w = r.random((blocks, 2, 16)).astype(np.float32)
+    pools = c.pools()
+    evict(c, pools, dev(w), S, tables, [90, 60], [48, 48], 5)
+    k, v, _, m = osv.evict(c.k, c.v, w, S, tables, [90, 60], [48, 48], 5)
+    kept = used_places(m, tables, blocks, 16)
+    for pool, want, which in zip(pools, (k, v), "kv"):
+        assert np.array_equal(logical(pool, c, which)[kept], want[kept])
+
+
+def test_attention_over_what_is_left_ignores_what_went():
+    """Keys without weight leave; the attention of a later token over the rest is that over all without them."""
+    r = np.random.default_rng(22)
+    qsl, S, tables, blocks = batch([1], [600], 16, 22)
+    c = Cache(blocks, 16, 1, 64, r, False)
+    q = queries(1, 4, 64, r)
+    t = np.arange(601)
+    far = (r.random(601) < 0.5) & (t < 600)
+    c.k[tables[0, t[far] // 16], t[far] % 16, 0] = 0.0
+    c.k[tables[0, t[far] // 16], t[far] % 16, 0, 0] = -4096.0
+    q[:, :, 0] = 8.0
+    pools = c.pools()
+    a, lse = attend(c, pools, qsl, S, tables, q, 0.125)
+    w = weigh(c, pools[0], qsl, S, tables, q, 0.125, lse, None)
+    m = int((~far).sum())
+    _, lens = evict(c, pools, w, S, tables, [m], None, 1)
+    assert lens[0] == m
+    b, lse2 = attend(c, pools, qsl, np.array([m], np.int32), tables, q, 0.125)
+    assert torch.allclose(lse, lse2, rtol=0, atol=1e-5)
+    err = (a.double() - b.double()).abs()
+    # the same weights and sums but for their order: each output within its rounding and the weights' (2^-8 of it and of the
+    # mean of |v|, at most max |v| = 5)
+    assert (err <= 2 * (2.0 ** -8 * a.double().abs() + 2.0 ** -8 * 5)).all()
+
+
+def test_replays_and_streams():
+    """Weights and eviction as a captured graph on its own inputs, replayed with eager calls between."""
+    r = np.random.default_rng(23)
+    qsl, S, tables, blocks = batch([5, 2], [300, 90], 16, 23)
+    c = Cache(blocks, 16, 2, 64, r, False)
+    q = queries(7, 8, 64, r)
+    k0, v0 = c.pools()
+    _, lse = attend(c, (k0, v0), qsl, S, tables, q, 0.125)
+    k, v = k0.clone(), v0.clone()
+    d = [dev(x) for x in (qsl, S, tables)]
+    w, w2 = torch.full((blocks, 2, 16), 3.0, device="cuda"), torch.zeros((blocks, 2, 16), device="cuda")
+    keep, new = dev(np.array([100, 50], np.int32)), torch.zeros(2, dtype=torch.int32, device="cuda")
+    ws = torch.empty(sx.spexis_evict_kv_workspace_size(2, 2, 305), dtype=torch.uint8, device="cuda")
+
+    def step(stream=None):
+        sx.spexis_attention_weights(k, blocks, 2, 16, 64, *d, 7, 5, 305, q, 8, 0.125, lse, w, stream=stream)
+        sx.spexis_evict_kv(k, v, w, blocks, 2, 16, 64, d[1], d[2], 305, keep, 9, w2, new, ws, stream=stream)
+    step()
+    torch.cuda.synchronize()
+    want = [x.clone() for x in (k, v, w, w2, new)]
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        step()
+    side = torch.cuda.Stream()
+    for turn in range(4):
+        k.copy_(k0)
+        v.copy_(v0)
+        w.fill_(3.0)
+        new.zero_()
+        torch.cuda.synchronize()
+        if turn == 2:
+            step(stream=side)
+        else:
+            g.replay()
+        torch.cuda.synchronize()
+        for x, y in zip((k, v, w, w2, new), want):
+            assert torch.equal(x, y), turn
+
+
+def test_refusals_of_the_binding():
+    r = np.random.default_rng(24)
+    qsl, S, tables, blocks = batch([4], [20], 16, 1)
+    c = Cache(blocks, 16, 2, 64, r, False)
+    k, v = c.pools()
+    q = queries(4, 8, 64, r)
+    w = torch.zeros((blocks, 2, 16), device="cuda")
+    lse = torch.zeros((4, 8), device="cuda")
+    ints = torch.ones(1, dtype=torch.int32, device="cuda")
+    ws = torch.empty(sx.spexis_evict_kv_workspace_size(1, 2, 24), dtype=torch.uint8, device="cuda")
+
+    def weights(**kw):
+        a = {**dict(k=k, q=q, lse=lse, w=w, w_in=None, acc=None), **kw}
+        sx.spexis_attention_weights(a["k"], blocks, 2, 16, 64, dev(qsl), dev(S), dev(tables), 4, 4, 24, a["q"], 8, 0.125, a["lse"],
+                                    a["w"], weights_in=a["w_in"], accepted_len=a["acc"])
+
+    def away(**kw):
+        a = {**dict(k=k, v=v, w=w, out=w, keep=ints, new=ints.clone(), first=None, ws=ws), **kw}
+        sx.spexis_evict_kv(a["k"], a["v"], a["w"], blocks, 2, 16, 64, dev(S), dev(tables), 24, a["keep"], 2, a["out"], a["new"],
+                           a["ws"], first_keys=a["first"])
+    weights()
+    away()
+    for kw in (dict(k=k[:-1]), dict(q=q[:3]), dict(lse=lse[:3]), dict(w=w[:-1]), dict(w_in=w[:-1]), dict(acc=ints[:0]), dict(w=w.cpu()),
+               dict(w_in=w.double())):
+        with pytest.raises(ValueError):
+            weights(**kw)
+    for kw in (dict(k=k[:-1]), dict(v=v.float()), dict(w=w[:-1]), dict(out=w[:-1]), dict(keep=ints[:0]), dict(new=ints[:0]),
+               dict(first=ints[:0]), dict(ws=ws.cpu())):
+        with pytest.raises(ValueError):
+            away(**kw)
+    with pytest.raises(sx.SpexisError):
+        away(ws=ws[:16])
