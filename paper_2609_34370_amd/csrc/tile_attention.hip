@@ -220,18 +220,22 @@ void tile_attn_kernel(TileAttnParams p) {
   sint32* table = (sint32*)p.block_tables + (int64_t)g.seq * p.max_blocks;
   const int last_block = (g.end - 1) / BS;
   // K: wave w stages keys 32 (w & 1) + col, half of the head dim; V: the 16 keys of unit w, all of it
-  const int k_key = (wave & 1) * 32 + col;
-  int k_slot = (k_key % BS), v_slot = (wave * 16) % BS;
+  const int k_key = (wave & 1) * 32 + col, k_slot = k_key % BS, v_slot = (wave * 16) % BS;
   u32x4 kr[NL], vr[NL];
   float ks = 0.f, vs = 0.f;
-  auto block_of = [&](int t, int key) {   // the block of step t's key
-    const int i = min((g.base + t * kKeys + key) / BS, last_block);
-    return (int64_t)clampi(table[i], 0, p.num_blocks - 1);
+  // Where a step's keys lie is looked up a step before they are loaded, and the answer not touched until then: the lookup's
+  // latency would stand in front of every step.
+  int kb0 = 0, kb1 = 0, vb = 0;
+  auto block_of = [&](int key) { return table[min((int)((uint32_t)(g.base + key) / BS), last_block)]; };
+  auto chunk_of = [&](int block) { return (int64_t)clampi(block, 0, p.num_blocks - 1) * p.hkv + h; };
+  auto find_k = [&](int t) {
+    kb0 = block_of(t * kKeys + (wave & 1) * 32);
+    kb1 = BS == 16 ? block_of(t * kKeys + (wave & 1) * 32 + 16) : kb0;
   };
+  auto find_v = [&](int t) { vb = block_of(t * kKeys + wave * 16); };
+  // (steps behind the last find its last block: a valid one)
   auto load_k = [&](int t) {
-    const int ka = BS == 16 ? (wave & 1) * 32 : k_key & ~31;
-    const int64_t b0 = block_of(t, ka), b1 = BS == 16 ? block_of(t, ka + 16) : b0;
-    const int64_t c = (col < 16 ? b0 : b1) * p.hkv + h;
+    const int64_t c0 = chunk_of(kb0), c1 = BS == 16 ? chunk_of(kb1) : c0, c = BS == 16 && col >= 16 ? c1 : c0;
     if (IN8) {
       const uint8_t* a = kc + c * kHead + (k_slot / 16) * 16 * D + (((wave >> 1) * (KS / 2) + half) * 16 + k_slot % 16) * 16;
 #pragma unroll
@@ -242,9 +246,10 @@ void tile_attn_kernel(TileAttnParams p) {
 #pragma unroll
       for (int i = 0; i < NL; ++i) kr[i] = ld16(a + i * 2 * BS * 16);
     }
+    find_k(t + 1);
   };
   auto load_v = [&](int t) {
-    const int64_t c = block_of(t, wave * 16) * p.hkv + h;
+    const int64_t c = chunk_of(vb);
     if (IN8) {
       const uint8_t* a = vc + c * kHead + (v_slot / 16) * 16 * D + (col * 2 + half) * 16;
 #pragma unroll
@@ -255,6 +260,7 @@ void tile_attn_kernel(TileAttnParams p) {
 #pragma unroll
       for (int i = 0; i < NL; ++i) vr[i] = ld16(a + i * 32 * BS * 2);
     }
+    find_v(t + 1);
   };
   auto store_k = [&](int buf) {
 #pragma unroll
@@ -285,15 +291,7 @@ void tile_attn_kernel(TileAttnParams p) {
   };
   auto store_v = [&](int buf, int t) {
     // 32-bit word w of a fragment holds this lane's keys 8 (w / 2) + 4 half + 2 (w % 2) and the next of unit `wave`
-    uint32_t keep[4] = {~0u, ~0u, ~0u, ~0u};
     const int over = g.end - (g.base + t * kKeys + wave * 16);   // keys of the unit in front of the sequence's end
-    if (over < 16) {   // what lies behind it may be anything
-#pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        const int key = 8 * (w >> 1) + 4 * half + 2 * (w & 1);
-        keep[w] = (key < over ? 0x0000FFFFu : 0u) | (key + 1 < over ? 0xFFFF0000u : 0u);
-      }
-    }
     const bool edge = t * kKeys + g.base + kKeys - 1 > sure0;   // some row does not see all of the step's keys
 #pragma unroll
     for (int i = 0; i < NL; ++i) {
@@ -307,9 +305,14 @@ void tile_attn_kernel(TileAttnParams p) {
 #pragma unroll
       for (int x = 0; x < (IN8 ? 2 : 1); ++x) {
         const int mt = IN8 ? 2 * i + x : i;
+        if (edge) {
 #pragma unroll
-        for (int w = 0; w < 4; ++w) v[x][w] &= keep[w];
-        if (edge) part_odd(v[x], 32 * mt + col, g.base + t * kKeys + wave * 16);
+          for (int w = 0; w < 4; ++w) {   // what lies behind the end may be anything
+            const int key = 8 * (w >> 1) + 4 * half + 2 * (w & 1);
+            v[x][w] &= (key < over ? 0x0000FFFFu : 0u) | (key + 1 < over ? 0xFFFF0000u : 0u);
+          }
+          part_odd(v[x], 32 * mt + col, g.base + t * kKeys + wave * 16);
+        }
         sm[buf][1][wave * MT + mt][lane] = v[x];
       }
     }
@@ -337,6 +340,8 @@ void tile_attn_kernel(TileAttnParams p) {
     for (int e = 0; e < 16; ++e) acc[mt][e] = 0.f;
 
   if (k0 < k1) {
+    find_k(k0);
+    find_v(k0);
     load_k(k0);
     load_v(k0);
     store_k(0);
