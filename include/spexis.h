@@ -420,7 +420,7 @@ size_t spexis_evict_kv_workspace_size(int32_t num_seqs, int32_t num_kv_heads, in
  *   seq_lens      [num_seqs] int32 (read);  new_seq_lens [num_seqs] int32 (written); may be seq_lens
  *   max_seq_len   host: >= max_b S_b (keys from it on are dropped)
  * The blocks of a sequence from the first key that moves on must be its own.  Pools, weights and workspace 16-byte aligned.
- * Supported: head_dim in {64, 128}, block_size in {16, 32}; num_seqs * Hkv < 2^21.
+ * Supported: head_dim in {64, 128}, block_size in {16, 32}; num_seqs * Hkv < 2^20.
  * Errors: INVALID_ARGUMENT, UNSUPPORTED, WORKSPACE_TOO_SMALL, HIP.
  */
 int spexis_evict_kv(void* k_cache, void* v_cache, const float* weights, int32_t num_blocks, int32_t num_kv_heads,

@@ -580,7 +580,7 @@ int spexis_attention_weights(const void* k_cache, int32_t num_blocks, int32_t nu
 size_t spexis_evict_kv_workspace_size(int32_t num_seqs, int32_t num_kv_heads, int32_t max_seq_len) {
   if (num_seqs <= 0 || num_kv_heads <= 0 || max_seq_len <= 0) return 0;
   const int64_t items = (int64_t)num_seqs * num_kv_heads;
-  return (size_t)(round_up(items * 8, 256) + round_up(items * max_seq_len * 4, 256));
+  return (size_t)(round_up(items * 8, 256) + items * round_up(max_seq_len, 128) * 4);
 }
 
 int spexis_evict_kv(void* k_cache, void* v_cache, const float* weights, int32_t num_blocks, int32_t num_kv_heads,
@@ -594,8 +594,8 @@ int spexis_evict_kv(void* k_cache, void* v_cache, const float* weights, int32_t 
   if (bad_cache_shape(block_size, head_dim))
     return fail(SPEXIS_ERR_UNSUPPORTED, "%s: block_size %d / head_dim %d not in {16,32} x {64,128}", name, block_size,
                 head_dim);
-  // a launch holds fewer than 2^32 threads: at most 2048 for a (sequence, KV head)
-  if ((int64_t)num_seqs * num_kv_heads >= (1ll << 21) || (int64_t)max_blocks_per_seq * block_size >= (1ll << 30) ||
+  // a launch holds fewer than 2^32 threads: at most 3072 for a (sequence, KV head)
+  if ((int64_t)num_seqs * num_kv_heads >= (1ll << 20) || (int64_t)max_blocks_per_seq * block_size >= (1ll << 30) ||
       max_seq_len >= (1 << 30))
     return fail(SPEXIS_ERR_UNSUPPORTED, "%s: too many sequences or slots", name);
   if (num_seqs == 0) return ok();
@@ -609,7 +609,7 @@ int spexis_evict_kv(void* k_cache, void* v_cache, const float* weights, int32_t 
   int32_t* ws = static_cast<int32_t*>(workspace);
   spexis::EvictParams p{k_cache, v_cache, weights, weights_out, seq_lens, block_tables, keep_lens, first_keys, new_seq_lens, ws,
                         ws + round_up((int64_t)num_seqs * num_kv_heads * 8, 256) / 4, num_blocks, num_kv_heads, block_size,
-                        head_dim, num_seqs, max_blocks_per_seq, max_seq_len, keep_last};
+                        head_dim, num_seqs, max_blocks_per_seq, max_seq_len, keep_last, round_up(max_seq_len, 128)};
   return hip_result(spexis::launch_evict(p, (hipStream_t)stream), name);
 }
 

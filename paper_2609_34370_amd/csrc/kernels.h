@@ -228,8 +228,9 @@ struct EvictParams {
   const int32_t* first_keys;      // or null
   int32_t* new_lens;
   int32_t* hdr;                   // [num_seqs][hkv][2]: keys that stay, the first that moves
-  int32_t* list;                  // [num_seqs][hkv][max_seq_len]: where each comes from
+  int32_t* list;                  // [num_seqs][hkv][pitch]: where each comes from
   int num_blocks, hkv, block_size, head_dim, num_seqs, max_blocks, max_seq_len, keep_last;
+  int64_t pitch;                  // max_seq_len in whole batches of 128
 };
 
 // LM-head projection logits = h W^T with the row statistics of its 128-column tiles.

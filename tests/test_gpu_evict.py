@@ -121,6 +121,9 @@ EVICT = [
     (3, 128, 16, [700, 300], [0, -3], [5, 5], 7),
     (2, 128, 32, [1024, 2048, 1025], [10, 2000, 1024], [3, 16, 1], 2000),
     (1, 128, 16, [40] * 90, list(range(90)), [i % 9 for i in range(90)], 3),
+    (2, 64, 16, [16384, 16385, 20000], [8000, 16384, 19000], [0, 4, 40], 50),     # longer than what a workgroup holds
+    (1, 64, 32, [40000], [3], [1], 1),
+    (1, 64, 32, [33000], [33000 - 1], None, 17000),
 ]
 
 
