@@ -573,7 +573,8 @@ int spexis_attention_weights(const void* k_cache, int32_t num_blocks, int32_t nu
   spexis::WeightParams p{k_cache, query_start_loc, seq_lens, block_tables, q, lse, accepted_len, weights_in, weights,
                          num_blocks, num_kv_heads, block_size, head_dim, num_seqs, max_blocks_per_seq, total_tokens,
                          max_query_len, max_seq_len, num_q_heads, num_q_heads / num_kv_heads,
-                         (float)((double)scale * 1.4426950408889634)};
+                         // (0 counts as the least that a masked score, infinite, can be multiplied with)
+                         scale == 0.f ? 1e-37f : (float)((double)scale * 1.4426950408889634)};
   return hip_result(spexis::launch_weights(p, (hipStream_t)stream), name);
 }
 

@@ -258,18 +258,30 @@ __global__ __launch_bounds__(256) void evict_move_kernel(EvictParams p) {
     constexpr int kLanes = BS / 2;   // lanes a block
     const int row = lane / 16, unit = (lane % 16) / 2, hf = lane % 2;
     const int last = list[m - 1], last_group = last >> 7;
-    // the block of this lane's bytes of a group (no farther than the last key that stays), and those bytes
-    auto find = [&](int g) { return table[min(min(g, last_group) * 128 + lane / kLanes * BS, last) / BS]; };
-    auto load = [&](int block) {
+    // The blocks of a window of groups come with one load, a window ahead; a lane's is handed to it.  (No farther than the
+    // last key that stays.)
+    constexpr int kPer = 128 / BS, kWindow = 64 / kPer;
+    auto look_up = [&](int w) { return table[min(w * 64 + lane, last / BS)]; };
+    int window = (list[first] >> 7) / kWindow, blocks = look_up(window), blocks_next = look_up(window + 1);
+    auto load = [&](int g) {   // for g in order
+      g = min(g, last_group);
+      if (g / kWindow > window) {
+        ++window;
+        blocks = blocks_next;
+        blocks_next = look_up(window + 1);
+      }
+      const int block = __builtin_amdgcn_ds_bpermute(4 * (g % kWindow * kPer + lane / kLanes), blocks);
       return ld16(v + ((int64_t)clampi(block, 0, p.num_blocks - 1) * p.hkv + h) * (BS * D) + (lane % kLanes) * 8);
     };
     // the lane's 8 new places of a batch: position hf * 8 + e of a unit of 16 holds slot 8 (e / 4) + 4 hf + e % 4
     auto place = [&](int t0, int e) { return t0 + unit * 16 + 8 * (e >> 2) + 4 * hf + (e & 3); };
     int t0 = first & ~127, g = list[first] >> 7;
     i32x4 s0 = *reinterpret_cast<const i32x4*>(list + place(t0, 0)), s1 = *reinterpret_cast<const i32x4*>(list + place(t0, 4));
-    // groups g + 1 and g + 2 are on their way, the blocks of g + 3 looked up
-    int b0 = find(g), b1 = find(g + 1), b2 = find(g + 2), b3 = find(g + 3);
-    u32x4 now = load(b0), next = load(b1), after = load(b2);
+    constexpr int kAhead = 3;   // groups on their way
+    u32x4 ahead[kAhead];
+    const u32x4 now = load(g);
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) ahead[i] = load(g + 1 + i);
     sm[lane] = now;
     wave_lds_fence();
     for (; t0 < m; t0 += 128) {
@@ -286,24 +298,25 @@ __global__ __launch_bounds__(256) void evict_move_kernel(EvictParams p) {
         s1 = *reinterpret_cast<const i32x4*>(list + place(t0 + 128, 4));
       }
       uint32_t x[8];
+      int at[8];   // where in a group, and which (what is in other groups is read too, and left)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] = 0;
+      for (int e = 0; e < 8; ++e) {
+        const int s = src[e] & 127;
+        at[e] = s / BS * (4 * BS) + row * BS + ((s % BS & ~12) | ((s >> 2 & 1) << 3) | ((s >> 3 & 1) << 2));
+        x[e] = 0;
+      }
       while (true) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const int s = src[e] & 127;
-          const int at = s / BS * (4 * BS) + row * BS + ((s % BS & ~12) | ((s >> 2 & 1) << 3) | ((s >> 3 & 1) << 2));
-          const uint32_t y = reinterpret_cast<const uint16_t*>(sm)[at];
-          x[e] = src[e] >> 7 == g ? y : x[e];
-        }
+        for (int e = 0; e < 8; ++e)
+          x[e] |= reinterpret_cast<const uint16_t*>(sm)[at[e]] & (src[e] >> 7 == g ? 0xFFFFu : 0u);
         if (g >= until) break;
         wave_lds_fence();
-        sm[lane] = next;
+        sm[lane] = ahead[0];
         wave_lds_fence();
         ++g;
-        next = after;
-        after = load(b3);
-        b3 = find(g + 3);
+#pragma unroll
+        for (int i = 0; i + 1 < kAhead; ++i) ahead[i] = ahead[i + 1];
+        ahead[kAhead - 1] = load(g + kAhead);
       }
       const int t = place(t0, 0);   // the chunk's first slot; its last is 11 on
       uint16_t* to = v + to_chunk + row * BS + (t % BS & 16) + 8 * hf;

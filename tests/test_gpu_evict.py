@@ -82,6 +82,21 @@ def test_weights_against_64_bits(shape, add):
         assert np.array_equal(own.double().cpu().numpy()[mask], got[mask])
 
 
+@pytest.mark.parametrize("scale", [0.0, -0.1, 1e-30])
+def test_scales(scale):
+    r = np.random.default_rng(7)
+    qsl, S, tables, blocks = batch([30, 2], [100, 7], 16, 7)
+    c = Cache(blocks, 16, 2, 64, r, False)
+    q = queries(32, 6, 64, r)
+    k, v = c.pools()
+    scale = float(np.float32(scale))
+    _, lse = attend(c, (k, v), qsl, S, tables, q, scale)
+    got = weigh(c, k, qsl, S, tables, q, scale, lse, None).double().cpu().numpy()
+    want, size = osv.attention_weights(c.k, qsl, S, tables, q.double().cpu().numpy(), scale, lse.double().cpu().numpy(), None)
+    mask = np.broadcast_to(used_places(S, tables, blocks, 16)[:, None, :], got.shape)
+    assert (np.abs(got - want) <= U * size + 1e-30)[mask].all()
+
+
 def test_weights_of_a_row_sum_to_its_heads():
     """Every query token's weights sum to 1 a head."""
     r = np.random.default_rng(2)
