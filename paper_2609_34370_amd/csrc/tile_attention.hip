@@ -92,22 +92,26 @@ __device__ __forceinline__ int tile_end(const TileAttnParams& p, const Segment& 
 }
 
 struct Unit {
+  Segment g;
   int seg, tile, part, parts, first;   // part of `parts` equal ones of the tile's keys; `first`: the unit of part 0
 };
 
-// The unit u of a head (false: there are fewer).  All threads of the workgroup call it; they look at 256 segments at a
-// time.  Where units are parts of tiles, a part is about `share` key tiles: sum(ceil(nt / share)) units.
+// The unit u of a head (false: there are fewer).  All threads of the workgroup call it, a segment each at a time; the one whose
+// segment has the unit hands it on.  Where units are parts of tiles, a part is about `share` key tiles: sum(ceil(nt / share))
+// units.
 __device__ __forceinline__ bool find_unit(const TileAttnParams& p, int u, Unit& o) {
   __shared__ int64_t sm_total[4];
-  __shared__ int sm_scan[4], sm_unit[5];
+  __shared__ int sm_rows[4], sm_scan[2][4];
+  __shared__ __attribute__((aligned(16))) int sm_unit[12];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int ns = p.num_groups + p.num_seqs;
+  Segment g{};
   int tiles = 0, nt = 0;
   auto load = [&](int base) {
     const int s = base + tid;
     tiles = nt = 0;
     if (s < ns) {
-      const Segment g = segment(p, s);
+      g = segment(p, s);
       tiles = row_tiles(g);
       nt = key_tiles(g);
     }
@@ -125,48 +129,46 @@ __device__ __forceinline__ bool find_unit(const TileAttnParams& p, int u, Unit& 
     rows = wave_sum_i32(rows);
     if (lane == 0) {
       sm_total[wave] = sum;
-      sm_scan[wave] = rows;
+      sm_rows[wave] = rows;
     }
     __syncthreads();
     sum = sm_total[0] + sm_total[1] + sm_total[2] + sm_total[3];
-    rows = sm_scan[0] + sm_scan[1] + sm_scan[2] + sm_scan[3];
+    rows = sm_rows[0] + sm_rows[1] + sm_rows[2] + sm_rows[3];
     const int64_t goal = tile_attn_parts(p.shares, rows);
     share = (int)min((int64_t)INT32_MAX, max((sum + goal - 1) / goal, (int64_t)kTileLeast));
-    __syncthreads();
   }
-  int before = 0;
-  if (tid == 0) sm_unit[0] = -1;
-  __syncthreads();
-  for (int base = 0; base < ns; base += 256) {
+  int before = 0, turn = 0;
+  for (int base = 0; base < ns; base += 256, turn ^= 1) {
     if (p.shares == 0 || ns > 256) load(base);
-    const int parts = (int)min((int64_t)1 << 20, ((int64_t)nt + share - 1) / share), mine = tiles * max(parts, 1);
+    const int parts = max((int)min((int64_t)1 << 20, ((int64_t)nt + share - 1) / share), 1), mine = tiles * parts;
     const int incl = wave_incl_scan_i32(mine, lane);
-    if (lane == 63) sm_scan[wave] = incl;
+    if (lane == 63) sm_scan[turn][wave] = incl;
     __syncthreads();
-    int at = before + incl - mine, all = 0;
+    int at = before + incl - mine;
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
-      if (w < wave) at += sm_scan[w];
-      all += sm_scan[w];
+      const int x = sm_scan[turn][w];
+      if (w < wave) at += x;
+      before += x;
     }
     if (u >= at && u < at + mine) {
-      const int n = max(parts, 1), t = (u - at) / n;
-      sm_unit[0] = base + tid;
-      sm_unit[1] = t;
-      sm_unit[2] = (u - at) % n;
-      sm_unit[3] = n;
-      sm_unit[4] = at + t * n;
+      const int t = (u - at) / parts;
+      *reinterpret_cast<u32x4*>(sm_unit) = u32x4{(uint32_t)g.q0, (uint32_t)g.rows, (uint32_t)g.seq, (uint32_t)g.base};
+      *reinterpret_cast<u32x4*>(sm_unit + 4) = u32x4{(uint32_t)g.end, (uint32_t)g.last, (uint32_t)g.group, (uint32_t)(base + tid)};
+      *reinterpret_cast<u32x4*>(sm_unit + 8) = u32x4{(uint32_t)t, (uint32_t)((u - at) % parts), (uint32_t)parts, (uint32_t)(at + t * parts)};
     }
-    before += all;
-    __syncthreads();
     if (before > u) break;   // (the same for all threads)
   }
-  o.seg = __builtin_amdgcn_readfirstlane(sm_unit[0]);
-  o.tile = __builtin_amdgcn_readfirstlane(sm_unit[1]);
-  o.part = __builtin_amdgcn_readfirstlane(sm_unit[2]);
-  o.parts = __builtin_amdgcn_readfirstlane(sm_unit[3]);
-  o.first = __builtin_amdgcn_readfirstlane(sm_unit[4]);
-  return o.seg >= 0;
+  if (before <= u) return false;
+  __syncthreads();
+  auto get = [&](int i) { return __builtin_amdgcn_readfirstlane(sm_unit[i]); };
+  o.g = {get(0), get(1), get(2), get(3), get(4), get(5), get(6)};
+  o.seg = get(7);
+  o.tile = get(8);
+  o.part = get(9);
+  o.parts = get(10);
+  o.first = get(11);
+  return true;
 }
 
 }  // namespace
@@ -186,11 +188,10 @@ void tile_attn_kernel(TileAttnParams p) {
   const int h = (int)blockIdx.x % p.hkv, u = (int)blockIdx.x / p.hkv;
 
   if (tid < D) sm_odd[tid] = INT32_MAX;
-  Unit un;
+  Unit un{};
   bool some = find_unit(p, u, un);
-  if (un.seg < p.num_groups && u >= p.prefix_units) some = false;   // groups that overlap
-  Segment g{};
-  if (some) g = segment(p, un.seg);
+  if (some && un.seg < p.num_groups && u >= p.prefix_units) some = false;   // groups that overlap
+  const Segment g = un.g;
   // the tiles of a sequence that see most keys first
   const int tile = some ? row_tiles(g) - 1 - un.tile : 0;
   const bool is_prefix = un.seg < p.num_groups;
