@@ -243,21 +243,26 @@ int64_t most_row_tiles(int64_t seqs, int64_t group, int64_t total_tokens, int64_
 struct TileLayout {
   int64_t units, prefix_units, groups_hdr, ws_prefix, ws_seq, total;   // offsets in bytes
   int shares, pitch;
-  bool partial;
+  bool shared, merge;
 };
 
-// Units, and where their partials lie.  Tiles are cut into parts where prefixes are shared (few tiles with many keys beside
-// many with few), and where one tile a workgroup would not fill the chip.
+// Units, and where their partials lie.  Prefixes count where sequences are longer than the least part (4 sequences of up to
+// 265 keys behind 160 that they share: 11 us as they are, 17 with the prefix apart).  They run together with the sequences up
+// to two workgroups a place that the chip has, and all tiles are cut into parts then, else the prefixes' alone.  Without
+// prefixes tiles are cut where one a workgroup fills less than half of the chip and there are keys enough for two parts.
 TileLayout tile_layout(int64_t seqs, int64_t groups, int64_t hq, int64_t hkv, int64_t head_dim, int64_t total_tokens,
-                       int64_t max_query_len) {
+                       int64_t max_query_len, int64_t max_seq_len) {
   TileLayout l{};
   const int64_t group = hq / hkv;
-  const int64_t pre = groups > 0 ? most_row_tiles(groups, group, total_tokens, total_tokens) : 0;
+  const bool is_long = max_seq_len > spexis::kTileLeast * spexis::kTileKeys;
+  l.shared = groups > 0 && is_long;
+  const int64_t pre = l.shared ? most_row_tiles(groups, group, total_tokens, total_tokens) : 0;
   const int64_t own = most_row_tiles(seqs, group, total_tokens, max_query_len);
-  l.partial = groups > 0 || own * hkv <= spexis::kTileSlots;
-  l.shares = l.partial ? (int)std::max<int64_t>(1, spexis::kTileSlots / hkv) : 0;
-  l.prefix_units = groups > 0 ? pre + l.shares : 0;
-  l.units = pre + own + l.shares;
+  const int shares = (int)std::max<int64_t>(1, spexis::kTileSlots / hkv);
+  l.merge = l.shared ? (pre + own) * hkv <= 2 * spexis::kTileSlots : is_long && own * hkv <= spexis::kTileSlots / 2;
+  l.shares = l.shared || l.merge ? shares : 0;
+  l.prefix_units = l.shared ? pre + shares : 0;
+  l.units = own + (l.merge ? pre + shares : 0);
   l.pitch = (int)std::min<int64_t>(spexis::kTileRows, group * max_query_len);
   int64_t off = 0;
   auto take = [&](int64_t bytes) {
@@ -265,12 +270,10 @@ TileLayout tile_layout(int64_t seqs, int64_t groups, int64_t hq, int64_t hkv, in
     off += round_up(bytes, 256);
     return at;
   };
-  if (l.partial) {
-    take(l.units * spexis::kTileHdrInts * 4);
-    l.groups_hdr = take(groups * 16);
-    l.ws_prefix = take(l.prefix_units * hkv * spexis::tile_slot_floats(spexis::kTileRows, (int)head_dim) * 4);
-    l.ws_seq = take(l.units * hkv * spexis::tile_slot_floats(l.pitch, (int)head_dim) * 4);
-  }
+  if (l.merge) take(l.units * spexis::kTileHdrInts * 4);
+  l.groups_hdr = take(l.shared ? groups * 16 : 0);
+  l.ws_prefix = take(l.prefix_units * hkv * spexis::tile_slot_floats(spexis::kTileRows, (int)head_dim) * 4);
+  l.ws_seq = l.merge ? take(l.units * hkv * spexis::tile_slot_floats(l.pitch, (int)head_dim) * 4) : 0;
   l.total = std::max<int64_t>(off, 16);
   return l;
 }
@@ -281,7 +284,8 @@ size_t tile_workspace_size(int32_t num_seqs, int32_t num_groups, int32_t num_q_h
       head_dim <= 0 || total_tokens <= 0 || max_query_len <= 0 || max_seq_len <= 0 ||
       (int64_t)total_tokens * num_q_heads >= (1ll << 31))
     return 0;
-  return (size_t)tile_layout(num_seqs, num_groups, num_q_heads, num_kv_heads, head_dim, total_tokens, max_query_len).total;
+  return (size_t)tile_layout(num_seqs, num_groups, num_q_heads, num_kv_heads, head_dim, total_tokens, max_query_len,
+                             max_seq_len).total;
 }
 
 // The four attention calls over many rows: their checks and the launch.  groups < 0: a call without shared prefixes.
@@ -314,9 +318,11 @@ int tile_attention(const char* name, bool in8, const void* k_cache, const void* 
   if (misaligned({k_cache, v_cache, scales, q, out, workspace}))
     return fail(SPEXIS_ERR_INVALID_ARGUMENT, "%s: a pointer that is not 16-byte aligned", name);
   if (q == out) return fail(SPEXIS_ERR_INVALID_ARGUMENT, "%s: out aliases q", name);
-  const TileLayout l = tile_layout(num_seqs, num_groups, num_q_heads, num_kv_heads, head_dim, total_tokens, max_query_len);
+  const TileLayout l = tile_layout(num_seqs, num_groups, num_q_heads, num_kv_heads, head_dim, total_tokens, max_query_len,
+                                   max_seq_len);
   // a launch holds fewer than 2^32 threads
-  if (l.units * num_kv_heads * 256 >= (1ll << 32)) return fail(SPEXIS_ERR_UNSUPPORTED, "%s: too many tokens or slots", name);
+  if (std::max(l.units, l.prefix_units) * num_kv_heads * 256 >= (1ll << 32))
+    return fail(SPEXIS_ERR_UNSUPPORTED, "%s: too many tokens or slots", name);
   if (!workspace || workspace_bytes < (size_t)l.total)
     return fail(SPEXIS_ERR_WORKSPACE_TOO_SMALL, "%s: workspace %zu bytes < %zu needed", name, workspace_bytes,
                 (size_t)l.total);
@@ -342,7 +348,7 @@ int tile_attention(const char* name, bool in8, const void* k_cache, const void* 
   p.block_size = block_size;
   p.head_dim = head_dim;
   p.num_seqs = num_seqs;
-  p.num_groups = num_groups;
+  p.num_groups = l.shared ? num_groups : 0;
   p.max_blocks = max_blocks_per_seq;
   p.total_tokens = total_tokens;
   p.max_query_len = max_query_len;
@@ -350,9 +356,9 @@ int tile_attention(const char* name, bool in8, const void* k_cache, const void* 
   p.group = num_q_heads / num_kv_heads;
   p.pitch = l.pitch;
   p.shares = l.shares;
+  p.merge = l.merge ? 1 : 0;
   p.units = (int)l.units;
   p.prefix_units = (int)l.prefix_units;
-  p.partial = l.partial ? 1 : 0;
   // the kernel takes maxima of scores before their scale, which is positive there: a negative one turns q's signs over, and
   // 0 counts as the least that a masked score (minus infinity) can be multiplied with
   p.q_sign = scale < 0.f ? 0x80008000u : 0u;

@@ -167,7 +167,7 @@ __host__ __device__ inline int64_t attn_ws_bytes(int nwaves, int rmax, int D) {
 // head that step through kTileKeys keys at a time.
 constexpr int kTileRows = 128, kTileKeys = 64;
 constexpr int kTileHdrInts = 8;
-constexpr int kTileLeast = 4;     // the fewest key tiles of a part
+constexpr int kTileLeast = 8;     // the fewest key tiles of a part
 constexpr int kTileSlots = 512;   // workgroups that run at a time: two a CU
 struct TileAttnParams {
   const void* k_cache;
@@ -188,9 +188,10 @@ struct TileAttnParams {
   int num_blocks, hkv, block_size, head_dim, num_seqs, num_groups, max_blocks, total_tokens, max_query_len;
   int hq, group;
   int pitch;                    // most rows of a sequence's tile
-  int shares;                   // row tiles are cut into parts, about so many a head; 0: they are not
-  int units, prefix_units;      // the most units a head, and of them in prefixes
-  int partial;                  // partials are written and joined
+  int shares;                   // row tiles (without a merge those of prefixes alone) are cut into parts, about so many a head; 0: not
+  int units, prefix_units;      // the most units a head of either launch
+  int merge;                    // prefixes and sequences in one launch, tile_merge_kernel joins partials
+  int seg_lo, seg_hi;           // (launcher) its segments: the groups' prefixes are 0 .. num_groups - 1, then the sequences
   uint32_t q_sign;              // a negative scale turns q's signs over
   float scale_log2e, lazy;      // |scale| log2(e); kLazy in scores before the scale
 };

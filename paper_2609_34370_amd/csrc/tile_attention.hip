@@ -2,12 +2,14 @@
 // batches whose sequences begin with a prefix that they share.
 //
 // Work decomposition.  A segment is a run of query tokens against a run of keys: a sequence against the keys that are its
-// own, causally; and, where a group of sequences shares a prefix, all tokens of the group against that prefix, once.  With
-// G query heads a KV head, a segment has G rows a token, in tiles of 128: row r is (token r / G, head r % G), so every row
-// of a tile reads the same K and V.  A unit, one workgroup, is a tile against the keys that any of its rows sees, or, where
-// there are too few tiles to fill the chip, against one of several equal parts of them.  A unit that is the whole of its
-// rows writes outputs; the others leave fp32 partials (reference maximum, sum, unnormalised output) in the workspace,
-// which tile_merge_kernel joins.
+// own, causally; and, where a group of sequences shares a prefix, all tokens of the group against that prefix, once.  With G query heads a KV head, a segment has G rows a token, in tiles of 128: row r is (token r / G, head
+// r % G), so every row of a tile reads the same K and V.  A unit, one workgroup, is a tile against the keys that any of its
+// rows sees, or, where there are too few tiles to fill the chip, against one of several equal parts of them.  Prefixes and
+// parts leave fp32 partials (reference maximum, sum, unnormalised output) in the workspace.  With few units prefixes and
+// sequences run together, and tile_merge_kernel joins what they leave; with many the prefixes run in a launch in front, and a
+// unit that has all of a sequence's own keys joins the prefix's partials to its registers (512 sequences of 9 tokens, 28
+// query heads over 4, in 16 groups: 219 us for 246, which had written and read 134 MB more; 64 sequences of 5 behind one
+// prefix of 4096 keys: together 68 us, 75 one after the other).
 //
 // Each of the four waves owns 32 rows.  The 64 keys of a step pass through LDS, where all waves read them: fetched into
 // registers one step ahead, widened there from the 8-bit cache, and stored in the order in which a wave reads matrix
@@ -43,9 +45,10 @@ __device__ __forceinline__ int prefix_of(const TileAttnParams& p, int b, int* gr
     if (p.group_start[mid] <= b) lo = mid;
     else hi = mid;
   }
-  if (p.group_start[lo] > b || p.group_start[lo + 1] <= b) return 0;
+  const int first = p.group_start[lo], behind = p.group_start[lo + 1], len = p.prefix_lens[lo];   // together
+  if (first > b || behind <= b) return 0;
   *group = lo;
-  return clampi(p.prefix_lens[lo], 0, p.max_blocks * p.block_size) & ~(p.block_size - 1);
+  return clampi(len, 0, p.max_blocks * p.block_size) & ~(p.block_size - 1);
 }
 
 // Segment s: the groups' prefixes, then the sequences.  Clamped so that every address derived from it stays in its buffer.
@@ -72,13 +75,14 @@ __device__ __forceinline__ Segment segment(const TileAttnParams& p, int s) {
     return g;
   }
   const int b = s - p.num_groups;
-  g.q0 = clampi(p.qsl[b], 0, p.total_tokens);
-  const int n = min(clampi(p.qsl[b + 1], g.q0, p.total_tokens) - g.q0, p.max_query_len);
+  const int q0 = p.qsl[b], q1 = p.qsl[b + 1], len = p.seq_lens[b], shared = prefix_of(p, b, &g.group);
+  g.q0 = clampi(q0, 0, p.total_tokens);
+  const int n = min(clampi(q1, g.q0, p.total_tokens) - g.q0, p.max_query_len);
   g.rows = n * p.group;
   g.seq = b;
-  g.end = clampi(p.seq_lens[b], max(n, 1), p.max_blocks * p.block_size);
+  g.end = clampi(len, max(n, 1), p.max_blocks * p.block_size);
   g.last = g.end - n;
-  g.base = min(prefix_of(p, b, &g.group), g.last & ~(p.block_size - 1));
+  g.base = min(shared, g.last & ~(p.block_size - 1));
   if (g.base == 0) g.group = -1;
   return g;
 }
@@ -96,7 +100,7 @@ struct Unit {
   int seg, tile, part, parts, first;   // part of `parts` equal ones of the tile's keys; `first`: the unit of part 0
 };
 
-// The unit u of a head (false: there are fewer).  All threads of the workgroup call it, a segment each at a time; the one whose
+// The unit u of a head, of the launch's segments [seg_lo, seg_hi) (false: there are fewer).  All threads of the workgroup call it, a segment each at a time; the one whose
 // segment has the unit hands it on.  Where units are parts of tiles, a part is about `share` key tiles: sum(ceil(nt / share))
 // units.
 __device__ __forceinline__ bool find_unit(const TileAttnParams& p, int u, Unit& o) {
@@ -104,13 +108,13 @@ __device__ __forceinline__ bool find_unit(const TileAttnParams& p, int u, Unit& 
   __shared__ int sm_rows[4], sm_scan[2][4];
   __shared__ __attribute__((aligned(16))) int sm_unit[12];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int ns = p.num_groups + p.num_seqs;
+  const int ns = p.seg_hi - p.seg_lo;
   Segment g{};
   int tiles = 0, nt = 0;
   auto load = [&](int base) {
-    const int s = base + tid;
+    const int s = p.seg_lo + base + tid;
     tiles = nt = 0;
-    if (s < ns) {
+    if (s < p.seg_hi) {
       g = segment(p, s);
       tiles = row_tiles(g);
       nt = key_tiles(g);
@@ -154,7 +158,7 @@ __device__ __forceinline__ bool find_unit(const TileAttnParams& p, int u, Unit& 
     if (u >= at && u < at + mine) {
       const int t = (u - at) / parts;
       *reinterpret_cast<u32x4*>(sm_unit) = u32x4{(uint32_t)g.q0, (uint32_t)g.rows, (uint32_t)g.seq, (uint32_t)g.base};
-      *reinterpret_cast<u32x4*>(sm_unit + 4) = u32x4{(uint32_t)g.end, (uint32_t)g.last, (uint32_t)g.group, (uint32_t)(base + tid)};
+      *reinterpret_cast<u32x4*>(sm_unit + 4) = u32x4{(uint32_t)g.end, (uint32_t)g.last, (uint32_t)g.group, (uint32_t)(p.seg_lo + base + tid)};
       *reinterpret_cast<u32x4*>(sm_unit + 8) = u32x4{(uint32_t)t, (uint32_t)((u - at) % parts), (uint32_t)parts, (uint32_t)(at + t * parts)};
     }
     if (before > u) break;   // (the same for all threads)
@@ -169,6 +173,22 @@ __device__ __forceinline__ bool find_unit(const TileAttnParams& p, int u, Unit& 
   o.parts = get(10);
   o.first = get(11);
   return true;
+}
+
+// Where the partials of the prefix of row r of a sequence (first query token q0) lie: slots first .. first + n - 1, row `row` of
+// each.  Headers that no unit wrote (inconsistent inputs) lead no farther than the workspace.
+struct PrefixParts {
+  int first, n, row;
+};
+__device__ __forceinline__ PrefixParts prefix_parts(const TileAttnParams& p, int group, int q0, int r) {
+  const u32x4 g = *reinterpret_cast<const u32x4*>(p.groups_hdr + (int64_t)group * 4);   // first token, tiles, parts, first unit
+  const int row = (int)min((int64_t)max(q0 - (int)g[0], 0) * p.group + r, (int64_t)p.total_tokens * p.group), tile = row / kRows;
+  PrefixParts o;
+  // units count tiles from the last
+  o.first = (int)min(max((int64_t)(int)g[3] + ((int64_t)(int)g[1] - 1 - tile) * (int)g[2], (int64_t)0), (int64_t)p.prefix_units);
+  o.n = clampi((int)g[2], 0, p.prefix_units - o.first);
+  o.row = row % kRows;
+  return o;
 }
 
 }  // namespace
@@ -189,22 +209,25 @@ void tile_attn_kernel(TileAttnParams p) {
 
   if (tid < D) sm_odd[tid] = INT32_MAX;
   Unit un{};
-  bool some = find_unit(p, u, un);
-  if (some && un.seg < p.num_groups && u >= p.prefix_units) some = false;   // groups that overlap
+  const bool some = find_unit(p, u, un);
   const Segment g = un.g;
   // the tiles of a sequence that see most keys first
   const int tile = some ? row_tiles(g) - 1 - un.tile : 0;
-  const bool is_prefix = un.seg < p.num_groups;
-  const bool whole = !is_prefix && un.parts == 1 && g.group < 0;
-  if (p.partial && h == 0 && tid == 0) {   // what the merge needs to know
-    int32_t* hdr = p.units_hdr + (int64_t)u * kTileHdrInts;
-    const bool joins = some && !is_prefix && un.part == 0 && !whole;
-    *reinterpret_cast<u32x4*>(hdr) =
-        u32x4{joins ? 1u : 0u, (uint32_t)g.q0, (uint32_t)(joins ? g.rows - tile * kRows : 0), (uint32_t)tile};
-    *reinterpret_cast<u32x4*>(hdr + 4) = u32x4{(uint32_t)un.parts, (uint32_t)un.first, (uint32_t)g.group, 0u};
-    if (some && is_prefix && un.tile == 0 && un.part == 0)
+  const bool is_prefix = some && un.seg < p.num_groups;
+  // joins the prefix's partials itself: they were written by the launch before
+  const bool whole = some && !is_prefix && un.parts == 1 && (g.group < 0 || p.seg_lo > 0);
+  if (is_prefix && u >= p.prefix_units) return;   // groups that overlap
+  if (h == 0 && tid == 0) {   // what those who join the partials need to know
+    if (is_prefix && un.tile == 0 && un.part == 0)
       *reinterpret_cast<u32x4*>(p.groups_hdr + (int64_t)un.seg * 4) =
           u32x4{(uint32_t)g.q0, (uint32_t)row_tiles(g), (uint32_t)un.parts, (uint32_t)un.first};
+    if (p.merge) {
+      int32_t* hdr = p.units_hdr + (int64_t)u * kTileHdrInts;
+      const bool joins = some && !is_prefix && un.part == 0 && !whole;
+      *reinterpret_cast<u32x4*>(hdr) =
+          u32x4{joins ? 1u : 0u, (uint32_t)g.q0, (uint32_t)(joins ? g.rows - tile * kRows : 0), (uint32_t)tile};
+      *reinterpret_cast<u32x4*>(hdr + 4) = u32x4{(uint32_t)un.parts, (uint32_t)un.first, (uint32_t)g.group, 0u};
+    }
   }
   if (!some) return;
 
@@ -319,6 +342,13 @@ void tile_attn_kernel(TileAttnParams p) {
     }
   };
 
+  if (k0 < k1) {
+    find_k(k0);
+    find_v(k0);
+    load_k(k0);
+    load_v(k0);
+  }
+
   // ---- this wave's rows
   const int rw = row0 + wave * 32;
   const bool active = rw < g.rows;
@@ -341,18 +371,24 @@ void tile_attn_kernel(TileAttnParams p) {
     for (int e = 0; e < 16; ++e) acc[mt][e] = 0.f;
 
   if (k0 < k1) {
-    find_k(k0);
-    find_v(k0);
-    load_k(k0);
-    load_v(k0);
     store_k(0);
     store_v(0, k0);
+    if (k0 + 1 < k1) {
+      load_k(k0 + 1);
+      load_v(k0 + 1);
+    }
   }
   for (int t = k0; t < k1; ++t) {
     const int buf = (t - k0) & 1;
     __syncthreads();
-    const bool more = t + 1 < k1;
-    if (more) load_k(t + 1);
+    if (t + 1 < k1) {
+      store_k(buf ^ 1);
+      store_v(buf ^ 1, t + 1);
+    }
+    if (t + 2 < k1) {
+      load_k(t + 2);
+      load_v(t + 2);
+    }
     const int t0 = g.base + t * kKeys;
     f32x16 sc[2];
     if (active) {
@@ -364,10 +400,6 @@ void tile_attn_kernel(TileAttnParams p) {
         for (int s = 0; s < KS; ++s)
           sc[kt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(sm[buf][0][kt * KS + s][lane]), as_bf16x8(qf[s]), sc[kt], 0, 0, 0);
       }
-    }
-    if (more) {
-      store_k(buf ^ 1);
-      load_v(t + 1);
     }
     if (active) {
       const bool need_mask = t0 + kKeys - 1 > sure;
@@ -419,7 +451,6 @@ void tile_attn_kernel(TileAttnParams p) {
         for (int mt = 0; mt < MT; ++mt)
           acc[mt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(sm[buf][1][s2 * MT + mt][lane]), as_bf16x8(pw[s2]), acc[mt], 0, 0, 0);
     }
-    if (more) store_v(buf ^ 1, t + 1);
   }
 
   // ---- outputs, through LDS (each wave its own quarter), so that a store instruction writes whole lines
@@ -436,7 +467,27 @@ void tile_attn_kernel(TileAttnParams p) {
           if (lim >= sm_odd[32 * mt + 8 * (e >> 2) + 4 * half + (e & 3)]) acc[mt][e] = __builtin_nanf("");
     }
   }
-  const float lt = halves_sum(l);
+  float lt = halves_sum(l);
+  float mb = m * p.scale_log2e;   // in the base-2 domain
+  if (whole && g.group >= 0) {    // the prefix's partials of the lane's row
+    const PrefixParts parts = prefix_parts(p, g.group, g.q0, r);
+    for (int c = 0; c < parts.n; ++c) {
+      const float* slot = p.ws_prefix + ((int64_t)(parts.first + c) * p.hkv + h) * tile_slot_floats(kRows, D);
+      const float mc = slot[kRows * D + parts.row], lc = slot[kRows * (D + 1) + parts.row];
+      f32x4 o[MT][4];
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+        for (int a = 0; a < 4; ++a) o[mt][a] = *reinterpret_cast<const f32x4*>(slot + parts.row * D + 32 * mt + 8 * a + 4 * half);
+      const float mn = fmaxf(mb, mc), x = fast_exp2(mb - mn), y = fast_exp2(mc - mn);
+      lt = lt * x + lc * y;
+      mb = mn;
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[mt][e] = acc[mt][e] * x + o[mt][e >> 2][e & 3] * y;
+    }
+  }
   u32x4* const scr = &sm[0][0][0][0] + wave * kFrags * kWave;
   const int left = g.rows - rw;   // rows of this wave
   if (whole) {
@@ -458,7 +509,7 @@ void tile_attn_kernel(TileAttnParams p) {
         st16(reinterpret_cast<uint16_t*>(p.out) + ((int64_t)(g.q0 + rr / p.group) * p.hq + h * p.group + rr % p.group) * D + 8 * c,
              scr[row * kOc + (c ^ (row & (kOc - 1)))]);
     }
-    if (p.lse && half == 0 && col < left) p.lse[qrow] = (m * p.scale_log2e + __builtin_amdgcn_logf(lt)) * kLn2;
+    if (p.lse && half == 0 && col < left) p.lse[qrow] = (mb + __builtin_amdgcn_logf(lt)) * kLn2;
   } else {
     // the partial: [pitch][D], then maxima (in the base-2 domain) and sums
     const int pitch = is_prefix ? kRows : p.pitch;
@@ -481,14 +532,14 @@ void tile_attn_kernel(TileAttnParams p) {
       if (row < left) st16(slot + (int64_t)(wave * 32 + row) * D + 4 * c, scr[row * kFc + (c ^ (row & (kFc - 1)))]);
     }
     if (half == 0 && col < left) {
-      slot[(int64_t)pitch * D + wave * 32 + col] = m * p.scale_log2e;
+      slot[(int64_t)pitch * D + wave * 32 + col] = mb;
       slot[(int64_t)pitch * (D + 1) + wave * 32 + col] = lt;
     }
   }
 }
 
-// Joins the partials of the rows that are no unit's whole: workgroup (unit, head, 16 rows) for the first unit of a
-// sequence's tile; the tile's other parts follow it, and the parts of the shared prefix are found by the group.
+// Joins the parts of a sequence's tiles: workgroup (unit, head, 16 rows) for the first unit of a tile in parts; the others
+// follow it, and the parts of the shared prefix are found by the group.
 //   o = sum_c acc_c 2^(m_c - M) / sum_c l_c 2^(m_c - M),   M = max_c m_c
 template <int D>
 __global__ __launch_bounds__(16 * D / 8) void tile_merge_kernel(TileAttnParams p) {
@@ -514,10 +565,9 @@ __global__ __launch_bounds__(16 * D / 8) void tile_merge_kernel(TileAttnParams p
   for (int c = 0; c < parts && first + c < p.units; ++c)
     add(p.ws_seq + ((int64_t)(first + c) * p.hkv + h) * tile_slot_floats(p.pitch, D), p.pitch, lr);
   if (group >= 0) {
-    const u32x4 g = *reinterpret_cast<const u32x4*>(p.groups_hdr + (int64_t)group * 4);
-    const int rg = max(q0 - (int)g[0], 0) * p.group + r, tile = rg / kRows, n = (int)g[2];
-    const int pf = max((int)g[3] + ((int)g[1] - 1 - tile) * n, 0);   // units count tiles from the last
-    for (int c = 0; c < n && pf + c < p.prefix_units; ++c) add(p.ws_prefix + ((int64_t)(pf + c) * p.hkv + h) * tile_slot_floats(kRows, D), kRows, rg % kRows);
+    const PrefixParts parts = prefix_parts(p, group, q0, r);
+    for (int c = 0; c < parts.n; ++c)
+      add(p.ws_prefix + ((int64_t)(parts.first + c) * p.hkv + h) * tile_slot_floats(kRows, D), kRows, parts.row);
   }
   const float inv = 1.0f / den;
   const int64_t row = (int64_t)(q0 + j) * p.hq + h * p.group + r % p.group;
@@ -528,13 +578,28 @@ __global__ __launch_bounds__(16 * D / 8) void tile_merge_kernel(TileAttnParams p
 }
 
 template <int D, int BS>
-static hipError_t launch_tiles_t(const TileAttnParams& p, hipStream_t s) {
-  const dim3 grid((unsigned)((int64_t)p.units * p.hkv));
+static hipError_t launch_units_t(const TileAttnParams& p, int units, hipStream_t s) {
+  const dim3 grid((unsigned)((int64_t)units * p.hkv));
   if (p.scales) hipLaunchKernelGGL((tile_attn_kernel<D, BS, true>), grid, dim3(256), 0, s, p);
   else hipLaunchKernelGGL((tile_attn_kernel<D, BS, false>), grid, dim3(256), 0, s, p);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess || !p.partial) return e;
-  hipLaunchKernelGGL((tile_merge_kernel<D>), dim3(grid.x, (unsigned)((p.pitch + 15) / 16)), dim3(16 * D / 8), 0, s, p);
+  return hipGetLastError();
+}
+
+template <int D, int BS>
+static hipError_t launch_tiles_t(TileAttnParams p, hipStream_t s) {
+  hipError_t e;
+  if (p.num_groups > 0 && !p.merge) {   // the prefixes in front
+    p.seg_hi = p.num_groups;
+    e = launch_units_t<D, BS>(p, p.prefix_units, s);
+    if (e != hipSuccess) return e;
+    p.seg_lo = p.num_groups;
+    p.shares = 0;
+  }
+  p.seg_hi = p.num_groups + p.num_seqs;
+  e = launch_units_t<D, BS>(p, p.units, s);
+  if (e != hipSuccess || !p.merge) return e;
+  hipLaunchKernelGGL((tile_merge_kernel<D>), dim3((unsigned)((int64_t)p.units * p.hkv), (unsigned)((p.pitch + 15) / 16)),
+                     dim3(16 * D / 8), 0, s, p);
   return hipGetLastError();
 }
 

@@ -58,11 +58,12 @@ class Cache:
         return tuple(out)
 
 
-def attend(c, pools, qsl, S, tables, q, scale, groups=None, lse=True, stream=None, space=None):
-    """Outputs and lse; rows that the call does not write hold 777."""
+def attend(c, pools, qsl, S, tables, q, scale, groups=None, lse=True, stream=None, longer=600):
+    """Outputs and lse; rows that the call does not write hold 777.  longer: how far the call's bound is above the longest
+    sequence (where it is at most 512, prefixes are not read apart and tiles not in parts)."""
     T, hq = q.shape[:2]
     n = int(np.diff(qsl).max())
-    most = max(n, 1), int(max(S.max(), 1))
+    most = max(n, 1), int(max(S.max(), 1)) + longer
     out, ls = torch.full_like(q, 777.0), torch.full((T, hq), 777.0, device="cuda") if lse else None
     where = (c.blocks, c.hkv, c.bs, c.D, dev(qsl), dev(S), dev(tables), T, *most)
     if groups is None:
@@ -72,7 +73,7 @@ def attend(c, pools, qsl, S, tables, q, scale, groups=None, lse=True, stream=Non
         size = sx.spexis_shared_attention_workspace_size(len(S), len(groups[1]), hq, c.hkv, c.D, T, *most)
         f = sx.spexis_shared_attention_kv8 if c.in8 else sx.spexis_shared_attention
         more = (dev(np.asarray(groups[0], np.int32)), dev(np.asarray(groups[1], np.int32)))
-    ws = torch.full((size,), 0x7F, dtype=torch.uint8, device="cuda") if space is None else space
+    ws = torch.full((size,), 0x7F, dtype=torch.uint8, device="cuda")
     f(*pools, *where, *more, q, hq, scale, out, ws, lse=ls, stream=stream)
     torch.cuda.synchronize()
     return out, ls
@@ -115,9 +116,9 @@ PROMPTS = [
 ]
 
 
-@pytest.mark.parametrize("in8", [False, True])
+@pytest.mark.parametrize("in8,longer", [(False, 0), (False, 600), (True, 600)])
 @pytest.mark.parametrize("shape", range(len(PROMPTS)))
-def test_prompts_against_64_bits(shape, in8):
+def test_prompts_against_64_bits(shape, in8, longer):
     hq, hkv, D, bs, n, ctx = PROMPTS[shape]
     r = np.random.default_rng(shape)
     qsl, S, tables, blocks = batch(n, ctx, bs, shape)
@@ -125,7 +126,7 @@ def test_prompts_against_64_bits(shape, in8):
     q = queries(int(qsl[-1]), hq, D, r)
     scale = float(np.float32(D ** -0.5))
     say(f"[prompt] {PROMPTS[shape][:4]} 8 bit {in8}")
-    out, lse = attend(c, c.pools(), qsl, S, tables, q, scale)
+    out, lse = attend(c, c.pools(), qsl, S, tables, q, scale, longer=longer)
     check(out, lse, c, qsl, S, tables, q, scale)
 
 
@@ -161,13 +162,14 @@ SHARED = [
     (16, 2, 64, 32, [(96, [(i % 7, i % 4) for i in range(290)])], ([], [])),    # some without query tokens
     (6, 3, 64, 16, [(77, [(20, 3), (31, 1)]), (47, [(0, 2), (1, 1)])], ([], [(9, 1)])),   # prefixes that end inside a block
     (2, 1, 128, 32, [(128, [(0, 200), (300, 1), (5, 40)])], ([], [])),         # prompts behind an instruction
-    (8, 8, 64, 16, [(160, [(11, 2)] * 6)] * 40, ([], [])),
+    (8, 8, 64, 16, [(160, [(11, 2)] * 6)] * 40, ([], [])),                     # prefixes in a launch of their own
+    (56, 8, 64, 32, [(2000, [(i % 50, 9) for i in range(66)]), (0, [(3, 1)] * 30), (320, [(7, 70)] * 20)], ([(9, 2)], [(0, 1)] * 3)),
 ]
 
 
-@pytest.mark.parametrize("in8", [False, True])
+@pytest.mark.parametrize("in8,longer", [(False, 0), (False, 600), (True, 600)])
 @pytest.mark.parametrize("shape", range(len(SHARED)))
-def test_shared_prefixes_against_64_bits(shape, in8):
+def test_shared_prefixes_against_64_bits(shape, in8, longer):
     hq, hkv, D, bs, groups, alone = SHARED[shape]
     r = np.random.default_rng(100 + shape)
     qsl, S, tables, blocks, g = shared_batch(bs, groups, alone, r, shape)
@@ -175,7 +177,7 @@ def test_shared_prefixes_against_64_bits(shape, in8):
     q = queries(int(qsl[-1]), hq, D, r)
     scale = float(np.float32(D ** -0.5))
     say(f"[shared] {SHARED[shape][:4]} 8 bit {in8}")
-    out, lse = attend(c, c.pools(), qsl, S, tables, q, scale, groups=g)
+    out, lse = attend(c, c.pools(), qsl, S, tables, q, scale, groups=g, longer=longer)
     check(out, lse, c, qsl, S, tables, q, scale)
 
 
@@ -290,8 +292,8 @@ def test_without_lse_and_without_groups():
     d, _ = attend(c, p, qsl, S, tables, q, 0.125, lse=False, groups=([0], []))
     assert torch.equal(a, b) and torch.equal(a, d)
     out = torch.zeros_like(q)
-    ws = torch.empty(sx.spexis_shared_attention_workspace_size(2, 0, 6, 2, 64, 43, 40, 703), dtype=torch.uint8, device="cuda")
-    sx.spexis_shared_attention(*p, c.blocks, 2, 32, 64, dev(qsl), dev(S), dev(tables), 43, 40, 703, None, None, q, 6, 0.125, out, ws)
+    ws = torch.empty(sx.spexis_shared_attention_workspace_size(2, 0, 6, 2, 64, 43, 40, 1303), dtype=torch.uint8, device="cuda")
+    sx.spexis_shared_attention(*p, c.blocks, 2, 32, 64, dev(qsl), dev(S), dev(tables), 43, 40, 1303, None, None, q, 6, 0.125, out, ws)
     assert torch.equal(a, out)
 
 
@@ -321,7 +323,7 @@ def test_replays_and_streams(shared):
     for n, ctx in (([30, 5], [500, 20]), ([7, 60, 1], [90, 0, 333])):
         qsl, S, tables, blocks = batch(n, ctx, 16, len(calls))
         c = Cache(blocks, 16, 2, 64, r, False)
-        T, most, keys = int(qsl[-1]), max(n), int(S.max())
+        T, most, keys = int(qsl[-1]), max(n), int(S.max()) + 600
         q, out = queries(T, 8, 64, r), torch.empty((T, 8, 64), dtype=torch.bfloat16, device="cuda")
         lse = torch.empty((T, 8), device="cuda")
         where = (c.blocks, 2, 16, 64, dev(qsl), dev(S), dev(tables), T, most, keys)
@@ -391,7 +393,7 @@ def test_refusals_of_the_binding():
                dict(shared=True, start=dev(np.array([0], np.int32)), prefix=dev(np.array([16], np.int32)))):
         with pytest.raises(ValueError):
             call(**kw)
-    for kw in (dict(ws=ws[:16]), dict(out=q), dict(q=torch.empty(4 * 8 * 64 + 4, dtype=torch.bfloat16, device="cuda")[4:]),
+    for kw in (dict(ws=ws[:8]), dict(out=q), dict(q=torch.empty(4 * 8 * 64 + 4, dtype=torch.bfloat16, device="cuda")[4:]),
                dict(shared=True, start=None, prefix=dev(np.array([16], np.int32)))):
         with pytest.raises(sx.SpexisError):
             call(**kw)
