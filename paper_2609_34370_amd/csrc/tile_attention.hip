@@ -138,13 +138,14 @@ __device__ __forceinline__ bool find_unit(const TileAttnParams& p, int u, Unit& 
     __syncthreads();
     sum = sm_total[0] + sm_total[1] + sm_total[2] + sm_total[3];
     rows = sm_rows[0] + sm_rows[1] + sm_rows[2] + sm_rows[3];
-    const int64_t goal = tile_attn_parts(p.shares, rows);
-    share = (int)min((int64_t)INT32_MAX, max((sum + goal - 1) / goal, (int64_t)kTileLeast));
+    const int goal = (int)tile_attn_parts(p.shares, rows);
+    // (64-bit divisions take hundreds of instructions; the sum is far below 2^53)
+    share = (int)fmin(fmax(ceil((double)sum / (double)goal), (double)kTileLeast), 2147483647.0);
   }
   int before = 0, turn = 0;
   for (int base = 0; base < ns; base += 256, turn ^= 1) {
     if (p.shares == 0 || ns > 256) load(base);
-    const int parts = max((int)min((int64_t)1 << 20, ((int64_t)nt + share - 1) / share), 1), mine = tiles * parts;
+    const int parts = nt > share ? (int)((uint32_t)(nt - 1) / (uint32_t)share) + 1 : 1, mine = tiles * parts;
     const int incl = wave_incl_scan_i32(mine, lane);
     if (lane == 63) sm_scan[turn][wave] = incl;
     __syncthreads();
@@ -156,10 +157,10 @@ __device__ __forceinline__ bool find_unit(const TileAttnParams& p, int u, Unit& 
       before += x;
     }
     if (u >= at && u < at + mine) {
-      const int t = (u - at) / parts;
+      const int t = (int)((uint32_t)(u - at) / (uint32_t)parts);
       *reinterpret_cast<u32x4*>(sm_unit) = u32x4{(uint32_t)g.q0, (uint32_t)g.rows, (uint32_t)g.seq, (uint32_t)g.base};
       *reinterpret_cast<u32x4*>(sm_unit + 4) = u32x4{(uint32_t)g.end, (uint32_t)g.last, (uint32_t)g.group, (uint32_t)(p.seg_lo + base + tid)};
-      *reinterpret_cast<u32x4*>(sm_unit + 8) = u32x4{(uint32_t)t, (uint32_t)((u - at) % parts), (uint32_t)parts, (uint32_t)(at + t * parts)};
+      *reinterpret_cast<u32x4*>(sm_unit + 8) = u32x4{(uint32_t)t, (uint32_t)(u - at - t * parts), (uint32_t)parts, (uint32_t)(at + t * parts)};
     }
     if (before > u) break;   // (the same for all threads)
   }
@@ -235,7 +236,7 @@ void tile_attn_kernel(TileAttnParams p) {
   const int sure0 = min((int64_t)g.end - 1, (int64_t)g.last + row0 / p.group);   // every row sees the keys up to this one
   const int end = tile_end(p, g, tile);                      // keys [g.base, end)
   const int nt = (end - g.base + kKeys - 1) / kKeys;
-  const int k0 = (int)((int64_t)nt * un.part / un.parts), k1 = (int)((int64_t)nt * (un.part + 1) / un.parts);
+  const int k0 = un.parts == 1 ? 0 : (int)((int64_t)nt * un.part / un.parts), k1 = un.parts == 1 ? nt : (int)((int64_t)nt * (un.part + 1) / un.parts);
 
   // ---- staging: this thread's part of a step's keys, global memory -> registers -> LDS
   const uint8_t* kc = reinterpret_cast<const uint8_t*>(p.k_cache);
