@@ -254,7 +254,7 @@ TileLayout tile_layout(int64_t seqs, int64_t groups, int64_t hq, int64_t hkv, in
                        int64_t max_query_len, int64_t max_seq_len) {
   TileLayout l{};
   const int64_t group = hq / hkv;
-  const bool is_long = max_seq_len > spexis::kTileLeast * spexis::kTileKeys;
+  const bool is_long = max_seq_len > spexis::kTileLeastKeys;
   l.shared = groups > 0 && is_long;
   const int64_t pre = l.shared ? most_row_tiles(groups, group, total_tokens, total_tokens) : 0;
   const int64_t own = most_row_tiles(seqs, group, total_tokens, max_query_len);
@@ -355,6 +355,7 @@ int tile_attention(const char* name, bool in8, const void* k_cache, const void* 
   p.hq = num_q_heads;
   p.group = num_q_heads / num_kv_heads;
   p.pitch = l.pitch;
+  p.step = spexis::tile_keys(head_dim);
   p.shares = l.shares;
   p.merge = l.merge ? 1 : 0;
   p.units = (int)l.units;

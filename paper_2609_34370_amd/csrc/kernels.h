@@ -164,11 +164,12 @@ __host__ __device__ inline int64_t attn_ws_bytes(int nwaves, int rmax, int D) {
 }
 
 // Attention of many query rows at once (whole prompts; batches that share prefixes): workgroups of kTileRows rows of a KV
-// head that step through kTileKeys keys at a time.
-constexpr int kTileRows = 128, kTileKeys = 64;
+// head that step through tile_keys(head_dim) keys at a time.
+constexpr int kTileRows = 128;
+__host__ __device__ constexpr int tile_keys(int head_dim) { return head_dim == 128 ? 32 : 64; }   // of a step
 constexpr int kTileHdrInts = 8;
-constexpr int kTileLeast = 8;     // the fewest key tiles of a part
-constexpr int kTileSlots = 512;   // workgroups that run at a time: two a CU
+constexpr int kTileLeastKeys = 512;   // the fewest keys of a part
+constexpr int kTileSlots = 768;   // workgroups that run at a time: three a CU
 struct TileAttnParams {
   const void* k_cache;
   const void* v_cache;
@@ -188,6 +189,7 @@ struct TileAttnParams {
   int num_blocks, hkv, block_size, head_dim, num_seqs, num_groups, max_blocks, total_tokens, max_query_len;
   int hq, group;
   int pitch;                    // most rows of a sequence's tile
+  int step;                     // tile_keys(head_dim)
   int shares;                   // row tiles (without a merge those of prefixes alone) are cut into parts, about so many a head; 0: not
   int units, prefix_units;      // the most units a head of either launch
   int merge;                    // prefixes and sequences in one launch, tile_merge_kernel joins partials

@@ -2,30 +2,40 @@
 // batches whose sequences begin with a prefix that they share.
 //
 // Work decomposition.  A segment is a run of query tokens against a run of keys: a sequence against the keys that are its
-// own, causally; and, where a group of sequences shares a prefix, all tokens of the group against that prefix, once.  With G query heads a KV head, a segment has G rows a token, in tiles of 128: row r is (token r / G, head
-// r % G), so every row of a tile reads the same K and V.  A unit, one workgroup, is a tile against the keys that any of its
-// rows sees, or, where there are too few tiles to fill the chip, against one of several equal parts of them.  Prefixes and
-// parts leave fp32 partials (reference maximum, sum, unnormalised output) in the workspace.  With few units prefixes and
-// sequences run together, and tile_merge_kernel joins what they leave; with many the prefixes run in a launch in front, and a
-// unit that has all of a sequence's own keys joins the prefix's partials to its registers (512 sequences of 9 tokens, 28
-// query heads over 4, in 16 groups: 219 us for 246, which had written and read 134 MB more; 64 sequences of 5 behind one
-// prefix of 4096 keys: together 68 us, 75 one after the other).
+// own, causally; and, where a group of sequences shares a prefix, all tokens of the group against that prefix, once.  With
+// G query heads a KV head, a segment has G rows a token, in tiles of 128: row r is (token r / G, head r % G), so every row of
+// a tile reads the same K and V.  A unit, one workgroup, is a tile against the keys that any of its rows sees, or, where there
+// are too few tiles to fill the chip, against one of several equal parts of them.  Prefixes and parts leave fp32 partials
+// (reference maximum, sum, unnormalised output) in the workspace.  With few units prefixes and sequences run together, and
+// tile_merge_kernel joins what they leave; with many the prefixes run in a launch in front, and a unit that has all of a
+// sequence's own keys joins the prefix's partials to its registers (512 sequences of 9 tokens, 28 query heads over 4, in 16
+// groups: 219 us for 246, which had written and read 134 MB more; 64 sequences of 5 behind one prefix of 4096 keys: together
+// 68 us, 75 one after the other).
 //
-// Each of the four waves owns 32 rows.  The 64 keys of a step pass through LDS, where all waves read them: fetched into
-// registers one step ahead, widened there from the 8-bit cache, and stored in the order in which a wave reads matrix
-// operands, 1 KB a fragment, so that no two lanes meet in a bank.  With v_mfma_f32_32x32x16_bf16 (operand A: lane l holds
+// Each of the four waves owns 32 rows.  The 32 keys of a step (64 of 64-wide heads) pass through LDS, where all waves read
+// them: fetched into registers two steps ahead, widened there from the 8-bit cache, and stored in the order in which a wave
+// reads matrix operands, 1 KB a fragment, so that no two lanes meet in a bank.  With v_mfma_f32_32x32x16_bf16 (operand A: lane l holds
 // row l%32, k-slice 8*(l/32)..+7; B: column l%32, same k-slice; C: lane l, value i holds row 8*(i/4) + 4*(l/32) + i%4,
 // column l%32):
 //   S^T[key][row] = K Q^T: lane l owns query row l%32, so a row's maximum is one over 32 values and one lane exchange;
 //   O^T[d][row] += V^T P^T: the V layouts hold slots in the order in which the score tile leaves them, so P^T is the
 //   lane's own values.
+//
+// Bound by LDS: a product of 32 cycles needs a fragment of 1 KB, of which a CU reads 64 bytes a cycle (measured), so its four
+// SIMDs' matrix cores can be busy half of the time.  16001 tokens of 32 query heads over 8 of 128 (2.1 TFLOP) take 2.01 to 2.10
+// ms on three cards, 1.00 to 1.04 PFLOP/s, the matrix cores busy for 47% of the cycles; prompts of 100 to 3500 tokens, eight
+// together, 374 to 397 us, 0.82 to 0.87 PFLOP/s; a large matrix product reaches 1.58.  Tried on the way (at 16001 tokens):
+// 64 keys a step and two workgroups a CU, the same but for shared prefixes (65 us for 60); eight waves that take turns at
+// the matrix cores, 1.94 ms for 2.03, prompts together 391 us for 372; 64 rows a wave, which halves the reads, 2.30 ms, one
+// wave a SIMD with nothing to run beside it; half or all of K loaded by every wave for itself, 2.32 and 2.30 ms; products
+// spread among the exponentials by hand, or waves' priorities, no difference.
 #include "attention.h"
 
 namespace spexis {
 
 namespace {
 
-constexpr int kRows = kTileRows, kKeys = kTileKeys;
+constexpr int kRows = kTileRows;
 
 // Eight e4m3 codes times a power of two, as a matrix operand.
 __device__ __forceinline__ u32x4 widen_codes(uint32_t lo, uint32_t hi, float scale) {
@@ -88,7 +98,7 @@ __device__ __forceinline__ Segment segment(const TileAttnParams& p, int s) {
 }
 
 __device__ __forceinline__ int row_tiles(const Segment& g) { return (g.rows + kRows - 1) / kRows; }
-__device__ __forceinline__ int key_tiles(const Segment& g) { return (g.end - g.base + kKeys - 1) / kKeys; }
+__device__ __forceinline__ int key_tiles(const TileAttnParams& p, const Segment& g) { return (g.end - g.base + p.step - 1) / p.step; }
 // The keys of a segment's row tile end in front of this one.
 __device__ __forceinline__ int tile_end(const TileAttnParams& p, const Segment& g, int tile) {
   const int r = min(g.rows, (tile + 1) * kRows) - 1;
@@ -117,7 +127,7 @@ __device__ __forceinline__ bool find_unit(const TileAttnParams& p, int u, Unit& 
     if (s < p.seg_hi) {
       g = segment(p, s);
       tiles = row_tiles(g);
-      nt = key_tiles(g);
+      nt = key_tiles(p, g);
     }
   };
   int share = INT32_MAX;
@@ -140,7 +150,7 @@ __device__ __forceinline__ bool find_unit(const TileAttnParams& p, int u, Unit& 
     rows = sm_rows[0] + sm_rows[1] + sm_rows[2] + sm_rows[3];
     const int goal = (int)tile_attn_parts(p.shares, rows);
     // (64-bit divisions take hundreds of instructions; the sum is far below 2^53)
-    share = (int)fmin(fmax(ceil((double)sum / (double)goal), (double)kTileLeast), 2147483647.0);
+    share = (int)fmin(fmax(ceil((double)sum / (double)goal), (double)(kTileLeastKeys / p.step)), 2147483647.0);
   }
   int before = 0, turn = 0;
   for (int base = 0; base < ns; base += 256, turn ^= 1) {
@@ -195,12 +205,13 @@ __device__ __forceinline__ PrefixParts prefix_parts(const TileAttnParams& p, int
 }  // namespace
 
 template <int D, int BS, bool IN8>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2)))
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3)))
 void tile_attn_kernel(TileAttnParams p) {
   constexpr int KS = D / 16;              // k-steps of the score product
   constexpr int MT = D / 32;              // 32-wide head-dim tiles of the output
-  constexpr int NL = IN8 ? D / 64 : D / 32;   // 16-byte loads of K, and of V, a thread and step
-  constexpr int kFrags = 2 * KS;          // fragments of 1 KB of K, and of V (= 4 * MT)
+  constexpr int KT = tile_keys(D) / 32, kKeys = 32 * KT;   // tiles of 32 keys a step
+  constexpr int NL = (IN8 ? D / 64 : D / 32) * KT / 2;   // 16-byte loads of K, and of V, a thread and step
+  constexpr int kFrags = KT * KS;         // fragments of 1 KB of K, and of V (= 2 * KT * MT)
   __shared__ u32x4 sm[2][2][kFrags][kWave];   // [buffer][K, V]
   __shared__ int sm_odd[D];
   const int tid = threadIdx.x, lane = tid & 63, col = lane & 31, half = lane >> 5;
@@ -244,30 +255,33 @@ void tile_attn_kernel(TileAttnParams p) {
   constexpr int64_t kHead = (int64_t)BS * D * (IN8 ? 1 : 2);   // bytes of one (block, head) chunk
   sint32* table = (sint32*)p.block_tables + (int64_t)g.seq * p.max_blocks;
   const int last_block = (g.end - 1) / BS;
-  // K: wave w stages keys 32 (w & 1) + col, half of the head dim; V: the 16 keys of unit w, all of it
-  const int k_key = (wave & 1) * 32 + col, k_slot = k_key % BS, v_slot = (wave * 16) % BS;
+  // K: wave w stages keys 32 kw + col, the k-steps from ks0 on (8 bits: two a load); V: the 16 keys of unit vw, the head-dim
+  // tiles from mt0 on (8 bits: two a load)
+  const int kw = KT == 2 ? wave & 1 : 0, ks0 = KT == 2 ? (wave >> 1) * (KS / 2) : wave * (KS / 4);
+  const int vw = KT == 2 ? wave : wave & 1, mt0 = KT == 2 ? 0 : (wave >> 1) * (MT / 2);
+  const int k_slot = col % BS, v_slot = (vw * 16) % BS;
   u32x4 kr[NL], vr[NL];
-  float ks = 0.f, vs = 0.f;
+  float k_scale = 0.f, v_scale = 0.f;
   // Where a step's keys lie is looked up a step before they are loaded, and the answer not touched until then: the lookup's
   // latency would stand in front of every step.
   int kb0 = 0, kb1 = 0, vb = 0;
   auto block_of = [&](int key) { return table[min((int)((uint32_t)(g.base + key) / BS), last_block)]; };
   auto chunk_of = [&](int block) { return (int64_t)clampi(block, 0, p.num_blocks - 1) * p.hkv + h; };
   auto find_k = [&](int t) {
-    kb0 = block_of(t * kKeys + (wave & 1) * 32);
-    kb1 = BS == 16 ? block_of(t * kKeys + (wave & 1) * 32 + 16) : kb0;
+    kb0 = block_of(t * kKeys + kw * 32);
+    kb1 = BS == 16 ? block_of(t * kKeys + kw * 32 + 16) : kb0;
   };
-  auto find_v = [&](int t) { vb = block_of(t * kKeys + wave * 16); };
+  auto find_v = [&](int t) { vb = block_of(t * kKeys + vw * 16); };
   // (steps behind the last find its last block: a valid one)
   auto load_k = [&](int t) {
     const int64_t c0 = chunk_of(kb0), c1 = BS == 16 ? chunk_of(kb1) : c0, c = BS == 16 && col >= 16 ? c1 : c0;
     if (IN8) {
-      const uint8_t* a = kc + c * kHead + (k_slot / 16) * 16 * D + (((wave >> 1) * (KS / 2) + half) * 16 + k_slot % 16) * 16;
+      const uint8_t* a = kc + c * kHead + (k_slot / 16) * 16 * D + ((ks0 + half) * 16 + k_slot % 16) * 16;
 #pragma unroll
       for (int i = 0; i < NL; ++i) kr[i] = ld16(a + i * 2 * 256);
-      ks = p.scales[2 * c];
+      k_scale = p.scales[2 * c];
     } else {
-      const uint8_t* a = kc + c * kHead + ((2 * ((wave >> 1) * (KS / 2)) + half) * BS + k_slot) * 16;
+      const uint8_t* a = kc + c * kHead + ((2 * ks0 + half) * BS + k_slot) * 16;
 #pragma unroll
       for (int i = 0; i < NL; ++i) kr[i] = ld16(a + i * 2 * BS * 16);
     }
@@ -276,12 +290,12 @@ void tile_attn_kernel(TileAttnParams p) {
   auto load_v = [&](int t) {
     const int64_t c = chunk_of(vb);
     if (IN8) {
-      const uint8_t* a = vc + c * kHead + (v_slot / 16) * 16 * D + (col * 2 + half) * 16;
+      const uint8_t* a = vc + c * kHead + (v_slot / 16) * 16 * D + mt0 / 2 * 1024 + (col * 2 + half) * 16;
 #pragma unroll
       for (int i = 0; i < NL; ++i) vr[i] = ld16(a + i * 1024);
-      vs = p.scales[2 * c + 1];
+      v_scale = p.scales[2 * c + 1];
     } else {
-      const uint8_t* a = vc + c * kHead + (col * BS + v_slot + 8 * half) * 2;
+      const uint8_t* a = vc + c * kHead + ((mt0 * 32 + col) * BS + v_slot + 8 * half) * 2;
 #pragma unroll
       for (int i = 0; i < NL; ++i) vr[i] = ld16(a + i * 32 * BS * 2);
     }
@@ -291,11 +305,11 @@ void tile_attn_kernel(TileAttnParams p) {
 #pragma unroll
     for (int i = 0; i < NL; ++i) {
       if (IN8) {
-        u32x4* f = &sm[buf][0][(wave & 1) * KS + (wave >> 1) * (KS / 2) + 2 * i + half][col];
-        f[0] = widen_codes(kr[i][0], kr[i][1], ks);
-        f[32] = widen_codes(kr[i][2], kr[i][3], ks);
+        u32x4* f = &sm[buf][0][kw * KS + ks0 + 2 * i + half][col];
+        f[0] = widen_codes(kr[i][0], kr[i][1], k_scale);
+        f[32] = widen_codes(kr[i][2], kr[i][3], k_scale);
       } else {
-        sm[buf][0][(wave & 1) * KS + (wave >> 1) * (KS / 2) + i][lane] = kr[i];
+        sm[buf][0][kw * KS + ks0 + i][lane] = kr[i];
       }
     }
   };
@@ -316,29 +330,29 @@ void tile_attn_kernel(TileAttnParams p) {
   };
   auto store_v = [&](int buf, int t) {
     // 32-bit word w of a fragment holds this lane's keys 8 (w / 2) + 4 half + 2 (w % 2) and the next of unit `wave`
-    const int over = g.end - (g.base + t * kKeys + wave * 16);   // keys of the unit in front of the sequence's end
+    const int over = g.end - (g.base + t * kKeys + vw * 16);   // keys of the unit in front of the sequence's end
     const bool edge = t * kKeys + g.base + kKeys - 1 > sure0;   // some row does not see all of the step's keys
 #pragma unroll
     for (int i = 0; i < NL; ++i) {
       u32x4 v[IN8 ? 2 : 1];
       if (IN8) {
-        v[0] = widen_codes(vr[i][0], vr[i][1], vs);
-        v[IN8 ? 1 : 0] = widen_codes(vr[i][2], vr[i][3], vs);
+        v[0] = widen_codes(vr[i][0], vr[i][1], v_scale);
+        v[IN8 ? 1 : 0] = widen_codes(vr[i][2], vr[i][3], v_scale);
       } else {
         v[0] = vr[i];
       }
 #pragma unroll
       for (int x = 0; x < (IN8 ? 2 : 1); ++x) {
-        const int mt = IN8 ? 2 * i + x : i;
+        const int mt = mt0 + (IN8 ? 2 * i + x : i);
         if (edge) {
 #pragma unroll
           for (int w = 0; w < 4; ++w) {   // what lies behind the end may be anything
             const int key = 8 * (w >> 1) + 4 * half + 2 * (w & 1);
             v[x][w] &= (key < over ? 0x0000FFFFu : 0u) | (key + 1 < over ? 0xFFFF0000u : 0u);
           }
-          part_odd(v[x], 32 * mt + col, g.base + t * kKeys + wave * 16);
+          part_odd(v[x], 32 * mt + col, g.base + t * kKeys + vw * 16);
         }
-        sm[buf][1][wave * MT + mt][lane] = v[x];
+        sm[buf][1][vw * MT + mt][lane] = v[x];
       }
     }
   };
@@ -353,12 +367,16 @@ void tile_attn_kernel(TileAttnParams p) {
   // ---- this wave's rows
   const int rw = row0 + wave * 32;
   const bool active = rw < g.rows;
-  const int r = min(rw + col, g.rows - 1), j = r / p.group;   // rows behind the last repeat it
-  const int lim = min((int64_t)g.end - 1, (int64_t)g.last + j);   // the last key the lane's row sees
-  const int64_t qrow = (int64_t)(g.q0 + j) * p.hq + h * p.group + r % p.group;
+  auto row_at = [&](int r) {   // of q and the outputs
+    const int j = r / p.group;
+    return (int64_t)(g.q0 + j) * p.hq + h * p.group + r - j * p.group;
+  };
+  int lim;   // the last key that the lane's row sees
   u32x4 qf[KS];
   {
-    const uint16_t* q = reinterpret_cast<const uint16_t*>(p.q) + qrow * D + 8 * half;
+    const int r = min(rw + col, g.rows - 1);   // rows behind the last repeat it
+    lim = min((int64_t)g.end - 1, (int64_t)g.last + r / p.group);
+    const uint16_t* q = reinterpret_cast<const uint16_t*>(p.q) + row_at(r) * D + 8 * half;
 #pragma unroll
     for (int s = 0; s < KS; ++s) qf[s] = ld16(q + 16 * s) ^ p.q_sign;
   }
@@ -391,10 +409,10 @@ void tile_attn_kernel(TileAttnParams p) {
       load_v(t + 2);
     }
     const int t0 = g.base + t * kKeys;
-    f32x16 sc[2];
+    f32x16 sc[KT];
     if (active) {
 #pragma unroll
-      for (int kt = 0; kt < 2; ++kt) {
+      for (int kt = 0; kt < KT; ++kt) {
 #pragma unroll
         for (int e = 0; e < 16; ++e) sc[kt][e] = 0.f;
 #pragma unroll
@@ -403,19 +421,19 @@ void tile_attn_kernel(TileAttnParams p) {
       }
     }
     if (active) {
-      const bool need_mask = t0 + kKeys - 1 > sure;
-      if (need_mask) {
+      if (t0 + kKeys - 1 > sure) {
+        const int seen = lim - t0 - 4 * half;
 #pragma unroll
-        for (int kt = 0; kt < 2; ++kt)
+        for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
           for (int e = 0; e < 16; ++e)
-            if (t0 + kt * 32 + (e >> 2) * 8 + 4 * half + (e & 3) > lim) sc[kt][e] = -INFINITY;
+            if (kt * 32 + (e >> 2) * 8 + (e & 3) > seen) sc[kt][e] = -INFINITY;
       }
       float mx = sc[0][0];
 #pragma unroll
-      for (int e = 1; e < 16; ++e) mx = fmaxf(mx, sc[0][e]);
+      for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
-      for (int e = 0; e < 16; ++e) mx = fmaxf(mx, sc[1][e]);
+        for (int e = kt == 0 ? 1 : 0; e < 16; ++e) mx = fmaxf(mx, sc[kt][e]);
       mx = halves_max(mx);
       // Lazy rescaling: the reference maximum moves only when a score exceeds it by more than 2^kLazy, so 2^(x - m)
       // stays <= 2^kLazy and the accumulators are rescaled rarely.
@@ -429,15 +447,14 @@ void tile_attn_kernel(TileAttnParams p) {
           for (int e = 0; e < 16; ++e) acc[mt][e] *= alpha;
       }
       const float mc = -m * p.scale_log2e;
-      float ps = 0.f;
-      u32x4 pw[4];
+      u32x4 pw[2 * KT];
 #pragma unroll
-      for (int kt = 0; kt < 2; ++kt) {
+      for (int kt = 0; kt < KT; ++kt) {
         float x[16];
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
           x[e] = fast_exp2(fmaf(sc[kt][e], p.scale_log2e, mc));
-          ps += x[e];
+          l += x[e];
         }
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
@@ -445,9 +462,9 @@ void tile_attn_kernel(TileAttnParams p) {
           pw[2 * kt + 1][w] = pack_bf16x2(x[8 + 2 * w], x[8 + 2 * w + 1]);
         }
       }
-      l += ps;
+      __builtin_amdgcn_sched_barrier(0);   // (products moved in front hold more registers than three waves a SIMD have)
 #pragma unroll
-      for (int s2 = 0; s2 < 4; ++s2)
+      for (int s2 = 0; s2 < 2 * KT; ++s2)
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt)
           acc[mt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(sm[buf][1][s2 * MT + mt][lane]), as_bf16x8(pw[s2]), acc[mt], 0, 0, 0);
@@ -471,7 +488,7 @@ void tile_attn_kernel(TileAttnParams p) {
   float lt = halves_sum(l);
   float mb = m * p.scale_log2e;   // in the base-2 domain
   if (whole && g.group >= 0) {    // the prefix's partials of the lane's row
-    const PrefixParts parts = prefix_parts(p, g.group, g.q0, r);
+    const PrefixParts parts = prefix_parts(p, g.group, g.q0, min(rw + col, g.rows - 1));
     for (int c = 0; c < parts.n; ++c) {
       const float* slot = p.ws_prefix + ((int64_t)(parts.first + c) * p.hkv + h) * tile_slot_floats(kRows, D);
       const float mc = slot[kRows * D + parts.row], lc = slot[kRows * (D + 1) + parts.row];
@@ -507,30 +524,35 @@ void tile_attn_kernel(TileAttnParams p) {
     for (int i = lane; i < 32 * kOc; i += kWave) {
       const int row = i / kOc, c = i % kOc, rr = rw + row;
       if (row < left)
-        st16(reinterpret_cast<uint16_t*>(p.out) + ((int64_t)(g.q0 + rr / p.group) * p.hq + h * p.group + rr % p.group) * D + 8 * c,
-             scr[row * kOc + (c ^ (row & (kOc - 1)))]);
+        st16(reinterpret_cast<uint16_t*>(p.out) + row_at(rr) * D + 8 * c, scr[row * kOc + (c ^ (row & (kOc - 1)))]);
     }
-    if (p.lse && half == 0 && col < left) p.lse[qrow] = (mb + __builtin_amdgcn_logf(lt)) * kLn2;
+    if (p.lse && half == 0 && col < left) p.lse[row_at(rw + col)] = (mb + __builtin_amdgcn_logf(lt)) * kLn2;
   } else {
     // the partial: [pitch][D], then maxima (in the base-2 domain) and sums
     const int pitch = is_prefix ? kRows : p.pitch;
     float* slot = is_prefix ? p.ws_prefix + ((int64_t)u * p.hkv + h) * tile_slot_floats(kRows, D)
                             : p.ws_seq + ((int64_t)u * p.hkv + h) * tile_slot_floats(p.pitch, D);
-    constexpr int kFc = D / 4;   // 16-byte chunks of an fp32 row; chunk c of row col at chunk c ^ (col mod kFc)
+    // in two halves of the head dim; chunk c of row col's half at chunk c ^ (col mod kHc)
+    constexpr int kHc = D / 8;   // 16-byte chunks of half an fp32 row
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt)
+    for (int hm = 0; hm < 2; ++hm) {
 #pragma unroll
-      for (int a = 0; a < 4; ++a) {
-        const int c = 8 * mt + 2 * a + half;
-        scr[col * kFc + (c ^ (col & (kFc - 1)))] =
-            u32x4{__float_as_uint(acc[mt][4 * a]), __float_as_uint(acc[mt][4 * a + 1]), __float_as_uint(acc[mt][4 * a + 2]),
-                  __float_as_uint(acc[mt][4 * a + 3])};
-      }
-    wave_lds_fence();
+      for (int mt = hm * MT / 2; mt < (hm + 1) * MT / 2; ++mt)
+#pragma unroll
+        for (int a = 0; a < 4; ++a) {
+          const int c = 8 * (mt - hm * MT / 2) + 2 * a + half;
+          scr[col * kHc + (c ^ (col & (kHc - 1)))] =
+              u32x4{__float_as_uint(acc[mt][4 * a]), __float_as_uint(acc[mt][4 * a + 1]), __float_as_uint(acc[mt][4 * a + 2]),
+                    __float_as_uint(acc[mt][4 * a + 3])};
+        }
+      wave_lds_fence();
 #pragma unroll 1
-    for (int i = lane; i < 32 * kFc; i += kWave) {
-      const int row = i / kFc, c = i % kFc;
-      if (row < left) st16(slot + (int64_t)(wave * 32 + row) * D + 4 * c, scr[row * kFc + (c ^ (row & (kFc - 1)))]);
+      for (int i = lane; i < 32 * kHc; i += kWave) {
+        const int row = i / kHc, c = i % kHc;
+        if (row < left)
+          st16(slot + (int64_t)(wave * 32 + row) * D + hm * (D / 2) + 4 * c, scr[row * kHc + (c ^ (row & (kHc - 1)))]);
+      }
+      wave_lds_fence();   // the second half's writes follow these reads
     }
     if (half == 0 && col < left) {
       slot[(int64_t)pitch * D + wave * 32 + col] = mb;
