@@ -390,7 +390,8 @@ int spexis_shared_attention_kv8(const void* k_cache, const void* v_cache, const 
  *   weights_in    [num_blocks][Hkv][block_size] fp32 (read), which may be `weights`, or NULL: all sums begin here
  *   weights       the same shape (written)
  *   max_seq_len   host: >= max_b S_b (keys from it on are left out)
- * A block that several sequences share gets the sums of one of them.
+ *   first_keys    [num_seqs] int32 or NULL (0): keys in front of it (clamped to [0, S_b]) are left as they were
+ * Of the sequences that share a block all but one must have it in front of their first key: the calls' sums are not added up.
  * Supported shapes as spexis_prompt_attention; num_seqs * Hkv * ceil(max_seq_len / 128) < 2^24.  k_cache, q, weights and
  * weights_in 16-byte aligned.
  * Errors: INVALID_ARGUMENT, UNSUPPORTED, HIP.
@@ -400,7 +401,7 @@ int spexis_attention_weights(const void* k_cache, int32_t num_blocks, int32_t nu
                              const int32_t* seq_lens, const int32_t* block_tables, int32_t max_blocks_per_seq,
                              int32_t total_tokens, int32_t max_query_len, int32_t max_seq_len, const void* q,
                              int32_t num_q_heads, float scale, const float* lse, const int32_t* accepted_len,
-                             const float* weights_in, float* weights, void* stream);
+                             const int32_t* first_keys, const float* weights_in, float* weights, void* stream);
 
 /* Bytes of workspace spexis_evict_kv needs (> 0 whenever the sizes are valid, else 0). */
 size_t spexis_evict_kv_workspace_size(int32_t num_seqs, int32_t num_kv_heads, int32_t max_seq_len);

@@ -201,7 +201,7 @@ def attention_rows(k, v, qsl, seq_lens, tables, q, scale):
     return out, mean, most, lse
 
 
-def attention_weights(k, qsl, seq_lens, tables, q, scale, lse, before, accepted=None):
+def attention_weights(k, qsl, seq_lens, tables, q, scale, lse, before, accepted=None, first=None):
     """`before` [block][KV head][slot] (None: zeros) with the sums of the step's weights; and the sums of the weights'
     relative errors in units of fp32's: what an exponent's rounding amounts to."""
     bs, hkv, D = k.shape[1:]
@@ -213,12 +213,12 @@ def attention_weights(k, qsl, seq_lens, tables, q, scale, lse, before, accepted=
         S, n = int(seq_lens[b]), int(qsl[b + 1] - qsl[b])
         if accepted is not None:
             n = min(n, int(accepted[b]) + 1)
-        t = np.arange(S)
+        t = np.arange(S)[0 if first is None else int(first[b]):]   # the keys that count
         place = tables[b, t // bs], slice(None), t % bs
         kb = k[tables[b, t // bs], t % bs]
-        total, err = np.zeros((S, hkv)), np.zeros((S, hkv))
+        total, err = np.zeros((len(t), hkv)), np.zeros((len(t), hkv))
         for j in range(n):
-            row, seen = int(qsl[b]) + j, S - n + j + 1
+            row, seen = int(qsl[b]) + j, max(S - n + j + 1 - (S - len(t)), 0)
             for h in range(q.shape[1]):
                 e = lse[row, h]
                 w = np.exp(kb[:seen, h // G] @ q[row, h] * scale - e)

@@ -14,6 +14,7 @@
 
 #include "kernels.h"
 #include "spexis.h"
+#include "tiles.h"
 
 namespace {
 
@@ -553,8 +554,8 @@ int spexis_attention_weights(const void* k_cache, int32_t num_blocks, int32_t nu
                              int32_t head_dim, int32_t num_seqs, const int32_t* query_start_loc, const int32_t* seq_lens,
                              const int32_t* block_tables, int32_t max_blocks_per_seq, int32_t total_tokens,
                              int32_t max_query_len, int32_t max_seq_len, const void* q, int32_t num_q_heads, float scale,
-                             const float* lse, const int32_t* accepted_len, const float* weights_in, float* weights,
-                             void* stream) {
+                             const float* lse, const int32_t* accepted_len, const int32_t* first_keys,
+                             const float* weights_in, float* weights, void* stream) {
   const char* name = "spexis_attention_weights";
   if (num_blocks <= 0 || num_kv_heads <= 0 || num_q_heads <= 0 || num_seqs < 0 || max_blocks_per_seq <= 0 ||
       total_tokens < 0 || max_query_len <= 0 || max_seq_len <= 0)
@@ -577,8 +578,8 @@ int spexis_attention_weights(const void* k_cache, int32_t num_blocks, int32_t nu
     return fail(SPEXIS_ERR_INVALID_ARGUMENT, "%s: null pointer", name);
   if (misaligned({k_cache, q, weights, weights_in}))
     return fail(SPEXIS_ERR_INVALID_ARGUMENT, "%s: a pointer that is not 16-byte aligned", name);
-  spexis::WeightParams p{k_cache, query_start_loc, seq_lens, block_tables, q, lse, accepted_len, weights_in, weights,
-                         num_blocks, num_kv_heads, block_size, head_dim, num_seqs, max_blocks_per_seq, total_tokens,
+  spexis::WeightParams p{k_cache, query_start_loc, seq_lens, block_tables, q, lse, accepted_len, first_keys,
+                         weights_in, weights, num_blocks, num_kv_heads, block_size, head_dim, num_seqs, max_blocks_per_seq, total_tokens,
                          max_query_len, max_seq_len, num_q_heads, num_q_heads / num_kv_heads,
                          // (0 counts as the least that a masked score, infinite, can be multiplied with)
                          scale == 0.f ? 1e-37f : (float)((double)scale * 1.4426950408889634)};

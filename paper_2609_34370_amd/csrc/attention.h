@@ -19,7 +19,6 @@ __device__ __forceinline__ float halves_sum(float v) {
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
-constexpr float kLn2 = 0.693147180559945309f, kLog2E = 1.44269504088896341f;
 constexpr float kNegBig = -1.0e30f;   // finite "minus infinity" of the running maxima
 
 // acc[mt] *= alpha (alpha per lane: the lane's query row), in place on the registers that hold the

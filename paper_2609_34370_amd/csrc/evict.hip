@@ -7,7 +7,7 @@
 // evict_move_kernel: the list's rows.  A key's new place is never behind its old one, so a wave that owns a slice of the
 // head dim moves it in place: what a step overwrites, no later one reads.
 #include "common.h"
-#include "kernels.h"
+#include "tiles.h"
 
 namespace spexis {
 

@@ -30,6 +30,7 @@
 // wave a SIMD with nothing to run beside it; half or all of K loaded by every wave for itself, 2.32 and 2.30 ms; products
 // spread among the exponentials by hand, or waves' priorities, no difference.
 #include "attention.h"
+#include "tiles.h"
 
 namespace spexis {
 

@@ -12,6 +12,7 @@
 // 363 MB) take 88 us, 4.2 TB/s.  With many rows by the latency of a tile's rows and the exponentials: 64 tokens of 28 heads over
 // 6 prompts of 2001 to 8000 keys (4 KV heads; 14.3 GFLOP) 26 us.  Two key tiles a wave took 106 and 37 us.
 #include "attention.h"
+#include "tiles.h"
 
 namespace spexis {
 
@@ -31,7 +32,8 @@ void weights_kernel(WeightParams p, int chunks) {
   int n = min(clampi(qsl[b + 1], q0, p.total_tokens) - q0, p.max_query_len);
   if (p.accepted) n = clampi(acc_len[b] + 1, 0, n);
   const int S = clampi(len, n, (int)min((int64_t)p.max_blocks * BS, (int64_t)p.max_seq_len));
-  if (key0 >= S) return;
+  const int first = p.first_keys ? clampi(((sint32*)p.first_keys)[b], 0, S) : 0;
+  if (key0 >= S || key0 + kWeightKeys <= first) return;
   const int L = S - n, R = n * p.group;
   sint32* table = (sint32*)p.block_tables + (int64_t)b * p.max_blocks;
   const int last = (S - 1) / BS;
@@ -106,7 +108,7 @@ void weights_kernel(WeightParams p, int chunks) {
   for (int a = 0; a < 4; ++a) {
     const int key = k0 + 8 * a + 4 * half;
     const int64_t at = (a >= 2 ? chunk[kPer - 1] : chunk[0]) * BS + key % BS;
-    if (key + 3 < S) {
+    if (key >= first && key + 3 < S) {
       f32x4 v = {acc[4 * a], acc[4 * a + 1], acc[4 * a + 2], acc[4 * a + 3]};
       if (p.weights_in && key < L) {
         const f32x4 w = *reinterpret_cast<const f32x4*>(p.weights_in + at);
@@ -117,7 +119,7 @@ void weights_kernel(WeightParams p, int chunks) {
     } else {
 #pragma unroll
       for (int e = 0; e < 4; ++e)
-        if (key + e < S) p.weights[at + e] = acc[4 * a + e] + (p.weights_in && key + e < L ? p.weights_in[at + e] : 0.f);
+        if (key + e >= first && key + e < S) p.weights[at + e] = acc[4 * a + e] + (p.weights_in && key + e < L ? p.weights_in[at + e] : 0.f);
     }
   }
 }

@@ -82,7 +82,7 @@ def lib():
             f = getattr(L, f"spexis_{kind}_attention{end}")
             f.argtypes = [P, P, *scales, i32, i32, i32, i32, i32, P, P, P, i32, i32, i32, i32, *groups, P, i32, f32, P, P, P, sz, P]
             f.restype = ctypes.c_int
-    L.spexis_attention_weights.argtypes = [P, i32, i32, i32, i32, i32, P, P, P, i32, i32, i32, i32, P, i32, f32, P, P, P, P, P]
+    L.spexis_attention_weights.argtypes = [P, i32, i32, i32, i32, i32, P, P, P, i32, i32, i32, i32, P, i32, f32, P, P, P, P, P, P]
     L.spexis_attention_weights.restype = ctypes.c_int
     L.spexis_evict_kv_workspace_size.argtypes, L.spexis_evict_kv_workspace_size.restype = [i32, i32, i32], sz
     L.spexis_evict_kv.argtypes = [P, P, P, i32, i32, i32, i32, i32, P, P, i32, i32, P, P, i32, P, P, P, sz, P]
@@ -363,7 +363,7 @@ def spexis_shared_attention_kv8(k_cache, v_cache, scales, num_blocks, num_kv_hea
 
 def spexis_attention_weights(k_cache, num_blocks, num_kv_heads, block_size, head_dim, query_start_loc, seq_lens,
                              block_tables, total_tokens, max_query_len, max_seq_len, q, num_q_heads, scale, lse, weights,
-                             weights_in=None, accepted_len=None, stream=None) -> None:
+                             weights_in=None, accepted_len=None, first_keys=None, stream=None) -> None:
     """weights and weights_in [num_blocks][Hkv][block_size] fp32 (weights_in may be weights)."""
     here, slots = torch._C._cuda_getDevice(), num_blocks * num_kv_heads * block_size
     rows, batch = total_tokens * num_q_heads, _batch_args(here, query_start_loc, seq_lens, block_tables)
@@ -371,6 +371,7 @@ def spexis_attention_weights(k_cache, num_blocks, num_kv_heads, block_size, head
         _on(k_cache, _BF16, here, slots * head_dim, "k_cache"), num_blocks, num_kv_heads, block_size, head_dim, *batch,
         total_tokens, max_query_len, max_seq_len, _on(q, _BF16, here, rows * head_dim, "q"), num_q_heads, scale,
         _on(lse, _F32, here, rows, "lse"), _on(accepted_len, _I32, here, batch[0], "accepted_len"),
+        _on(first_keys, _I32, here, batch[0], "first_keys"),
         _on(weights_in, _F32, here, slots, "weights_in"), _on(weights, _F32, here, slots, "weights"),
         _stream_on(stream, here)))
 

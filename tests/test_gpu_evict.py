@@ -24,12 +24,13 @@ def say(*a):
     print(*a, file=sys.stderr, flush=True)
 
 
-def weigh(c, k_pool, qsl, S, tables, q, scale, lse, before, accepted=None, out=None, max_s=None):
+def weigh(c, k_pool, qsl, S, tables, q, scale, lse, before, accepted=None, out=None, max_s=None, first=None):
     n = max(int(np.diff(qsl).max()), 1)
     w = torch.full((c.blocks, c.hkv, c.bs), 777.0, device="cuda") if out is None else out
     sx.spexis_attention_weights(k_pool, c.blocks, c.hkv, c.bs, c.D, dev(qsl), dev(S), dev(tables), q.shape[0], n,
                                 max_s or int(max(S.max(), 1)), q, q.shape[1], scale, lse, w, weights_in=before,
-                                accepted_len=None if accepted is None else dev(np.asarray(accepted, np.int32)))
+                                accepted_len=None if accepted is None else dev(np.asarray(accepted, np.int32)),
+                                first_keys=None if first is None else dev(np.asarray(first, np.int32)))
     torch.cuda.synchronize()
     return w
 
@@ -95,6 +96,25 @@ def test_scales(scale):
     want, size = osv.attention_weights(c.k, qsl, S, tables, q.double().cpu().numpy(), scale, lse.double().cpu().numpy(), None)
     mask = np.broadcast_to(used_places(S, tables, blocks, 16)[:, None, :], got.shape)
     assert (np.abs(got - want) <= U * size + 1e-30)[mask].all()
+
+
+@pytest.mark.parametrize("bs", [16, 32])
+def test_keys_in_front_of_the_first_are_left_as_they_are(bs):
+    r = np.random.default_rng(9)
+    qsl, S, tables, blocks = batch([9, 5, 1, 40, 3, 2], [500, 131, 17, 0, 200, 9], bs, 9)
+    c = Cache(blocks, bs, 2, 64, r, False)
+    q = queries(60, 6, 64, r)
+    k, v = c.pools()
+    _, lse = attend(c, (k, v), qsl, S, tables, q, 0.125)
+    first = [130, 128, 100, 17, -3, 0]   # behind the end: nothing is written
+    for before in (None, torch.rand((blocks, 2, bs), device="cuda")):
+        got = weigh(c, k, qsl, S, tables, q, 0.125, lse, before, first=first).double().cpu().numpy()
+        lo = np.clip(first, 0, S)
+        want, size = osv.attention_weights(c.k, qsl, S, tables, q.double().cpu().numpy(), 0.125, lse.double().cpu().numpy(),
+                                           None if before is None else before.double().cpu().numpy(), None, lo)
+        mask = used_places(S, tables, blocks, bs) & ~used_places(lo, tables, blocks, bs)
+        mask = np.broadcast_to(mask[:, None, :], got.shape)
+        assert (np.abs(got - want) <= U * size + 1e-30)[mask].all() and (got[~mask] == 777.0).all()
 
 
 def test_weights_of_a_row_sum_to_its_heads():
