@@ -4,7 +4,10 @@ Holds the device buffers of a batch (metadata, pools, outputs, workspaces sized 
 library's queries) and calls the three entry points of libspexis in order on one stream.
 
 Options: a cache held in 8 bits (AttentionInputs8 in place of AttentionInputs), q and keys that the append
-rotates by position (rotary), and the emitted tokens' log probabilities behind the acceptance (top_logprobs).
+rotates by position (rotary), the emitted tokens' log probabilities behind the acceptance (top_logprobs), prefixes
+that sequences share (shared), and the attention weights that a later eviction goes by (weights).
+
+Without acceptance (acc None) the step is that of prompts, of any length: append and attention.
 """
 from __future__ import annotations
 
@@ -21,11 +24,15 @@ from .workloads import AcceptInputs, AttentionInputs, AttentionInputs8, Batch, R
 class VerifyStep:
     def __init__(self, batch: Batch, attn: Union[AttentionInputs, AttentionInputs8], acc: Optional[AcceptInputs],
                  kv_chunk_tokens: int = 0, kind: int = sx.SPEXIS_INPUT_LOGITS, device="cuda",
-                 rotary: Optional[RotaryInputs] = None, top_logprobs: Optional[int] = None):
+                 rotary: Optional[RotaryInputs] = None, top_logprobs: Optional[int] = None, shared: Optional[tuple] = None,
+                 weights: Optional[torch.Tensor] = None):
         """rotary: attn's q and new_k are not rotated yet; the append does it (the rotated q is self.q).
         top_logprobs: with acceptance from logits, the emitted tokens' log probabilities and entropies, and that many
         alternatives of each (0: none); self.logprob, entropy [B][max_k+1], top_ids, top_logprob
-        [B][max_k+1][top_logprobs]."""
+        [B][max_k+1][top_logprobs].
+        shared: (group_start_loc, prefix_lens) of sequences that begin with the same blocks.
+        weights [num_blocks][Hkv][block_size] fp32: the sums of the cached keys' attention weights, to which the step adds
+        those of its accepted tokens (of all tokens without acceptance); bf16 cache only.  Shared keys have none."""
         spec = batch.spec
         self.batch, self.spec, self.kind = batch, spec, kind
         self.kv_chunk_tokens = kv_chunk_tokens
@@ -42,10 +49,35 @@ class VerifyStep:
         self.q = attn.q if rotary is None else torch.empty_like(attn.q)
         self.out = torch.empty_like(attn.q)
         self.scale = 1.0 / math.sqrt(spec.head_dim)
-        size = sx.spexis_verify_attention_kv8_workspace_size if self.in8 else sx.spexis_verify_attention_workspace_size
-        ws = size(batch.B, spec.num_q_heads, spec.num_kv_heads, spec.head_dim, batch.max_query_len, batch.max_seq_len,
-                  kv_chunk_tokens)
+        if weights is not None and self.in8:
+            raise ValueError("attention weights are kept for a bf16 cache")
+        self.weights = weights
+        self.shared = None if shared is None else tuple(torch.as_tensor(x, dtype=torch.int32, device=dev) for x in shared)
+        heads = (spec.num_q_heads, spec.num_kv_heads, spec.head_dim)
+        # more rows a KV head than the verification attention takes, and what it does not give
+        self.tiles = (shared is not None or weights is not None or
+                      spec.num_q_heads // spec.num_kv_heads * batch.max_query_len > 64)
+        if self.shared is not None:
+            ws = sx.spexis_shared_attention_workspace_size(batch.B, len(self.shared[1]), *heads, batch.T, batch.max_query_len,
+                                                           batch.max_seq_len)
+        elif self.tiles:
+            ws = sx.spexis_prompt_attention_workspace_size(batch.B, *heads, batch.T, batch.max_query_len, batch.max_seq_len)
+        else:
+            size = sx.spexis_verify_attention_kv8_workspace_size if self.in8 else sx.spexis_verify_attention_workspace_size
+            ws = size(batch.B, *heads, batch.max_query_len, batch.max_seq_len, kv_chunk_tokens)
         self.attn_ws = torch.empty(max(ws, 16), dtype=torch.uint8, device=dev)
+        self.lse = self.first_keys = None
+        if weights is not None:
+            self.lse = torch.empty(attn.q.shape[:2], device=dev)
+            # the lengths after the step (with acceptance, without the rejected tokens) and after an eviction
+            self.lens_after, self.lens_evicted = torch.empty_like(self.seq_lens), torch.empty_like(self.seq_lens)
+            ws = sx.spexis_evict_kv_workspace_size(batch.B, spec.num_kv_heads, batch.max_seq_len)
+            self.evict_ws = torch.empty(max(ws, 16), dtype=torch.uint8, device=dev)
+            if shared is not None:   # the keys that every sequence shares, in whole blocks
+                first = np.zeros(batch.B, np.int32)
+                for start, end, n in zip(shared[0], shared[0][1:], shared[1]):
+                    first[start:end] = n // spec.block_size * spec.block_size
+                self.first_keys = torch.as_tensor(first, device=dev)
         self.acc = acc
         self.max_k = batch.max_k
         if acc is not None:
@@ -89,6 +121,15 @@ class VerifyStep:
             sx.spexis_append_kv(*self._cache(), *new, stream=stream)
 
     def attention(self, stream=None):
+        if self.tiles:
+            rows = (self.q, self.spec.num_q_heads, self.scale, self.out, self.attn_ws)
+            if self.shared is not None:
+                f = sx.spexis_shared_attention_kv8 if self.in8 else sx.spexis_shared_attention
+                f(*self._cache(), self.batch.max_seq_len, *self.shared, *rows, lse=self.lse, stream=stream)
+            else:
+                f = sx.spexis_prompt_attention_kv8 if self.in8 else sx.spexis_prompt_attention
+                f(*self._cache(), self.batch.max_seq_len, *rows, lse=self.lse, stream=stream)
+            return
         f = sx.spexis_verify_attention_kv8 if self.in8 else sx.spexis_verify_attention
         f(*self._cache(), self.batch.max_seq_len, self.q, self.spec.num_q_heads, self.scale, self.out, self.attn_ws,
           kv_chunk_tokens=self.kv_chunk_tokens, stream=stream)
@@ -108,11 +149,36 @@ class VerifyStep:
                                  entropy=self.entropy, top_ids=self.top_ids, top_logprobs=self.top_logprob,
                                  temperature=self.acc.temperature, stream=stream)
 
+    def add_weights(self, stream=None):
+        """To self.weights, those of the accepted tokens, by the lengths after the step (self.lens_after)."""
+        s, b, a = self.spec, self.batch, self.attn
+        sx.spexis_attention_weights(a.k_pool, b.num_blocks, s.num_kv_heads, s.block_size, s.head_dim, self.qsl, self.lens_after,
+                                    self.tables, b.T, b.max_query_len, b.max_seq_len, self.q, s.num_q_heads, self.scale, self.lse,
+                                    self.weights, weights_in=self.weights,
+                                    accepted_len=self.accepted_len if self.acc is not None else None,
+                                    first_keys=self.first_keys, stream=stream)
+
+    def evict(self, keep_lens, keep_last, stream=None) -> torch.Tensor:
+        """Behind the step, drops all but keep_lens keys of each sequence, those of least weight; shared keys and the last
+        keep_last stay.  The new lengths (self.lens_evicted)."""
+        s, b, a = self.spec, self.batch, self.attn
+        if self.weights is None:
+            raise ValueError("no attention weights to go by")
+        sx.spexis_evict_kv(a.k_pool, a.v_pool, self.weights, b.num_blocks, s.num_kv_heads, s.block_size, s.head_dim,
+                           self.lens_after, self.tables, b.max_seq_len, keep_lens, keep_last, self.weights,
+                           self.lens_evicted, self.evict_ws, first_keys=self.first_keys, stream=stream)
+        return self.lens_evicted
+
     def run(self, stream=None):
         self.append(stream)
         self.attention(stream)
+        if self.weights is not None:
+            with torch.cuda.stream(stream or torch.cuda.current_stream()):
+                self.lens_after.copy_(self.seq_lens)
         if self.acc is not None:
-            self.accept(stream=stream)
+            self.accept(stream=stream, seq_lens_inout=self.lens_after if self.weights is not None else None)
+        if self.weights is not None:
+            self.add_weights(stream)
         if self.top_logprobs is not None:
             self.logprobs(stream)
 
