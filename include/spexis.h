@@ -294,7 +294,7 @@ int spexis_verify_attention_kv8(const void* k_cache, const void* v_cache, const 
 
 /*
  * Bytes of workspace spexis_prompt_attention and spexis_prompt_attention_kv8 need (> 0 whenever the sizes are valid, else
- * 0): 16 where rows fill the chip without cutting their keys, at most about 120 MB (head_dim 128) where they do not.
+ * 0): 16 where rows fill the chip without cutting their keys, at most about 80 MB (head_dim 128) where they do not.
  */
 size_t spexis_prompt_attention_workspace_size(int32_t num_seqs, int32_t num_q_heads, int32_t num_kv_heads,
                                               int32_t head_dim, int32_t total_tokens, int32_t max_query_len,
@@ -336,7 +336,11 @@ int spexis_prompt_attention_kv8(const void* k_cache, const void* v_cache, const 
                                 int32_t num_q_heads, float scale, void* out, float* lse,
                                 void* workspace, size_t workspace_bytes, void* stream);
 
-/* Bytes of workspace spexis_shared_attention and spexis_shared_attention_kv8 need (> 0 whenever the sizes are valid, else 0). */
+/*
+ * Bytes of workspace spexis_shared_attention and spexis_shared_attention_kv8 need (> 0 whenever the sizes are valid, else 0):
+ * up to about 300 MB (head_dim 128) for few rows, else the fp32 partials of the rows (4 (head_dim + 2) bytes a query token and
+ * head) and about 50 MB.
+ */
 size_t spexis_shared_attention_workspace_size(int32_t num_seqs, int32_t num_groups, int32_t num_q_heads,
                                               int32_t num_kv_heads, int32_t head_dim, int32_t total_tokens,
                                               int32_t max_query_len, int32_t max_seq_len);

@@ -249,8 +249,8 @@ struct TileLayout {
 
 // Units, and where their partials lie.  Prefixes count where sequences are longer than the least part (4 sequences of up to
 // 265 keys behind 160 that they share: 11 us as they are, 17 with the prefix apart).  They run together with the sequences up
-// to two workgroups a place that the chip has, and all tiles are cut into parts then, else the prefixes' alone.  Without
-// prefixes tiles are cut where one a workgroup fills less than half of the chip and there are keys enough for two parts.
+// to two workgroups a place that the chip has (kTileSlots), and all tiles are cut into parts then, else the prefixes' alone.
+// Without prefixes tiles are cut where one a workgroup leaves half of the places free and there are keys enough for two parts.
 TileLayout tile_layout(int64_t seqs, int64_t groups, int64_t hq, int64_t hkv, int64_t head_dim, int64_t total_tokens,
                        int64_t max_query_len, int64_t max_seq_len) {
   TileLayout l{};
@@ -603,7 +603,7 @@ int spexis_evict_kv(void* k_cache, void* v_cache, const float* weights, int32_t 
   if (bad_cache_shape(block_size, head_dim))
     return fail(SPEXIS_ERR_UNSUPPORTED, "%s: block_size %d / head_dim %d not in {16,32} x {64,128}", name, block_size,
                 head_dim);
-  // a launch holds fewer than 2^32 threads: at most 3072 for a (sequence, KV head)
+  // a launch holds fewer than 2^32 threads: at most 12 workgroups of 256 for a (sequence, KV head)
   if ((int64_t)num_seqs * num_kv_heads >= (1ll << 20) || (int64_t)max_blocks_per_seq * block_size >= (1ll << 30) ||
       max_seq_len >= (1 << 30))
     return fail(SPEXIS_ERR_UNSUPPORTED, "%s: too many sequences or slots", name);
