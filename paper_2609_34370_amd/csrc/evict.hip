@@ -4,8 +4,13 @@
 // evict_choose_kernel, a workgroup a (sequence, head): the weights come into registers once; the last one that stays is found
 // by its bits, from the highest in which the weights differ on, eight a pass (counts of a digit in LDS: whole numbers, so
 // their order does not matter); then one scan gives every key its new place, in a list of where the rows come from.
-// evict_move_kernel: the list's rows.  A key's new place is never behind its old one, so a wave that owns a slice of the
-// head dim moves it in place: what a step overwrites, no later one reads.
+// evict_move_kernel: the list's rows.  A key's new place is never behind its old one, so a workgroup that owns a slice of the
+// head dim moves it in place, in rounds: what a round overwrites, no later one reads.
+//
+// Bound by memory for a batch: 64 sequences of 1024 to 4096 keys cut to about a half (8 KV heads of 128) take 22 us to choose
+// and 235 to move: the lines of K hold keys that go beside those that stay, and V is read whole, so 1.0 GB where the kept rows
+// alone are 724 MB, 4.3 TB/s.  For one sequence by latency: 16001 keys cut to a quarter take 27 us to choose, eight workgroups
+// on their way through the passes, and 25 to move.  One wave a slice, without rounds, took 227 and 79.
 #include "common.h"
 #include "tiles.h"
 
@@ -13,7 +18,8 @@ namespace spexis {
 
 namespace {
 
-constexpr int kChoose = 1024, kWaves = kChoose / kWave;
+constexpr int kChoose = 1024, kWaves = kChoose / kWave;   // threads that choose
+constexpr int kMove = 256;   // and that move a slice
 
 // A weight's bits in the order of the values: -0 counts as 0, a NaN as less than any number; never 0 or 0xFFFFFFFF.
 __device__ __forceinline__ uint32_t rank_bits(float w) {
@@ -27,7 +33,8 @@ __device__ __forceinline__ uint32_t rank_bits(float w) {
 template <int kHeld>
 __global__ __launch_bounds__(kChoose) __attribute__((amdgpu_waves_per_eu(kHeld == 4 ? 8 : 4)))
 void evict_choose_kernel(EvictParams p) {
-  __shared__ int sm_hist[256], sm_wave[kWaves], sm_pick[3], sm_more[kHeld][kWaves], sm_equal[kHeld][kWaves], sm_first;
+  __shared__ uint32_t sm_set[kWaves], sm_clear[kWaves];
+  __shared__ int sm_hist[256], sm_pick[3], sm_more[kHeld][kWaves], sm_equal[kHeld][kWaves], sm_first;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int b = (int)blockIdx.x / p.hkv, h = (int)blockIdx.x % p.hkv, bs = p.block_size;
   const int S = clampi(p.seq_lens[b], 0, (int)min((int64_t)p.max_blocks * bs, (int64_t)p.max_seq_len));
@@ -74,17 +81,25 @@ void evict_choose_kernel(EvictParams p) {
   uint32_t least = 0xFFFFFFFEu;
   int equal = 0, want = m - f - last;
   if (want > 0) {
-    const uint32_t one = rank_bits(p.weights[place(lo)]);
-    uint32_t differ = 0;
-    each([&](uint32_t k) { differ |= k ^ one; });
-    differ = (uint32_t)wave_or((int)differ);
-    if (lane == 0) sm_wave[wave] = (int)differ;
+    uint32_t set = 0, clear = 0;   // the bits that some have, and that some have not
+    each([&](uint32_t k) {
+      set |= k;
+      clear |= ~k;
+    });
+    set = (uint32_t)wave_or((int)set);
+    clear = (uint32_t)wave_or((int)clear);
+    if (lane == 0) {
+      sm_set[wave] = set;
+      sm_clear[wave] = clear;
+    }
     __syncthreads();
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) differ |= (uint32_t)sm_wave[w];
-    int shift = 32 - __builtin_clz(differ | 1);   // ranks agree from this bit up
-    if (differ == 0) shift = 0;
-    uint32_t prefix = (uint32_t)((uint64_t)one >> shift);
+    for (int w = 0; w < kWaves; ++w) {
+      set |= sm_set[w];
+      clear |= sm_clear[w];
+    }
+    int shift = (set & clear) != 0 ? 32 - __builtin_clz(set & clear) : 0;   // ranks agree from this bit up
+    uint32_t prefix = (uint32_t)((uint64_t)set >> shift);
     while (true) {
       if (shift == 0) {
         least = prefix;
@@ -203,142 +218,165 @@ void evict_choose_kernel(EvictParams p) {
   }
 }
 
-// Wave s of a (sequence, head): slice s of K (8 of the head dim: 16 bytes a row), or of V (4 rows of the head dim).
-//   K: 16 bytes a lane from each row's old place to its new one, kBatch times 64 rows read, then written.
-//   V holds a row's elements apart, two bytes each; gathered from memory by twos they took 51 cycles for each 64.  So the wave
-//   streams the old blocks whole through LDS, 128 slots a group, and picks the elements there: lane l makes of head-dim row
-//   l / 16 and 128 new places the 16 bytes of 8 slots.
+// A workgroup moves a slice of a (sequence, head): 8 of the head dim of K (16 bytes a row), or 4 rows of the head dim
+// of V.  Rows go in rounds, in order: all of a round are read, the workgroup meets, then they are written.  The next round's
+// may be on their way meanwhile: they lie where this one does not write.
+//   K: 16 bytes a lane from each row's old place to its new one, kBatch a thread and round.
+//   V holds a row's elements apart, two bytes each; gathered from memory by twos they took 51 cycles for each 64.  So a wave,
+//   for 128 new places, streams the old blocks that they come from through LDS, 128 slots a group, and picks the elements there:
+//   lane l makes of head-dim row l / 16 the 16 bytes of 8 slots.
 template <int D, int BS>
-__global__ __launch_bounds__(256) void evict_move_kernel(EvictParams p) {
-  constexpr int kSlices = D / 8;
+__global__ __launch_bounds__(kMove) void evict_move_kernel(EvictParams p) {
+  constexpr int W = kMove / kWave;
+  constexpr int kSlices = D / 8, kAll = 3 * kSlices;   // kSlices of K, twice as many of V
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
-  const int per = 3 * kSlices / 4;   // kSlices of K, twice as many of V
-  const int item = (int)(blockIdx.x / per), slice = (int)(blockIdx.x % per) * 4 + wave;
+  const int item = (int)(blockIdx.x / kAll), slice = (int)(blockIdx.x % kAll);
   const int b = item / p.hkv, h = item % p.hkv;
   const int m = p.hdr[2 * (int64_t)item], first = p.hdr[2 * (int64_t)item + 1];
-  if (slice == 0 && h == 0 && lane == 0) p.new_lens[b] = m;
+  if (slice == 0 && h == 0 && threadIdx.x == 0) p.new_lens[b] = m;
   if (first >= m) return;
   const int32_t* table = p.block_tables + (int64_t)b * p.max_blocks;
-  auto chunk = [&](int t) { return ((int64_t)clampi(table[t / BS], 0, p.num_blocks - 1) * p.hkv + h) * (BS * D); };
+  const int32_t* list = p.list + (int64_t)item * p.pitch;
+  auto chunk_of = [&](int block) { return ((int64_t)clampi(block, 0, p.num_blocks - 1) * p.hkv + h) * (BS * D); };
   if (slice < kSlices) {
-    constexpr int kBatch = 4;
-    const int32_t* list = p.list + (int64_t)item * p.pitch;
+    constexpr int kBatch = 4, kRound = 64 * W * kBatch;
     uint16_t* k = reinterpret_cast<uint16_t*>(p.k_cache) + slice * BS * 8;
-    auto from = [&](int t) { return list[min(max(t, first), m - 1)]; };
-    int src[kBatch];
-    int t0 = first & ~63;
+    int r0 = (first & ~63) + (int)threadIdx.x;
+    int src[kBatch], to[kBatch];   // old places; the new ones' blocks
+    u32x4 v[kBatch];
+    auto look_up = [&](int r) {
 #pragma unroll
-    for (int i = 0; i < kBatch; ++i) src[i] = from(t0 + 64 * i + lane);
-    for (; t0 < m; t0 += 64 * kBatch) {
-      u32x4 v[kBatch];
-      int64_t at[kBatch], to[kBatch];
+      for (int i = 0; i < kBatch; ++i) src[i] = list[min(max(r + 64 * W * i, first), m - 1)];
+    };
+    auto read = [&](u32x4* v) {
+      int block[kBatch];
 #pragma unroll
-      for (int i = 0; i < kBatch; ++i) at[i] = chunk(src[i]) + (src[i] % BS) * 8;
+      for (int i = 0; i < kBatch; ++i) block[i] = table[src[i] / BS];
 #pragma unroll
-      for (int i = 0; i < kBatch; ++i) v[i] = ld16(k + at[i]);
+      for (int i = 0; i < kBatch; ++i) v[i] = ld16(k + chunk_of(block[i]) + (src[i] % BS) * 8);
+    };
+    look_up(r0);
+    read(v);
+    for (int left = m - (first & ~63); left > 0; left -= kRound, r0 += kRound) {
+#pragma unroll
+      for (int i = 0; i < kBatch; ++i) to[i] = table[min(r0 + 64 * W * i, m - 1) / BS];
+      look_up(r0 + kRound);
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // the round's rows are here
+      __syncthreads();
+      u32x4 next[kBatch];
+      if (left > kRound) read(next);
 #pragma unroll
       for (int i = 0; i < kBatch; ++i) {
-        to[i] = chunk(min(t0 + 64 * i + lane, m - 1));
-        src[i] = from(t0 + 64 * (kBatch + i) + lane);
+        const int t = r0 + 64 * W * i;
+        if (t >= first && t < m) st16(k + chunk_of(to[i]) + (t % BS) * 8, v[i]);
       }
 #pragma unroll
-      for (int i = 0; i < kBatch; ++i) {
-        const int t = t0 + 64 * i + lane;
-        if (t >= first && t < m) st16(k + to[i] + (t % BS) * 8, v[i]);
-      }
+      for (int i = 0; i < kBatch; ++i) v[i] = next[i];
     }
   } else {
     typedef int i32x4 __attribute__((ext_vector_type(4)));
-    __shared__ u32x4 sm_group[4][kWave];
+    __shared__ u32x4 sm_group[W][kWave];
     u32x4* const sm = sm_group[wave];
-    const int32_t* list = p.list + (int64_t)item * p.pitch;
     uint16_t* v = reinterpret_cast<uint16_t*>(p.v_cache) + (slice - kSlices) * 4 * BS;
     // a group's bytes, 16 a lane: its blocks, of each 4 rows of BS slots
     constexpr int kLanes = BS / 2;   // lanes a block
     const int row = lane / 16, unit = (lane % 16) / 2, hf = lane % 2;
-    const int last = list[m - 1], last_group = last >> 7;
-    // The blocks of a window of groups come with one load, a window ahead; a lane's is handed to it.  (No farther than the
-    // last key that stays.)
-    constexpr int kPer = 128 / BS, kWindow = 64 / kPer;
-    auto look_up = [&](int w) { return table[min(w * 64 + lane, last / BS)]; };
-    int window = (list[first] >> 7) / kWindow, blocks = look_up(window), blocks_next = look_up(window + 1);
-    auto load = [&](int g) {   // for g in order
-      g = min(g, last_group);
-      if (g / kWindow > window) {
-        ++window;
-        blocks = blocks_next;
-        blocks_next = look_up(window + 1);
-      }
-      const int block = __builtin_amdgcn_ds_bpermute(4 * (g % kWindow * kPer + lane / kLanes), blocks);
-      return ld16(v + ((int64_t)clampi(block, 0, p.num_blocks - 1) * p.hkv + h) * (BS * D) + (lane % kLanes) * 8);
-    };
     // the lane's 8 new places of a batch: position hf * 8 + e of a unit of 16 holds slot 8 (e / 4) + 4 hf + e % 4
     auto place = [&](int t0, int e) { return t0 + unit * 16 + 8 * (e >> 2) + 4 * hf + (e & 3); };
-    int t0 = first & ~127, g = list[first] >> 7;
-    i32x4 s0 = *reinterpret_cast<const i32x4*>(list + place(t0, 0)), s1 = *reinterpret_cast<const i32x4*>(list + place(t0, 4));
-    constexpr int kAhead = 3;   // groups on their way
-    u32x4 ahead[kAhead];
-    const u32x4 now = load(g);
-#pragma unroll
-    for (int i = 0; i < kAhead; ++i) ahead[i] = load(g + 1 + i);
-    sm[lane] = now;
-    wave_lds_fence();
-    for (; t0 < m; t0 += 128) {
-      int src[8];
+    // A batch's old places (the list's pitch holds whole batches), of its groups the first block and the last.
+    i32x4 s0, s1;
+    int from = 0, until = 0;
+    auto look_up = [&](int t0) {
+      s0 = *reinterpret_cast<const i32x4*>(list + place(t0, 0));
+      s1 = *reinterpret_cast<const i32x4*>(list + place(t0, 4));
+      from = list[max(t0, first)] / BS;
+      until = list[min(t0 + 127, m - 1)] / BS;
+    };
+    // The blocks of a window of groups come with one load; a lane's is handed to it.
+    constexpr int kPer = 128 / BS, kWindow = 64 / kPer, kAhead = 3;   // (kAhead: groups on their way)
+    int block0 = 0, last = 0, window = 0, blocks = 0, blocks_next = 0;
+    u32x4 now, ahead[kAhead];
+    auto load = [&](int g) {   // for g in order
+      if (g / kWindow > window) blocks = table[min(block0 + ++window * 64 + lane, last)];
+      const int block = __builtin_amdgcn_ds_bpermute(4 * (g % kWindow * kPer + lane / kLanes), blocks);
+      return ld16(v + chunk_of(block) + (lane % kLanes) * 8);
+    };
+    auto look_further = [&]() { blocks_next = table[min(from + lane, until)]; };
+    int src[8];   // from the first block on; -1: not of the batch
+    auto begin = [&](int t0) {
+      block0 = __builtin_amdgcn_readfirstlane(from);
+      last = __builtin_amdgcn_readfirstlane(until);
+      window = 0;
+      blocks = blocks_next;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         const int t = place(t0, e);
-        src[e] = t >= first && t < m ? (e < 4 ? s0[e & 3] : s1[e & 3]) : -1;
+        src[e] = t >= first && t < m ? (e < 4 ? s0[e & 3] : s1[e & 3]) - block0 * BS : -1;
       }
-      const int until = t0 + 128 <= m ? __builtin_amdgcn_readlane(src[7], 15) >> 7 : last_group;
-      const int64_t to_chunk = chunk(min(place(t0, 0), m - 1));
-      if (t0 + 128 < m) {   // the list's pitch holds whole batches
-        s0 = *reinterpret_cast<const i32x4*>(list + place(t0 + 128, 0));
-        s1 = *reinterpret_cast<const i32x4*>(list + place(t0 + 128, 4));
-      }
-      uint32_t x[8];
-      int at[8];   // where in a group, and which (what is in other groups is read too, and left)
+      now = load(0);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const int s = src[e] & 127;
-        at[e] = s / BS * (4 * BS) + row * BS + ((s % BS & ~12) | ((s >> 2 & 1) << 3) | ((s >> 3 & 1) << 2));
-        x[e] = 0;
-      }
-      while (true) {
+      for (int i = 0; i < kAhead; ++i) ahead[i] = load(min(1 + i, (last - block0) / kPer));
+    };
+    constexpr int kRound = 128 * W;
+    int t0 = (first & ~127) + 128 * wave;
+    if (t0 < m) {
+      look_up(t0);
+      look_further();
+      begin(t0);
+    }
+    if (t0 + kRound < m) look_up(t0 + kRound);
+    for (int left = m - (first & ~127); left > 0; left -= kRound, t0 += kRound) {
+      u32x4 w = {0, 0, 0, 0};
+      const int t = place(t0, 0);   // the lane's first place; its last is 11 on
+      const int to = table[min(t, m - 1) / BS];
+      if (t0 + kRound < m) look_further();
+      if (t0 < m) {
+        const int groups = (last - block0) / kPer;
+        uint32_t x[8];
+        int at[8];   // where in a group, and which (what is in other groups is read too, and left)
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-          x[e] |= reinterpret_cast<const uint16_t*>(sm)[at[e]] & (src[e] >> 7 == g ? 0xFFFFu : 0u);
-        if (g >= until) break;
-        wave_lds_fence();
-        sm[lane] = ahead[0];
-        wave_lds_fence();
-        ++g;
+        for (int e = 0; e < 8; ++e) {
+          const int s = src[e] & 127;
+          at[e] = s / BS * (4 * BS) + row * BS + ((s % BS & ~12) | ((s >> 2 & 1) << 3) | ((s >> 3 & 1) << 2));
+          x[e] = 0;
+        }
+        for (int g = 0; g <= groups; ++g) {
+          wave_lds_fence();
+          sm[lane] = now;
+          wave_lds_fence();
+          now = ahead[0];
 #pragma unroll
-        for (int i = 0; i + 1 < kAhead; ++i) ahead[i] = ahead[i + 1];
-        ahead[kAhead - 1] = load(g + kAhead);
-      }
-      const int t = place(t0, 0);   // the chunk's first slot; its last is 11 on
-      uint16_t* to = v + to_chunk + row * BS + (t % BS & 16) + 8 * hf;
-      if (t >= first && t + 11 < m) {
-        u32x4 w;
+          for (int i = 0; i + 1 < kAhead; ++i) ahead[i] = ahead[i + 1];
+          if (g + kAhead < groups) ahead[kAhead - 1] = load(g + 1 + kAhead);
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            x[e] |= reinterpret_cast<const uint16_t*>(sm)[at[e]] & (src[e] >> 7 == g ? 0xFFFFu : 0u);
+        }
 #pragma unroll
         for (int c = 0; c < 4; ++c) w[c] = x[2 * c] | x[2 * c + 1] << 16;
-        st16(to, w);
+      }
+      if (t0 + kRound < m) begin(t0 + kRound);
+      if (t0 + 2 * kRound < m) look_up(t0 + 2 * kRound);
+      __syncthreads();   // the round's elements are picked
+      uint16_t* const at = v + chunk_of(to) + row * BS + (t % BS & 16) + 8 * hf;
+      if (t >= first && t + 11 < m) {
+        st16(at, w);
       } else {
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-          if (src[e] >= 0) to[e] = (uint16_t)x[e];
+        for (int e = 0; e < 8; ++e) {
+          const int place_e = place(t0, e);
+          if (place_e >= first && place_e < m) at[e] = (uint16_t)(w[e >> 1] >> 16 * (e & 1));
+        }
       }
     }
   }
 }
 
-template <int D>
+template <int D, int BS>
 static hipError_t launch_move_t(const EvictParams& p, hipStream_t s) {
-  const dim3 grid((unsigned)((int64_t)p.num_seqs * p.hkv * (3 * (D / 8) / 4)));
-  if (p.block_size == 16) hipLaunchKernelGGL((evict_move_kernel<D, 16>), grid, dim3(256), 0, s, p);
-  else hipLaunchKernelGGL((evict_move_kernel<D, 32>), grid, dim3(256), 0, s, p);
+  const dim3 grid((unsigned)((int64_t)p.num_seqs * p.hkv * (3 * (D / 8))));
+  hipLaunchKernelGGL((evict_move_kernel<D, BS>), grid, dim3(kMove), 0, s, p);
   return hipGetLastError();
 }
 
@@ -348,7 +386,8 @@ hipError_t launch_evict(const EvictParams& p, hipStream_t s) {
   else hipLaunchKernelGGL((evict_choose_kernel<16>), items, dim3(kChoose), 0, s, p);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  return p.head_dim == 128 ? launch_move_t<128>(p, s) : launch_move_t<64>(p, s);
+  if (p.head_dim == 128) return p.block_size == 16 ? launch_move_t<128, 16>(p, s) : launch_move_t<128, 32>(p, s);
+  return p.block_size == 16 ? launch_move_t<64, 16>(p, s) : launch_move_t<64, 32>(p, s);
 }
 
 }  // namespace spexis

@@ -159,6 +159,8 @@ EVICT = [
     (2, 64, 16, [16384, 16385, 20000], [8000, 16384, 19000], [0, 4, 40], 50),     # longer than what a workgroup holds
     (1, 64, 32, [40000], [3], [1], 1),
     (1, 64, 32, [33000], [33000 - 1], None, 17000),
+    (2, 128, 16, [9000, 3300, 12000], [300, 2600, 520], [0, 640, 5], 3),   # few of many keys; several rounds of moves
+    (1, 128, 32, [6000, 12000], [1100, 700], None, 600),
 ]
 
 
