@@ -393,7 +393,7 @@ int spexis_shared_attention_kv8(const void* k_cache, const void* v_cache, const 
  *                 [0, n_b]), and S_b is its length with them: spexis_accept's accepted_len and seq_lens_inout after it
  *   weights_in    [num_blocks][Hkv][block_size] fp32 (read), which may be `weights`, or NULL: all sums begin here
  *   weights       the same shape (written)
- *   max_seq_len   host: >= max_b S_b (keys from it on are left out)
+ *   max_seq_len   host: >= max_b S_b
  *   first_keys    [num_seqs] int32 or NULL (0): keys in front of it (clamped to [0, S_b]) are left as they were
  * Of the sequences that share a block all but one must have it in front of their first key: the calls' sums are not added up.
  * Supported shapes as spexis_prompt_attention; num_seqs * Hkv * ceil(max_seq_len / 128) < 2^24.  k_cache, q, weights and
@@ -425,7 +425,7 @@ size_t spexis_evict_kv_workspace_size(int32_t num_seqs, int32_t num_kv_heads, in
  *   seq_lens      [num_seqs] int32 (read);  new_seq_lens [num_seqs] int32 (written); may be seq_lens
  *   max_seq_len   host: >= max_b S_b (keys from it on are dropped)
  * The blocks of a sequence from the first key that moves on must be its own.  Pools, weights and workspace 16-byte aligned.
- * Supported: head_dim in {64, 128}, block_size in {16, 32}; num_seqs * Hkv < 2^20.
+ * Supported: head_dim in {64, 128}, block_size in {16, 32}; num_seqs * Hkv < 2^18.
  * Errors: INVALID_ARGUMENT, UNSUPPORTED, WORKSPACE_TOO_SMALL, HIP.
  */
 int spexis_evict_kv(void* k_cache, void* v_cache, const float* weights, int32_t num_blocks, int32_t num_kv_heads,

@@ -603,8 +603,8 @@ int spexis_evict_kv(void* k_cache, void* v_cache, const float* weights, int32_t 
   if (bad_cache_shape(block_size, head_dim))
     return fail(SPEXIS_ERR_UNSUPPORTED, "%s: block_size %d / head_dim %d not in {16,32} x {64,128}", name, block_size,
                 head_dim);
-  // a launch holds fewer than 2^32 threads: at most 12 workgroups of 256 for a (sequence, KV head)
-  if ((int64_t)num_seqs * num_kv_heads >= (1ll << 20) || (int64_t)max_blocks_per_seq * block_size >= (1ll << 30) ||
+  // a launch holds fewer than 2^32 threads: at most 48 workgroups of 256 for a (sequence, KV head)
+  if ((int64_t)num_seqs * num_kv_heads >= (1ll << 18) || (int64_t)max_blocks_per_seq * block_size >= (1ll << 30) ||
       max_seq_len >= (1 << 30))
     return fail(SPEXIS_ERR_UNSUPPORTED, "%s: too many sequences or slots", name);
   if (num_seqs == 0) return ok();

@@ -229,7 +229,6 @@ void tile_attn_kernel(TileAttnParams p) {
   const bool is_prefix = some && un.seg < p.num_groups;
   // joins the prefix's partials itself: they were written by the launch before
   const bool whole = some && !is_prefix && un.parts == 1 && (g.group < 0 || p.seg_lo > 0);
-  if (is_prefix && u >= p.prefix_units) return;   // groups that overlap
   if (h == 0 && tid == 0) {   // what those who join the partials need to know
     if (is_prefix && un.tile == 0 && un.part == 0)
       *reinterpret_cast<u32x4*>(p.groups_hdr + (int64_t)un.seg * 4) =
@@ -242,7 +241,7 @@ void tile_attn_kernel(TileAttnParams p) {
       *reinterpret_cast<u32x4*>(hdr + 4) = u32x4{(uint32_t)un.parts, (uint32_t)un.first, (uint32_t)g.group, 0u};
     }
   }
-  if (!some) return;
+  if (!some || (is_prefix && u >= p.prefix_units)) return;   // (the latter: groups that overlap)
 
   const int row0 = tile * kRows;
   const int sure0 = min((int64_t)g.end - 1, (int64_t)g.last + row0 / p.group);   // every row sees the keys up to this one

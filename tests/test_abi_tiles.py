@@ -87,7 +87,7 @@ def test_eviction():
                dict(wo=ODD), dict(ws=ODD)):
         assert evict(**kw) == INVALID, kw
         assert sx.lib().spexis_last_error().startswith(b"spexis_evict_kv:")
-    for kw in (dict(bs=8), dict(d=96), dict(mb=2**26), dict(B=2**19), dict(ms=2**30)):
+    for kw in (dict(bs=8), dict(d=96), dict(mb=2**26), dict(B=2**17), dict(ms=2**30)):
         assert evict(**kw) == UNSUPPORTED, kw
     need = sx.spexis_evict_kv_workspace_size(2, 2, 640)
     assert need > 0 and evict(wsb=need - 1) == SMALL and evict(ws=None) == SMALL

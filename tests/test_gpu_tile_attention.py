@@ -281,6 +281,30 @@ def test_a_padded_batch(shared):
     assert (out[T:] == 777.0).all() and (lse[T:] == 777.0).all()
 
 
+@pytest.mark.parametrize("hkv", [2, 16])   # together and merged; the prefixes in front
+def test_groups_that_overlap_write_nothing_outside(hkv):
+    """More prefix units than an ascending list of groups can have: outputs unspecified, what is around them as it was, also
+    with a workspace in which a call of more rows has left its headers."""
+    r = np.random.default_rng(12)
+    n, G, groups = [5, 9, 3, 8], 16, 400
+    qsl, S, tables, blocks = batch(n, [700, 650, 800, 640], 16, 12)
+    tables[:, :38] = tables[0, :38]
+    c = Cache(blocks, 16, hkv, 64, r, False)
+    k, v = c.pools()
+    T, more = int(qsl[-1]), 40
+    q, out = queries(T + more, G * hkv, 64, r), torch.full((T + more, G * hkv, 64), 3.0, dtype=torch.bfloat16, device="cuda")
+    lse = torch.full((T + more, G * hkv), 5.0, device="cuda")
+    starts = np.array([0, 4] * (groups // 2) + [4], np.int32)   # every other group is all of them
+    lens = np.full(groups, 38 * 16, np.int32)
+    size = sx.spexis_shared_attention_workspace_size(4, groups, G * hkv, hkv, 64, T, 9, 809)
+    ws = torch.zeros(size, dtype=torch.uint8, device="cuda")
+    ws[: size // 16 * 16].view(torch.int32).view(-1, 4)[:] = torch.tensor([1, T + 20, 16, 0], dtype=torch.int32, device="cuda")
+    sx.spexis_shared_attention(k, v, blocks, hkv, 16, 64, dev(qsl), dev(S), dev(tables), T, 9, 809, dev(starts), dev(lens), q,
+                               G * hkv, 0.125, out, ws, lse=lse)
+    torch.cuda.synchronize()
+    assert (out[T:] == 3.0).all() and (lse[T:] == 5.0).all()
+
+
 def test_without_lse_and_without_groups():
     r = np.random.default_rng(9)
     qsl, S, tables, blocks = batch([40, 3], [20, 700], 32, 9)
