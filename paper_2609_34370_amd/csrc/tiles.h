@@ -37,6 +37,7 @@ struct TileAttnParams {
   int shares;                   // row tiles (without a merge those of prefixes alone) are cut into parts, about so many a head; 0: not
   int units, prefix_units;      // the most units a head of either launch
   int merge;                    // prefixes and sequences in one launch, tile_merge_kernel joins partials
+  int single;                   // (launcher) every segment has one tile at most: unit u is segment u
   int seg_lo, seg_hi;           // (launcher) its segments: the groups' prefixes are 0 .. num_groups - 1, then the sequences
   uint32_t q_sign;              // a negative scale turns q's signs over
   float scale_log2e, lazy;      // |scale| log2(e); kLazy in scores before the scale

@@ -113,6 +113,8 @@ PROMPTS = [
     (16, 8, 64, 32, [900] * 9, [0] * 9),     # more tiles than workgroups at a time: no parts
     (4, 2, 128, 32, [1], [4000]),
     (3, 1, 64, 16, [1], [0]),
+    (4, 2, 64, 16, [0] * 300 + [1], [0] * 300 + [9]),   # fewer row tiles than sequences
+    (8, 2, 128, 32, [0, 3, 0, 0, 200, 1] * 30, [40, 3, 0, 700, 90, 5] * 30),
 ]
 
 
