@@ -25,11 +25,12 @@ class VerifyStep:
     def __init__(self, batch: Batch, attn: Union[AttentionInputs, AttentionInputs8], acc: Optional[AcceptInputs],
                  kv_chunk_tokens: int = 0, kind: int = sx.SPEXIS_INPUT_LOGITS, device="cuda",
                  rotary: Optional[RotaryInputs] = None, top_logprobs: Optional[int] = None, shared: Optional[tuple] = None,
-                 weights: Optional[torch.Tensor] = None):
+                 weights: Optional[torch.Tensor] = None, positions: Optional[np.ndarray] = None):
         """rotary: attn's q and new_k are not rotated yet; the append does it (the rotated q is self.q).
         top_logprobs: with acceptance from logits, the emitted tokens' log probabilities and entropies, and that many
         alternatives of each (0: none); self.logprob, entropy [B][max_k+1], top_ids, top_logprob
         [B][max_k+1][top_logprobs].
+        positions [T]: where the rotation turns the tokens to, if not to their places in the cache (after an eviction).
         shared: (group_start_loc, prefix_lens) of sequences that begin with the same blocks.
         weights [num_blocks][Hkv][block_size] fp32: the sums of the cached keys' attention weights, to which the step adds
         those of its accepted tokens (of all tokens without acceptance); bf16 cache only.  Shared keys have none."""
@@ -42,7 +43,16 @@ class VerifyStep:
         self.tables = torch.as_tensor(batch.block_tables, device=dev)
         self.attn = attn
         self.in8 = isinstance(attn, AttentionInputs8)
-        if rotary is not None and rotary.cos_sin.shape[0] < batch.max_seq_len:
+        self.positions = None
+        if positions is not None:
+            if rotary is None:
+                raise ValueError("positions without a rotation")
+            positions = np.asarray(positions, np.int32)
+            if positions.min() < 0 or positions.max() >= rotary.cos_sin.shape[0]:
+                raise ValueError(f"the rotation's table ends at position {rotary.cos_sin.shape[0]}, "
+                                 f"the tokens at {positions.max()}")
+            self.positions = torch.as_tensor(positions, device=dev)
+        elif rotary is not None and rotary.cos_sin.shape[0] < batch.max_seq_len:
             raise ValueError(f"the rotation's table ends at position {rotary.cos_sin.shape[0]}, "
                              f"the longest sequence at {batch.max_seq_len}")
         self.rotary = rotary
@@ -52,6 +62,11 @@ class VerifyStep:
         if weights is not None and self.in8:
             raise ValueError("attention weights are kept for a bf16 cache")
         self.weights = weights
+        if shared is not None:
+            for start, end, n in zip(shared[0], shared[0][1:], shared[1]):
+                blocks = batch.block_tables[start:end, : n // spec.block_size]
+                if (batch.ctx_lens[start:end] < n).any() or (blocks != blocks[:1]).any():
+                    raise ValueError(f"sequences {start} to {end - 1} do not share {n} cached tokens")
         self.shared = None if shared is None else tuple(torch.as_tensor(x, dtype=torch.int32, device=dev) for x in shared)
         heads = (spec.num_q_heads, spec.num_kv_heads, spec.head_dim)
         # more rows a KV head than the verification attention takes, and what it does not give
@@ -112,7 +127,8 @@ class VerifyStep:
         new = (self.attn.new_k, self.attn.new_v)
         rotation = {}
         if self.rotary is not None:
-            rotation = dict(cos_sin=self.rotary.cos_sin, style=self.rotary.style, q=self.attn.q, q_out=self.q)
+            rotation = dict(cos_sin=self.rotary.cos_sin, style=self.rotary.style, positions=self.positions,
+                            q=self.attn.q, q_out=self.q)
         if self.in8:
             sx.spexis_rotate_append_kv8(*self._cache(), *new, **rotation, stream=stream)
         elif rotation:

@@ -178,9 +178,30 @@ def test_a_step_chooses_its_attention():
     spec = wl.spec_with(1, batch=2)
     for k, kw, tiles in (([4, 2], {}, False), ([300, 2], {}, True), ([4, 2], dict(shared=([0, 2], [16])), True),
                          ([4, 2], dict(weights=torch.zeros(1)), True)):
-        batch = wl.make_batch(spec, ctx_lens=[30, 70], k=k)
+        batch = wl.make_batch(spec, ctx_lens=[40, 70], k=k)
+        batch.block_tables[1, 0] = batch.block_tables[0, 0]
         s = VerifyStep(batch, wl.make_attention_inputs(spec, batch), None, device="cpu", **kw)
         assert s.tiles == tiles
-    batch = wl.make_batch(spec, ctx_lens=[30, 70], k=[4, 2])
+    batch = wl.make_batch(spec, ctx_lens=[40, 70], k=[4, 2])
+    batch.block_tables[1, :2] = batch.block_tables[0, :2]
     s = VerifyStep(batch, wl.make_attention_inputs(spec, batch), None, device="cpu", shared=([0, 2], [31]), weights=torch.zeros(1))
     assert s.first_keys.tolist() == [31 // spec.block_size * spec.block_size] * 2
+
+
+@pytest.mark.skipif(not os.path.exists(sx.LIB_PATH), reason="libspexis.so not built")
+def test_what_a_step_refuses():
+    from paper_2609_34370_amd import workloads as wl
+    from paper_2609_34370_amd.step import VerifyStep
+    spec = wl.spec_with(1, batch=2)
+    batch = wl.make_batch(spec, ctx_lens=[40, 70], k=[4, 2])
+    batch.block_tables[1, :2] = batch.block_tables[0, :2]
+    attn, bs = wl.make_attention_inputs(spec, batch), spec.block_size
+    rotary = wl.make_rotary_inputs(80, spec.head_dim)
+    VerifyStep(batch, attn, None, device="cpu", shared=([0, 2], [2 * bs]))
+    for kw in (dict(shared=([0, 2], [3 * bs])), dict(shared=([0, 2], [41])), dict(positions=[1] * batch.T),
+               dict(rotary=rotary, positions=[80] * batch.T), dict(rotary=rotary, positions=[-1] * batch.T)):
+        with pytest.raises(ValueError):
+            VerifyStep(batch, attn, None, device="cpu", **kw)
+    VerifyStep(batch, attn, None, device="cpu", rotary=rotary, positions=[79] * batch.T)
+    with pytest.raises(ValueError):
+        VerifyStep(batch, wl.make_attention_inputs8(spec, batch), None, device="cpu", weights=torch.zeros(1))

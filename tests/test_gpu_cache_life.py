@@ -1,5 +1,6 @@
 """Prompts, steps behind a shared prefix, attention weights and evictions together, as a serving loop runs them, against the
 64-bit forms on the GPU's own inputs of each stage; as a replayed graph and on another stream, bit for bit."""
+import dataclasses
 import sys
 
 import numpy as np
@@ -105,6 +106,26 @@ def test_step_weights_and_eviction():
     now = View(s)
     assert np.array_equal(now.k[kept], k[kept]) and np.array_equal(now.v[kept], v[kept])
     assert np.array_equal(s.weights.cpu().numpy().transpose(0, 2, 1)[kept], w2.transpose(0, 2, 1)[kept])
+    # the next step's tokens follow behind what is left, at the positions that they have in the text
+    n = np.array([3, 1, 5, 2, 2, 4], np.int32)   # (no further than the blocks that the sequences have)
+    qsl = np.concatenate([[0], np.cumsum(n)]).astype(np.int32)
+    b2 = wl.Batch(spec, m, n - 1, qsl, (m + n).astype(np.int32), b.block_tables, b.num_blocks)
+    attn = dataclasses.replace(wl.make_attention_inputs(spec, b2, device="cuda", seed=7), k_pool=s.attn.k_pool, v_pool=s.attn.v_pool)
+    positions = np.concatenate([lens[i] + np.arange(n[i]) for i in range(b.B)])
+    s2 = VerifyStep(b2, attn, None, rotary=s.rotary, positions=positions, shared=share(b2, spec.block_size, 608 // spec.block_size), weights=s.weights)
+    before = s.weights.double().cpu().numpy()
+    s2.run()
+    torch.cuda.synchronize()
+    turned = osv.rotate(attn.q.double().cpu().numpy(), s.rotary.cos_sin.cpu().numpy(), positions, s.rotary.style)
+    assert np.allclose(s2.q.double().cpu().numpy(), turned, rtol=2 ** -8, atol=1e-5)   # its rounding; the products' in fp32
+    check_attention(s2)
+    want, size = osv.attention_weights(View(s2).k, qsl, b2.seq_lens, b.block_tables, s2.q.double().cpu().numpy(),
+                                       float(np.float32(s2.scale)), s2.lse.double().cpu().numpy(), before, None, np.full(b.B, 608))
+    got = s.weights.double().cpu().numpy()
+    own = used_places(b2.seq_lens, b.block_tables, b.num_blocks, spec.block_size)
+    own[b.block_tables[0, : 608 // spec.block_size]] = False
+    own = np.broadcast_to(own[:, None, :], got.shape)
+    assert (np.abs(got - want) <= U * size + 1e-30)[own].all() and np.array_equal(got[~own], before[~own])
 
 
 def test_step_over_the_8_bit_cache():
