@@ -9,8 +9,9 @@
 // and one reduction over the lanes at the end gives the sums, always in the same order.
 //
 // Bound by the bytes of K for a step's rows: 64 sequences of 1024 to 4096 keys (32 query heads over 8 of 128, up to 5 tokens;
-// 363 MB) take 88 us, 4.2 TB/s.  With many rows by the latency of a tile's rows and the exponentials: 64 tokens of 28 heads over
-// 6 prompts of 2001 to 8000 keys (4 KV heads; 14.3 GFLOP) 26 us.  Two key tiles a wave took 106 and 37 us.
+// 363 MB) take 73 to 88 us on four cards, 4.1 to 5.0 TB/s.  With many rows by a workgroup's start and the LDS reads of q: 64
+// tokens of 28 heads over 6 prompts of 2001 to 8000 keys (4 KV heads; 14.3 GFLOP) 25 to 27 us.  Two key tiles a wave, which halve
+// those reads, took 108 and 39 us with three instead of five waves a SIMD; rows fetched two tiles ahead 79 and 29.
 #include "attention.h"
 #include "tiles.h"
 

@@ -273,6 +273,29 @@ def test_replays_and_streams():
             assert torch.equal(x, y), turn
 
 
+def test_an_offset_past_31_bits():
+    """The sequence at the end of pools of more than 2^31 elements: the same bits as in small ones."""
+    r, hkv, bs, D = np.random.default_rng(31), 2, 16, 64
+    qsl, S, tables, own = batch([5], [900], bs, 31)
+    c = Cache(own, bs, hkv, D, r, False)
+    blocks = (1 << 31) // (hkv * bs * D) + own
+    q, small = queries(5, 4, D, r), c.pools()
+    _, lse = attend(c, small, qsl, S, tables, q, 0.1)
+    big = [torch.zeros(blocks * hkv * bs * D, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    for f, s in zip(big, small):
+        f[-s.numel():] = s
+    w = weigh(c, small[0], qsl, S, tables, q, 0.1, lse, None)
+    new_w, _ = evict(c, small, w, S, tables, [400], [7], 30)
+    c.blocks = blocks
+    high = tables + blocks - own
+    w_big = weigh(c, big[0], qsl, S, high, q, 0.1, lse, None)
+    assert torch.equal(w_big[-own:], w) and (w_big[:-own] == 777.0).all()
+    new_big, _ = evict(c, big, w_big, S, high, [400], [7], 30)
+    assert torch.equal(new_big[-own:], new_w)
+    for f, s in zip(big, small):
+        assert torch.equal(f[-s.numel():], s) and not f[:-s.numel()].any()
+
+
 def test_refusals_of_the_binding():
     r = np.random.default_rng(24)
     qsl, S, tables, blocks = batch([4], [20], 16, 1)
