@@ -234,58 +234,13 @@ int verify_attention(const char* name, bool in8, const void* k_cache, const void
 
 // ---- attention of many rows at once
 
-// The most row tiles a head of sequences whose tokens come to total_tokens: each may end with a tile that is not full.
-int64_t most_row_tiles(int64_t seqs, int64_t group, int64_t total_tokens, int64_t longest) {
-  const int64_t all = (total_tokens * group + seqs * (spexis::kTileRows - 1)) / spexis::kTileRows;
-  const int64_t each = (group * longest + spexis::kTileRows - 1) / spexis::kTileRows;
-  return std::min(all, seqs * each);
-}
-
-struct TileLayout {
-  int64_t units, prefix_units, groups_hdr, ws_prefix, ws_seq, total;   // offsets in bytes
-  int shares, pitch;
-  bool shared, merge;
-};
-
-// Units, and where their partials lie.  Prefixes count where sequences are longer than the least part (4 sequences of up to
-// 265 keys behind 160 that they share: 11 us as they are, 17 with the prefix apart).  They run together with the sequences up
-// to two workgroups a place that the chip has (kTileSlots), and all tiles are cut into parts then, else the prefixes' alone.
-// Without prefixes tiles are cut where one a workgroup leaves half of the places free and there are keys enough for two parts.
-TileLayout tile_layout(int64_t seqs, int64_t groups, int64_t hq, int64_t hkv, int64_t head_dim, int64_t total_tokens,
-                       int64_t max_query_len, int64_t max_seq_len) {
-  TileLayout l{};
-  const int64_t group = hq / hkv;
-  const bool is_long = max_seq_len > spexis::kTileLeastKeys;
-  l.shared = groups > 0 && is_long;
-  const int64_t pre = l.shared ? most_row_tiles(groups, group, total_tokens, total_tokens) : 0;
-  const int64_t own = most_row_tiles(seqs, group, total_tokens, max_query_len);
-  const int shares = (int)std::max<int64_t>(1, spexis::kTileSlots / hkv);
-  l.merge = l.shared ? (pre + own) * hkv <= 2 * spexis::kTileSlots : is_long && own * hkv <= spexis::kTileSlots / 2;
-  l.shares = l.shared || l.merge ? shares : 0;
-  l.prefix_units = l.shared ? pre + shares : 0;
-  l.units = own + (l.merge ? pre + shares : 0);
-  l.pitch = (int)std::min<int64_t>(spexis::kTileRows, group * max_query_len);
-  int64_t off = 0;
-  auto take = [&](int64_t bytes) {
-    const int64_t at = off;
-    off += round_up(bytes, 256);
-    return at;
-  };
-  if (l.merge) take(l.units * spexis::kTileHdrInts * 4);
-  l.groups_hdr = take(l.shared ? groups * 16 : 0);
-  l.ws_prefix = take(l.prefix_units * hkv * spexis::tile_slot_floats(spexis::kTileRows, (int)head_dim) * 4);
-  l.ws_seq = l.merge ? take(l.units * hkv * spexis::tile_slot_floats(l.pitch, (int)head_dim) * 4) : 0;
-  l.total = std::max<int64_t>(off, 16);
-  return l;
-}
-
 size_t tile_workspace_size(int32_t num_seqs, int32_t num_groups, int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim,
                            int32_t total_tokens, int32_t max_query_len, int32_t max_seq_len) {
   if (num_seqs <= 0 || num_groups < 0 || num_kv_heads <= 0 || num_q_heads <= 0 || num_q_heads % num_kv_heads != 0 ||
       head_dim <= 0 || total_tokens <= 0 || max_query_len <= 0 || max_seq_len <= 0 ||
       (int64_t)total_tokens * num_q_heads >= (1ll << 31))
     return 0;
-  return (size_t)tile_layout(num_seqs, num_groups, num_q_heads, num_kv_heads, head_dim, total_tokens, max_query_len,
+  return (size_t)spexis::tile_layout(num_seqs, num_groups, num_q_heads, num_kv_heads, head_dim, total_tokens, max_query_len,
                              max_seq_len).total;
 }
 
@@ -319,7 +274,7 @@ int tile_attention(const char* name, bool in8, const void* k_cache, const void* 
   if (misaligned({k_cache, v_cache, scales, q, out, workspace}))
     return fail(SPEXIS_ERR_INVALID_ARGUMENT, "%s: a pointer that is not 16-byte aligned", name);
   if (q == out) return fail(SPEXIS_ERR_INVALID_ARGUMENT, "%s: out aliases q", name);
-  const TileLayout l = tile_layout(num_seqs, num_groups, num_q_heads, num_kv_heads, head_dim, total_tokens, max_query_len,
+  const spexis::TileLayout l = spexis::tile_layout(num_seqs, num_groups, num_q_heads, num_kv_heads, head_dim, total_tokens, max_query_len,
                                    max_seq_len);
   // a launch holds fewer than 2^32 threads
   if (std::max(l.units, l.prefix_units) * num_kv_heads * 256 >= (1ll << 32))

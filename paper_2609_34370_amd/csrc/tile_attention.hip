@@ -37,7 +37,6 @@ namespace spexis {
 namespace {
 
 constexpr int kRows = kTileRows;
-constexpr int kSorted = 64;   // segments that are taken in the order of their lengths
 
 // Eight e4m3 codes times a power of two, as a matrix operand.
 __device__ __forceinline__ u32x4 widen_codes(uint32_t lo, uint32_t hi, float scale) {
@@ -114,13 +113,14 @@ struct Unit {
 
 // The unit u of a head, of the launch's segments [seg_lo, seg_hi) (false: there are fewer).  All threads of the workgroup call
 // it, a segment each at a time; the one whose segment has the unit hands it on.  Where units are parts of tiles, a part is about
-// `share` key tiles: sum(ceil(nt / share)) units.  Few segments are taken in the order of their lengths, so that what ends last is
-// short (eight prompts of 100 to 3500 tokens 379 us for 392; tile by tile over all of them 2% less, but 2% more in 8 bits: neighbours
-// no longer read the same keys).  Steps of short sequences need no search (512 sequences behind 16
-// prefixes 192 us for 204).
+// `share` key tiles: sum(ceil(nt / share)) units.  Few segments without prefixes are taken in the order of their lengths, so that
+// what ends last is short (eight prompts of 100 to 3500 tokens 379 us for 392; tile by tile over all of them 2% less, but 2% more in 8 bits:
+// neighbours no longer read the same keys).  With prefixes in the launch the search for that order costs what it gives or more: 32
+// sequences of 5 tokens behind 4096 keys, 32 + 8 heads, 42.0 us ordered, 38.1 by number; 60 behind 512, 32 + 16 heads, 123 and 115; 8 prompts
+// behind 1024 148 and 148.  Steps of short sequences need no search (512 sequences behind 16 prefixes 192 us for 204).
 __device__ __forceinline__ bool find_unit(const TileAttnParams& p, int u, Unit& o) {
   __shared__ int64_t sm_total[4];
-  __shared__ int sm_rows[4], sm_scan[2][4], sm_sort[kSorted][2];
+  __shared__ int sm_rows[4], sm_scan[2][4], sm_sort[64][2];
   __shared__ __attribute__((aligned(16))) int sm_unit[12];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int ns = p.seg_hi - p.seg_lo;
@@ -163,27 +163,20 @@ __device__ __forceinline__ bool find_unit(const TileAttnParams& p, int u, Unit& 
     __syncthreads();
     sum = sm_total[0] + sm_total[1] + sm_total[2] + sm_total[3];
     rows = sm_rows[0] + sm_rows[1] + sm_rows[2] + sm_rows[3];
-    const int goal = (int)tile_attn_parts(p.shares, rows);
-    // (64-bit divisions take hundreds of instructions; the sum is far below 2^53)
-    share = (int)fmin(fmax(ceil((double)sum / (double)goal), (double)(kTileLeastKeys / p.step)), 2147483647.0);
+    share = tile_attn_share(p.shares, p.step, sum, rows);
   }
   int before = 0, turn = 0;
   for (int base = 0; base < ns; base += 256, turn ^= 1) {
     if (p.shares == 0 || ns > 256) load(base);
-    const int parts = nt > share ? (int)((uint32_t)(nt - 1) / (uint32_t)share) + 1 : 1, mine = tiles * parts;
+    const int parts = tile_parts(nt, share), mine = tiles * parts;
     int at;
-    if (ns <= kSorted) {   // the longest first: what ends last is short
-      if (tid < kSorted) {
+    if (tile_by_length(p.num_groups, ns)) {   // the longest first: what ends last is short
+      if (tid < ns) {
         sm_sort[tid][0] = nt;
         sm_sort[tid][1] = mine;
       }
       __syncthreads();
-      at = 0;
-      for (int s = 0; s < ns; ++s) {
-        const int other = sm_sort[s][0], units = sm_sort[s][1];
-        at += other > nt || (other == nt && s < tid) ? units : 0;
-        before += units;
-      }
+      at = tile_first_unit(sm_sort, ns, min(tid, ns - 1), &before);
     } else {
       const int incl = wave_incl_scan_i32(mine, lane);
       if (lane == 63) sm_scan[turn][wave] = incl;

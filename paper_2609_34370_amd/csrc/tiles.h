@@ -1,6 +1,10 @@
 // Parameters and launches of the attention of many query rows, of the attention weights and of evictions by them.
 #pragma once
 
+#include <math.h>
+
+#include <algorithm>
+
 #include "kernels.h"
 
 namespace spexis {
@@ -48,6 +52,76 @@ __host__ __device__ inline int64_t tile_attn_parts(int shares, int tiles) {
   return rest > half ? rest : half;
 }
 __host__ __device__ inline int64_t tile_slot_floats(int rows, int D) { return ((int64_t)rows * (D + 2) + 15) / 16 * 16; }
+// Key tiles of a part, where all row tiles (`tiles`) have `sum` key tiles.  (64-bit divisions take hundreds of instructions; the
+// sum is far below 2^53.)
+__host__ __device__ inline int tile_attn_share(int shares, int step, int64_t sum, int tiles) {
+  const double each = ceil((double)sum / (double)(int)tile_attn_parts(shares, tiles));
+  return (int)fmin(fmax(each, (double)(kTileLeastKeys / step)), 2147483647.0);
+}
+// Parts of a row tile of nt key tiles.
+__host__ __device__ inline int tile_parts(int nt, int share) { return nt > share ? (int)((uint32_t)(nt - 1) / (uint32_t)share) + 1 : 1; }
+
+// Whether segments are taken in the order of their lengths: few ones, of a call without prefixes.  Prefixes come first, in their
+// order: their partials lie in slots of their units' numbers, of which there are as many as prefixes can need.
+__host__ __device__ inline bool tile_by_length(int num_groups, int segments) { return num_groups == 0 && segments <= 64; }
+// The first unit of segment s of ns by falling length; sorted[][0], [1]: their key tiles and units; `before`: all units.
+template <class Segments>
+__host__ __device__ inline int tile_first_unit(const Segments& sorted, int ns, int s, int* before) {
+  int at = 0;
+  const int nt = sorted[s][0];
+  for (int i = 0; i < ns; ++i) {
+    const int other = sorted[i][0], units = sorted[i][1];
+    at += other > nt || (other == nt && i < s) ? units : 0;
+    *before += units;
+  }
+  return at;
+}
+
+// The most row tiles a head of sequences whose tokens come to total_tokens: each may end with a tile that is not full.
+inline int64_t most_row_tiles(int64_t seqs, int64_t group, int64_t total_tokens, int64_t longest) {
+  const int64_t all = (total_tokens * group + seqs * (kTileRows - 1)) / kTileRows;
+  const int64_t each = (group * longest + kTileRows - 1) / kTileRows;
+  return std::min(all, seqs * each);
+}
+
+struct TileLayout {
+  int64_t units, prefix_units, groups_hdr, ws_prefix, ws_seq, total;   // offsets in bytes
+  int shares, pitch;
+  bool shared, merge;
+};
+
+// Units, and where their partials lie.  Prefixes count where sequences are longer than the least part (4 sequences of up to
+// 265 keys behind 160 that they share: 11 us as they are, 17 with the prefix apart).  They run together with the sequences up
+// to two workgroups a place that the chip has (kTileSlots), and all tiles are cut into parts then, else the prefixes' alone.
+// Without prefixes tiles are cut where one a workgroup leaves half of the places free and there are keys enough for two parts.
+inline TileLayout tile_layout(int64_t seqs, int64_t groups, int64_t hq, int64_t hkv, int64_t head_dim, int64_t total_tokens,
+                              int64_t max_query_len, int64_t max_seq_len) {
+  TileLayout l{};
+  const int64_t group = hq / hkv;
+  const bool is_long = max_seq_len > kTileLeastKeys;
+  l.shared = groups > 0 && is_long;
+  const int64_t pre = l.shared ? most_row_tiles(groups, group, total_tokens, total_tokens) : 0;
+  const int64_t own = most_row_tiles(seqs, group, total_tokens, max_query_len);
+  const int shares = (int)std::max<int64_t>(1, kTileSlots / hkv);
+  l.merge = l.shared ? (pre + own) * hkv <= 2 * kTileSlots : is_long && own * hkv <= kTileSlots / 2;
+  l.shares = l.shared || l.merge ? shares : 0;
+  // (parts of prefixes are no more than their tiles and `shares`, whatever else is in the launch)
+  l.prefix_units = l.shared ? pre + shares : 0;
+  l.units = own + (l.merge ? pre + shares : 0);
+  l.pitch = (int)std::min<int64_t>(kTileRows, group * max_query_len);
+  int64_t off = 0;
+  auto take = [&](int64_t bytes) {
+    const int64_t at = off;
+    off += (bytes + 255) / 256 * 256;
+    return at;
+  };
+  if (l.merge) take(l.units * kTileHdrInts * 4);
+  l.groups_hdr = take(l.shared ? groups * 16 : 0);
+  l.ws_prefix = take(l.prefix_units * hkv * tile_slot_floats(kTileRows, (int)head_dim) * 4);
+  l.ws_seq = l.merge ? take(l.units * hkv * tile_slot_floats(l.pitch, (int)head_dim) * 4) : 0;
+  l.total = std::max<int64_t>(off, 16);
+  return l;
+}
 
 // Softmax weights of the cached keys, summed over the query rows of their KV head.
 struct WeightParams {
