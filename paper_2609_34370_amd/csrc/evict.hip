@@ -38,10 +38,8 @@ void evict_choose_kernel(EvictParams p) {
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int b = (int)blockIdx.x / p.hkv, h = (int)blockIdx.x % p.hkv, bs = p.block_size;
   const int S = clampi(p.seq_lens[b], 0, (int)min((int64_t)p.max_blocks * bs, (int64_t)p.max_seq_len));
-  const int m = clampi(p.keep_lens[b], 0, S);
-  const int f = p.first_keys ? clampi(p.first_keys[b], 0, m) : 0;
-  const int last = min(p.keep_last, m - f);
-  const int lo = f, hi = S - last;   // the keys that are chosen among
+  const EvictRange range = evict_range(S, p.keep_lens[b], p.first_keys ? p.first_keys[b] : 0, p.keep_last);
+  const int m = range.m, lo = range.lo, hi = range.hi;
   const int32_t* table = p.block_tables + (int64_t)b * p.max_blocks;
   const int shift = bs == 16 ? 4 : 5;
   auto block_of = [&](int t) { return clampi(table[t >> shift], 0, p.num_blocks - 1); };
@@ -74,12 +72,12 @@ void evict_choose_kernel(EvictParams p) {
 #pragma unroll
     for (int i = 0; i < kHeld; ++i)
       if (i < rounds && key[i] - 1 < 0xFFFFFFFEu) f(key[i]);
-    for (int t = kHeld * kChoose + tid; t < hi; t += kChoose) f(rank_bits(p.weights[place(t)]));
+    for (int t = evict_rest(kHeld * kChoose, lo) + tid; t < hi; t += kChoose) f(rank_bits(p.weights[place(t)]));
   };
   // `least`, the rank of the last one that stays, from the highest bit in which the ranks differ on, up to eight bits a pass;
   // `equal`, how many of those of this rank stay: the first ones.
   uint32_t least = 0xFFFFFFFEu;
-  int equal = 0, want = m - f - last;
+  int equal = 0, want = m - lo - (S - hi);
   if (want > 0) {
     uint32_t set = 0, clear = 0;   // the bits that some have, and that some have not
     each([&](uint32_t k) {
@@ -239,6 +237,7 @@ __global__ __launch_bounds__(kMove) void evict_move_kernel(EvictParams p) {
   const int32_t* table = p.block_tables + (int64_t)b * p.max_blocks;
   const int32_t* list = p.list + (int64_t)item * p.pitch;
   auto chunk_of = [&](int block) { return ((int64_t)clampi(block, 0, p.num_blocks - 1) * p.hkv + h) * (BS * D); };
+  auto from_list = [&](int i) { return clampi(list[i], 0, p.max_blocks * BS - 1); };   // (leads no farther than the table)
   if (slice < kSlices) {
     constexpr int kBatch = 4, kRound = 64 * W * kBatch;
     uint16_t* k = reinterpret_cast<uint16_t*>(p.k_cache) + slice * BS * 8;
@@ -247,7 +246,7 @@ __global__ __launch_bounds__(kMove) void evict_move_kernel(EvictParams p) {
     u32x4 v[kBatch];
     auto look_up = [&](int r) {
 #pragma unroll
-      for (int i = 0; i < kBatch; ++i) src[i] = list[min(max(r + 64 * W * i, first), m - 1)];
+      for (int i = 0; i < kBatch; ++i) src[i] = from_list(min(max(r + 64 * W * i, first), m - 1));
     };
     auto read = [&](u32x4* v) {
       int block[kBatch];
@@ -290,8 +289,8 @@ __global__ __launch_bounds__(kMove) void evict_move_kernel(EvictParams p) {
     auto look_up = [&](int t0) {
       s0 = *reinterpret_cast<const i32x4*>(list + place(t0, 0));
       s1 = *reinterpret_cast<const i32x4*>(list + place(t0, 4));
-      from = list[max(t0, first)] / BS;
-      until = list[min(t0 + 127, m - 1)] / BS;
+      from = from_list(max(t0, first)) / BS;
+      until = from_list(min(t0 + 127, m - 1)) / BS;
     };
     // The blocks of a window of groups come with one load; a lane's is handed to it.
     constexpr int kPer = 128 / BS, kWindow = 64 / kPer, kAhead = 3;   // (kAhead: groups on their way)

@@ -156,6 +156,20 @@ struct EvictParams {
   int64_t pitch;                  // max_seq_len in whole batches of 128
 };
 
+// Of S keys: how many stay, and the keys [lo, hi) that are chosen among (those in front and behind stay anyhow).
+struct EvictRange {
+  int m, lo, hi;
+};
+__host__ __device__ inline EvictRange evict_range(int S, int keep, int first, int keep_last) {
+  EvictRange r;
+  r.m = keep < 0 ? 0 : (keep > S ? S : keep);
+  r.lo = first < 0 ? 0 : (first > r.m ? r.m : first);
+  r.hi = S - (keep_last < r.m - r.lo ? keep_last : r.m - r.lo);
+  return r;
+}
+// The first key that is chosen among and not one of the `held` in registers.
+__host__ __device__ inline int evict_rest(int held, int lo) { return held > lo ? held : lo; }
+
 hipError_t launch_tile_attention(const TileAttnParams& p, hipStream_t s);
 hipError_t launch_weights(const WeightParams& p, hipStream_t s);
 hipError_t launch_evict(const EvictParams& p, hipStream_t s);
