@@ -393,6 +393,7 @@ int spexis_shared_attention_kv8(const void* k_cache, const void* v_cache, const 
  *                 [0, n_b]), and S_b is its length with them: spexis_accept's accepted_len and seq_lens_inout after it
  *                 (a sequence of row status 3, whose length is not rolled back, gets sums without a meaning)
  *   weights_in    [num_blocks][Hkv][block_size] fp32 (read), which may be `weights`, or NULL: all sums begin here
+ *                 (total_tokens 0: those of another array are copied, with NULL nothing is written; q and lse may be NULL)
  *   weights       the same shape (written)
  *   max_seq_len   host: >= max_b S_b
  *   first_keys    [num_seqs] int32 or NULL (0): keys in front of it (clamped to [0, S_b]) are left as they were

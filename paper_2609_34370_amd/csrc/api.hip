@@ -528,8 +528,9 @@ int spexis_attention_weights(const void* k_cache, int32_t num_blocks, int32_t nu
   if ((int64_t)total_tokens * num_q_heads >= (1ll << 31) || (int64_t)max_blocks_per_seq * block_size >= (1ll << 30) ||
       (double)num_seqs * num_kv_heads * (((int64_t)max_seq_len + 127) / 128) * 256.0 >= 4294967296.0)
     return fail(SPEXIS_ERR_UNSUPPORTED, "%s: too many tokens or slots", name);
-  if (num_seqs == 0 || total_tokens == 0) return ok();
-  if (!k_cache || !query_start_loc || !seq_lens || !block_tables || !q || !lse || !weights)
+  // (without query tokens there is nothing to add; sums of another array still have to come over)
+  if (num_seqs == 0 || (total_tokens == 0 && (!weights_in || weights_in == weights))) return ok();
+  if (!k_cache || !query_start_loc || !seq_lens || !block_tables || (total_tokens > 0 && (!q || !lse)) || !weights)
     return fail(SPEXIS_ERR_INVALID_ARGUMENT, "%s: null pointer", name);
   if (misaligned({k_cache, q, weights, weights_in}))
     return fail(SPEXIS_ERR_INVALID_ARGUMENT, "%s: a pointer that is not 16-byte aligned", name);
