@@ -85,7 +85,7 @@ class VerifyStep:
         if weights is not None:
             self.lse = torch.empty(attn.q.shape[:2], device=dev)
             # the lengths after the step (with acceptance, without the rejected tokens) and after an eviction
-            self.lens_after, self.lens_evicted = torch.empty_like(self.seq_lens), torch.empty_like(self.seq_lens)
+            self.lens_after, self.lens_evicted = self.seq_lens.clone(), torch.empty_like(self.seq_lens)
             ws = sx.spexis_evict_kv_workspace_size(batch.B, spec.num_kv_heads, batch.max_seq_len)
             self.evict_ws = torch.empty(max(ws, 16), dtype=torch.uint8, device=dev)
             if shared is not None:   # the keys that every sequence shares, in whole blocks
@@ -150,8 +150,17 @@ class VerifyStep:
         f(*self._cache(), self.batch.max_seq_len, self.q, self.spec.num_q_heads, self.scale, self.out, self.attn_ws,
           kv_chunk_tokens=self.kv_chunk_tokens, stream=stream)
 
+    def _begin_lens(self, stream):
+        """self.lens_after with the step's new tokens, rejected ones among them."""
+        with torch.cuda.stream(stream or torch.cuda.current_stream()):
+            self.lens_after.copy_(self.seq_lens)
+
     def accept(self, target=None, draft=None, kind=None, stream=None, seq_lens_inout=None):
+        """seq_lens_inout: the lengths that lose the rejected tokens; self.lens_after of a step with weights."""
         a = self.acc
+        if self.weights is not None and seq_lens_inout is None:
+            self._begin_lens(stream)
+            seq_lens_inout = self.lens_after
         kind = self.kind if kind is None else kind
         target = a.target_logits if target is None else target
         draft = a.draft_logits if draft is None else draft
@@ -166,8 +175,10 @@ class VerifyStep:
                                  temperature=self.acc.temperature, stream=stream)
 
     def add_weights(self, stream=None):
-        """To self.weights, those of the accepted tokens, by the lengths after the step (self.lens_after)."""
+        """To self.weights, those of the accepted tokens, by the lengths after the step (self.lens_after, of the acceptance)."""
         s, b, a = self.spec, self.batch, self.attn
+        if self.acc is None:
+            self._begin_lens(stream)
         sx.spexis_attention_weights(a.k_pool, b.num_blocks, s.num_kv_heads, s.block_size, s.head_dim, self.qsl, self.lens_after,
                                     self.tables, b.T, b.max_query_len, b.max_seq_len, self.q, s.num_q_heads, self.scale, self.lse,
                                     self.weights, weights_in=self.weights,
@@ -188,11 +199,8 @@ class VerifyStep:
     def run(self, stream=None):
         self.append(stream)
         self.attention(stream)
-        if self.weights is not None:
-            with torch.cuda.stream(stream or torch.cuda.current_stream()):
-                self.lens_after.copy_(self.seq_lens)
         if self.acc is not None:
-            self.accept(stream=stream, seq_lens_inout=self.lens_after if self.weights is not None else None)
+            self.accept(stream=stream)
         if self.weights is not None:
             self.add_weights(stream)
         if self.top_logprobs is not None:
