@@ -187,13 +187,15 @@ class VerifyStep:
 
     def evict(self, keep_lens, keep_last, stream=None) -> torch.Tensor:
         """Behind the step, drops all but keep_lens keys of each sequence, those of least weight; shared keys and the last
-        keep_last stay.  The new lengths (self.lens_evicted)."""
+        keep_last stay.  The new lengths (self.lens_evicted), from which another eviction before the next step goes on."""
         s, b, a = self.spec, self.batch, self.attn
         if self.weights is None:
             raise ValueError("no attention weights to go by")
         sx.spexis_evict_kv(a.k_pool, a.v_pool, self.weights, b.num_blocks, s.num_kv_heads, s.block_size, s.head_dim,
                            self.lens_after, self.tables, b.max_seq_len, keep_lens, keep_last, self.weights,
                            self.lens_evicted, self.evict_ws, first_keys=self.first_keys, stream=stream)
+        with torch.cuda.stream(stream or torch.cuda.current_stream()):
+            self.lens_after.copy_(self.lens_evicted)
         return self.lens_evicted
 
     def run(self, stream=None):

@@ -1,11 +1,14 @@
-"""What a step with attention weights leaves behind however it is run: as a whole, call by call, behind an eviction.  The
-same kernels on the same inputs: bit for bit."""
+"""What a step with attention weights leaves behind however it is run: as a whole, call by call, behind an eviction,
+evicted from more than once.  The same kernels on the same inputs: bit for bit."""
+import numpy as np
 import pytest
 import torch
 
+from oracle import serving as osv
 from paper_2609_34370_amd import workloads as wl
 from paper_2609_34370_amd.step import VerifyStep
-from tests.test_gpu_cache_life import life
+from tests.test_gpu_cache_life import View, life
+from tests.test_gpu_evict import used_places
 
 pytestmark = pytest.mark.gpu
 
@@ -64,3 +67,24 @@ def test_a_step_behind_an_eviction_starts_from_its_own_lengths(capture):
         torch.cuda.synchronize()
         for x, y in zip((s.out, s.lse, s.weights, s.lens_after, s.attn.k_pool, s.attn.v_pool), want):
             assert torch.equal(x, y)
+
+
+def test_evictions_one_after_the_other():
+    """The second goes on from what the first has left."""
+    s = life()
+    b, spec = s.batch, s.spec
+    s.run()
+    torch.cuda.synchronize()
+    lens, w = s.lens_after.cpu().numpy(), s.weights.cpu().numpy().copy()
+    c, first = View(s), np.full(b.B, 608)
+    k, v = c.k, c.v
+    for most in (640, 620, 620):
+        keep = np.minimum(most, lens).astype(np.int32)
+        new = s.evict(torch.as_tensor(keep).cuda(), 8)
+        torch.cuda.synchronize()
+        k, v, w, lens = osv.evict(k, v, w, lens, b.block_tables, keep, first, 8)
+        assert np.array_equal(new.cpu().numpy(), lens)
+        kept = used_places(lens, b.block_tables, b.num_blocks, spec.block_size)
+        now = View(s)
+        assert np.array_equal(now.k[kept], k[kept]) and np.array_equal(now.v[kept], v[kept])
+        assert np.array_equal(s.weights.cpu().numpy().transpose(0, 2, 1)[kept], w.transpose(0, 2, 1)[kept])
