@@ -213,12 +213,15 @@ class VerifyStep:
         step at once.  Every buffer is allocated in __init__ and the library calls neither
         allocate nor set memory (the acceptance counters are cleared by its first kernel), so the
         graph holds only the step's kernel launches.  A replay reads the current contents of the
-        input buffers; the sizes are those of this batch."""
+        input buffers; the sizes are those of this batch.  The warm-up's attention weights do not count."""
         side = torch.cuda.Stream()
         side.wait_stream(torch.cuda.current_stream())
         with torch.cuda.stream(side):
+            before = self.weights.clone() if self.weights is not None else None
             for _ in range(warmup):
                 self.run()
+            if before is not None:
+                self.weights.copy_(before)
         torch.cuda.current_stream().wait_stream(side)
         self.graph = torch.cuda.CUDAGraph()
         with torch.cuda.graph(self.graph):

@@ -1,5 +1,5 @@
 """What a step with attention weights leaves behind however it is run: as a whole, call by call, behind an eviction,
-evicted from more than once.  The same kernels on the same inputs: bit for bit."""
+captured, evicted from more than once.  The same kernels on the same inputs: bit for bit."""
 import numpy as np
 import pytest
 import torch
@@ -88,3 +88,21 @@ def test_evictions_one_after_the_other():
         now = View(s)
         assert np.array_equal(now.k[kept], k[kept]) and np.array_equal(now.v[kept], v[kept])
         assert np.array_equal(s.weights.cpu().numpy().transpose(0, 2, 1)[kept], w.transpose(0, 2, 1)[kept])
+
+
+def test_capture_adds_no_weights():
+    """Two replays add the weights of two steps: recording runs the step for warm-up, which must not count."""
+    s = life()
+    w0 = s.weights.clone()
+    s.run()
+    s.run()
+    torch.cuda.synchronize()
+    want = s.weights.clone()
+    s.weights.copy_(w0)
+    s.capture(warmup=2)
+    torch.cuda.synchronize()
+    assert torch.equal(s.weights, w0)
+    s.replay()
+    s.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(s.weights, want)
