@@ -468,7 +468,8 @@ void tile_attn_kernel(TileAttnParams p) {
 #pragma unroll
           for (int e = 0; e < 16; ++e) acc[mt][e] *= alpha;
       }
-      const float mc = -m * p.scale_log2e;
+      // (finite where a row has seen no key yet, whatever the scale: its scores are minus infinity and weigh 0)
+      const float mc = fminf(-m * p.scale_log2e, 3.0e38f);
       u32x4 pw[2 * KT];
 #pragma unroll
       for (int kt = 0; kt < KT; ++kt) {
