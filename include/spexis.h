@@ -339,7 +339,7 @@ int spexis_prompt_attention_kv8(const void* k_cache, const void* v_cache, const 
 /*
  * Bytes of workspace spexis_shared_attention and spexis_shared_attention_kv8 need (> 0 whenever the sizes are valid, else 0):
  * up to about 300 MB (head_dim 128) for few rows, else the fp32 partials of the rows (4 (head_dim + 2) bytes a query token and
- * head) and about 50 MB.
+ * head), up to one tile of 128 such rows more a group and KV head (67 KB at head_dim 128), and about 50 MB.
  */
 size_t spexis_shared_attention_workspace_size(int32_t num_seqs, int32_t num_groups, int32_t num_q_heads,
                                               int32_t num_kv_heads, int32_t head_dim, int32_t total_tokens,

@@ -8,7 +8,7 @@
 // head dim moves it in place, in rounds: what a round overwrites, no later one reads.
 //
 // Bound by memory for a batch: 64 sequences of 1024 to 4096 keys cut to about a half (8 KV heads of 128) take 22 us to choose
-// and 235 to 247 to move: the lines of K hold keys that go beside those that stay, and V is read whole, so 1.08 GB (counted)
+// and 235 to 250 to move: the lines of K hold keys that go beside those that stay, and V is read whole, so 1.08 GB (counted)
 // where the kept rows alone are 724 MB, 4.4 TB/s.  For one sequence by latency: 16001 keys cut to a quarter take 27 us to choose, eight workgroups
 // on their way through the passes, and 25 to move.  One wave a slice, without rounds, took 227 and 79.
 #include "common.h"

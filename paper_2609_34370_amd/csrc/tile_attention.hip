@@ -21,14 +21,15 @@
 //   O^T[d][row] += V^T P^T: the V layouts hold slots in the order in which the score tile leaves them, so P^T is the
 //   lane's own values.
 //
-// Bound by LDS: a product of 32 cycles needs a fragment of 1 KB, of which a CU reads 64 bytes a cycle (measured), so its four
-// SIMDs' matrix cores can be busy half of the time.  16001 tokens of 32 query heads over 8 of 128 (2.1 TFLOP) take 2.01 to 2.10
-// ms on three cards, 1.00 to 1.04 PFLOP/s, the matrix cores busy for 47% of the cycles; prompts of 100 to 3500 tokens, eight
-// together, 374 to 397 us, 0.82 to 0.87 PFLOP/s; a large matrix product reaches 1.58.  Tried on the way (at 16001 tokens):
-// 64 keys a step and two workgroups a CU, the same but for shared prefixes (65 us for 60); eight waves that take turns at
-// the matrix cores, 1.94 ms for 2.03, prompts together 391 us for 372; 64 rows a wave, which halves the reads, 2.30 ms, one
-// wave a SIMD with nothing to run beside it; half or all of K loaded by every wave for itself, 2.32 and 2.30 ms; products
-// spread among the exponentials by hand, or waves' priorities, no difference.
+// Bound by the SIMDs' instructions: 16001 tokens of 32 query heads over 8 of 128 (2.1 TFLOP) take 2.01 to 2.10 ms on four cards,
+// 1.00 to 1.04 PFLOP/s; the matrix cores are busy for 51% of the cycles, and for 52% vector instructions are active (maxima,
+// exponentials, sums, the weights' roundings, staging): three waves a SIMD hide little of the one behind the other.  LDS is
+// not the limit: busy for 39% of the cycles, 0.1% of them conflicts; 12 waves read up to 600 bytes a ns from it, and products
+// with a read for each reach 2.1 PFLOP/s.  Prompts of 100 to 3500 tokens, eight together, 374 to 397 us, 0.82 to 0.87
+// PFLOP/s; a large matrix product reaches 1.58.  Tried on the way (at 16001 tokens): 64 keys a step and two workgroups a CU, the
+// same but for shared prefixes (65 us for 60); eight waves that take turns at the matrix cores, 1.94 ms for 2.03, prompts
+// together 391 us for 372; 64 rows a wave, 2.30 ms, one wave a SIMD with nothing to run beside it; half or all of K loaded by
+// every wave for itself, 2.32 and 2.30 ms; products spread among the exponentials by hand, or waves' priorities, no difference.
 #include "attention.h"
 #include "tiles.h"
 

@@ -9,9 +9,9 @@
 // and one reduction over the lanes at the end gives the sums, always in the same order.
 //
 // Bound by the bytes of K for a step's rows: 64 sequences of 1024 to 4096 keys (32 query heads over 8 of 128, up to 5 tokens;
-// 363 MB) take 73 to 88 us on four cards, 4.1 to 5.0 TB/s.  With many rows by a workgroup's start and the LDS reads of q: 64
-// tokens of 28 heads over 6 prompts of 2001 to 8000 keys (4 KV heads; 14.3 GFLOP) 25 to 27 us.  Two key tiles a wave, which halve
-// those reads, took 108 and 39 us with three instead of five waves a SIMD; rows fetched two tiles ahead 79 and 29.
+// 363 MB) take 73 to 88 us on four cards, 4.1 to 5.0 TB/s.  With many rows by a workgroup's start and its chain of row
+// tiles: 64 tokens of 28 heads over 6 prompts of 2001 to 8000 keys (4 KV heads; 14.3 GFLOP) 25 to 27 us, vector instructions active
+// for 42% of the cycles, the matrix cores 18%, LDS 14%.  Two key tiles a wave, which halve the reads of q, took 108 and 39 us with three instead of five waves a SIMD; rows fetched two tiles ahead 79 and 29.
 #include "attention.h"
 #include "tiles.h"
 

@@ -33,7 +33,9 @@ class VerifyStep:
         positions [T]: where the rotation turns the tokens to, if not to their places in the cache (after an eviction).
         shared: (group_start_loc, prefix_lens) of sequences that begin with the same blocks.
         weights [num_blocks][Hkv][block_size] fp32: the sums of the cached keys' attention weights, to which the step adds
-        those of its accepted tokens (of all tokens without acceptance); bf16 cache only.  Shared keys have none."""
+        those of its accepted tokens (of all tokens without acceptance); bf16 cache only.  Shared keys have none.
+        With shared or weights, or more than 64 query rows a KV head, the attention is that of prompts (weights need its lse;
+        workload 2: 146 us for the verification attention's 128), which cuts keys by itself: kv_chunk_tokens is not used."""
         spec = batch.spec
         self.batch, self.spec, self.kind = batch, spec, kind
         self.kv_chunk_tokens = kv_chunk_tokens
