@@ -114,14 +114,15 @@ struct Unit {
 
 // The unit u of a head, of the launch's segments [seg_lo, seg_hi) (false: there are fewer).  All threads of the workgroup call
 // it, a segment each at a time; the one whose segment has the unit hands it on.  Where units are parts of tiles, a part is about
-// `share` key tiles: sum(ceil(nt / share)) units.  Few segments without prefixes are taken in the order of their lengths, so that
-// what ends last is short (eight prompts of 100 to 3500 tokens 379 us for 392; tile by tile over all of them 2% less, but 2% more in 8 bits:
-// neighbours no longer read the same keys).  With prefixes in the launch the search for that order costs what it gives or more: 32
-// sequences of 5 tokens behind 4096 keys, 32 + 8 heads, 42.0 us ordered, 38.1 by number; 60 behind 512, 32 + 16 heads, 123 and 115; 8 prompts
-// behind 1024 148 and 148.  Steps of short sequences need no search (512 sequences behind 16 prefixes 192 us for 204).
+// `share` key tiles: sum(ceil(nt / share)) units.  A few sequences with whole tiles are taken in the order of their
+// lengths, so that what ends last is short (prompts of 100 to 3500 tokens, 32 + 8 heads: four 115 us for 122 by number, six 197 and 205, eight
+// 352 to 435 and 361 to 435; of equal lengths 182 and 180; tile by tile over all of them 2% less, but 2% more in 8 bits: neighbours no
+// longer read the same keys).  Beyond that the search for the order costs what it gives or more (12 and 16 prompts within 1%, 64 of 300
+// tokens 143 for 116; in parts 16 steps of 5 tokens 27.3 for 25.6; 32 steps behind a prefix of 4096 42.0 for 38.1, 60 behind 512, 32 + 16
+// heads, 123 and 115).  Steps of short sequences need no search (512 sequences behind 16 prefixes 192 us for 204).
 __device__ __forceinline__ bool find_unit(const TileAttnParams& p, int u, Unit& o) {
   __shared__ int64_t sm_total[4];
-  __shared__ int sm_rows[4], sm_scan[2][4], sm_sort[64][2];
+  __shared__ int sm_rows[4], sm_scan[2][4], sm_sort[kByLength][2];
   __shared__ __attribute__((aligned(16))) int sm_unit[12];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int ns = p.seg_hi - p.seg_lo;
@@ -171,7 +172,7 @@ __device__ __forceinline__ bool find_unit(const TileAttnParams& p, int u, Unit& 
     if (p.shares == 0 || ns > 256) load(base);
     const int parts = tile_parts(nt, share), mine = tiles * parts;
     int at;
-    if (tile_by_length(p.num_groups, ns)) {   // the longest first: what ends last is short
+    if (tile_by_length(p.num_groups, p.shares, ns)) {   // the longest first: what ends last is short
       if (tid < ns) {
         sm_sort[tid][0] = nt;
         sm_sort[tid][1] = mine;

@@ -61,9 +61,12 @@ __host__ __device__ inline int tile_attn_share(int shares, int step, int64_t sum
 // Parts of a row tile of nt key tiles.
 __host__ __device__ inline int tile_parts(int nt, int share) { return nt > share ? (int)((uint32_t)(nt - 1) / (uint32_t)share) + 1 : 1; }
 
-// Whether segments are taken in the order of their lengths: few ones, of a call without prefixes.  Prefixes come first, in their
-// order: their partials lie in slots of their units' numbers, of which there are as many as prefixes can need.
-__host__ __device__ inline bool tile_by_length(int num_groups, int segments) { return num_groups == 0 && segments <= 64; }
+// Whether segments are taken in the order of their lengths: few ones with whole tiles, of a call without prefixes.  Prefixes come
+// first, in their order: their partials lie in slots of their units' numbers, of which there are as many as prefixes can need.
+constexpr int kByLength = 8;
+__host__ __device__ inline bool tile_by_length(int num_groups, int shares, int segments) {
+  return num_groups == 0 && shares == 0 && segments <= kByLength;
+}
 // The first unit of segment s of ns by falling length; sorted[][0], [1]: their key tiles and units; `before`: all units.
 template <class Segments>
 __host__ __device__ inline int tile_first_unit(const Segments& sorted, int ns, int s, int* before) {

@@ -16,7 +16,7 @@ SHAPES = [
     # prefixes shorter than some sequences and longer than others
     (32, 16, 64, 32, [(128, [(500, 3)] * 17), (640, [(60, 7)] * 15), (64, [(450, 2)] * 22)]),
     (24, 24, 64, 16, [(64, [(500, 5)] * 20), (576, [(600, 1)] * 8), (128, [(90, 6)] * 10)]),
-    # 64 segments, as many as are ordered by their lengths where there are no prefixes, and 65
+    # 64 segments and 65
     (16, 16, 64, 16, [(128, [(450, 9)] * 63)]),
     (16, 16, 64, 16, [(128, [(450, 9)] * 64)]),
     # eight KV heads, more than one row tile a sequence
