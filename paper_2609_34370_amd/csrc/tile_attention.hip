@@ -21,11 +21,11 @@
 //   O^T[d][row] += V^T P^T: the V layouts hold slots in the order in which the score tile leaves them, so P^T is the
 //   lane's own values.
 //
-// Bound by the SIMDs' instructions: 16001 tokens of 32 query heads over 8 of 128 (2.1 TFLOP) take 2.01 to 2.10 ms on four cards,
-// 1.00 to 1.04 PFLOP/s; the matrix cores are busy for 51% of the cycles, and for 52% vector instructions are active (maxima,
+// Bound by the SIMDs' instructions: 16001 tokens of 32 query heads over 8 of 128 (2.1 TFLOP) take 1.99 to 2.10 ms on several cards,
+// 1.00 to 1.05 PFLOP/s; the matrix cores are busy for 51% of the cycles, and for 52% vector instructions are active (maxima,
 // exponentials, sums, the weights' roundings, staging): three waves a SIMD hide little of the one behind the other.  LDS is
 // not the limit: busy for 39% of the cycles, 0.1% of them conflicts; 12 waves read up to 600 bytes a ns from it, and products
-// with a read for each reach 2.1 PFLOP/s.  Prompts of 100 to 3500 tokens, eight together, 374 to 397 us, 0.82 to 0.87
+// with a read for each reach 2.1 PFLOP/s.  Prompts of 100 to 3500 tokens, eight together, 359 to 397 us, 0.82 to 0.91
 // PFLOP/s; a large matrix product reaches 1.58.  Tried on the way (at 16001 tokens): 64 keys a step and two workgroups a CU, the
 // same but for shared prefixes (65 us for 60); eight waves that take turns at the matrix cores, 1.94 ms for 2.03, prompts
 // together 391 us for 372; 64 rows a wave, 2.30 ms, one wave a SIMD with nothing to run beside it; half or all of K loaded by
